@@ -339,6 +339,86 @@ size_t nvfp4_sum_workspace_bytes(void);
 int nvfp4_sum_f64(const double* v, int64_t n, double* out, void* workspace,
                   size_t workspace_bytes, void* stream);
 
+/*
+ * Microscaled FP4 (OCP Microscaling Formats, MXFP4): E2M1 values in blocks of 32 consecutive
+ * elements of a row, one E8M0 scale 2^(code - 127) each, the form that gfx950's matrix
+ * instructions multiply directly.
+ *   q       [rows, 16 kb] bytes, kb = ceil(cols / 32), nibbles as above; the last block of a row is
+ *           filled up with zeros.  16-byte aligned.
+ *   scales  [rows, kb] bytes, E8M0 codes; 255 is NaN: every value of the block reads as NaN.
+ */
+
+/* scale = 2^E, E = floor(log2 max|x|) - 2 over the block, clamped to -127 .. 127 (code 0 for a block
+ * of zeros); q = RNE_E2M1(x / 2^E), saturating at 6, the sign kept.  A block that holds an infinity
+ * or a NaN gets code 255 (its nibbles are unspecified).  x: [rows, cols] contiguous, binary32 or
+ * bfloat16, 16-byte aligned, any cols.  No workspace; one kernel. */
+int mxfp4_quant(const void* x, int dtype, int64_t rows, int64_t cols, uint8_t* q, uint8_t* scales, void* stream);
+
+/* x_hat = q 2^E into out [rows, cols], binary32 or bfloat16 (both exact; above their range infinity),
+ * 16-byte aligned. */
+int mxfp4_dequant(const uint8_t* q, const uint8_t* scales, int64_t rows, int64_t cols, int out_dtype, void* out,
+                  void* stream);
+
+/*
+ * Matrix products.  m rows of activations (tokens), n outputs, k the contraction of the forward
+ * product; weights are [n, k] row-major as the quantizers take them.  Sums are held in binary32
+ * and rounded once to the output, [m, n] or [m, k] contiguous, bfloat16 or binary32 (out_dtype).
+ * The order of a sum depends on the sizes alone, so results are deterministic.
+ *   - m, n or k may be 0 (a sum over nothing is 0).  n, k <= 2^20, row strides <= 2^21, else
+ *     NVFP4_ERR_SHAPE.
+ *   - x, dy: bfloat16, rows ldx / ld elements apart (>= their width).
+ *   - Pointers to values and outputs are 16-byte aligned, E8M0 scales 4-byte, the workspace 256-byte;
+ *     else NVFP4_ERR_ALIGN.
+ *   - workspace: at least the call's *_workspace_bytes(...) for the same sizes and strides (which
+ *     return a negative nvfp4_status for invalid ones), no initialization; NULL where that is 0.
+ */
+
+/* y = x W^T S of bfloat16 x [m, k] and NVFP4 weights (q, scales, *tensor_scale) of `block` (16, 32, 64 or 128;
+ * k % block == 0), scales row-major.  The weights' values q s enter exactly, the sums are multiplied
+ * by S.  ldx % 8 == 0, else NVFP4_ERR_ALIGN. */
+int64_t nvfp4_matmul_workspace_bytes(int64_t m, int64_t n, int64_t k);
+int nvfp4_matmul(const void* x, int64_t ldx, const uint8_t* q, const uint8_t* scales, int block,
+                 const float* tensor_scale, int64_t m, int64_t n, int64_t k, int out_dtype, void* out, void* workspace,
+                 size_t workspace_bytes, void* stream);
+
+/* Its gradient with respect to x: dx = dy W S, dy bfloat16 [m, n], any ld >= n. */
+int64_t nvfp4_matmul_grad_input_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t ld);
+int nvfp4_matmul_grad_input(const void* dy, int64_t ld, const uint8_t* q, const uint8_t* scales, int block,
+                            const float* tensor_scale, int64_t m, int64_t n, int64_t k, int out_dtype, void* dx,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
+/* y = A B^T of microscaled A [m, k] and B [n, k] (any k: their rows hold whole blocks). */
+int64_t mxfp4_matmul_workspace_bytes(int64_t m, int64_t n, int64_t k);
+int mxfp4_matmul(const uint8_t* a_q, const uint8_t* a_scales, const uint8_t* b_q, const uint8_t* b_scales, int64_t m,
+                 int64_t n, int64_t k, int out_dtype, void* out, void* workspace, size_t workspace_bytes,
+                 void* stream);
+
+/* dx = dy B of bfloat16 dy [m, n] and microscaled B [n, k]: the gradient of the product above with
+ * respect to A, straight through A's quantization. */
+int64_t mxfp4_matmul_grad_input_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t ld);
+int mxfp4_matmul_grad_input(const void* dy, int64_t ld, const uint8_t* q, const uint8_t* scales, int64_t m, int64_t n,
+                            int64_t k, int out_dtype, void* dx, void* workspace, size_t workspace_bytes,
+                            void* stream);
+
+/* The gated feed-forward block in one kernel: g = x Wg^T, u = x Wu^T, h = silu(g) u with
+ * silu(g) = g / (1 + e^-g), all bfloat16 with sums in binary32; h is formed from the unrounded sums.
+ * x [m, k] (rows ldx apart), w_gate and w_up [n, k] (rows ldw apart), any k.  h [m, n]; gate and up
+ * [m, n] receive g and u for a backward pass, or are both NULL. */
+int64_t nvfp4_swiglu_ffn_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t ldx, int64_t ldw);
+int nvfp4_swiglu_ffn(const void* x, int64_t ldx, const void* w_gate, const void* w_up, int64_t ldw, int64_t m,
+                     int64_t n, int64_t k, void* h, void* gate, void* up, void* workspace, size_t workspace_bytes,
+                     void* stream);
+
+/* Its gradients from dh [m, n] and the forward's gate and up [m, n] (contiguous): with s = 1 / (1 + e^-g),
+ *   dg = dh u s (1 + g (1 - s)),  du = dh g s  (rounded to bfloat16 for the products),
+ *   dx [m, k] = dg Wg + du Wu,  dw_gate [n, k] = dg^T x,  dw_up [n, k] = du^T x.
+ * dx, or both dw_gate and dw_up, may be NULL: not computed. */
+int64_t nvfp4_swiglu_ffn_backward_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t ldx, int64_t ldw);
+int nvfp4_swiglu_ffn_backward(const void* dh, const void* x, int64_t ldx, const void* w_gate, const void* w_up,
+                              int64_t ldw, const void* gate, const void* up, int64_t m, int64_t n, int64_t k,
+                              void* dx, void* dw_gate, void* dw_up, void* workspace, size_t workspace_bytes,
+                              void* stream);
+
 #ifdef __cplusplus
 }
 #endif

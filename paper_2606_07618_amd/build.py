@@ -9,7 +9,8 @@ HERE = Path(__file__).resolve().parent
 ROOT = HERE.parent
 SRC = HERE / "csrc" / "nvfp4ss.hip"
 SOURCES = [SRC, HERE / "csrc" / "optimum.hip", HERE / "csrc" / "importance.hip",
-           HERE / "csrc" / "gptq.hip"]
+           HERE / "csrc" / "gptq.hip", HERE / "csrc" / "mxfp4.hip", HERE / "csrc" / "matmul.hip",
+           HERE / "csrc" / "ffn.hip"]
 LIB = HERE / "libnvfp4ss.so"
 
 HIPCC_FLAGS = [

@@ -1,0 +1,272 @@
+// Matrix products with 4-bit weights on AMD Instinct MI355X (gfx950).
+//   NVFP4 weights W = q s S [n, k], activations in bfloat16:  y = x W^T,  dx = dy W
+//   microscaled FP4 (E8M0 scale for each 32 values):          y = A B^T,  dx = dy B
+#include "product_host.h"
+
+namespace product_host {
+
+namespace {
+
+constexpr int kPackThreads = 256;
+
+template <typename V>
+__global__ __launch_bounds__(kPackThreads) void pack_kernel(const V* __restrict__ src, int64_t count, int64_t width,
+                                                            int64_t ld, V* __restrict__ dst, int64_t dst_ld) {
+    for (int64_t i = (int64_t)blockIdx.x * kPackThreads + threadIdx.x; i < count; i += (int64_t)gridDim.x * kPackThreads) {
+        const int64_t r = i / dst_ld, c = i % dst_ld;
+        dst[i] = c < width ? src[r * ld + c] : V(0);
+    }
+}
+
+template <typename V>
+int pack(const V* src, int64_t rows, int64_t width, int64_t ld, V* dst, int64_t dst_ld, hipStream_t stream) {
+    const int64_t count = rows * dst_ld, groups = ceil_div(count, kPackThreads);
+    if (count == 0) return NVFP4_OK;
+    hipLaunchKernelGGL((pack_kernel<V>), dim3((unsigned)(groups < 8192 ? groups : 8192)), dim3(kPackThreads), 0, stream,
+                       src, count, width, ld, dst, dst_ld);
+    return launched();
+}
+
+}  // namespace
+
+int pack_bf16_rows(const void* src, int64_t rows, int64_t width, int64_t ld, void* dst, hipStream_t stream) {
+    return pack(static_cast<const uint16_t*>(src), rows, width, ld, static_cast<uint16_t*>(dst), packed_ld(width), stream);
+}
+
+int pack_scale_rows(const uint8_t* src, int64_t rows, int64_t width, uint8_t* dst, int64_t dst_ld, hipStream_t stream) {
+    return pack(src, rows, width, width, dst, dst_ld, stream);
+}
+
+}  // namespace product_host
+
+namespace {
+
+using namespace product_host;
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+using Big = Tile<256, 256, 2, 4>;
+
+// ---- weights expanded to bfloat16 -----------------------------------------------------------
+
+// q s of NVFP4 (without S) or q 2^E of microscaled FP4, 8 values a lane, both exact: an E2M1 value has
+// two significand bits and an E4M3 scale four, bfloat16 eight (values below 2^-133 aside, which only
+// microscaled blocks of codes under 2 hold).
+__device__ __forceinline__ float e4m3_f32(uint32_t c) {
+    // the field as a binary32 number scaled by 2^-120, made whole by one exact product
+    return __uint_as_float((c & 0x7Fu) << 20) * 0x1p120f;
+}
+
+template <Kind KIND>
+__device__ __forceinline__ uint4 expand8(uint32_t n, uint32_t code) {
+    f32x2 d[4];
+    if constexpr (KIND == kMx) {
+        const float s = __uint_as_float(code << 23);
+        d[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(n, s, 0);
+        d[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(n, s, 1);
+        d[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(n, s, 2);
+        d[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(n, s, 3);
+        if (code == 255) d[0] = d[1] = d[2] = d[3] = f32x2{__uint_as_float(0x7FC00000u), __uint_as_float(0x7FC00000u)};
+    } else {
+        const float s = e4m3_f32(code);
+        d[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(n, 1.0f, 0) * s;
+        d[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(n, 1.0f, 1) * s;
+        d[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(n, 1.0f, 2) * s;
+        d[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(n, 1.0f, 3) * s;
+    }
+    return make_uint4(pack_bf16(d[0][0], d[0][1]), pack_bf16(d[1][0], d[1][1]), pack_bf16(d[2][0], d[2][1]),
+                      pack_bf16(d[3][0], d[3][1]));
+}
+
+constexpr int kExpandThreads = 256;
+
+// The weights are a run of blocks of 2^shift units of 8 values.
+template <Kind KIND>
+__global__ __launch_bounds__(kExpandThreads) void expand_kernel(const uint32_t* __restrict__ q,
+                                                                const uint8_t* __restrict__ scales, int64_t units,
+                                                                int shift, uint4* __restrict__ out) {
+    const int64_t u = (int64_t)blockIdx.x * kExpandThreads + threadIdx.x;
+    if (u < units) out[u] = expand8<KIND>(q[u], scales[u >> shift]);
+}
+
+template <Kind KIND>
+int expand(const uint8_t* q, const uint8_t* scales, int64_t n, int64_t k, int block, void* out, hipStream_t stream) {
+    const int64_t units = n * (k / 8), groups = ceil_div(units, kExpandThreads);
+    if (units == 0) return NVFP4_OK;
+    if (groups > 0x7FFFFFFF) return NVFP4_ERR_SHAPE;
+    int shift = 1;
+    while (8 << shift < block) ++shift;
+    hipLaunchKernelGGL((expand_kernel<KIND>), dim3((unsigned)groups), dim3(kExpandThreads), 0, stream,
+                       reinterpret_cast<const uint32_t*>(q), scales, units, shift, static_cast<uint4*>(out));
+    return launched();
+}
+
+bool valid_out(int dtype) { return dtype == NVFP4_IN_F32 || dtype == NVFP4_IN_BF16; }
+
+// ---- y = x W^T ------------------------------------------------------------------------------
+
+int64_t linear_workspace(int64_t m, int64_t n, int64_t k) {
+    (void)m;
+    return up(n * k * 2, 256);
+}
+
+int run_linear(const void* x, int64_t ldx, const uint8_t* q, const uint8_t* scales, int block, const float* S,
+               int64_t m, int64_t n, int64_t k, int out_dtype, void* out, void* ws, hipStream_t stream) {
+    if (const int rc = expand<kBf16>(q, scales, n, k, block, ws, stream)) return rc;
+    Args p = {};
+    p.a.p = static_cast<const char*>(x), p.a.ld = ldx * 2;
+    p.b.p = static_cast<const char*>(ws), p.b.ld = k * 2;
+    p.m = m, p.n = n, p.inner = k, p.scale = S, p.out = out, p.out_ld = n, p.out_f32 = out_dtype == NVFP4_IN_F32;
+    return launch_product<kBf16, kAlong, kAlong, kSingle, kSums, Big>(p, stream);
+}
+
+// ---- dx = dy W ------------------------------------------------------------------------------
+
+int64_t grad_workspace(int64_t m, int64_t n, int64_t k32, int64_t ld) {
+    Carver c{nullptr};
+    c.take(n * k32 * 2);
+    if (needs_pack(n, ld)) c.take(m * packed_ld(n) * 2);
+    return c.at;
+}
+
+// k32: the width of the weights' rows (k filled up to whole blocks); dx has k columns.
+template <Kind KIND>
+int run_grad(const void* dy, int64_t ld, const uint8_t* q, const uint8_t* scales, int block, const float* S, int64_t m,
+             int64_t n, int64_t k, int64_t k32, int out_dtype, void* out, void* ws, hipStream_t stream) {
+    Carver c{static_cast<char*>(ws)};
+    void* w = c.take(n * k32 * 2);
+    if (const int rc = expand<KIND>(q, scales, n, k32, block, w, stream)) return rc;
+    if (needs_pack(n, ld)) {
+        void* packed = c.take(m * packed_ld(n) * 2);
+        if (const int rc = pack_bf16_rows(dy, m, n, ld, packed, stream)) return rc;
+        dy = packed, ld = packed_ld(n);
+    }
+    Args p = {};
+    p.a.p = static_cast<const char*>(dy), p.a.ld = ld * 2;
+    p.b.p = static_cast<const char*>(w), p.b.ld = k32 * 2;
+    p.m = m, p.n = k, p.inner = n, p.scale = S, p.out = out, p.out_ld = k, p.out_f32 = out_dtype == NVFP4_IN_F32;
+    return launch_product<kBf16, kAlong, kAcross, kSingle, kSums, Big>(p, stream);
+}
+
+// ---- y = A B^T, both microscaled --------------------------------------------------------------
+
+// The tiles read a row's scales four at a time: rows of another width are copied to one of eights.
+int64_t mx_workspace(int64_t m, int64_t n, int64_t blocks) {
+    Carver c{nullptr};
+    if (blocks % 4) {
+        c.take(m * up(blocks, 8));
+        c.take(n * up(blocks, 8));
+    }
+    return c.at;
+}
+
+int run_mx(const uint8_t* aq, const uint8_t* as, const uint8_t* bq, const uint8_t* bs, int64_t m, int64_t n,
+           int64_t blocks, int out_dtype, void* out, void* ws, hipStream_t stream) {
+    int64_t scale_ld = blocks;
+    if (blocks % 4) {
+        Carver c{static_cast<char*>(ws)};
+        scale_ld = up(blocks, 8);
+        uint8_t* pa = static_cast<uint8_t*>(c.take(m * scale_ld));
+        uint8_t* pb = static_cast<uint8_t*>(c.take(n * scale_ld));
+        if (const int rc = pack_scale_rows(as, m, blocks, pa, scale_ld, stream)) return rc;
+        if (const int rc = pack_scale_rows(bs, n, blocks, pb, scale_ld, stream)) return rc;
+        as = pa, bs = pb;
+    }
+    Args p = {};
+    p.a.p = reinterpret_cast<const char*>(aq), p.a.ld = blocks * 16, p.a.scales = as, p.a.scale_ld = scale_ld;
+    p.b.p = reinterpret_cast<const char*>(bq), p.b.ld = blocks * 16, p.b.scales = bs, p.b.scale_ld = scale_ld;
+    p.m = m, p.n = n, p.inner = blocks * 32, p.out = out, p.out_ld = n, p.out_f32 = out_dtype == NVFP4_IN_F32;
+    return launch_product<kMx, kAlong, kAlong, kSingle, kSums, Big>(p, stream);
+}
+
+int check_ws(const void* ws, size_t bytes, int64_t need) {
+    if (need > 0 && (!ws || (int64_t)bytes < need)) return NVFP4_ERR_WORKSPACE;
+    return aligned(ws, 256) || need == 0 ? NVFP4_OK : NVFP4_ERR_ALIGN;
+}
+
+int check_nvfp4(int64_t m, int64_t n, int64_t k, int block) {
+    if (block != 16 && block != 32 && block != 64 && block != 128) return NVFP4_ERR_BLOCK;
+    if (const int rc = check_dims(m, n, k)) return rc;
+    return k % block ? NVFP4_ERR_SHAPE : NVFP4_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t nvfp4_matmul_workspace_bytes(int64_t m, int64_t n, int64_t k) {
+    if (const int rc = check_dims(m, n, k)) return rc;
+    return linear_workspace(m, n, k);
+}
+
+int nvfp4_matmul(const void* x, int64_t ldx, const uint8_t* q, const uint8_t* scales, int block,
+                 const float* tensor_scale, int64_t m, int64_t n, int64_t k, int out_dtype, void* out, void* workspace,
+                 size_t workspace_bytes, void* stream) {
+    if (!valid_out(out_dtype)) return NVFP4_ERR_DTYPE;
+    if (const int rc = check_nvfp4(m, n, k, block)) return rc;
+    if (ldx < k || ldx > kMaxLd) return NVFP4_ERR_SHAPE;
+    if (m == 0 || n == 0) return NVFP4_OK;
+    if (!out || !tensor_scale || (k > 0 && (!x || !q || !scales))) return NVFP4_ERR_NULL;
+    if (!aligned(x, 16) || ldx % 8 || !aligned(q, 16) || !aligned(out, 16) || !aligned(tensor_scale, 4))
+        return NVFP4_ERR_ALIGN;
+    if (const int rc = check_ws(workspace, workspace_bytes, linear_workspace(m, n, k))) return rc;
+    return run_linear(x, ldx, q, scales, block, tensor_scale, m, n, k, out_dtype, out, workspace, (hipStream_t)stream);
+}
+
+int64_t nvfp4_matmul_grad_input_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t ld) {
+    if (const int rc = check_dims(m, n, k)) return rc;
+    return grad_workspace(m, n, k, ld);
+}
+
+int nvfp4_matmul_grad_input(const void* dy, int64_t ld, const uint8_t* q, const uint8_t* scales, int block,
+                            const float* tensor_scale, int64_t m, int64_t n, int64_t k, int out_dtype, void* dx,
+                            void* workspace, size_t workspace_bytes, void* stream) {
+    if (!valid_out(out_dtype)) return NVFP4_ERR_DTYPE;
+    if (const int rc = check_nvfp4(m, n, k, block)) return rc;
+    if (ld < n || ld > kMaxLd) return NVFP4_ERR_SHAPE;
+    if (m == 0 || k == 0) return NVFP4_OK;
+    if (!dx || !tensor_scale || (n > 0 && (!dy || !q || !scales))) return NVFP4_ERR_NULL;
+    if (!aligned(dy, 16) || !aligned(q, 16) || !aligned(dx, 16) || !aligned(tensor_scale, 4)) return NVFP4_ERR_ALIGN;
+    if (const int rc = check_ws(workspace, workspace_bytes, grad_workspace(m, n, k, ld))) return rc;
+    return run_grad<kBf16>(dy, ld, q, scales, block, tensor_scale, m, n, k, k, out_dtype, dx, workspace,
+                           (hipStream_t)stream);
+}
+
+int64_t mxfp4_matmul_workspace_bytes(int64_t m, int64_t n, int64_t k) {
+    if (const int rc = check_dims(m, n, k)) return rc;
+    return mx_workspace(m, n, ceil_div(k, 32));
+}
+
+int mxfp4_matmul(const uint8_t* a_q, const uint8_t* a_scales, const uint8_t* b_q, const uint8_t* b_scales, int64_t m,
+                 int64_t n, int64_t k, int out_dtype, void* out, void* workspace, size_t workspace_bytes,
+                 void* stream) {
+    if (!valid_out(out_dtype)) return NVFP4_ERR_DTYPE;
+    if (const int rc = check_dims(m, n, k)) return rc;
+    if (m == 0 || n == 0) return NVFP4_OK;
+    if (!out || (k > 0 && (!a_q || !a_scales || !b_q || !b_scales))) return NVFP4_ERR_NULL;
+    if (!aligned(a_q, 16) || !aligned(b_q, 16) || !aligned(a_scales, 4) || !aligned(b_scales, 4) || !aligned(out, 16))
+        return NVFP4_ERR_ALIGN;
+    const int64_t blocks = ceil_div(k, 32);
+    if (const int rc = check_ws(workspace, workspace_bytes, mx_workspace(m, n, blocks))) return rc;
+    return run_mx(a_q, a_scales, b_q, b_scales, m, n, blocks, out_dtype, out, workspace, (hipStream_t)stream);
+}
+
+int64_t mxfp4_matmul_grad_input_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t ld) {
+    if (const int rc = check_dims(m, n, k)) return rc;
+    return grad_workspace(m, n, up(k, 32), ld);
+}
+
+int mxfp4_matmul_grad_input(const void* dy, int64_t ld, const uint8_t* q, const uint8_t* scales, int64_t m, int64_t n,
+                            int64_t k, int out_dtype, void* dx, void* workspace, size_t workspace_bytes,
+                            void* stream) {
+    if (!valid_out(out_dtype)) return NVFP4_ERR_DTYPE;
+    if (const int rc = check_dims(m, n, k)) return rc;
+    if (ld < n || ld > kMaxLd) return NVFP4_ERR_SHAPE;
+    if (m == 0 || k == 0) return NVFP4_OK;
+    if (!dx || (n > 0 && (!dy || !q || !scales))) return NVFP4_ERR_NULL;
+    if (!aligned(dy, 16) || !aligned(q, 16) || !aligned(dx, 16)) return NVFP4_ERR_ALIGN;
+    if (const int rc = check_ws(workspace, workspace_bytes, grad_workspace(m, n, up(k, 32), ld))) return rc;
+    return run_grad<kMx>(dy, ld, q, scales, 32, nullptr, m, n, k, up(k, 32), out_dtype, dx, workspace,
+                         (hipStream_t)stream);
+}
+
+}  // extern "C"

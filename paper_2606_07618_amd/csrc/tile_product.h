@@ -1,0 +1,368 @@
+// Tiled matrix product on the matrix cores of gfx950, D[m][n] = sum_k A[m][k] B[n][k], sums in
+// binary32, for bfloat16 operands and for microscaled FP4 ones (E2M1 nibbles with an E8M0 scale
+// for each 32 values of a row).  The kernels built from it differ in where their operands lie and
+// in what is done with the sums; both are template arguments.
+//
+// Both element types share one geometry: a step takes 128 bytes of every row of the tile (64
+// bfloat16 values, 256 FP4 ones), and a lane's operand of one matrix instruction is 16 of them (8
+// values of 16x16x32, 32 of 16x16x128), so staging, LDS layout and register tiles are the same.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <stdint.h>
+
+namespace tile_product {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((address_space(3))) char lds_char;
+
+constexpr int kLanes = 64;
+constexpr int kStepBytes = 128;                  // of a row, a step of the contraction
+constexpr int kChunk = 16;                       // bytes of a lane's load
+constexpr uint32_t kOutside = 0x80000000u;       // an offset that the buffer's size excludes: reads as zero
+
+// A window of 2 GiB from `base`: loads at offsets of kOutside and up return zero without an access.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t window(const void* base) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, (int)kOutside, 0x00020000);
+}
+
+template <int V> struct Const { static constexpr int value = V; };
+
+enum Kind { kBf16, kMx };
+// How an operand lies in memory: its rows hold the contraction (kAlong), or the contraction runs down
+// its rows and a row holds the operand's outer index (kAcross; bfloat16 only).
+enum Layout { kAlong, kAcross };
+
+struct Operand {
+    const char* p;              // element (0, 0)
+    const char* p2;             // the second matrix of a pair (see Pair)
+    int64_t ld;                 // bytes from row to row
+    const uint8_t* scales;      // microscaled: E8M0 codes [outer, scale_ld]
+    int64_t scale_ld;
+};
+
+// Where operand B is two matrices.  kPairOuter: the tile's outer indexes are taken half from each, so
+// that both products of one output meet in one lane.  kPairInner: the contraction runs over the first,
+// then over the second.
+enum Pair { kSingle, kPairOuter, kPairInner };
+
+__device__ __forceinline__ float silu(float g) {
+    // g / (1 + e^-g): e^-g overflows to infinity below -88, where the quotient's reciprocal is zero.
+    const float e = __builtin_amdgcn_exp2f(g * -1.44269504f);
+    return g * __builtin_amdgcn_rcpf(1.0f + e);
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+    bf16x2 v = {(__bf16)a, (__bf16)b};
+    return __builtin_bit_cast(uint32_t, v);
+}
+
+// The sequence of tiles: workgroups go to the eight XCDs in turn, so each XCD gets a contiguous run of
+// the sequence, and the sequence walks kGroup tile rows at a time: what an XCD works on at one time shares
+// rows of A and of B in its L2.
+constexpr int kXcds = 8, kGroup = 8;
+struct TileIndex { int64_t m, n; };
+__device__ __forceinline__ TileIndex tile_of(int64_t id, int64_t count, int64_t tiles_m, int64_t tiles_n) {
+    const int64_t xcd = id % kXcds, each = count / kXcds, rest = count % kXcds;
+    const int64_t seq = xcd * each + (xcd < rest ? xcd : rest) + id / kXcds;
+    const int64_t per_group = kGroup * tiles_n;
+    const int64_t first = seq / per_group * kGroup;
+    const int64_t height = tiles_m - first < kGroup ? tiles_m - first : kGroup;
+    const int64_t in = seq % per_group;
+    return {first + in % height, in / height};
+}
+
+// One operand's side of a tile: R outer indexes, staged by THREADS threads.
+template <Kind KIND, Layout LAYOUT, int R, int THREADS, bool HALF>
+struct Side {
+    static_assert(LAYOUT == kAlong || KIND == kBf16, "microscaled operands lie along their rows");
+    static constexpr int kBytes = R * kStepBytes;
+    static constexpr int kLoads = kBytes / (THREADS * kChunk);
+    static_assert(kBytes % (THREADS * kChunk) == 0, "whole loads");
+    static constexpr int kRowChunks = LAYOUT == kAlong ? kStepBytes / kChunk : R / 8;
+    // what a step takes of the contraction: bytes of a row, or rows
+    static constexpr int kFull = LAYOUT == kAlong ? kStepBytes : kStepBytes / 2;
+    static constexpr int kScaleLoads = (R * 2 + THREADS - 1) / THREADS;
+    static constexpr int kScaleBytes = KIND == kMx ? R * 8 : 0;
+
+    // LDS holds a step as rows of chunks.  A chunk's place in its row is exchanged by the row, so that
+    // the lanes of a read hit all banks: along, 16 lanes read one chunk of 16 rows, and the row's
+    // parity and the exchanged place cover the 256 bytes of the banks; across, 32 lanes read 8
+    // contraction rows by 32 bytes, and the place of a 32-byte unit is exchanged by those rows.
+    __device__ static __forceinline__ int exchange(int row) {
+        if constexpr (LAYOUT == kAlong) return (row >> 1) & 7;
+        constexpr int kUnits = R / 16 < 8 ? R / 16 : 8;
+        return (((row & 3) | (((row >> 3) & 1) << 2)) & (kUnits - 1)) << 1;
+    }
+
+    uint32_t offset[kLoads];             // of this thread's loads from the step's base
+    uint32_t scale_offset[kScaleLoads];
+
+    // left: the outer indexes from the tile's first one on.  With HALF, rows from R / 2 on are the same
+    // outer indexes of the second matrix.
+    __device__ __forceinline__ void init(int64_t left, int64_t ld, int64_t scale_ld, int tid) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int id = i * THREADS + tid, row = id / kRowChunks;
+            const int chunk = (id % kRowChunks) ^ exchange(row);
+            const int r = HALF ? row % (R / 2) : row;
+            const bool in = LAYOUT == kAlong ? r < left : chunk * 8 < left;
+            offset[i] = in ? (uint32_t)r * (uint32_t)ld + chunk * kChunk : kOutside;
+        }
+        if constexpr (KIND == kMx) {
+#pragma unroll
+            for (int i = 0; i < kScaleLoads; ++i) {
+                const int id = i * THREADS + tid, row = id / 2;
+                scale_offset[i] = row < left ? (uint32_t)row * (uint32_t)scale_ld + id % 2 * 4 : kOutside;
+            }
+        }
+    }
+
+    // Starts the loads of one step into LDS.  ahead: what is left of the contraction from the step's
+    // first value on, in units of kFull; beyond it LDS gets zeros.
+    __device__ __forceinline__ void load(const char* base, const char* base2, char* lds, int64_t ahead, int tid,
+                                         int wave) const {
+        const __amdgpu_buffer_rsrc_t w = window(base), w2 = HALF ? window(base2) : w;
+        const bool whole = ahead >= kFull;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const bool second = HALF && i * THREADS / kRowChunks >= R / 2;
+            uint32_t off = offset[i];
+            if (!whole) {
+                const int id = i * THREADS + tid, row = id / kRowChunks;
+                const int at = LAYOUT == kAlong ? ((id % kRowChunks) ^ exchange(row)) * kChunk : row;
+                if (at >= ahead) off = kOutside;
+            }
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(second ? w2 : w,
+                                                     (lds_void*)(lds + (i * THREADS + wave * kLanes) * kChunk), kChunk,
+                                                     (int)off, 0, 0, 0);
+        }
+    }
+
+    // The step's scales, 8 bytes a row (microscaled).  ahead: the row's scales from the step's first one on.
+    __device__ __forceinline__ void load_scales(const uint8_t* base, char* lds, int64_t ahead, int tid,
+                                                int wave) const {
+        const __amdgpu_buffer_rsrc_t w = window(base);
+#pragma unroll
+        for (int i = 0; i < kScaleLoads; ++i) {
+            if (i * THREADS + wave * kLanes >= R * 2) break;
+            const uint32_t off = tid % 2 * 4 < ahead ? scale_offset[i] : kOutside;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(w, (lds_void*)(lds + (i * THREADS + wave * kLanes) * 4), 4,
+                                                     (int)off, 0, 0, 0);
+        }
+    }
+
+    // This lane's 16 bytes of the operand at outer indexes row0 .. row0 + 15 of the tile, half KK of the step.
+    // bfloat16: values 32 KK + 8 (lane / 16) on.  Microscaled: the 32-value block 2 (lane / 16) + KK, so that
+    // the two halves' scales are neighbours.
+    template <int KK>
+    __device__ static __forceinline__ i32x4 read(const char* lds, int row0, int lane) {
+        const int g = lane / 16, i = lane % 16;
+        if constexpr (LAYOUT == kAlong) {
+            const int row = row0 + i, chunk = KIND == kMx ? 2 * g + KK : 4 * KK + g;
+            return *reinterpret_cast<const i32x4*>(lds + row * kStepBytes + ((chunk ^ exchange(row)) * kChunk));
+        } else {
+            // ds_read_b64_tr_b16: 16 lanes read four rows of 16 values, four each, and get a column each
+            const int row = 32 * KK + 8 * g + (i >> 2);
+            const int unit = (row0 / 16) ^ (exchange(row) >> 1);
+            const char* at = lds + row * (R * 2) + unit * 32 + (i & 3) * 8;
+            typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 4 * R * 2));
+            return __builtin_bit_cast(i32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+    }
+};
+
+// Workgroup tile M_ x N_ by WM x WN waves.
+template <int M_, int N_, int WM_, int WN_>
+struct Tile {
+    static constexpr int M = M_, N = N_, WM = WM_, WN = WN_, kThreads = WM_ * WN_ * kLanes;
+    static constexpr int MF = M_ / WM_ / 16, NF = N_ / WN_ / 16;     // a wave's matrix instructions
+};
+
+// What happens to the sums.
+enum Out {
+    kSums,        // scale * sum, as bfloat16 or binary32
+    kPartial,     // the sum of this part of the contraction, binary32, for a later reduction
+    kGate,        // silu(sum of the first matrix) * sum of the second, and both sums where asked for
+    kTwoRows      // rows below `half_rows` to the first output, those from there on to the second
+};
+
+struct Args {
+    Operand a, b;
+    int64_t m, n;               // outer indexes of A and of B (kPairOuter: of each of B's two)
+    int64_t inner;              // values of the contraction (kPairInner: of each of B's two)
+    int64_t steps, split_steps; // of the whole contraction, and of one part of it
+    int64_t tiles_m, tiles_n;
+    int parts;
+    int out_f32;
+    const float* scale;         // NULL: 1
+    void *out, *out2, *out3;
+    int64_t half_rows, out_rows;   // kTwoRows
+    int64_t out_ld;
+};
+
+__device__ __forceinline__ void store4(void* out, int f32, int64_t at, int64_t left, bool vec, f32x4 v) {
+    if (f32) {
+        float* o = static_cast<float*>(out) + at;
+        if (vec && left >= 4) { *reinterpret_cast<f32x4*>(o) = v; return; }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) if (r < left) o[r] = v[r];
+    } else {
+        const uint2 p = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+        uint16_t* o = static_cast<uint16_t*>(out) + at;
+        if (vec && left >= 4) { *reinterpret_cast<uint2*>(o) = p; return; }
+        if (left > 0) o[0] = (uint16_t)p.x;
+        if (left > 1) o[1] = (uint16_t)(p.x >> 16);
+        if (left > 2) o[2] = (uint16_t)p.y;
+        if (left > 3) o[3] = (uint16_t)(p.y >> 16);
+    }
+}
+
+template <Kind KIND, Layout LA, Layout LB, Pair PAIR, Out OUT, class T>
+__global__ __launch_bounds__(T::kThreads, 2) void product_kernel(Args p) {
+    constexpr bool HALF = PAIR == kPairOuter;
+    using A = Side<KIND, LA, T::M, T::kThreads, false>;
+    using B = Side<KIND, LB, T::N, T::kThreads, HALF>;
+    constexpr int kStage = A::kBytes + B::kBytes + A::kScaleBytes + B::kScaleBytes;
+    __shared__ __attribute__((aligned(1024))) char lds[2][kStage];
+    constexpr int kOutN = HALF ? T::N / 2 : T::N;          // output columns of a tile
+    constexpr int NF = T::NF, MF = T::MF;
+
+    const int tid = threadIdx.x, lane = tid % kLanes;
+    const int wave = __builtin_amdgcn_readfirstlane(tid / kLanes);
+    const int wm = wave / T::WN, wn = wave % T::WN;
+    const int64_t tiles = p.tiles_m * p.tiles_n;
+    const int64_t part = blockIdx.x / tiles;
+    const TileIndex t = tile_of(blockIdx.x % tiles, tiles, p.tiles_m, p.tiles_n);
+    const int64_t m0 = t.m * T::M, n0 = t.n * kOutN;
+    const int64_t s0 = part * p.split_steps;
+    const int64_t s1 = s0 + p.split_steps < p.steps ? s0 + p.split_steps : p.steps;
+
+    A sa;
+    B sb;
+    sa.init(p.m - m0, p.a.ld, p.a.scale_ld, tid);
+    sb.init(p.n - n0, p.b.ld, p.b.scale_ld, tid);
+    const char* a0 = p.a.p + (LA == kAlong ? m0 * p.a.ld : m0 * 2);
+    const int64_t b_at = LB == kAlong ? n0 * p.b.ld : n0 * 2;
+    const int64_t pair_steps = PAIR == kPairInner ? p.steps / 2 : p.steps;
+    auto fetch = [&](int64_t s, int stage) {
+        char* l = lds[stage];
+        constexpr int kElem = KIND == kMx ? 1 : 2;         // twice the values of a byte
+        const int64_t ia = LA == kAlong ? (p.inner * kElem >> (KIND == kMx ? 1 : 0)) : p.inner;
+        const int64_t sb_in = PAIR == kPairInner && s >= pair_steps ? s - pair_steps : s;
+        // kPairInner: A's rows hold both contractions one after the other, each filled up with zeros
+        const int64_t a_ahead = PAIR == kPairInner ? A::kFull : ia - s * A::kFull;
+        sa.load(a0 + (LA == kAlong ? s * kStepBytes : s * A::kFull * p.a.ld), nullptr, l, a_ahead, tid, wave);
+        const int64_t ib = LB == kAlong ? (p.inner * kElem >> (KIND == kMx ? 1 : 0)) : p.inner;
+        const int64_t step = LB == kAlong ? sb_in * kStepBytes : sb_in * B::kFull * p.b.ld;
+        const char* b = PAIR == kPairInner && s >= pair_steps ? p.b.p2 : p.b.p;
+        sb.load(b + b_at + step, HALF ? p.b.p2 + b_at + step : nullptr, l + A::kBytes, ib - sb_in * B::kFull, tid, wave);
+        if constexpr (KIND == kMx) {
+            const int64_t left = p.inner / 32 - s * 8;
+            sa.load_scales(p.a.scales + m0 * p.a.scale_ld + s * 8, l + A::kBytes + B::kBytes, left, tid, wave);
+            sb.load_scales(p.b.scales + n0 * p.b.scale_ld + s * 8, l + A::kBytes + B::kBytes + A::kScaleBytes, left,
+                           tid, wave);
+        }
+    };
+
+    // first rows of this wave's fragments in the tile
+    auto a_row = [&](int i) { return wm * (T::M / T::WM) + i * 16; };
+    auto b_row = [&](int j) {
+        if constexpr (!HALF) return wn * (T::N / T::WN) + j * 16;
+        return (j < NF / 2 ? 0 : T::N / 2) + wn * (T::N / 2 / T::WN) + j % (NF / 2) * 16;
+    };
+
+    f32x4 acc[MF][NF];
+#pragma unroll
+    for (int i = 0; i < MF; ++i)
+#pragma unroll
+        for (int j = 0; j < NF; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+
+    if (s0 < s1) fetch(s0, 0);
+    for (int64_t s = s0; s < s1; ++s) {
+        const int stage = (int)(s - s0) & 1;
+        __syncthreads();                 // the step has arrived, and the other stage has been read
+        if (s + 1 < s1) fetch(s + 1, stage ^ 1);
+        const char* la = lds[stage];
+        const char* lb = la + A::kBytes;
+        int xa[MF], xb[NF];
+        if constexpr (KIND == kMx) {
+            const char* ls = lb + B::kBytes + lane / 16 * 2;
+#pragma unroll
+            for (int i = 0; i < MF; ++i) xa[i] = *reinterpret_cast<const uint16_t*>(ls + (a_row(i) + lane % 16) * 8);
+#pragma unroll
+            for (int j = 0; j < NF; ++j)
+                xb[j] = *reinterpret_cast<const uint16_t*>(ls + A::kScaleBytes + (b_row(j) + lane % 16) * 8);
+        }
+        auto half = [&](auto kk) {
+            constexpr int KK = decltype(kk)::value;
+            i32x4 fb[NF];
+#pragma unroll
+            for (int j = 0; j < NF; ++j) fb[j] = B::template read<KK>(lb, b_row(j), lane);
+#pragma unroll
+            for (int i = 0; i < MF; ++i) {
+                const i32x4 fa = A::template read<KK>(la, a_row(i), lane);
+#pragma unroll
+                for (int j = 0; j < NF; ++j) {
+                    // B's values as the instruction's rows: a lane gets four neighbouring outputs of a row of D
+                    if constexpr (KIND == kBf16) {
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fb[j]),
+                                                                            __builtin_bit_cast(bf16x8, fa), acc[i][j], 0, 0, 0);
+                    } else {
+                        const i32x8 wb = {fb[j][0], fb[j][1], fb[j][2], fb[j][3], 0, 0, 0, 0};
+                        const i32x8 wa = {fa[0], fa[1], fa[2], fa[3], 0, 0, 0, 0};
+                        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wb, wa, acc[i][j], 4, 4, KK, xb[j],
+                                                                                     KK, xa[i]);
+                    }
+                }
+            }
+        };
+        half(Const<0>{});
+        half(Const<1>{});
+    }
+
+    const int mi = lane % 16, nj = lane / 16 * 4;
+    const bool vec = p.out_ld % 4 == 0;
+    const float scale = OUT == kSums && p.scale ? *p.scale : 1.0f;
+#pragma unroll
+    for (int i = 0; i < MF; ++i) {
+        const int64_t m = m0 + a_row(i) + mi;
+        if (m >= p.m) continue;
+#pragma unroll
+        for (int j = 0; j < (HALF ? NF / 2 : NF); ++j) {
+            const int64_t n = n0 + b_row(j) + nj, left = p.n - n;
+            if constexpr (OUT == kSums) {
+                store4(p.out, p.out_f32, m * p.out_ld + n, left, vec, acc[i][j] * scale);
+            } else if constexpr (OUT == kPartial) {
+                store4(p.out, 1, (part * p.m + m) * p.out_ld + n, left, vec, acc[i][j]);
+            } else if constexpr (OUT == kTwoRows) {
+                const int64_t row = m < p.half_rows ? m : m - p.half_rows;
+                if (row < p.out_rows)
+                    store4(m < p.half_rows ? p.out : p.out2, 0, row * p.out_ld + n, left, vec, acc[i][j]);
+            } else {
+                const f32x4 g = acc[i][j], u = acc[i][NF / 2 + j];
+                f32x4 h;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) h[r] = silu(g[r]) * u[r];
+                store4(p.out, 0, m * p.out_ld + n, left, vec, h);
+                if (p.out2) {
+                    store4(p.out2, 0, m * p.out_ld + n, left, vec, g);
+                    store4(p.out3, 0, m * p.out_ld + n, left, vec, u);
+                }
+            }
+        }
+    }
+}
+
+}  // namespace tile_product

@@ -58,6 +58,20 @@ def _load():
         "nvfp4_channel_sq_norms": (I, [P, I, I64, I64, I64, I64, I64, I64, P, P, SZ, P]),
         "nvfp4_ldlq_workspace_bytes": (SZ, [I64, I64]),
         "nvfp4_ldlq": (I, [P, I, I64, I64, I, P, P, P, ctypes.c_double, P, P, P, SZ, P]),
+        "mxfp4_quant": (I, [P, I, I64, I64, P, P, P]),
+        "mxfp4_dequant": (I, [P, P, I64, I64, I, P, P]),
+        "mxfp4_matmul_workspace_bytes": (I64, [I64, I64, I64]),
+        "mxfp4_matmul": (I, [P, P, P, P, I64, I64, I64, I, P, P, SZ, P]),
+        "mxfp4_matmul_grad_input_workspace_bytes": (I64, [I64, I64, I64, I64]),
+        "mxfp4_matmul_grad_input": (I, [P, I64, P, P, I64, I64, I64, I, P, P, SZ, P]),
+        "nvfp4_matmul_workspace_bytes": (I64, [I64, I64, I64]),
+        "nvfp4_matmul": (I, [P, I64, P, P, I, P, I64, I64, I64, I, P, P, SZ, P]),
+        "nvfp4_matmul_grad_input_workspace_bytes": (I64, [I64, I64, I64, I64]),
+        "nvfp4_matmul_grad_input": (I, [P, I64, P, P, I, P, I64, I64, I64, I, P, P, SZ, P]),
+        "nvfp4_swiglu_ffn_workspace_bytes": (I64, [I64, I64, I64, I64, I64]),
+        "nvfp4_swiglu_ffn": (I, [P, I64, P, P, I64, I64, I64, I64, P, P, P, P, SZ, P]),
+        "nvfp4_swiglu_ffn_backward_workspace_bytes": (I64, [I64, I64, I64, I64, I64]),
+        "nvfp4_swiglu_ffn_backward": (I, [P, P, I64, P, P, I64, P, P, I64, I64, I64, P, P, P, P, SZ, P]),
     }
     for name, (res, args) in sigs.items():
         fn = getattr(L, name)
