@@ -3,6 +3,7 @@
 //   s = 1 / (1 + e^-g),  dg = dh u s (1 + g (1 - s)),  du = dh g s,
 //   dx = dg Wg + du Wu,  dWg = dg^T x,  dWu = du^T x.
 #include "product_host.h"
+#include "thin_product.h"
 
 namespace {
 
@@ -122,6 +123,14 @@ int nvfp4_swiglu_ffn(const void* x, int64_t ldx, const void* w_gate, const void*
     if (const int rc = packed(c, rx, m, k, needs_pack(k, ldx), st)) return rc;
     if (const int rc = packed(c, rg, n, k, pw, st)) return rc;
     if (const int rc = packed(c, ru, n, k, pw, st)) return rc;
+    if (m <= thin_product::kRows) {
+        thin_product::Args t = {};
+        t.w = static_cast<const char*>(rg.p), t.w2 = static_cast<const char*>(ru.p), t.ldw = rg.ld * 2;
+        t.x = static_cast<const char*>(rx.p), t.ldx = rx.ld * 2, t.m = (int)m, t.n = n, t.k = k;
+        t.out = h, t.out2 = gate, t.out3 = up_out;
+        thin_product::launch_thin<thin_product::kGated, 8, 4, true>(t, st);
+        return launched();
+    }
     Args p = {};
     p.a.p = static_cast<const char*>(rx.p), p.a.ld = rx.ld * 2;
     p.b.p = static_cast<const char*>(rg.p), p.b.p2 = static_cast<const char*>(ru.p), p.b.ld = rg.ld * 2;

@@ -2,6 +2,7 @@
 //   NVFP4 weights W = q s S [n, k], activations in bfloat16:  y = x W^T,  dx = dy W
 //   microscaled FP4 (E8M0 scale for each 32 values):          y = A B^T,  dx = dy B
 #include "product_host.h"
+#include "thin_product.h"
 
 namespace product_host {
 
@@ -51,11 +52,6 @@ using Big = Tile<256, 256, 2, 4>;
 // q s of NVFP4 (without S) or q 2^E of microscaled FP4, 8 values a lane, both exact: an E2M1 value has
 // two significand bits and an E4M3 scale four, bfloat16 eight (values below 2^-133 aside, which only
 // microscaled blocks of codes under 2 hold).
-__device__ __forceinline__ float e4m3_f32(uint32_t c) {
-    // the field as a binary32 number scaled by 2^-120, made whole by one exact product
-    return __uint_as_float((c & 0x7Fu) << 20) * 0x1p120f;
-}
-
 template <Kind KIND>
 __device__ __forceinline__ uint4 expand8(uint32_t n, uint32_t code) {
     f32x2 d[4];
@@ -67,11 +63,7 @@ __device__ __forceinline__ uint4 expand8(uint32_t n, uint32_t code) {
         d[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(n, s, 3);
         if (code == 255) d[0] = d[1] = d[2] = d[3] = f32x2{__uint_as_float(0x7FC00000u), __uint_as_float(0x7FC00000u)};
     } else {
-        const float s = e4m3_f32(code);
-        d[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(n, 1.0f, 0) * s;
-        d[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(n, 1.0f, 1) * s;
-        d[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(n, 1.0f, 2) * s;
-        d[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(n, 1.0f, 3) * s;
+        return __builtin_bit_cast(uint4, thin_product::expand8(n, thin_product::e4m3_f32(code)));
     }
     return make_uint4(pack_bf16(d[0][0], d[0][1]), pack_bf16(d[1][0], d[1][1]), pack_bf16(d[2][0], d[2][1]),
                       pack_bf16(d[3][0], d[3][1]));
@@ -105,12 +97,21 @@ bool valid_out(int dtype) { return dtype == NVFP4_IN_F32 || dtype == NVFP4_IN_BF
 // ---- y = x W^T ------------------------------------------------------------------------------
 
 int64_t linear_workspace(int64_t m, int64_t n, int64_t k) {
-    (void)m;
-    return up(n * k * 2, 256);
+    return m <= thin_product::kRows ? 0 : up(n * k * 2, 256);
 }
 
 int run_linear(const void* x, int64_t ldx, const uint8_t* q, const uint8_t* scales, int block, const float* S,
                int64_t m, int64_t n, int64_t k, int out_dtype, void* out, void* ws, hipStream_t stream) {
+    if (m <= thin_product::kRows) {
+        thin_product::Args t = {};
+        t.w = reinterpret_cast<const char*>(q), t.ldw = k / 2, t.w_scales = scales, t.w_scale_ld = k / block;
+        t.x = static_cast<const char*>(x), t.ldx = ldx * 2, t.m = (int)m, t.n = n, t.k = k;
+        t.shift = block == 16 ? 4 : block == 32 ? 5 : block == 64 ? 6 : 7;
+        t.scale = S, t.out = out, t.out_f32 = out_dtype == NVFP4_IN_F32;
+        if (k % 32 == 0) thin_product::launch_thin<thin_product::kNvfp4, 8, 2, true>(t, stream);
+        else thin_product::launch_thin<thin_product::kNvfp4, 8, 2, false>(t, stream);
+        return launched();
+    }
     if (const int rc = expand<kBf16>(q, scales, n, k, block, ws, stream)) return rc;
     Args p = {};
     p.a.p = static_cast<const char*>(x), p.a.ld = ldx * 2;
@@ -152,7 +153,7 @@ int run_grad(const void* dy, int64_t ld, const uint8_t* q, const uint8_t* scales
 // The tiles read a row's scales four at a time: rows of another width are copied to one of eights.
 int64_t mx_workspace(int64_t m, int64_t n, int64_t blocks) {
     Carver c{nullptr};
-    if (blocks % 4) {
+    if (blocks % 4 && m > thin_product::kRows) {
         c.take(m * up(blocks, 8));
         c.take(n * up(blocks, 8));
     }
@@ -161,6 +162,14 @@ int64_t mx_workspace(int64_t m, int64_t n, int64_t blocks) {
 
 int run_mx(const uint8_t* aq, const uint8_t* as, const uint8_t* bq, const uint8_t* bs, int64_t m, int64_t n,
            int64_t blocks, int out_dtype, void* out, void* ws, hipStream_t stream) {
+    if (m <= thin_product::kRows) {
+        thin_product::Args t = {};
+        t.w = reinterpret_cast<const char*>(bq), t.ldw = blocks * 16, t.w_scales = bs, t.w_scale_ld = blocks;
+        t.x = reinterpret_cast<const char*>(aq), t.ldx = blocks * 16, t.x_scales = as, t.m = (int)m, t.n = n, t.k = blocks * 32;
+        t.out = out, t.out_f32 = out_dtype == NVFP4_IN_F32;
+        thin_product::launch_thin<thin_product::kMicroscaled, 8, 4, true>(t, stream);
+        return launched();
+    }
     int64_t scale_ld = blocks;
     if (blocks % 4) {
         Carver c{static_cast<char*>(ws)};
