@@ -5,7 +5,7 @@
 //
 // Both element types share one geometry: a step takes 128 bytes of every row of the tile (64
 // bfloat16 values, 256 FP4 ones), and a lane's operand of one matrix instruction is 16 of them (8
-// values of 16x16x32, 32 of 16x16x128), so staging, LDS layout and register tiles are the same.
+// values of 32x32x16, 32 of 32x32x64), so staging, LDS layout and register tiles are the same.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -15,6 +15,7 @@
 namespace tile_product {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -27,6 +28,7 @@ typedef __attribute__((address_space(3))) char lds_char;
 
 constexpr int kLanes = 64;
 constexpr int kStepBytes = 128;                  // of a row, a step of the contraction
+constexpr int kQuarters = kStepBytes / 32;      // matrix instructions a step along the contraction
 constexpr int kChunk = 16;                       // bytes of a lane's load
 constexpr uint32_t kOutside = 0x80000000u;       // an offset that the buffer's size excludes: reads as zero
 
@@ -66,6 +68,12 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
     return __builtin_bit_cast(uint32_t, v);
 }
 
+// All but this wave's last LEFT loads into LDS have arrived and its reads of LDS are done, then all waves'.
+template <int LEFT>
+__device__ __forceinline__ void arrive() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
+}
+
 // The sequence of tiles: workgroups go to the eight XCDs in turn, so each XCD gets a contiguous run of
 // the sequence, and the sequence walks kGroup tile rows at a time: what an XCD works on at one time shares
 // rows of A and of B in its L2.
@@ -91,25 +99,22 @@ struct Side {
     static constexpr int kRowChunks = LAYOUT == kAlong ? kStepBytes / kChunk : R / 8;
     // what a step takes of the contraction: bytes of a row, or rows
     static constexpr int kFull = LAYOUT == kAlong ? kStepBytes : kStepBytes / 2;
-    static constexpr int kScaleLoads = (R * 2 + THREADS - 1) / THREADS;
-    static constexpr int kScaleBytes = KIND == kMx ? R * 8 : 0;
 
     // LDS holds a step as rows of chunks.  A chunk's place in its row is exchanged by the row, so that
     // the lanes of a read hit all banks: along, 16 lanes read one chunk of 16 rows, and the row's
-    // parity and the exchanged place cover the 256 bytes of the banks; across, 32 lanes read 8
-    // contraction rows by 32 bytes, and the place of a 32-byte unit is exchanged by those rows.
+    // parity and the exchanged place cover the 256 bytes of the banks; across, 32 lanes read four
+    // contraction rows by 64 bytes, and the place of a 64-byte unit is exchanged by those rows.
     __device__ static __forceinline__ int exchange(int row) {
         if constexpr (LAYOUT == kAlong) return (row >> 1) & 7;
-        constexpr int kUnits = R / 16 < 8 ? R / 16 : 8;
-        return (((row & 3) | (((row >> 3) & 1) << 2)) & (kUnits - 1)) << 1;
+        constexpr int kUnits = R / 32 < 4 ? R / 32 : 4;
+        return (row & (kUnits - 1)) << 2;
     }
 
     uint32_t offset[kLoads];             // of this thread's loads from the step's base
-    uint32_t scale_offset[kScaleLoads];
 
     // left: the outer indexes from the tile's first one on.  With HALF, rows from R / 2 on are the same
     // outer indexes of the second matrix.
-    __device__ __forceinline__ void init(int64_t left, int64_t ld, int64_t scale_ld, int tid) {
+    __device__ __forceinline__ void init(int64_t left, int64_t ld, int tid) {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int id = i * THREADS + tid, row = id / kRowChunks;
@@ -118,13 +123,6 @@ struct Side {
             const bool in = LAYOUT == kAlong ? r < left : chunk * 8 < left;
             offset[i] = in ? (uint32_t)r * (uint32_t)ld + chunk * kChunk : kOutside;
         }
-        if constexpr (KIND == kMx) {
-#pragma unroll
-            for (int i = 0; i < kScaleLoads; ++i) {
-                const int id = i * THREADS + tid, row = id / 2;
-                scale_offset[i] = row < left ? (uint32_t)row * (uint32_t)scale_ld + id % 2 * 4 : kOutside;
-            }
-        }
     }
 
     // Starts the loads of one step into LDS.  ahead: what is left of the contraction from the step's
@@ -132,49 +130,33 @@ struct Side {
     __device__ __forceinline__ void load(const char* base, const char* base2, char* lds, int64_t ahead, int tid,
                                          int wave) const {
         const __amdgpu_buffer_rsrc_t w = window(base), w2 = HALF ? window(base2) : w;
-        const bool whole = ahead >= kFull;
+        const int left = ahead > kFull ? kFull : ahead > 0 ? (int)ahead : 0;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const bool second = HALF && i * THREADS / kRowChunks >= R / 2;
-            uint32_t off = offset[i];
-            if (!whole) {
-                const int id = i * THREADS + tid, row = id / kRowChunks;
-                const int at = LAYOUT == kAlong ? ((id % kRowChunks) ^ exchange(row)) * kChunk : row;
-                if (at >= ahead) off = kOutside;
-            }
+            const int id = i * THREADS + tid, row = id / kRowChunks;
+            const int at = LAYOUT == kAlong ? ((id % kRowChunks) ^ exchange(row)) * kChunk : row;
+            const uint32_t off = at < left ? offset[i] : kOutside;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(second ? w2 : w,
                                                      (lds_void*)(lds + (i * THREADS + wave * kLanes) * kChunk), kChunk,
                                                      (int)off, 0, 0, 0);
         }
     }
 
-    // The step's scales, 8 bytes a row (microscaled).  ahead: the row's scales from the step's first one on.
-    __device__ __forceinline__ void load_scales(const uint8_t* base, char* lds, int64_t ahead, int tid,
-                                                int wave) const {
-        const __amdgpu_buffer_rsrc_t w = window(base);
-#pragma unroll
-        for (int i = 0; i < kScaleLoads; ++i) {
-            if (i * THREADS + wave * kLanes >= R * 2) break;
-            const uint32_t off = tid % 2 * 4 < ahead ? scale_offset[i] : kOutside;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(w, (lds_void*)(lds + (i * THREADS + wave * kLanes) * 4), 4,
-                                                     (int)off, 0, 0, 0);
-        }
-    }
-
-    // This lane's 16 bytes of the operand at outer indexes row0 .. row0 + 15 of the tile, half KK of the step.
-    // bfloat16: values 32 KK + 8 (lane / 16) on.  Microscaled: the 32-value block 2 (lane / 16) + KK, so that
-    // the two halves' scales are neighbours.
-    template <int KK>
+    // This lane's 16 bytes of the operand at outer indexes row0 .. row0 + 31 of the tile, quarter Q of the step.
+    // bfloat16: values 16 Q + 8 (lane / 32) on.  Microscaled: the 32-value block 4 (lane / 32) + Q, so that the
+    // quarters' scales are the bytes of one word.
+    template <int Q>
     __device__ static __forceinline__ i32x4 read(const char* lds, int row0, int lane) {
-        const int g = lane / 16, i = lane % 16;
+        const int g = lane / 32;
         if constexpr (LAYOUT == kAlong) {
-            const int row = row0 + i, chunk = KIND == kMx ? 2 * g + KK : 4 * KK + g;
+            const int row = row0 + lane % 32, chunk = KIND == kMx ? kQuarters * g + Q : 2 * Q + g;
             return *reinterpret_cast<const i32x4*>(lds + row * kStepBytes + ((chunk ^ exchange(row)) * kChunk));
         } else {
             // ds_read_b64_tr_b16: 16 lanes read four rows of 16 values, four each, and get a column each
-            const int row = 32 * KK + 8 * g + (i >> 2);
-            const int unit = (row0 / 16) ^ (exchange(row) >> 1);
-            const char* at = lds + row * (R * 2) + unit * 32 + (i & 3) * 8;
+            const int i = lane % 16, row = 16 * Q + 8 * g + (i >> 2);
+            const int chunk = (row0 / 8 + lane / 16 % 2 * 2 + ((i & 3) >> 1)) ^ exchange(row);
+            const char* at = lds + row * (R * 2) + chunk * kChunk + (i & 1) * 8;
             typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
             const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
             const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 4 * R * 2));
@@ -187,7 +169,8 @@ struct Side {
 template <int M_, int N_, int WM_, int WN_>
 struct Tile {
     static constexpr int M = M_, N = N_, WM = WM_, WN = WN_, kThreads = WM_ * WN_ * kLanes;
-    static constexpr int MF = M_ / WM_ / 16, NF = N_ / WN_ / 16;     // a wave's matrix instructions
+    static constexpr int kWavesPerSimd = M_ * N_ / (WM_ * WN_) > 8192 ? 1 : 2;   // 512 or 256 registers
+    static constexpr int MF = M_ / WM_ / 32, NF = N_ / WN_ / 32;     // a wave's matrix instructions
 };
 
 // What happens to the sums.
@@ -230,12 +213,17 @@ __device__ __forceinline__ void store4(void* out, int f32, int64_t at, int64_t l
 }
 
 template <Kind KIND, Layout LA, Layout LB, Pair PAIR, Out OUT, class T>
-__global__ __launch_bounds__(T::kThreads, 2) void product_kernel(Args p) {
+__global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(Args p) {
     constexpr bool HALF = PAIR == kPairOuter;
     using A = Side<KIND, LA, T::M, T::kThreads, false>;
     using B = Side<KIND, LB, T::N, T::kThreads, HALF>;
-    constexpr int kStage = A::kBytes + B::kBytes + A::kScaleBytes + B::kScaleBytes;
-    __shared__ __attribute__((aligned(1024))) char lds[2][kStage];
+    constexpr int kScales = KIND == kMx ? (T::M + T::N) * 2 * kQuarters : 0;   // eight bytes a row and step
+    constexpr int kScaleLoads = kScales / (T::kThreads * 4);
+    static_assert(kScales % (T::kThreads * 4) == 0, "whole loads");
+    constexpr int kStage = A::kBytes + B::kBytes + kScales;
+    constexpr int kSlots = 2;
+    constexpr int kLoads = A::kLoads + B::kLoads + kScaleLoads;
+    __shared__ __attribute__((aligned(1024))) char lds[kSlots][kStage];
     constexpr int kOutN = HALF ? T::N / 2 : T::N;          // output columns of a tile
     constexpr int NF = T::NF, MF = T::MF;
 
@@ -251,8 +239,16 @@ __global__ __launch_bounds__(T::kThreads, 2) void product_kernel(Args p) {
 
     A sa;
     B sb;
-    sa.init(p.m - m0, p.a.ld, p.a.scale_ld, tid);
-    sb.init(p.n - n0, p.b.ld, p.b.scale_ld, tid);
+    sa.init(p.m - m0, p.a.ld, tid);
+    sb.init(p.n - n0, p.b.ld, tid);
+    // the scales of A's rows, then of B's; a load is of one operand's rows
+    uint32_t scale_offset[kScaleLoads + 1];
+#pragma unroll
+    for (int i = 0; i < kScaleLoads; ++i) {
+        const int row = (i * T::kThreads + tid) / 2, rb = row - T::M, word = tid % 2 * 4;
+        scale_offset[i] = row < T::M ? (row < p.m - m0 ? (uint32_t)row * (uint32_t)p.a.scale_ld + word : kOutside)
+                                     : (rb < p.n - n0 ? (uint32_t)rb * (uint32_t)p.b.scale_ld + word : kOutside);
+    }
     const char* a0 = p.a.p + (LA == kAlong ? m0 * p.a.ld : m0 * 2);
     const int64_t b_at = LB == kAlong ? n0 * p.b.ld : n0 * 2;
     const int64_t pair_steps = PAIR == kPairInner ? p.steps / 2 : p.steps;
@@ -262,102 +258,159 @@ __global__ __launch_bounds__(T::kThreads, 2) void product_kernel(Args p) {
         const int64_t ia = LA == kAlong ? (p.inner * kElem >> (KIND == kMx ? 1 : 0)) : p.inner;
         const int64_t sb_in = PAIR == kPairInner && s >= pair_steps ? s - pair_steps : s;
         // kPairInner: A's rows hold both contractions one after the other, each filled up with zeros
-        const int64_t a_ahead = PAIR == kPairInner ? A::kFull : ia - s * A::kFull;
+        const int64_t a_ahead = PAIR == kPairInner ? (p.steps - s) * A::kFull : ia - s * A::kFull;
         sa.load(a0 + (LA == kAlong ? s * kStepBytes : s * A::kFull * p.a.ld), nullptr, l, a_ahead, tid, wave);
         const int64_t ib = LB == kAlong ? (p.inner * kElem >> (KIND == kMx ? 1 : 0)) : p.inner;
         const int64_t step = LB == kAlong ? sb_in * kStepBytes : sb_in * B::kFull * p.b.ld;
         const char* b = PAIR == kPairInner && s >= pair_steps ? p.b.p2 : p.b.p;
         sb.load(b + b_at + step, HALF ? p.b.p2 + b_at + step : nullptr, l + A::kBytes, ib - sb_in * B::kFull, tid, wave);
         if constexpr (KIND == kMx) {
-            const int64_t left = p.inner / 32 - s * 8;
-            sa.load_scales(p.a.scales + m0 * p.a.scale_ld + s * 8, l + A::kBytes + B::kBytes, left, tid, wave);
-            sb.load_scales(p.b.scales + n0 * p.b.scale_ld + s * 8, l + A::kBytes + B::kBytes + A::kScaleBytes, left,
-                           tid, wave);
+            const bool any = p.inner / 32 - s * 8 > tid % 2 * 4;
+            const __amdgpu_buffer_rsrc_t ra = window(p.a.scales + m0 * p.a.scale_ld + s * 8),
+                                         rb = window(p.b.scales + n0 * p.b.scale_ld + s * 8);
+#pragma unroll
+            for (int i = 0; i < kScaleLoads; ++i) {
+                const int first = i * T::kThreads + wave * kLanes;
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(first / 2 < T::M ? ra : rb,
+                                                         (lds_void*)(l + A::kBytes + B::kBytes + first * 4), 4,
+                                                         (int)(any ? scale_offset[i] : kOutside), 0, 0, 0);
+            }
         }
     };
 
     // first rows of this wave's fragments in the tile
-    auto a_row = [&](int i) { return wm * (T::M / T::WM) + i * 16; };
+    auto a_row = [&](int i) { return wm * (T::M / T::WM) + i * 32; };
     auto b_row = [&](int j) {
-        if constexpr (!HALF) return wn * (T::N / T::WN) + j * 16;
-        return (j < NF / 2 ? 0 : T::N / 2) + wn * (T::N / 2 / T::WN) + j % (NF / 2) * 16;
+        if constexpr (!HALF) return wn * (T::N / T::WN) + j * 32;
+        return (j < NF / 2 ? 0 : T::N / 2) + wn * (T::N / 2 / T::WN) + j % (NF / 2) * 32;
     };
 
-    f32x4 acc[MF][NF];
+    f32x16 acc[MF][NF];
 #pragma unroll
     for (int i = 0; i < MF; ++i)
 #pragma unroll
-        for (int j = 0; j < NF; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int j = 0; j < NF; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
 
-    if (s0 < s1) fetch(s0, 0);
-    for (int64_t s = s0; s < s1; ++s) {
-        const int stage = (int)(s - s0) & 1;
-        __syncthreads();                 // the step has arrived, and the other stage has been read
-        if (s + 1 < s1) fetch(s + 1, stage ^ 1);
+    // Registers run a quarter of a step ahead of the matrix instructions, LDS kSlots steps: while one
+    // quarter's fragments are multiplied the next one's are read, and the one barrier of a step stands
+    // where its last fragments have been read, so that its LDS is free for the step kSlots on.  What a step
+    // waits for at its barrier are the loads that were started kSlots - 1 steps before, and no later ones.
+    i32x4 fa[2][MF], fb[2][NF];
+    int xa[2][MF], xb[2][NF];                  // scales of this step and of the next
+    auto read = [&](auto q, int stage) {
+        constexpr int Q = decltype(q)::value;
         const char* la = lds[stage];
         const char* lb = la + A::kBytes;
-        int xa[MF], xb[NF];
-        if constexpr (KIND == kMx) {
-            const char* ls = lb + B::kBytes + lane / 16 * 2;
 #pragma unroll
-            for (int i = 0; i < MF; ++i) xa[i] = *reinterpret_cast<const uint16_t*>(ls + (a_row(i) + lane % 16) * 8);
+        for (int j = 0; j < NF; ++j) fb[Q % 2][j] = B::template read<Q>(lb, b_row(j), lane);
+#pragma unroll
+        for (int i = 0; i < MF; ++i) fa[Q % 2][i] = A::template read<Q>(la, a_row(i), lane);
+        if constexpr (KIND == kMx && Q == 0) {
+            const char* ls = lb + B::kBytes + lane / 32 * 4;
 #pragma unroll
             for (int j = 0; j < NF; ++j)
-                xb[j] = *reinterpret_cast<const uint16_t*>(ls + A::kScaleBytes + (b_row(j) + lane % 16) * 8);
+                xb[1][j] = *reinterpret_cast<const int*>(ls + (T::M + b_row(j) + lane % 32) * 8);
+#pragma unroll
+            for (int i = 0; i < MF; ++i)
+                xa[1][i] = *reinterpret_cast<const int*>(ls + (a_row(i) + lane % 32) * 8);
         }
-        auto half = [&](auto kk) {
-            constexpr int KK = decltype(kk)::value;
-            i32x4 fb[NF];
+    };
+    auto multiply = [&](auto q) {
+        constexpr int Q = decltype(q)::value;
 #pragma unroll
-            for (int j = 0; j < NF; ++j) fb[j] = B::template read<KK>(lb, b_row(j), lane);
+        for (int i = 0; i < MF; ++i) {
 #pragma unroll
-            for (int i = 0; i < MF; ++i) {
-                const i32x4 fa = A::template read<KK>(la, a_row(i), lane);
-#pragma unroll
-                for (int j = 0; j < NF; ++j) {
-                    // B's values as the instruction's rows: a lane gets four neighbouring outputs of a row of D
-                    if constexpr (KIND == kBf16) {
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fb[j]),
-                                                                            __builtin_bit_cast(bf16x8, fa), acc[i][j], 0, 0, 0);
-                    } else {
-                        const i32x8 wb = {fb[j][0], fb[j][1], fb[j][2], fb[j][3], 0, 0, 0, 0};
-                        const i32x8 wa = {fa[0], fa[1], fa[2], fa[3], 0, 0, 0, 0};
-                        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wb, wa, acc[i][j], 4, 4, KK, xb[j],
-                                                                                     KK, xa[i]);
-                    }
+            for (int j = 0; j < NF; ++j) {
+                // B's values as the instruction's rows: a lane gets runs of four neighbouring outputs of a row of D
+                const i32x4 b = fb[Q % 2][j], a = fa[Q % 2][i];
+                if constexpr (KIND == kBf16) {
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, b),
+                                                                        __builtin_bit_cast(bf16x8, a), acc[i][j], 0, 0, 0);
+                } else {
+                    const i32x8 wb = {b[0], b[1], b[2], b[3], 0, 0, 0, 0}, wa = {a[0], a[1], a[2], a[3], 0, 0, 0, 0};
+                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wb, wa, acc[i][j], 4, 4, Q, xb[0][j], Q,
+                                                                                xa[0][i]);
                 }
             }
-        };
-        half(Const<0>{});
-        half(Const<1>{});
+        }
+    };
+    // the LDS reads of a quarter spread among the one before's matrix instructions
+    auto interleave = [&]() {
+        constexpr int kReads = MF * (LA == kAcross ? 2 : 1) + NF * (LB == kAcross ? 2 : 1), kOps = MF * NF;
+        constexpr int kEach = kReads > kOps ? (kReads + kOps - 1) / kOps : 1;
+#pragma unroll
+        for (int r = 0; r < kOps; ++r) {
+            __builtin_amdgcn_sched_group_barrier(0x100, kEach, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        }
+    };
+    auto next_scales = [&]() {
+        if constexpr (KIND == kMx) {
+#pragma unroll
+            for (int i = 0; i < MF; ++i) xa[0][i] = xa[1][i];
+#pragma unroll
+            for (int j = 0; j < NF; ++j) xb[0][j] = xb[1][j];
+        }
+    };
+    if (s0 < s1) {
+#pragma unroll
+        for (int i = 0; i < kSlots; ++i) fetch(s0 + i, i);          // past the contraction's end: zeros
+        arrive<(kSlots - 1) * kLoads>();
+        read(Const<0>{}, 0);
+        int slot = 0;
+        for (int64_t s = s0; s < s1; ++s) {
+            const int next = slot + 1 == kSlots ? 0 : slot + 1;
+            next_scales();
+            read(Const<1>{}, slot);
+            multiply(Const<0>{});
+            interleave();
+            read(Const<2>{}, slot);
+            multiply(Const<1>{});
+            interleave();
+            read(Const<3>{}, slot);
+            multiply(Const<2>{});
+            interleave();
+            arrive<(kSlots - 2) * kLoads>();
+            fetch(s + kSlots, slot);
+            read(Const<0>{}, next);
+            multiply(Const<3>{});
+            interleave();
+            slot = next;
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");            // no load into LDS outlives the workgroup
     }
 
-    const int mi = lane % 16, nj = lane / 16 * 4;
+    // a lane holds, of row lane % 32 of D, the runs of four columns from 4 (lane / 32) on, eight apart
     const bool vec = p.out_ld % 4 == 0;
     const float scale = OUT == kSums && p.scale ? *p.scale : 1.0f;
 #pragma unroll
     for (int i = 0; i < MF; ++i) {
-        const int64_t m = m0 + a_row(i) + mi;
+        const int64_t m = m0 + a_row(i) + lane % 32;
         if (m >= p.m) continue;
 #pragma unroll
-        for (int j = 0; j < (HALF ? NF / 2 : NF); ++j) {
-            const int64_t n = n0 + b_row(j) + nj, left = p.n - n;
+        for (int jr = 0; jr < (HALF ? NF / 2 : NF) * 4; ++jr) {
+            const int j = jr / 4, r = jr % 4 * 4;
+            const int64_t n = n0 + b_row(j) + r * 2 + lane / 32 * 4, left = p.n - n;
+            const f32x4 v = {acc[i][j][r], acc[i][j][r + 1], acc[i][j][r + 2], acc[i][j][r + 3]};
             if constexpr (OUT == kSums) {
-                store4(p.out, p.out_f32, m * p.out_ld + n, left, vec, acc[i][j] * scale);
+                store4(p.out, p.out_f32, m * p.out_ld + n, left, vec, v * scale);
             } else if constexpr (OUT == kPartial) {
-                store4(p.out, 1, (part * p.m + m) * p.out_ld + n, left, vec, acc[i][j]);
+                store4(p.out, 1, (part * p.m + m) * p.out_ld + n, left, vec, v);
             } else if constexpr (OUT == kTwoRows) {
                 const int64_t row = m < p.half_rows ? m : m - p.half_rows;
                 if (row < p.out_rows)
-                    store4(m < p.half_rows ? p.out : p.out2, 0, row * p.out_ld + n, left, vec, acc[i][j]);
+                    store4(m < p.half_rows ? p.out : p.out2, 0, row * p.out_ld + n, left, vec, v);
             } else {
-                const f32x4 g = acc[i][j], u = acc[i][NF / 2 + j];
+                constexpr int H = HALF ? NF / 2 : 0;
+                const f32x4 u = {acc[i][H + j][r], acc[i][H + j][r + 1], acc[i][H + j][r + 2], acc[i][H + j][r + 3]};
                 f32x4 h;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) h[r] = silu(g[r]) * u[r];
+                for (int e = 0; e < 4; ++e) h[e] = silu(v[e]) * u[e];
                 store4(p.out, 0, m * p.out_ld + n, left, vec, h);
                 if (p.out2) {
-                    store4(p.out2, 0, m * p.out_ld + n, left, vec, g);
+                    store4(p.out2, 0, m * p.out_ld + n, left, vec, v);
                     store4(p.out3, 0, m * p.out_ld + n, left, vec, u);
                 }
             }
