@@ -2,6 +2,7 @@
 //   NVFP4 weights W = q s S [n, k], activations in bfloat16:  y = x W^T,  dx = dy W
 //   microscaled FP4 (E8M0 scale for each 32 values):          y = A B^T,  dx = dy B
 #include "product_host.h"
+#include "stream_product.h"
 #include "thin_product.h"
 
 namespace product_host {
@@ -94,23 +95,90 @@ int expand(const uint8_t* q, const uint8_t* scales, int64_t n, int64_t k, int bl
 
 bool valid_out(int dtype) { return dtype == NVFP4_IN_F32 || dtype == NVFP4_IN_BF16; }
 
+// ---- sums of parts of the contraction -----------------------------------------------------------
+
+constexpr int kJoinThreads = 256;
+
+template <bool VEC>
+__global__ __launch_bounds__(kJoinThreads) void join_kernel(const float* __restrict__ part, int parts, int64_t count,
+                                                            const float* __restrict__ scale, void* __restrict__ out,
+                                                            int f32) {
+    constexpr int kPer = VEC ? 4 : 1;
+    const int64_t at = ((int64_t)blockIdx.x * kJoinThreads + threadIdx.x) * kPer;
+    if (at >= count) return;
+    float v[kPer] = {};
+    for (int p = 0; p < parts; ++p) {
+        const float* from = part + p * count + at;
+        if constexpr (VEC) {
+            const float4 w = *reinterpret_cast<const float4*>(from);
+            v[0] += w.x, v[1] += w.y, v[2] += w.z, v[3] += w.w;
+        } else {
+            v[0] += *from;
+        }
+    }
+    const float s = scale ? *scale : 1.0f;
+    if constexpr (VEC) store4(out, f32, at, 4, true, f32x4{v[0], v[1], v[2], v[3]} * s);
+    else store4(out, f32, at, 1, false, f32x4{v[0] * s, 0.0f, 0.0f, 0.0f});
+}
+
+// out = scale * (the parts' sums [parts, count], added in order)
+int join(const float* part, int parts, int64_t count, const float* scale, void* out, int f32, hipStream_t stream) {
+    const bool vec = count % 4 == 0;
+    const int64_t groups = ceil_div(vec ? count / 4 : count, kJoinThreads);
+    if (groups > 0x7FFFFFFF) return NVFP4_ERR_SHAPE;
+    hipLaunchKernelGGL((vec ? join_kernel<true> : join_kernel<false>), dim3((unsigned)groups), dim3(kJoinThreads), 0, stream,
+                       part, parts, count, scale, out, f32);
+    return launched();
+}
+
 // ---- y = x W^T ------------------------------------------------------------------------------
 
+constexpr int64_t kStreamRows = 512;             // see run_linear
+
 int64_t linear_workspace(int64_t m, int64_t n, int64_t k) {
-    return m <= thin_product::kRows ? 0 : up(n * k * 2, 256);
+    if (m <= thin_product::kRows) return 0;
+    if (m <= kStreamRows) {
+        const int parts = stream_product::parts(m, n, k);
+        return parts > 1 ? up(parts * m * n * 4, 256) : 0;
+    }
+    return up(n * k * 2, 256);
+}
+
+template <int MF>
+void launch_stream(const stream_product::Args& p, hipStream_t stream) {
+    const dim3 grid((unsigned)(p.tiles_n * p.tiles_m * p.parts)), threads(stream_product::kThreads);
+    const bool even = p.k % 32 == 0, pairs = p.shift == 4;
+    auto kernel = even ? (pairs ? stream_product::stream_kernel<MF, true, true> : stream_product::stream_kernel<MF, true, false>)
+                       : stream_product::stream_kernel<MF, false, true>;     // blocks of 32 and up: k is a multiple
+    hipLaunchKernelGGL(kernel, grid, threads, 0, stream, p);
 }
 
 int run_linear(const void* x, int64_t ldx, const uint8_t* q, const uint8_t* scales, int block, const float* S,
                int64_t m, int64_t n, int64_t k, int out_dtype, void* out, void* ws, hipStream_t stream) {
+    const int shift = block == 16 ? 4 : block == 32 ? 5 : block == 64 ? 6 : 7;
+    const int f32 = out_dtype == NVFP4_IN_F32;
     if (m <= thin_product::kRows) {
         thin_product::Args t = {};
         t.w = reinterpret_cast<const char*>(q), t.ldw = k / 2, t.w_scales = scales, t.w_scale_ld = k / block;
         t.x = static_cast<const char*>(x), t.ldx = ldx * 2, t.m = (int)m, t.n = n, t.k = k;
-        t.shift = block == 16 ? 4 : block == 32 ? 5 : block == 64 ? 6 : 7;
-        t.scale = S, t.out = out, t.out_f32 = out_dtype == NVFP4_IN_F32;
+        t.shift = shift, t.scale = S, t.out = out, t.out_f32 = f32;
         if (k % 32 == 0) thin_product::launch_thin<thin_product::kNvfp4, 8, 2, true>(t, stream);
         else thin_product::launch_thin<thin_product::kNvfp4, 8, 2, false>(t, stream);
         return launched();
+    }
+    if (m <= kStreamRows) {
+        stream_product::Args t = {};
+        t.q = reinterpret_cast<const char*>(q), t.scales = scales, t.x = static_cast<const char*>(x), t.ldx = ldx * 2;
+        t.m = m, t.n = n, t.k = k, t.shift = shift, t.scale = S, t.out = out, t.out_f32 = f32;
+        t.steps = ceil_div(k, stream_product::kStep), t.tiles_n = ceil_div(n, stream_product::kRowsN);
+        t.tiles_m = stream_product::tiles_m(m), t.parts = stream_product::parts(m, n, k);
+        t.split_steps = ceil_div(t.steps, t.parts);
+        if (t.parts > 1) t.out = ws;
+        if (m <= 32) launch_stream<1>(t, stream);
+        else if (m <= 64) launch_stream<2>(t, stream);
+        else launch_stream<4>(t, stream);
+        if (const int rc = launched()) return rc;
+        return t.parts > 1 ? join(static_cast<const float*>(ws), t.parts, m * n, S, out, f32, stream) : NVFP4_OK;
     }
     if (const int rc = expand<kBf16>(q, scales, n, k, block, ws, stream)) return rc;
     Args p = {};

@@ -64,9 +64,9 @@ def test_matmul(nv):
     assert call(block=24) == call(block=0) == -3
     assert call(dtype=2) == -4
     assert call(x=OFF8) == call(q=OFF8) == call(out=OFF8) == call(S=OFF2) == call(ldx=68) == -7
-    need = nv.nvfp4_matmul_workspace_bytes(200, 512, 512)
+    need = nv.nvfp4_matmul_workspace_bytes(2000, 512, 512)
     assert need > 0
-    big = dict(m=200, n=512, k=512, ldx=512)
+    big = dict(m=2000, n=512, k=512, ldx=512)
     assert call(ws=None, **big) == call(wsb=need - 1, **big) == -6
     assert call(ws=P(0x100010), **big) == -7
     assert call(m=0, x=None) == call(n=0, out=None) == 0
