@@ -2,6 +2,7 @@
 //   NVFP4 weights W = q s S [n, k], activations in bfloat16:  y = x W^T,  dx = dy W
 //   microscaled FP4 (E8M0 scale for each 32 values):          y = A B^T,  dx = dy B
 #include "product_host.h"
+#include "dot_product.h"
 #include "stream_product.h"
 #include "thin_product.h"
 
@@ -136,7 +137,7 @@ int join(const float* part, int parts, int64_t count, const float* scale, void* 
 constexpr int64_t kStreamRows = 512;             // see run_linear
 
 int64_t linear_workspace(int64_t m, int64_t n, int64_t k) {
-    if (m <= thin_product::kRows) return 0;
+    if (m <= dot_product::kMostRows) return 0;
     if (m <= kStreamRows) {
         const int parts = stream_product::parts(m, n, k);
         return parts > 1 ? up(parts * m * n * 4, 256) : 0;
@@ -146,7 +147,7 @@ int64_t linear_workspace(int64_t m, int64_t n, int64_t k) {
 
 template <int MF>
 void launch_stream(const stream_product::Args& p, hipStream_t stream) {
-    const dim3 grid((unsigned)(p.tiles_n * p.tiles_m * p.parts)), threads(stream_product::kThreads);
+    const dim3 grid((unsigned)(p.tiles_n * p.tiles_m * p.parts)), threads(256 * stream_product::kWavesK);
     const bool even = p.k % 32 == 0, pairs = p.shift == 4;
     auto kernel = even ? (pairs ? stream_product::stream_kernel<MF, true, true> : stream_product::stream_kernel<MF, true, false>)
                        : stream_product::stream_kernel<MF, false, true>;     // blocks of 32 and up: k is a multiple
@@ -157,26 +158,32 @@ int run_linear(const void* x, int64_t ldx, const uint8_t* q, const uint8_t* scal
                int64_t m, int64_t n, int64_t k, int out_dtype, void* out, void* ws, hipStream_t stream) {
     const int shift = block == 16 ? 4 : block == 32 ? 5 : block == 64 ? 6 : 7;
     const int f32 = out_dtype == NVFP4_IN_F32;
-    if (m <= thin_product::kRows) {
-        thin_product::Args t = {};
-        t.w = reinterpret_cast<const char*>(q), t.ldw = k / 2, t.w_scales = scales, t.w_scale_ld = k / block;
-        t.x = static_cast<const char*>(x), t.ldx = ldx * 2, t.m = (int)m, t.n = n, t.k = k;
-        t.shift = shift, t.scale = S, t.out = out, t.out_f32 = f32;
-        if (k % 32 == 0) thin_product::launch_thin<thin_product::kNvfp4, 8, 2, true>(t, stream);
-        else thin_product::launch_thin<thin_product::kNvfp4, 8, 2, false>(t, stream);
+    if (m <= dot_product::kMostRows) {
+        dot_product::Args t = {};
+        t.q = reinterpret_cast<const char*>(q), t.scales = scales, t.x = static_cast<const char*>(x), t.ldx = ldx * 2;
+        t.n = n, t.k = k, t.shift = shift, t.scale = S, t.out = out, t.out_f32 = f32;
+        for (t.along = 1; t.along < dot_product::kWaves && t.along * dot_product::kSpan < k;) t.along *= 2;
+        switch (m) {
+            case 1: dot_product::launch_dot<1>(t, stream); break;
+            case 2: dot_product::launch_dot<2>(t, stream); break;
+            case 3: dot_product::launch_dot<3>(t, stream); break;
+            default: dot_product::launch_dot<4>(t, stream);
+        }
         return launched();
     }
     if (m <= kStreamRows) {
         stream_product::Args t = {};
         t.q = reinterpret_cast<const char*>(q), t.scales = scales, t.x = static_cast<const char*>(x), t.ldx = ldx * 2;
         t.m = m, t.n = n, t.k = k, t.shift = shift, t.scale = S, t.out = out, t.out_f32 = f32;
-        t.steps = ceil_div(k, stream_product::kStep), t.tiles_n = ceil_div(n, stream_product::kRowsN);
+        t.steps = stream_product::steps(k), t.tiles_n = ceil_div(n, stream_product::kRowsN);
         t.tiles_m = stream_product::tiles_m(m), t.parts = stream_product::parts(m, n, k);
         t.split_steps = ceil_div(t.steps, t.parts);
         if (t.parts > 1) t.out = ws;
-        if (m <= 32) launch_stream<1>(t, stream);
-        else if (m <= 64) launch_stream<2>(t, stream);
-        else launch_stream<4>(t, stream);
+        switch (stream_product::rows_of(m)) {
+            case 1: launch_stream<1>(t, stream); break;
+            case 2: launch_stream<2>(t, stream); break;
+            default: launch_stream<4>(t, stream);
+        }
         if (const int rc = launched()) return rc;
         return t.parts > 1 ? join(static_cast<const float*>(ws), t.parts, m * n, S, out, f32, stream) : NVFP4_OK;
     }

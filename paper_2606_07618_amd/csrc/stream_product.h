@@ -1,10 +1,10 @@
 // NVFP4 products with some tens or hundreds of activation rows: the weights are read once for each 128 rows and
 // expanded in registers, on their way into the matrix instructions, so no expanded copy of them is written.
 //
-// A workgroup owns 128 weight rows and up to 128 activation rows.  Its eight waves are four times 32 weight rows
-// by the two halves of each step of the contraction (128 values); a wave loads its weights (32 rows by two lanes of
+// A workgroup owns 128 weight rows and up to 128 activation rows.  Its waves are four times 32 weight rows by KW
+// parts of each step of the contraction (64 values each); a wave loads its weights (32 rows by two lanes of
 // 16 bytes) into registers, D steps ahead, and all waves share the step's activations in LDS, as many steps
-// ahead, so that a step's wait is for what was started D - 1 steps before.  The halves' sums meet in LDS at the end.
+// ahead, so that a step's wait is for what was started D - 1 steps before.  The parts' sums meet in LDS at the end.
 // Few weight rows: the contraction is split over workgroups as well, whose sums a second kernel adds in order.
 #pragma once
 
@@ -20,7 +20,8 @@ using thin_product::load1;
 using thin_product::load16;
 using thin_product::load8;
 
-constexpr int kWaves = 8, kThreads = kWaves * kLanes, kRowsN = 128, kStep = 128;
+constexpr int kRowsN = 128;                      // weight rows of a workgroup, 32 a wave
+constexpr int kWavesK = 2;                       // waves along a step
 
 struct Args {
     const char* q;
@@ -36,12 +37,13 @@ struct Args {
 
 // MF: 32 activation rows each.  EVEN: k is a multiple of 32.  PAIRS: blocks of 16, two scales a lane.
 template <int MF, bool EVEN, bool PAIRS>
-__global__ __launch_bounds__(kThreads, 2) void stream_kernel(Args p) {
-    constexpr int D = MF == 4 ? 4 : MF == 2 ? 6 : 8;
+__global__ __launch_bounds__(256 * kWavesK, kWavesK) void stream_kernel(Args p) {
+    constexpr int KW = kWavesK, D = MF == 4 ? 5 : 8;
+    constexpr int kThreads = 256 * KW, kStep = 64 * KW, kChunks = 8 * KW;      // of a row of a step
     constexpr int kStage = MF * 32 * kStep * 2;
     constexpr int kLeast = 2 + MF;               // loads of a step, at least
     __shared__ __attribute__((aligned(1024))) char lds[D][kStage];
-    static_assert(4 * MF * 16 * kLanes * 4 <= D * kStage, "the halves' sums");
+    static_assert((KW - 1) * 4 * MF * 16 * kLanes * 4 <= D * kStage, "the other parts' sums");
 
     const int tid = threadIdx.x, lane = tid % kLanes, g = lane / 32, i32 = lane % 32;
     const int wave = __builtin_amdgcn_readfirstlane(tid / kLanes), r = wave % 4, h = wave / 4;
@@ -76,8 +78,8 @@ __global__ __launch_bounds__(kThreads, 2) void stream_kernel(Args p) {
                         load1(rs, in1 ? s_row + (uint32_t)(v >> 4) + 1 : kOutside) << 8;
 #pragma unroll
         for (int i = 0; i < MF; ++i) {
-            // rows of 16 chunks, a chunk's place exchanged by its row: 16 lanes read one chunk of 16 rows
-            const int id = i * kThreads + tid, xr = id / 16, chunk = id % 16 ^ xr % 16;
+            // a chunk's place in its row is exchanged by the row: 16 lanes read one chunk of 16 rows
+            const int id = i * kThreads + tid, xr = id / kChunks, chunk = id % kChunks ^ xr % 16;
             const bool in = m0 + xr < p.m && s < s1 && k0 + chunk * 8 < p.k;
             const uint32_t off = in ? (uint32_t)xr * (uint32_t)p.ldx + (uint32_t)(k0 + chunk * 8) * 2 : kOutside;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (lds_void*)(lds[slot] + (i * kThreads + wave * kLanes) * kChunk), kChunk,
@@ -91,38 +93,55 @@ __global__ __launch_bounds__(kThreads, 2) void stream_kernel(Args p) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[i][e] = 0.0f;
 
+    // Registers: this step's activations and the next one's, read while this one's are multiplied.
+    bf16x8 xv[2][4][MF];
+    auto read = [&](int slot, int to, int j) {
+#pragma unroll
+        for (int i = 0; i < MF; ++i) {
+            const int chunk = (h * 8 + g * 4 + j) ^ i32 % 16;
+            xv[to][j][i] = *reinterpret_cast<const bf16x8*>(lds[slot] + (i * 32 + i32) * (kStep * 2) + chunk * kChunk);
+        }
+    };
 #pragma unroll
     for (int d = 0; d < D - 1; ++d) fetch(s0 + d, d);
-    for (int64_t s = s0; s < s1; s += D) {
+    arrive<(D - 2) * kLeast>();
 #pragma unroll
-        for (int d = 0; d < D; ++d) {
+    for (int j = 0; j < 4; ++j) read(0, 0, j);
+    constexpr int kTurn = D % 2 ? 2 * D : D;     // steps after which slots and registers recur
+    for (int64_t s = s0; s < s1; s += kTurn) {
+#pragma unroll
+        for (int d = 0; d < kTurn; ++d) {
             if (s + d >= s1) break;
-            arrive<(D - 2) * kLeast>();          // the step's activations are here, the step before's are read
+            arrive<(D - 3) * kLeast>();          // the next step's activations are here, this one's are read
             fetch(s + d + D - 1, (d + D - 1) % D);
-            const float f0 = e4m3_f32(sc[d]), f1 = PAIRS ? e4m3_f32(sc[d] >> 8) : f0;
+            const int slot = d % D;
+            const float f0 = e4m3_f32(sc[slot]), f1 = PAIRS ? e4m3_f32(sc[slot] >> 8) : f0;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const bf16x8 wv = expand8((uint32_t)w[d][j], j < 2 ? f0 : f1);
+                read((d + 1) % D, (d + 1) % 2, j);
+                const bf16x8 wv = expand8((uint32_t)w[slot][j], j < 2 ? f0 : f1);
 #pragma unroll
-                for (int i = 0; i < MF; ++i) {
-                    const int chunk = (h * 8 + g * 4 + j) ^ i32 % 16;
-                    const bf16x8 xv = *reinterpret_cast<const bf16x8*>(lds[d] + (i * 32 + i32) * (kStep * 2) + chunk * kChunk);
-                    acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wv, xv, acc[i], 0, 0, 0);
-                }
+                for (int i = 0; i < MF; ++i) acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wv, xv[d % 2][j][i], acc[i], 0, 0, 0);
             }
         }
     }
 
     arrive<0>();
-    float* sums = reinterpret_cast<float*>(lds[0]);      // of the second half, a lane's place in each word row
-    if (h == 1) {
+    float* sums = reinterpret_cast<float*>(lds[0]);      // [KW - 1][4][MF][16][lanes]
+    if (h > 0) {
 #pragma unroll
         for (int i = 0; i < MF; ++i)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) sums[((r * MF + i) * 16 + e) * kLanes + lane] = acc[i][e];
+            for (int e = 0; e < 16; ++e) sums[((((h - 1) * 4 + r) * MF + i) * 16 + e) * kLanes + lane] = acc[i][e];
     }
     __syncthreads();
-    if (h == 1) return;
+    if (h > 0) return;
+#pragma unroll
+    for (int o = 0; o < KW - 1; ++o)
+#pragma unroll
+        for (int i = 0; i < MF; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][e] += sums[(((o * 4 + r) * MF + i) * 16 + e) * kLanes + lane];
     const float scale = p.parts == 1 && p.scale ? *p.scale : 1.0f;
     const bool vec = p.n % 4 == 0;
 #pragma unroll
@@ -131,23 +150,22 @@ __global__ __launch_bounds__(kThreads, 2) void stream_kernel(Args p) {
         if (m >= p.m) continue;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            f32x4 v;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                v[e] = (acc[i][q * 4 + e] + sums[((r * MF + i) * 16 + q * 4 + e) * kLanes + lane]) * scale;
+            const f32x4 v = f32x4{acc[i][q * 4], acc[i][q * 4 + 1], acc[i][q * 4 + 2], acc[i][q * 4 + 3]} * scale;
             const int64_t n = n0 + r * 32 + q * 8 + g * 4;
             store4(p.out, p.parts > 1 || p.out_f32, ((p.parts > 1 ? part * p.m : 0) + m) * p.n + n, p.n - n, vec, v);
         }
     }
 }
 
+inline int rows_of(int64_t m) { return m <= 32 ? 1 : m <= 64 ? 2 : 4; }
 inline int tiles_m(int64_t m) { return (int)((m + 127) / 128); }
-// Workgroups hold about 100 KB of LDS, one to a compute unit: parts of the contraction, of at least eight
-// steps, until 256 units have work.
+inline int64_t steps(int64_t k) { return (k + 64 * kWavesK - 1) / (64 * kWavesK); }
+// A workgroup takes a compute unit's LDS: parts of the contraction, of at least eight steps, until 256 units
+// have work.
 inline int parts(int64_t m, int64_t n, int64_t k) {
-    const int64_t groups = (n + kRowsN - 1) / kRowsN * tiles_m(m), steps = (k + kStep - 1) / kStep;
+    const int64_t groups = (n + kRowsN - 1) / kRowsN * tiles_m(m);
     int64_t want = (256 + groups / 2) / (groups ? groups : 1);
-    if (want > steps / 8) want = steps / 8;
+    if (want > steps(k) / 8) want = steps(k) / 8;
     if (want > 16) want = 16;
     return want < 1 ? 1 : (int)want;
 }
