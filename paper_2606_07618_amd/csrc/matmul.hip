@@ -140,7 +140,7 @@ int64_t linear_workspace(int64_t m, int64_t n, int64_t k) {
     if (m <= dot_product::kMostRows) return 0;
     if (m <= kStreamRows) {
         const int parts = stream_product::parts(m, n, k);
-        return parts > 1 ? up(parts * m * n * 4, 256) : 0;
+        return up(m * k * 2, 256) + up(m * 4, 256) + (parts > 1 ? up(parts * m * n * 4, 256) : 0);
     }
     return up(n * k * 2, 256);
 }
@@ -148,9 +148,10 @@ int64_t linear_workspace(int64_t m, int64_t n, int64_t k) {
 template <int MF>
 void launch_stream(const stream_product::Args& p, hipStream_t stream) {
     const dim3 grid((unsigned)(p.tiles_n * p.tiles_m * p.parts)), threads(256 * stream_product::kWavesK);
-    const bool even = p.k % 32 == 0, pairs = p.shift == 4;
-    auto kernel = even ? (pairs ? stream_product::stream_kernel<MF, true, true> : stream_product::stream_kernel<MF, true, false>)
-                       : stream_product::stream_kernel<MF, false, true>;     // blocks of 32 and up: k is a multiple
+    using namespace stream_product;
+    const bool wide = p.k % stream_product::kGroup == 0;   // whole groups, whose scales start on whole words
+    auto kernel = p.shift == 4 ? (wide ? stream_kernel<MF, kWide16> : p.k % 32 == 0 ? stream_kernel<MF, kPair> : stream_kernel<MF, kOdd>)
+                               : p.shift == 5 && wide ? stream_kernel<MF, kWide32> : stream_kernel<MF, kOne>;
     hipLaunchKernelGGL(kernel, grid, threads, 0, stream, p);
 }
 
@@ -172,20 +173,26 @@ int run_linear(const void* x, int64_t ldx, const uint8_t* q, const uint8_t* scal
         return launched();
     }
     if (m <= kStreamRows) {
+        Carver c{static_cast<char*>(ws)};
+        uint16_t* x16 = static_cast<uint16_t*>(c.take(m * k * 2));
+        int* exponents = static_cast<int*>(c.take(m * 4));
+        hipLaunchKernelGGL(stream_product::scale_rows_kernel, dim3((unsigned)m), dim3(stream_product::kScaleThreads), 0, stream,
+                           static_cast<const uint16_t*>(x), ldx, (int)k, x16, exponents);
+        if (const int rc = launched()) return rc;
         stream_product::Args t = {};
-        t.q = reinterpret_cast<const char*>(q), t.scales = scales, t.x = static_cast<const char*>(x), t.ldx = ldx * 2;
+        t.q = reinterpret_cast<const char*>(q), t.scales = scales, t.x = reinterpret_cast<const char*>(x16), t.exponents = exponents;
         t.m = m, t.n = n, t.k = k, t.shift = shift, t.scale = S, t.out = out, t.out_f32 = f32;
-        t.steps = stream_product::steps(k), t.tiles_n = ceil_div(n, stream_product::kRowsN);
-        t.tiles_m = stream_product::tiles_m(m), t.parts = stream_product::parts(m, n, k);
-        t.split_steps = ceil_div(t.steps, t.parts);
-        if (t.parts > 1) t.out = ws;
+        t.tiles_n = ceil_div(n, stream_product::kRowsN), t.tiles_m = stream_product::tiles_m(m);
+        t.parts = stream_product::parts(m, n, k), t.part_values = stream_product::part_values(k, t.parts);
+        float* partial = t.parts > 1 ? static_cast<float*>(c.take(t.parts * m * n * 4)) : nullptr;
+        if (partial) t.out = partial;
         switch (stream_product::rows_of(m)) {
             case 1: launch_stream<1>(t, stream); break;
             case 2: launch_stream<2>(t, stream); break;
             default: launch_stream<4>(t, stream);
         }
         if (const int rc = launched()) return rc;
-        return t.parts > 1 ? join(static_cast<const float*>(ws), t.parts, m * n, S, out, f32, stream) : NVFP4_OK;
+        return partial ? join(partial, t.parts, m * n, nullptr, out, f32, stream) : NVFP4_OK;
     }
     if (const int rc = expand<kBf16>(q, scales, n, k, block, ws, stream)) return rc;
     Args p = {};

@@ -1,10 +1,18 @@
-// NVFP4 products with some tens or hundreds of activation rows: the weights are read once for each 128 rows and
+// NVFP4 products with some to some hundreds of activation rows: the weights are read once for each 128 rows and
 // expanded in registers, on their way into the matrix instructions, so no expanded copy of them is written.
 //
-// A workgroup owns 128 weight rows and up to 128 activation rows.  Its waves are four times 32 weight rows by KW
-// parts of each step of the contraction (64 values each); a wave loads its weights (32 rows by two lanes of
-// 16 bytes) into registers, D steps ahead, and all waves share the step's activations in LDS, as many steps
-// ahead, so that a step's wait is for what was started D - 1 steps before.  The parts' sums meet in LDS at the end.
+// The instructions of the expansion are what bounds it (each costs 4.8 cycles of a SIMD's four), so it is done in
+// binary16: q s has six significand bits and lies in 2^-10 .. 2688, exact there, and takes one conversion and
+// one packed product a pair; in bfloat16 it would take four instructions.  The activations are converted once,
+// each row scaled by a power of two so that its largest value lies in [2^14, 2^15): values down to 2^-29 of it
+// stay exact, and what is lost of smaller ones is below 2^-40 of it, far under the sums' own rounding.
+//
+// A workgroup owns 128 weight rows and up to 128 activation rows.  Its waves are four times 32 weight rows by the
+// two halves of its contraction; a wave loads its weights (32 rows by two lanes of 16 bytes) into
+// registers, D steps ahead, and all waves share the step's activations in LDS, as many steps ahead, so that a
+// step's wait is for what was started D - 1 steps before.  The halves' sums meet in LDS at the end.
+// The scales of 256 values of a row come in one load where their rows allow it: two bytes at a time, each
+// visit to a row of scales would fetch its line anew.
 // Few weight rows: the contraction is split over workgroups as well, whose sums a second kernel adds in order.
 #pragma once
 
@@ -13,79 +21,175 @@
 namespace stream_product {
 
 using namespace tile_product;
-using thin_product::e4m3_f32;
-using thin_product::expand8;
 using thin_product::i32x2;
 using thin_product::load1;
 using thin_product::load16;
 using thin_product::load8;
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kRowsN = 128;                      // weight rows of a workgroup, 32 a wave
-constexpr int kWavesK = 2;                       // waves along a step
+constexpr int kWavesK = 2;                       // waves along the contraction, a half each
+constexpr int kPiece = 64;                       // values of a weight row in one load of a wave
+constexpr int kGroup = 256;                      // values of a weight row whose scales are loaded together
 
 struct Args {
     const char* q;
     const uint8_t* scales;
-    const char* x;                               // [m, ldx bytes]
-    int64_t ldx, m, n, k;
-    int64_t steps, split_steps, tiles_n;
-    int parts, tiles_m, shift;
+    const char* x;                               // [m, k] binary16
+    const int* exponents;                        // of the rows' powers of two
+    int64_t m, n, k;
+    int64_t tiles_n;
+    int parts, tiles_m, shift, part_values;      // part_values: of the contraction, a part
     const float* scale;
     void* out;
     int out_f32;
 };
 
-// MF: 32 activation rows each.  EVEN: k is a multiple of 32.  PAIRS: blocks of 16, two scales a lane.
-template <int MF, bool EVEN, bool PAIRS>
+// Rows of x in binary16 times 2^-e, and e.  A row of zeros has e = 0; one with an infinity or a NaN keeps it.
+constexpr int kScaleThreads = 256;
+__global__ __launch_bounds__(kScaleThreads) void scale_rows_kernel(const uint16_t* __restrict__ x, int64_t ldx, int k,
+                                                                   uint16_t* __restrict__ out, int* __restrict__ exponents) {
+    __shared__ uint32_t tops[kScaleThreads / kLanes];
+    const uint16_t* row = x + blockIdx.x * ldx;
+    uint32_t top = 0;
+    for (int c = threadIdx.x * 8; c < k; c += kScaleThreads * 8) {
+        const uint4 v = *reinterpret_cast<const uint4*>(row + c);
+        for (const uint32_t w : {v.x, v.y, v.z, v.w}) {
+            const uint32_t lo = w & 0x7FFFu, hi = w >> 16 & 0x7FFFu;
+            top = top > lo ? top : lo;
+            top = top > hi ? top : hi;
+        }
+    }
+#pragma unroll
+    for (int d = 1; d < kLanes; d *= 2) {
+        const uint32_t o = __shfl_xor(top, d);
+        top = top > o ? top : o;
+    }
+    if (threadIdx.x % kLanes == 0) tops[threadIdx.x / kLanes] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kScaleThreads / kLanes; ++w) top = top > tops[w] ? top : tops[w];
+    int field = (int)(top >> 7);                 // 127 + floor(log2 max|x|)
+    field = field == 255 ? 254 : field < 1 ? 1 : field;
+    const int e = top == 0 ? 0 : field - 127 - 14;
+    if (threadIdx.x == 0) exponents[blockIdx.x] = e;
+    for (int c = threadIdx.x * 8; c < k; c += kScaleThreads * 8) {
+        const uint4 v = *reinterpret_cast<const uint4*>(row + c);
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        uint32_t o[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const f16x2 h = {(_Float16)ldexpf(__uint_as_float(w[i] << 16), -e), (_Float16)ldexpf(__uint_as_float(w[i] & 0xFFFF0000u), -e)};
+            o[i] = __builtin_bit_cast(uint32_t, h);
+        }
+        *reinterpret_cast<uint4*>(out + blockIdx.x * (int64_t)k + c) = make_uint4(o[0], o[1], o[2], o[3]);
+    }
+}
+
+// An E4M3 code's fields as a binary16 number: the scale times 2^-8, subnormal codes included.
+__device__ __forceinline__ f16x2 e4m3_f16(uint32_t c) {
+    const uint32_t h = (c & 0x7Fu) << 7;
+    return __builtin_bit_cast(f16x2, h | h << 16);
+}
+
+// Eight values times 2^8 and a scale times 2^-8.
+__device__ __forceinline__ f16x8 expand8(uint32_t n, f16x2 s) {
+    const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(n, 256.0f, 0) * s, b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(n, 256.0f, 1) * s,
+                c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(n, 256.0f, 2) * s, d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(n, 256.0f, 3) * s;
+    return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// How a lane gets its scales: those of a whole group of its row (blocks of 16: four words, of 32: two), or of its
+// own 32 values, one or two; kOdd: k is an odd multiple of 16, and a lane's 16 bytes may be half outside.
+enum Scales { kWide16, kWide32, kPair, kOne, kOdd };
+
+// MF: 32 activation rows each.
+template <int MF, Scales SCALES>
 __global__ __launch_bounds__(256 * kWavesK, kWavesK) void stream_kernel(Args p) {
-    constexpr int KW = kWavesK, D = MF == 4 ? 5 : 8;
-    constexpr int kThreads = 256 * KW, kStep = 64 * KW, kChunks = 8 * KW;      // of a row of a step
-    constexpr int kStage = MF * 32 * kStep * 2;
-    constexpr int kLeast = 2 + MF;               // loads of a step, at least
+    constexpr bool WIDE = SCALES == kWide16 || SCALES == kWide32, PAIRS = SCALES == kWide16 || SCALES == kPair || SCALES == kOdd;
+    constexpr int A = MF == 4 ? 1 : 2;           // pieces of a wave in a step
+    constexpr int D = MF == 1 ? 8 : 4;
+    constexpr int kTurn = 8;                     // steps after which slots and registers recur
+    constexpr int kThreads = 256 * kWavesK, kStep = kPiece * A, kChunks = kStep * kWavesK / 8;   // chunks of a row
+    constexpr int kStage = MF * 32 * kChunks * kChunk, kX = kStage / (kThreads * kChunk);
+    constexpr int kLeast = A + kX;               // loads of a step, at least
+    constexpr int G = WIDE ? kGroup / kStep : 1; // steps of a load of scales
+    constexpr int kWords = SCALES == kWide16 ? 4 : SCALES == kWide32 ? 2 : A;
     __shared__ __attribute__((aligned(1024))) char lds[D][kStage];
-    static_assert((KW - 1) * 4 * MF * 16 * kLanes * 4 <= D * kStage, "the other parts' sums");
+    static_assert((kWavesK - 1) * 4 * MF * 16 * kLanes * 4 <= D * kStage, "the other half's sums");
 
     const int tid = threadIdx.x, lane = tid % kLanes, g = lane / 32, i32 = lane % 32;
     const int wave = __builtin_amdgcn_readfirstlane(tid / kLanes), r = wave % 4, h = wave / 4;
     // neighbouring workgroups take the same weights for other activation rows
     const int64_t tile_m = blockIdx.x % p.tiles_m, rest = blockIdx.x / p.tiles_m;
     const int64_t n0 = rest % p.tiles_n * kRowsN, part = rest / p.tiles_n, m0 = tile_m * MF * 32;
-    const int64_t s0 = part * p.split_steps;
-    const int64_t s1 = s0 + p.split_steps < p.steps ? s0 + p.split_steps : p.steps;
+    const int k = (int)p.k, half = p.part_values / kWavesK, begin = (int)part * p.part_values;
+    const int k_begin = begin + h * half, k_end = k_begin + half < k ? k_begin + half : k;
+    const int steps = ((half < k - begin ? half : k - begin) + kStep - 1) / kStep;   // the first half is the longer one
 
-    const uint32_t q_ld = (uint32_t)(p.k / 2), s_ld = (uint32_t)(p.k >> p.shift);
-    const __amdgpu_buffer_rsrc_t rq = window(p.q + n0 * q_ld), rs = window(p.scales + n0 * s_ld), rx = window(p.x + m0 * p.ldx);
+    const uint32_t q_ld = (uint32_t)k / 2, s_ld = (uint32_t)k >> p.shift;
+    const __amdgpu_buffer_rsrc_t rq = window(p.q + n0 * q_ld), rs = window(p.scales + n0 * s_ld), rx = window(p.x + m0 * k * 2);
     const int row = r * 32 + i32;
-    const bool row_in = n0 + row < p.n;
-    const uint32_t q_row = (uint32_t)row * q_ld, s_row = (uint32_t)row * s_ld;
-
-    i32x4 w[D];
-    uint32_t sc[D];
-    auto fetch = [&](int64_t s, int slot) {
-        const int64_t k0 = s * kStep;
-        const int64_t v = k0 + h * 64 + g * 32;                // this lane's 32 values
-        const bool in0 = row_in && s < s1 && v < p.k, in1 = EVEN ? in0 : in0 && v + 16 < p.k;
-        if constexpr (EVEN) {
-            w[slot] = load16(rq, in0 ? q_row + (uint32_t)v / 2 : kOutside);
-        } else {
-            const i32x2 lo = load8(rq, in0 ? q_row + (uint32_t)v / 2 : kOutside), hi = load8(rq, in1 ? q_row + (uint32_t)v / 2 + 8 : kOutside);
-            w[slot] = i32x4{lo[0], lo[1], hi[0], hi[1]};
-        }
-        if constexpr (!PAIRS) sc[slot] = load1(rs, in0 ? s_row + (uint32_t)(v >> p.shift) : kOutside);
-        else if constexpr (EVEN)
-            sc[slot] = (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rs, (int)(in0 ? s_row + (uint32_t)(v >> 4) : kOutside), 0, 0);
-        else sc[slot] = load1(rs, in0 ? s_row + (uint32_t)(v >> 4) : kOutside) |
-                        load1(rs, in1 ? s_row + (uint32_t)(v >> 4) + 1 : kOutside) << 8;
+    // offsets of rows that are not there stay outside with any column added
+    const uint32_t q_row = n0 + row < p.n ? (uint32_t)row * q_ld : kOutside, s_row = n0 + row < p.n ? (uint32_t)row * s_ld : kOutside;
+    uint32_t x_row[kX];
+    int x_left[kX];                              // values from the chunk's first place to its half's end
 #pragma unroll
-        for (int i = 0; i < MF; ++i) {
-            // a chunk's place in its row is exchanged by the row: 16 lanes read one chunk of 16 rows
-            const int id = i * kThreads + tid, xr = id / kChunks, chunk = id % kChunks ^ xr % 16;
-            const bool in = m0 + xr < p.m && s < s1 && k0 + chunk * 8 < p.k;
-            const uint32_t off = in ? (uint32_t)xr * (uint32_t)p.ldx + (uint32_t)(k0 + chunk * 8) * 2 : kOutside;
+    for (int i = 0; i < kX; ++i) {
+        // a chunk's place in its row is exchanged by the row: 16 lanes read one chunk of 16 rows
+        const int id = i * kThreads + tid, xr = id / kChunks, chunk = id % kChunks ^ xr % 16;
+        const int from = begin + chunk / (kStep / 8) * half, at = from + chunk % (kStep / 8) * 8;
+        x_row[i] = m0 + xr < p.m ? ((uint32_t)xr * (uint32_t)k + at) * 2 : kOutside;
+        x_left[i] = (from + half < k ? from + half : k) - at;
+    }
+
+    i32x4 w[D][A];
+    uint32_t sc[kTurn / G][kWords];
+    auto fetch = [&](int s, int slot, int group) {         // group: the scales' registers, or -1: not this step
+        const int k0 = k_begin + s * kStep;
+#pragma unroll
+        for (int a = 0; a < A; ++a) {
+            const int v = k0 + a * kPiece + g * 32;        // this lane's 32 values
+            const bool in0 = v < k_end;
+            const uint32_t q_at = q_row + (uint32_t)v / 2;
+            if constexpr (SCALES == kOdd) {
+                const i32x2 lo = load8(rq, in0 ? q_at : kOutside), hi = load8(rq, v + 16 < k_end ? q_at + 8 : kOutside);
+                w[slot][a] = i32x4{lo[0], lo[1], hi[0], hi[1]};
+            } else {
+                w[slot][a] = load16(rq, in0 ? q_at : kOutside);
+            }
+            if constexpr (!WIDE) {
+                const uint32_t s_at = s_row + ((uint32_t)v >> p.shift);
+                uint32_t c;
+                if constexpr (SCALES == kOne) c = load1(rs, in0 ? s_at : kOutside);
+                else if constexpr (SCALES == kPair)
+                    c = (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rs, (int)(in0 ? s_at : kOutside), 0, 0);
+                else c = load1(rs, in0 ? s_at : kOutside) | load1(rs, v + 16 < k_end ? s_at + 1 : kOutside) << 8;
+                sc[group][a] = c;
+            }
+        }
+        if constexpr (SCALES == kWide16) {                 // k is a multiple of the group
+            if (group >= 0) {
+                const uint32_t s_at = s_row + (uint32_t)k0 / 16;
+                const i32x4 c = load16(rs, k0 < k_end ? s_at : kOutside);
+                sc[group][0] = (uint32_t)c[0], sc[group][1] = (uint32_t)c[1], sc[group][2] = (uint32_t)c[2], sc[group][3] = (uint32_t)c[3];
+            }
+        }
+        if constexpr (SCALES == kWide32) {
+            if (group >= 0) {
+                const i32x2 c = load8(rs, k0 < k_end ? s_row + (uint32_t)k0 / 32 : kOutside);
+                sc[group][0] = (uint32_t)c[0], sc[group][1] = (uint32_t)c[1];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kX; ++i) {
+            const uint32_t off = s * kStep < x_left[i] ? x_row[i] + (uint32_t)s * (kStep * 2) : kOutside;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (lds_void*)(lds[slot] + (i * kThreads + wave * kLanes) * kChunk), kChunk,
                                                      (int)off, 0, 0, 0);
         }
     };
+    auto group_of = [](int s) { return s % G == 0 ? s / G % (kTurn / G) : -1; };
 
     f32x16 acc[MF];
 #pragma unroll
@@ -93,41 +197,51 @@ __global__ __launch_bounds__(256 * kWavesK, kWavesK) void stream_kernel(Args p) 
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[i][e] = 0.0f;
 
-    // Registers: this step's activations and the next one's, read while this one's are multiplied.
-    bf16x8 xv[2][4][MF];
-    auto read = [&](int slot, int to, int j) {
+    // Registers: this piece's activations and the next one's, read while this one's are multiplied.
+    f16x8 xv[2][4][MF];
+    auto read = [&](int slot, int a, int to, int j) {
 #pragma unroll
         for (int i = 0; i < MF; ++i) {
-            const int chunk = (h * 8 + g * 4 + j) ^ i32 % 16;
-            xv[to][j][i] = *reinterpret_cast<const bf16x8*>(lds[slot] + (i * 32 + i32) * (kStep * 2) + chunk * kChunk);
+            const int chunk = ((h * A + a) * 8 + g * 4 + j) ^ i32 % 16;
+            xv[to][j][i] = *reinterpret_cast<const f16x8*>(lds[slot] + ((i * 32 + i32) * kChunks + chunk) * kChunk);
         }
     };
 #pragma unroll
-    for (int d = 0; d < D - 1; ++d) fetch(s0 + d, d);
+    for (int d = 0; d < D - 1; ++d) fetch(d, d, group_of(d));
     arrive<(D - 2) * kLeast>();
 #pragma unroll
-    for (int j = 0; j < 4; ++j) read(0, 0, j);
-    constexpr int kTurn = D % 2 ? 2 * D : D;     // steps after which slots and registers recur
-    for (int64_t s = s0; s < s1; s += kTurn) {
+    for (int j = 0; j < 4; ++j) read(0, 0, 0, j);
+    for (int s = 0; s < steps; s += kTurn) {
 #pragma unroll
         for (int d = 0; d < kTurn; ++d) {
-            if (s + d >= s1) break;
-            arrive<(D - 3) * kLeast>();          // the next step's activations are here, this one's are read
-            fetch(s + d + D - 1, (d + D - 1) % D);
+            if (s + d >= steps) break;
             const int slot = d % D;
-            const float f0 = e4m3_f32(sc[slot]), f1 = PAIRS ? e4m3_f32(sc[slot] >> 8) : f0;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                read((d + 1) % D, (d + 1) % 2, j);
-                const bf16x8 wv = expand8((uint32_t)w[slot][j], j < 2 ? f0 : f1);
+            for (int a = 0; a < A; ++a) {
+                const int now = (d * A + a) % 2, piece = d % G * A + a;      // of the group
+                uint32_t c;                                // blocks of 16: two codes, else one
+                if constexpr (SCALES == kWide16) c = sc[d / G][piece] >> (g * 16);
+                else if constexpr (SCALES == kWide32) c = sc[d / G][piece / 2] >> (piece % 2 * 16 + g * 8);
+                else c = sc[d][a];
+                const f16x2 f0 = e4m3_f16(c), f1 = PAIRS ? e4m3_f16(c >> 8) : f0;
+                if (a == A - 1) {
+                    arrive<(D - 3) * kLeast>();            // the next step's activations are here, this one's are read
+                    fetch(s + d + D - 1, (d + D - 1) % D, group_of(d + D - 1));
+                }
 #pragma unroll
-                for (int i = 0; i < MF; ++i) acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wv, xv[d % 2][j][i], acc[i], 0, 0, 0);
+                for (int j = 0; j < 4; ++j) {
+                    read(a == A - 1 ? (d + 1) % D : slot, a == A - 1 ? 0 : a + 1, now ^ 1, j);
+                    const f16x8 wv = expand8((uint32_t)w[slot][a][j], j < 2 ? f0 : f1);
+#pragma unroll
+                    for (int i = 0; i < MF; ++i)
+                        acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(wv, xv[now][j][i], acc[i], 0, 0, 0);
+                }
             }
         }
     }
 
     arrive<0>();
-    float* sums = reinterpret_cast<float*>(lds[0]);      // [KW - 1][4][MF][16][lanes]
+    float* sums = reinterpret_cast<float*>(lds[0]);        // [kWavesK - 1][4][MF][16][lanes]
     if (h > 0) {
 #pragma unroll
         for (int i = 0; i < MF; ++i)
@@ -137,20 +251,23 @@ __global__ __launch_bounds__(256 * kWavesK, kWavesK) void stream_kernel(Args p) 
     __syncthreads();
     if (h > 0) return;
 #pragma unroll
-    for (int o = 0; o < KW - 1; ++o)
+    for (int o = 0; o < kWavesK - 1; ++o)
 #pragma unroll
         for (int i = 0; i < MF; ++i)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][e] += sums[(((o * 4 + r) * MF + i) * 16 + e) * kLanes + lane];
-    const float scale = p.parts == 1 && p.scale ? *p.scale : 1.0f;
+    const float scale = *p.scale;
     const bool vec = p.n % 4 == 0;
 #pragma unroll
     for (int i = 0; i < MF; ++i) {
         const int64_t m = m0 + i * 32 + i32;
         if (m >= p.m) continue;
+        const int e = p.exponents[m];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const f32x4 v = f32x4{acc[i][q * 4], acc[i][q * 4 + 1], acc[i][q * 4 + 2], acc[i][q * 4 + 3]} * scale;
+            f32x4 v;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) v[c] = ldexpf(acc[i][q * 4 + c] * scale, e);
             const int64_t n = n0 + r * 32 + q * 8 + g * 4;
             store4(p.out, p.parts > 1 || p.out_f32, ((p.parts > 1 ? part * p.m : 0) + m) * p.n + n, p.n - n, vec, v);
         }
@@ -159,15 +276,19 @@ __global__ __launch_bounds__(256 * kWavesK, kWavesK) void stream_kernel(Args p) 
 
 inline int rows_of(int64_t m) { return m <= 32 ? 1 : m <= 64 ? 2 : 4; }
 inline int tiles_m(int64_t m) { return (int)((m + 127) / 128); }
-inline int64_t steps(int64_t k) { return (k + 64 * kWavesK - 1) / (64 * kWavesK); }
-// A workgroup takes a compute unit's LDS: parts of the contraction, of at least eight steps, until 256 units
+// A workgroup takes a compute unit's LDS: parts of the contraction, of at least 1024 values, until 256 units
 // have work.
 inline int parts(int64_t m, int64_t n, int64_t k) {
     const int64_t groups = (n + kRowsN - 1) / kRowsN * tiles_m(m);
     int64_t want = (256 + groups / 2) / (groups ? groups : 1);
-    if (want > steps(k) / 8) want = steps(k) / 8;
+    if (want > k / 1024) want = k / 1024;
     if (want > 16) want = 16;
     return want < 1 ? 1 : (int)want;
+}
+// Values of a part: halves of whole groups.
+inline int part_values(int64_t k, int parts) {
+    constexpr int64_t kUnit = kGroup * kWavesK;
+    return (int)(((k + parts - 1) / parts + kUnit - 1) / kUnit * kUnit);
 }
 
 }  // namespace stream_product
