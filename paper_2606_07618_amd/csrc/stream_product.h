@@ -9,10 +9,10 @@
 //
 // A workgroup owns 128 weight rows and up to 128 activation rows.  Its waves are four times 32 weight rows by the
 // two halves of its contraction; a wave loads its weights (32 rows by two lanes of 16 bytes) into
-// registers, D steps ahead, and all waves share the step's activations in LDS, as many steps ahead, so that a
-// step's wait is for what was started D - 1 steps before.  The halves' sums meet in LDS at the end.
-// The scales of 256 values of a row come in one load where their rows allow it: two bytes at a time, each
-// visit to a row of scales would fetch its line anew.
+// registers, kAhead groups ahead, and all waves share a step's activations in LDS, D - 1 steps ahead; a step waits
+// for what was started then and for nothing later.  The halves' sums meet in LDS at the end.
+// Weights are loaded by groups of 256 values of a row, whole lines of 128 bytes, and so are the group's scales
+// where their rows allow it: visited in smaller pieces, a line would have left the L1 between two visits.
 // Few weight rows: the contraction is split over workgroups as well, whose sums a second kernel adds in order.
 #pragma once
 
@@ -109,13 +109,14 @@ template <int MF, Scales SCALES>
 __global__ __launch_bounds__(256 * kWavesK, kWavesK) void stream_kernel(Args p) {
     constexpr bool WIDE = SCALES == kWide16 || SCALES == kWide32, PAIRS = SCALES == kWide16 || SCALES == kPair || SCALES == kOdd;
     constexpr int A = MF == 4 ? 1 : 2;           // pieces of a wave in a step
-    constexpr int D = MF == 1 ? 8 : 4;
-    constexpr int kTurn = 8;                     // steps after which slots and registers recur
+    constexpr int D = 4, kTurn = MF == 4 ? 8 : 4;              // kTurn: steps after which slots and registers recur
     constexpr int kThreads = 256 * kWavesK, kStep = kPiece * A, kChunks = kStep * kWavesK / 8;   // chunks of a row
     constexpr int kStage = MF * 32 * kChunks * kChunk, kX = kStage / (kThreads * kChunk);
-    constexpr int kLeast = A + kX;               // loads of a step, at least
-    constexpr int G = WIDE ? kGroup / kStep : 1; // steps of a load of scales
-    constexpr int kWords = SCALES == kWide16 ? 4 : SCALES == kWide32 ? 2 : A;
+    constexpr int kPieces = kGroup / kPiece, G = kGroup / kStep;             // of a group; steps of a group
+    constexpr int kGroups = kTurn / G, kAhead = 1;
+    constexpr int kWords = SCALES == kWide16 ? 4 : SCALES == kWide32 ? 2 : kPieces;
+    // loads of a group; kOdd's halves are left out of the count, which can only make a wait longer
+    constexpr int kLoads = SCALES == kOdd ? 0 : kPieces + (WIDE ? 1 : kPieces);
     __shared__ __attribute__((aligned(1024))) char lds[D][kStage];
     static_assert((kWavesK - 1) * 4 * MF * 16 * kLanes * 4 <= D * kStage, "the other half's sums");
 
@@ -144,44 +145,42 @@ __global__ __launch_bounds__(256 * kWavesK, kWavesK) void stream_kernel(Args p) 
         x_left[i] = (from + half < k ? from + half : k) - at;
     }
 
-    i32x4 w[D][A];
-    uint32_t sc[kTurn / G][kWords];
-    auto fetch = [&](int s, int slot, int group) {         // group: the scales' registers, or -1: not this step
-        const int k0 = k_begin + s * kStep;
+    i32x4 w[kGroups][kPieces];
+    uint32_t sc[kGroups][kWords];
+    auto fetch_weights = [&](int group, auto to) {
+        constexpr int T = decltype(to)::value;
+        const int k0 = k_begin + group * kGroup;
 #pragma unroll
-        for (int a = 0; a < A; ++a) {
+        for (int a = 0; a < kPieces; ++a) {
             const int v = k0 + a * kPiece + g * 32;        // this lane's 32 values
             const bool in0 = v < k_end;
             const uint32_t q_at = q_row + (uint32_t)v / 2;
             if constexpr (SCALES == kOdd) {
                 const i32x2 lo = load8(rq, in0 ? q_at : kOutside), hi = load8(rq, v + 16 < k_end ? q_at + 8 : kOutside);
-                w[slot][a] = i32x4{lo[0], lo[1], hi[0], hi[1]};
+                w[T][a] = i32x4{lo[0], lo[1], hi[0], hi[1]};
             } else {
-                w[slot][a] = load16(rq, in0 ? q_at : kOutside);
+                w[T][a] = load16(rq, in0 ? q_at : kOutside);
             }
             if constexpr (!WIDE) {
                 const uint32_t s_at = s_row + ((uint32_t)v >> p.shift);
-                uint32_t c;
-                if constexpr (SCALES == kOne) c = load1(rs, in0 ? s_at : kOutside);
+                if constexpr (SCALES == kOne) sc[T][a] = load1(rs, in0 ? s_at : kOutside);
                 else if constexpr (SCALES == kPair)
-                    c = (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rs, (int)(in0 ? s_at : kOutside), 0, 0);
-                else c = load1(rs, in0 ? s_at : kOutside) | load1(rs, v + 16 < k_end ? s_at + 1 : kOutside) << 8;
-                sc[group][a] = c;
+                    sc[T][a] = (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rs, (int)(in0 ? s_at : kOutside), 0, 0);
+                else sc[T][a] = load1(rs, in0 ? s_at : kOutside) | load1(rs, v + 16 < k_end ? s_at + 1 : kOutside) << 8;
             }
         }
         if constexpr (SCALES == kWide16) {                 // k is a multiple of the group
-            if (group >= 0) {
-                const uint32_t s_at = s_row + (uint32_t)k0 / 16;
-                const i32x4 c = load16(rs, k0 < k_end ? s_at : kOutside);
-                sc[group][0] = (uint32_t)c[0], sc[group][1] = (uint32_t)c[1], sc[group][2] = (uint32_t)c[2], sc[group][3] = (uint32_t)c[3];
-            }
+            const i32x4 c = load16(rs, k0 < k_end ? s_row + (uint32_t)k0 / 16 : kOutside);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sc[T][j] = (uint32_t)c[j];
         }
         if constexpr (SCALES == kWide32) {
-            if (group >= 0) {
-                const i32x2 c = load8(rs, k0 < k_end ? s_row + (uint32_t)k0 / 32 : kOutside);
-                sc[group][0] = (uint32_t)c[0], sc[group][1] = (uint32_t)c[1];
-            }
+            const i32x2 c = load8(rs, k0 < k_end ? s_row + (uint32_t)k0 / 32 : kOutside);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) sc[T][j] = (uint32_t)c[j];
         }
+    };
+    auto fetch_x = [&](int s, int slot) {
 #pragma unroll
         for (int i = 0; i < kX; ++i) {
             const uint32_t off = s * kStep < x_left[i] ? x_row[i] + (uint32_t)s * (kStep * 2) : kOutside;
@@ -189,7 +188,12 @@ __global__ __launch_bounds__(256 * kWavesK, kWavesK) void stream_kernel(Args p) 
                                                      (int)off, 0, 0, 0);
         }
     };
-    auto group_of = [](int s) { return s % G == 0 ? s / G % (kTurn / G) : -1; };
+    // what step s (d of its turn) starts: a group's weights in a group's first step, then a later step's activations
+    auto fetch = [&](int s, auto dc) {
+        constexpr int d = decltype(dc)::value;
+        if constexpr (d % G == 0) fetch_weights(s / G + kAhead, Const<(d / G + kAhead) % kGroups>{});
+        fetch_x(s + D - 1, (d + D - 1) % D);
+    };
 
     f32x16 acc[MF];
 #pragma unroll
@@ -197,47 +201,62 @@ __global__ __launch_bounds__(256 * kWavesK, kWavesK) void stream_kernel(Args p) 
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[i][e] = 0.0f;
 
-    // Registers: this piece's activations and the next one's, read while this one's are multiplied.
-    f16x8 xv[2][4][MF];
-    auto read = [&](int slot, int a, int to, int j) {
+    // Registers: the activations of four matrix instructions along the contraction, read two ahead of their use.
+    f16x8 xv[4][MF];
+    int x_lane = (i32 * kChunks + ((h * A * 8 + g * 4) ^ i32 % 16)) * kChunk;      // of piece 0, instruction 0
+    auto read = [&](int slot, int a, int j) {
 #pragma unroll
         for (int i = 0; i < MF; ++i) {
-            const int chunk = ((h * A + a) * 8 + g * 4 + j) ^ i32 % 16;
-            xv[to][j][i] = *reinterpret_cast<const f16x8*>(lds[slot] + ((i * 32 + i32) * kChunks + chunk) * kChunk);
+            xv[j][i] = *reinterpret_cast<const f16x8*>(lds[slot] + i * (32 * kChunks * kChunk) + (x_lane ^ (a * 8 + j) * kChunk));
         }
     };
+    // One step; past the last one it multiplies zeros.
+    auto step = [&](int s, auto dc) {
+        constexpr int d = decltype(dc)::value, slot = d % D;
+        asm volatile("" : "+v"(x_lane));                   // addresses are made in each step, not kept for all
 #pragma unroll
-    for (int d = 0; d < D - 1; ++d) fetch(d, d, group_of(d));
-    arrive<(D - 2) * kLeast>();
+        for (int a = 0; a < A; ++a) {
+            const int piece = d % G * A + a;               // of the group
+            uint32_t c;                                    // blocks of 16: two codes, else one
+            if constexpr (SCALES == kWide16) c = sc[d / G][piece] >> (g * 16);
+            else if constexpr (SCALES == kWide32) c = sc[d / G][piece / 2] >> (piece % 2 * 16 + g * 8);
+            else c = sc[d / G][piece];
+            const f16x2 f0 = e4m3_f16(c), f1 = PAIRS ? e4m3_f16(c >> 8) : f0;
+            if (a == A - 1) {
+                // the next step's activations are here, the last one's are read; later loads: of the D - 3 steps before
+                constexpr int first = d + 3 - D + kTurn, last = d - 1 + kTurn;   // of the turn before, on
+                constexpr int kStarts = last / G - (first - 1) / G;          // groups begun in them
+                arrive<(D - 3) * kX + kStarts * kLoads>();
+                fetch(s, dc);
+            }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) read(0, 0, 0, j);
-    for (int s = 0; s < steps; s += kTurn) {
+            for (int j = 0; j < 4; ++j) {
+                if (j < 2) read(slot, a, j + 2);
+                else read(a == A - 1 ? (d + 1) % D : slot, a == A - 1 ? 0 : a + 1, j - 2);
+                int n = w[d / G][piece][j];
+                asm volatile("" : "+v"(n));              // expanded here, where its registers are needed, not a step ahead
+                const f16x8 wv = expand8((uint32_t)n, j < 2 ? f0 : f1);
 #pragma unroll
-        for (int d = 0; d < kTurn; ++d) {
-            if (s + d >= steps) break;
-            const int slot = d % D;
-#pragma unroll
-            for (int a = 0; a < A; ++a) {
-                const int now = (d * A + a) % 2, piece = d % G * A + a;      // of the group
-                uint32_t c;                                // blocks of 16: two codes, else one
-                if constexpr (SCALES == kWide16) c = sc[d / G][piece] >> (g * 16);
-                else if constexpr (SCALES == kWide32) c = sc[d / G][piece / 2] >> (piece % 2 * 16 + g * 8);
-                else c = sc[d][a];
-                const f16x2 f0 = e4m3_f16(c), f1 = PAIRS ? e4m3_f16(c >> 8) : f0;
-                if (a == A - 1) {
-                    arrive<(D - 3) * kLeast>();            // the next step's activations are here, this one's are read
-                    fetch(s + d + D - 1, (d + D - 1) % D, group_of(d + D - 1));
-                }
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    read(a == A - 1 ? (d + 1) % D : slot, a == A - 1 ? 0 : a + 1, now ^ 1, j);
-                    const f16x8 wv = expand8((uint32_t)w[slot][a][j], j < 2 ? f0 : f1);
-#pragma unroll
-                    for (int i = 0; i < MF; ++i)
-                        acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(wv, xv[now][j][i], acc[i], 0, 0, 0);
-                }
+                for (int i = 0; i < MF; ++i) acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(wv, xv[j][i], acc[i], 0, 0, 0);
             }
         }
+    };
+    // What the steps before the first one would have started, in their order: the waits count on it.
+    auto in_order = [] { asm volatile("" ::: "memory"); };
+    static_assert(kAhead == 1 && kGroups == 2, "one group ahead");
+#pragma unroll
+    for (int d = 0; d < D - 1; ++d) {
+        if (d == (G < D - 1 ? D - 1 - G : 0)) fetch_weights(0, Const<0>{});
+        in_order();
+        fetch_x(d, d);
+        in_order();
+    }
+    arrive<(D - 2) * kX>();
+#pragma unroll
+    for (int j = 0; j < 2; ++j) read(0, 0, j);
+    for (int s = 0; s < steps; s += kTurn) {
+        step(s, Const<0>{}), step(s + 1, Const<1>{}), step(s + 2, Const<2>{}), step(s + 3, Const<3>{});
+        if constexpr (kTurn == 8) step(s + 4, Const<4>{}), step(s + 5, Const<5>{}), step(s + 6, Const<6>{}), step(s + 7, Const<7>{});
     }
 
     arrive<0>();
