@@ -9,18 +9,17 @@ namespace {
 
 using namespace product_host;
 
-using Big = Tile<256, 256, 2, 4>;
 constexpr int kEdgeThreads = 256;
 
 __device__ __forceinline__ float bf16_f32(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }
 
-// dg and du, side by side: d [m, 2 * half], du from column `half` on, zeros past n.  Their rounding to
+// dg and du, side by side: d [m, ld], du from column `half` on, zeros from n to half.  Their rounding to
 // bfloat16 is what the matrix cores take; the products' sums stay in binary32.
 template <bool VEC>
 __global__ __launch_bounds__(kEdgeThreads) void gate_grad_kernel(const uint16_t* __restrict__ dh,
                                                                  const uint16_t* __restrict__ gate,
                                                                  const uint16_t* __restrict__ up_, int64_t m, int64_t n,
-                                                                 int64_t half, uint16_t* __restrict__ d) {
+                                                                 int64_t half, int64_t ld, uint16_t* __restrict__ d) {
     const int64_t row_units = half / 8, units = m * row_units;
     for (int64_t i = (int64_t)blockIdx.x * kEdgeThreads + threadIdx.x; i < units;
          i += (int64_t)gridDim.x * kEdgeThreads) {
@@ -54,8 +53,8 @@ __global__ __launch_bounds__(kEdgeThreads) void gate_grad_kernel(const uint16_t*
             og[j] = pack_bf16(dg[0], dg[1]);
             ou[j] = pack_bf16(du[0], du[1]);
         }
-        *reinterpret_cast<uint4*>(d + r * 2 * half + c) = make_uint4(og[0], og[1], og[2], og[3]);
-        *reinterpret_cast<uint4*>(d + r * 2 * half + half + c) = make_uint4(ou[0], ou[1], ou[2], ou[3]);
+        *reinterpret_cast<uint4*>(d + r * ld + c) = make_uint4(og[0], og[1], og[2], og[3]);
+        *reinterpret_cast<uint4*>(d + r * ld + half + c) = make_uint4(ou[0], ou[1], ou[2], ou[3]);
     }
 }
 
@@ -83,7 +82,7 @@ int64_t pack_workspace(int64_t m, int64_t n, int64_t k, int64_t ldx, int64_t ldw
 int64_t half_of(int64_t n) { return up(n, 64); }       // whole steps of the contraction
 
 int64_t backward_workspace(int64_t m, int64_t n, int64_t k, int64_t ldx, int64_t ldw) {
-    return pack_workspace(m, n, k, ldx, ldw) + up(m * 2 * half_of(n) * 2, 256);
+    return pack_workspace(m, n, k, ldx, ldw) + up(m * spread_ld(2 * half_of(n)) * 2, 256) + parts_bytes<kBf16, kAcross, kPairInner>(m, k, n);
 }
 
 int check_call(int64_t m, int64_t n, int64_t k, int64_t ldx, int64_t ldw) {
@@ -135,7 +134,8 @@ int nvfp4_swiglu_ffn(const void* x, int64_t ldx, const void* w_gate, const void*
     p.a.p = static_cast<const char*>(rx.p), p.a.ld = rx.ld * 2;
     p.b.p = static_cast<const char*>(rg.p), p.b.p2 = static_cast<const char*>(ru.p), p.b.ld = rg.ld * 2;
     p.m = m, p.n = n, p.inner = k, p.out = h, p.out2 = gate, p.out3 = up_out, p.out_ld = n;
-    return launch_product<kBf16, kAlong, kAlong, kPairOuter, kGate, Big>(p, st);
+    p.parts = 1;
+    return launch_product<kBf16, kAlong, kAlong, kPairOuter, kGate>(p, plan_product<kBf16, kAlong, kPairOuter>(m, n, k, false).tile, st);
 }
 
 int64_t nvfp4_swiglu_ffn_backward_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t ldx, int64_t ldw) {
@@ -160,13 +160,14 @@ int nvfp4_swiglu_ffn_backward(const void* dh, const void* x, int64_t ldx, const 
     hipStream_t st = (hipStream_t)stream;
     Carver c{static_cast<char*>(workspace)};
     const int64_t half = half_of(n);
-    uint16_t* d = static_cast<uint16_t*>(c.take(m * 2 * half * 2));
+    const int64_t ld = spread_ld(2 * half);
+    uint16_t* d = static_cast<uint16_t*>(c.take(m * ld * 2));
     const int64_t units = m * (half / 8), groups = ceil_div(units, kEdgeThreads);
     if (units > 0) {
         hipLaunchKernelGGL((n % 8 == 0 ? gate_grad_kernel<true> : gate_grad_kernel<false>),
                            dim3((unsigned)(groups < 16384 ? groups : 16384)), dim3(kEdgeThreads), 0, st,
                            static_cast<const uint16_t*>(dh), static_cast<const uint16_t*>(gate),
-                           static_cast<const uint16_t*>(up_in), m, n, half, d);
+                           static_cast<const uint16_t*>(up_in), m, n, half, ld, d);
         if (const int rc = launched()) return rc;
     }
     Rows rx{x, ldx}, rg{w_gate, ldw}, ru{w_up, ldw};
@@ -175,19 +176,21 @@ int nvfp4_swiglu_ffn_backward(const void* dh, const void* x, int64_t ldx, const 
         if (const int rc = packed(c, rg, n, k, pw, st)) return rc;
         if (const int rc = packed(c, ru, n, k, pw, st)) return rc;
         Args p = {};
-        p.a.p = reinterpret_cast<const char*>(d), p.a.ld = 2 * half * 2;
+        p.a.p = reinterpret_cast<const char*>(d), p.a.ld = ld * 2;
         p.b.p = static_cast<const char*>(rg.p), p.b.p2 = static_cast<const char*>(ru.p), p.b.ld = rg.ld * 2;
         p.m = m, p.n = k, p.inner = n, p.out = dx, p.out_ld = k;
-        if (const int rc = launch_product<kBf16, kAlong, kAcross, kPairInner, kSums, Big>(p, st)) return rc;
+        if (const int rc = run_sums<kBf16, kAlong, kAcross, kPairInner>(p, static_cast<float*>(c.take(0)), st)) return rc;
     }
     if (want_w) {
         if (const int rc = packed(c, rx, m, k, needs_pack(k, ldx), st)) return rc;
         Args p = {};
-        p.a.p = reinterpret_cast<const char*>(d), p.a.ld = 2 * half * 2;
+        p.a.p = reinterpret_cast<const char*>(d), p.a.ld = ld * 2;
         p.b.p = static_cast<const char*>(rx.p), p.b.ld = rx.ld * 2;
         p.m = 2 * half, p.n = k, p.inner = m, p.half_rows = half, p.out_rows = n;
         p.out = dw_gate, p.out2 = dw_up, p.out_ld = k;
-        if (const int rc = launch_product<kBf16, kAcross, kAcross, kSingle, kTwoRows, Big>(p, st)) return rc;
+        p.parts = 1;
+        const int tile = plan_product<kBf16, kAcross, kSingle>(p.m, k, m, false).tile;
+        if (const int rc = launch_product<kBf16, kAcross, kAcross, kSingle, kTwoRows>(p, tile, st)) return rc;
     }
     return NVFP4_OK;
 }

@@ -30,6 +30,31 @@ int pack(const V* src, int64_t rows, int64_t width, int64_t ld, V* dst, int64_t 
     return launched();
 }
 
+// Sums of parts of the contraction.
+constexpr int kJoinThreads = 256;
+
+template <bool VEC>
+__global__ __launch_bounds__(kJoinThreads) void join_kernel(const float* __restrict__ part, int parts, int64_t count,
+                                                            const float* __restrict__ scale, void* __restrict__ out,
+                                                            int f32) {
+    constexpr int kPer = VEC ? 4 : 1;
+    const int64_t at = ((int64_t)blockIdx.x * kJoinThreads + threadIdx.x) * kPer;
+    if (at >= count) return;
+    float v[kPer] = {};
+    for (int p = 0; p < parts; ++p) {
+        const float* from = part + p * count + at;
+        if constexpr (VEC) {
+            const float4 w = *reinterpret_cast<const float4*>(from);
+            v[0] += w.x, v[1] += w.y, v[2] += w.z, v[3] += w.w;
+        } else {
+            v[0] += *from;
+        }
+    }
+    const float s = scale ? *scale : 1.0f;
+    if constexpr (VEC) store4(out, f32, at, 4, true, f32x4{v[0], v[1], v[2], v[3]} * s);
+    else store4(out, f32, at, 1, false, f32x4{v[0] * s, 0.0f, 0.0f, 0.0f});
+}
+
 }  // namespace
 
 int pack_bf16_rows(const void* src, int64_t rows, int64_t width, int64_t ld, void* dst, hipStream_t stream) {
@@ -40,14 +65,22 @@ int pack_scale_rows(const uint8_t* src, int64_t rows, int64_t width, uint8_t* ds
     return pack(src, rows, width, width, dst, dst_ld, stream);
 }
 
+
+int join_parts(const float* part, int parts, int64_t count, const float* scale, void* out, int f32, hipStream_t stream) {
+    const bool vec = count % 4 == 0;
+    const int64_t groups = ceil_div(vec ? count / 4 : count, kJoinThreads);
+    if (groups > 0x7FFFFFFF) return NVFP4_ERR_SHAPE;
+    hipLaunchKernelGGL((vec ? join_kernel<true> : join_kernel<false>), dim3((unsigned)groups), dim3(kJoinThreads), 0, stream,
+                       part, parts, count, scale, out, f32);
+    return launched();
+}
+
 }  // namespace product_host
 
 namespace {
 
 using namespace product_host;
 typedef float f32x2 __attribute__((ext_vector_type(2)));
-
-using Big = Tile<256, 256, 2, 4>;
 
 // ---- weights expanded to bfloat16 -----------------------------------------------------------
 
@@ -73,64 +106,32 @@ __device__ __forceinline__ uint4 expand8(uint32_t n, uint32_t code) {
 
 constexpr int kExpandThreads = 256;
 
-// The weights are a run of blocks of 2^shift units of 8 values.
+// Rows of row_units units of 8 values, a scale for each 2^shift of them; a workgroup expands a piece of one row.
 template <Kind KIND>
 __global__ __launch_bounds__(kExpandThreads) void expand_kernel(const uint32_t* __restrict__ q,
-                                                                const uint8_t* __restrict__ scales, int64_t units,
-                                                                int shift, uint4* __restrict__ out) {
-    const int64_t u = (int64_t)blockIdx.x * kExpandThreads + threadIdx.x;
-    if (u < units) out[u] = expand8<KIND>(q[u], scales[u >> shift]);
+                                                                const uint8_t* __restrict__ scales, uint32_t row_units,
+                                                                uint32_t row_groups, int shift, int64_t ld_units,
+                                                                uint4* __restrict__ out) {
+    const uint32_t row = blockIdx.x / row_groups, u = blockIdx.x % row_groups * kExpandThreads + threadIdx.x;
+    if (u >= row_units) return;
+    const int64_t at = (int64_t)row * row_units + u;
+    out[row * ld_units + u] = expand8<KIND>(q[at], scales[at >> shift]);
 }
 
 template <Kind KIND>
 int expand(const uint8_t* q, const uint8_t* scales, int64_t n, int64_t k, int block, void* out, hipStream_t stream) {
-    const int64_t units = n * (k / 8), groups = ceil_div(units, kExpandThreads);
-    if (units == 0) return NVFP4_OK;
-    if (groups > 0x7FFFFFFF) return NVFP4_ERR_SHAPE;
+    const int64_t row_units = k / 8, row_groups = ceil_div(row_units, kExpandThreads);
+    if (n * row_units == 0) return NVFP4_OK;
+    if (n * row_groups > 0x7FFFFFFF) return NVFP4_ERR_SHAPE;
     int shift = 1;
     while (8 << shift < block) ++shift;
-    hipLaunchKernelGGL((expand_kernel<KIND>), dim3((unsigned)groups), dim3(kExpandThreads), 0, stream,
-                       reinterpret_cast<const uint32_t*>(q), scales, units, shift, static_cast<uint4*>(out));
+    hipLaunchKernelGGL((expand_kernel<KIND>), dim3((unsigned)(n * row_groups)), dim3(kExpandThreads), 0, stream,
+                       reinterpret_cast<const uint32_t*>(q), scales, (uint32_t)row_units, (uint32_t)row_groups, shift,
+                       spread_ld(k) / 8, static_cast<uint4*>(out));
     return launched();
 }
 
 bool valid_out(int dtype) { return dtype == NVFP4_IN_F32 || dtype == NVFP4_IN_BF16; }
-
-// ---- sums of parts of the contraction -----------------------------------------------------------
-
-constexpr int kJoinThreads = 256;
-
-template <bool VEC>
-__global__ __launch_bounds__(kJoinThreads) void join_kernel(const float* __restrict__ part, int parts, int64_t count,
-                                                            const float* __restrict__ scale, void* __restrict__ out,
-                                                            int f32) {
-    constexpr int kPer = VEC ? 4 : 1;
-    const int64_t at = ((int64_t)blockIdx.x * kJoinThreads + threadIdx.x) * kPer;
-    if (at >= count) return;
-    float v[kPer] = {};
-    for (int p = 0; p < parts; ++p) {
-        const float* from = part + p * count + at;
-        if constexpr (VEC) {
-            const float4 w = *reinterpret_cast<const float4*>(from);
-            v[0] += w.x, v[1] += w.y, v[2] += w.z, v[3] += w.w;
-        } else {
-            v[0] += *from;
-        }
-    }
-    const float s = scale ? *scale : 1.0f;
-    if constexpr (VEC) store4(out, f32, at, 4, true, f32x4{v[0], v[1], v[2], v[3]} * s);
-    else store4(out, f32, at, 1, false, f32x4{v[0] * s, 0.0f, 0.0f, 0.0f});
-}
-
-// out = scale * (the parts' sums [parts, count], added in order)
-int join(const float* part, int parts, int64_t count, const float* scale, void* out, int f32, hipStream_t stream) {
-    const bool vec = count % 4 == 0;
-    const int64_t groups = ceil_div(vec ? count / 4 : count, kJoinThreads);
-    if (groups > 0x7FFFFFFF) return NVFP4_ERR_SHAPE;
-    hipLaunchKernelGGL((vec ? join_kernel<true> : join_kernel<false>), dim3((unsigned)groups), dim3(kJoinThreads), 0, stream,
-                       part, parts, count, scale, out, f32);
-    return launched();
-}
 
 // ---- y = x W^T ------------------------------------------------------------------------------
 
@@ -142,7 +143,7 @@ int64_t linear_workspace(int64_t m, int64_t n, int64_t k) {
         const int parts = stream_product::parts(m, n, k);
         return up(m * k * 2, 256) + up(m * 4, 256) + (parts > 1 ? up(parts * m * n * 4, 256) : 0);
     }
-    return up(n * k * 2, 256);
+    return up(n * spread_ld(k) * 2, 256) + parts_bytes<kBf16, kAlong, kSingle>(m, n, k);
 }
 
 template <int MF>
@@ -192,23 +193,25 @@ int run_linear(const void* x, int64_t ldx, const uint8_t* q, const uint8_t* scal
             default: launch_stream<4>(t, stream);
         }
         if (const int rc = launched()) return rc;
-        return partial ? join(partial, t.parts, m * n, nullptr, out, f32, stream) : NVFP4_OK;
+        return partial ? join_parts(partial, t.parts, m * n, nullptr, out, f32, stream) : NVFP4_OK;
     }
-    if (const int rc = expand<kBf16>(q, scales, n, k, block, ws, stream)) return rc;
+    Carver c{static_cast<char*>(ws)};
+    void* w = c.take(n * spread_ld(k) * 2);
+    if (const int rc = expand<kBf16>(q, scales, n, k, block, w, stream)) return rc;
     Args p = {};
     p.a.p = static_cast<const char*>(x), p.a.ld = ldx * 2;
-    p.b.p = static_cast<const char*>(ws), p.b.ld = k * 2;
+    p.b.p = static_cast<const char*>(w), p.b.ld = spread_ld(k) * 2;
     p.m = m, p.n = n, p.inner = k, p.scale = S, p.out = out, p.out_ld = n, p.out_f32 = out_dtype == NVFP4_IN_F32;
-    return launch_product<kBf16, kAlong, kAlong, kSingle, kSums, Big>(p, stream);
+    return run_sums<kBf16, kAlong, kAlong, kSingle>(p, static_cast<float*>(c.take(0)), stream);
 }
 
 // ---- dx = dy W ------------------------------------------------------------------------------
 
-int64_t grad_workspace(int64_t m, int64_t n, int64_t k32, int64_t ld) {
+int64_t grad_workspace(int64_t m, int64_t n, int64_t k, int64_t k32, int64_t ld) {
     Carver c{nullptr};
-    c.take(n * k32 * 2);
+    c.take(n * spread_ld(k32) * 2);
     if (needs_pack(n, ld)) c.take(m * packed_ld(n) * 2);
-    return c.at;
+    return c.at + parts_bytes<kBf16, kAcross, kSingle>(m, k, n);
 }
 
 // k32: the width of the weights' rows (k filled up to whole blocks); dx has k columns.
@@ -216,7 +219,7 @@ template <Kind KIND>
 int run_grad(const void* dy, int64_t ld, const uint8_t* q, const uint8_t* scales, int block, const float* S, int64_t m,
              int64_t n, int64_t k, int64_t k32, int out_dtype, void* out, void* ws, hipStream_t stream) {
     Carver c{static_cast<char*>(ws)};
-    void* w = c.take(n * k32 * 2);
+    void* w = c.take(n * spread_ld(k32) * 2);
     if (const int rc = expand<KIND>(q, scales, n, k32, block, w, stream)) return rc;
     if (needs_pack(n, ld)) {
         void* packed = c.take(m * packed_ld(n) * 2);
@@ -225,9 +228,9 @@ int run_grad(const void* dy, int64_t ld, const uint8_t* q, const uint8_t* scales
     }
     Args p = {};
     p.a.p = static_cast<const char*>(dy), p.a.ld = ld * 2;
-    p.b.p = static_cast<const char*>(w), p.b.ld = k32 * 2;
+    p.b.p = static_cast<const char*>(w), p.b.ld = spread_ld(k32) * 2;
     p.m = m, p.n = k, p.inner = n, p.scale = S, p.out = out, p.out_ld = k, p.out_f32 = out_dtype == NVFP4_IN_F32;
-    return launch_product<kBf16, kAlong, kAcross, kSingle, kSums, Big>(p, stream);
+    return run_sums<kBf16, kAlong, kAcross, kSingle>(p, static_cast<float*>(c.take(0)), stream);
 }
 
 // ---- y = A B^T, both microscaled --------------------------------------------------------------
@@ -239,7 +242,7 @@ int64_t mx_workspace(int64_t m, int64_t n, int64_t blocks) {
         c.take(m * up(blocks, 8));
         c.take(n * up(blocks, 8));
     }
-    return c.at;
+    return c.at + (m > thin_product::kRows ? parts_bytes<kMx, kAlong, kSingle>(m, n, blocks * 32) : 0);
 }
 
 int run_mx(const uint8_t* aq, const uint8_t* as, const uint8_t* bq, const uint8_t* bs, int64_t m, int64_t n,
@@ -253,8 +256,8 @@ int run_mx(const uint8_t* aq, const uint8_t* as, const uint8_t* bq, const uint8_
         return launched();
     }
     int64_t scale_ld = blocks;
+    Carver c{static_cast<char*>(ws)};
     if (blocks % 4) {
-        Carver c{static_cast<char*>(ws)};
         scale_ld = up(blocks, 8);
         uint8_t* pa = static_cast<uint8_t*>(c.take(m * scale_ld));
         uint8_t* pb = static_cast<uint8_t*>(c.take(n * scale_ld));
@@ -266,7 +269,7 @@ int run_mx(const uint8_t* aq, const uint8_t* as, const uint8_t* bq, const uint8_
     p.a.p = reinterpret_cast<const char*>(aq), p.a.ld = blocks * 16, p.a.scales = as, p.a.scale_ld = scale_ld;
     p.b.p = reinterpret_cast<const char*>(bq), p.b.ld = blocks * 16, p.b.scales = bs, p.b.scale_ld = scale_ld;
     p.m = m, p.n = n, p.inner = blocks * 32, p.out = out, p.out_ld = n, p.out_f32 = out_dtype == NVFP4_IN_F32;
-    return launch_product<kMx, kAlong, kAlong, kSingle, kSums, Big>(p, stream);
+    return run_sums<kMx, kAlong, kAlong, kSingle>(p, static_cast<float*>(c.take(0)), stream);
 }
 
 int check_ws(const void* ws, size_t bytes, int64_t need) {
@@ -305,7 +308,7 @@ int nvfp4_matmul(const void* x, int64_t ldx, const uint8_t* q, const uint8_t* sc
 
 int64_t nvfp4_matmul_grad_input_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t ld) {
     if (const int rc = check_dims(m, n, k)) return rc;
-    return grad_workspace(m, n, k, ld);
+    return grad_workspace(m, n, k, k, ld);
 }
 
 int nvfp4_matmul_grad_input(const void* dy, int64_t ld, const uint8_t* q, const uint8_t* scales, int block,
@@ -317,7 +320,7 @@ int nvfp4_matmul_grad_input(const void* dy, int64_t ld, const uint8_t* q, const 
     if (m == 0 || k == 0) return NVFP4_OK;
     if (!dx || !tensor_scale || (n > 0 && (!dy || !q || !scales))) return NVFP4_ERR_NULL;
     if (!aligned(dy, 16) || !aligned(q, 16) || !aligned(dx, 16) || !aligned(tensor_scale, 4)) return NVFP4_ERR_ALIGN;
-    if (const int rc = check_ws(workspace, workspace_bytes, grad_workspace(m, n, k, ld))) return rc;
+    if (const int rc = check_ws(workspace, workspace_bytes, grad_workspace(m, n, k, k, ld))) return rc;
     return run_grad<kBf16>(dy, ld, q, scales, block, tensor_scale, m, n, k, k, out_dtype, dx, workspace,
                            (hipStream_t)stream);
 }
@@ -343,7 +346,7 @@ int mxfp4_matmul(const uint8_t* a_q, const uint8_t* a_scales, const uint8_t* b_q
 
 int64_t mxfp4_matmul_grad_input_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t ld) {
     if (const int rc = check_dims(m, n, k)) return rc;
-    return grad_workspace(m, n, up(k, 32), ld);
+    return grad_workspace(m, n, k, up(k, 32), ld);
 }
 
 int mxfp4_matmul_grad_input(const void* dy, int64_t ld, const uint8_t* q, const uint8_t* scales, int64_t m, int64_t n,
@@ -355,7 +358,7 @@ int mxfp4_matmul_grad_input(const void* dy, int64_t ld, const uint8_t* q, const 
     if (m == 0 || k == 0) return NVFP4_OK;
     if (!dx || (n > 0 && (!dy || !q || !scales))) return NVFP4_ERR_NULL;
     if (!aligned(dy, 16) || !aligned(q, 16) || !aligned(dx, 16)) return NVFP4_ERR_ALIGN;
-    if (const int rc = check_ws(workspace, workspace_bytes, grad_workspace(m, n, up(k, 32), ld))) return rc;
+    if (const int rc = check_ws(workspace, workspace_bytes, grad_workspace(m, n, k, up(k, 32), ld))) return rc;
     return run_grad<kMx>(dy, ld, q, scales, 32, nullptr, m, n, k, up(k, 32), out_dtype, dx, workspace,
                          (hipStream_t)stream);
 }

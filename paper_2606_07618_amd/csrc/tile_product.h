@@ -166,8 +166,9 @@ struct Side {
 };
 
 // Workgroup tile M_ x N_ by WM x WN waves.
-template <int M_, int N_, int WM_, int WN_>
+template <int M_, int N_, int WM_, int WN_, int SLOTS = 2>
 struct Tile {
+    static constexpr int kSlots = SLOTS;                             // steps of the contraction in LDS
     static constexpr int M = M_, N = N_, WM = WM_, WN = WN_, kThreads = WM_ * WN_ * kLanes;
     static constexpr int kWavesPerSimd = M_ * N_ / (WM_ * WN_) > 8192 ? 1 : 2;   // 512 or 256 registers
     static constexpr int MF = M_ / WM_ / 32, NF = N_ / WN_ / 32;     // a wave's matrix instructions
@@ -218,11 +219,11 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
     using A = Side<KIND, LA, T::M, T::kThreads, false>;
     using B = Side<KIND, LB, T::N, T::kThreads, HALF>;
     constexpr int kScales = KIND == kMx ? (T::M + T::N) * 2 * kQuarters : 0;   // eight bytes a row and step
-    constexpr int kScaleLoads = kScales / (T::kThreads * 4);
-    static_assert(kScales % (T::kThreads * 4) == 0, "whole loads");
+    constexpr int kScaleLoads = (kScales + T::kThreads * 4 - 1) / (T::kThreads * 4);
+    constexpr bool kEven = kScales % (T::kThreads * 4) == 0;               // else the last waves' last load is not one
     constexpr int kStage = A::kBytes + B::kBytes + kScales;
-    constexpr int kSlots = 2;
-    constexpr int kLoads = A::kLoads + B::kLoads + kScaleLoads;
+    constexpr int kSlots = T::kSlots;
+    constexpr int kLoads = A::kLoads + B::kLoads + kScales / (T::kThreads * 4);   // of a step, every wave's
     __shared__ __attribute__((aligned(1024))) char lds[kSlots][kStage];
     constexpr int kOutN = HALF ? T::N / 2 : T::N;          // output columns of a tile
     constexpr int NF = T::NF, MF = T::MF;
@@ -271,6 +272,7 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
 #pragma unroll
             for (int i = 0; i < kScaleLoads; ++i) {
                 const int first = i * T::kThreads + wave * kLanes;
+                if (!kEven && first * 4 >= kScales) break;
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(first / 2 < T::M ? ra : rb,
                                                          (lds_void*)(l + A::kBytes + B::kBytes + first * 4), 4,
                                                          (int)(any ? scale_offset[i] : kOutside), 0, 0, 0);
