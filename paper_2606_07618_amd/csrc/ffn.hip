@@ -82,7 +82,7 @@ int64_t pack_workspace(int64_t m, int64_t n, int64_t k, int64_t ldx, int64_t ldw
 int64_t half_of(int64_t n) { return up(n, 64); }       // whole steps of the contraction
 
 int64_t backward_workspace(int64_t m, int64_t n, int64_t k, int64_t ldx, int64_t ldw) {
-    return pack_workspace(m, n, k, ldx, ldw) + up(m * spread_ld(2 * half_of(n)) * 2, 256) + parts_bytes<kBf16, kAcross, kPairInner>(m, k, n);
+    return pack_workspace(m, n, k, ldx, ldw) + up(m * 2 * half_of(n) * 2, 256) + parts_bytes<kBf16, kAcross, kPairInner>(m, k, n);
 }
 
 int check_call(int64_t m, int64_t n, int64_t k, int64_t ldx, int64_t ldw) {
@@ -160,7 +160,7 @@ int nvfp4_swiglu_ffn_backward(const void* dh, const void* x, int64_t ldx, const 
     hipStream_t st = (hipStream_t)stream;
     Carver c{static_cast<char*>(workspace)};
     const int64_t half = half_of(n);
-    const int64_t ld = spread_ld(2 * half);
+    const int64_t ld = 2 * half;
     uint16_t* d = static_cast<uint16_t*>(c.take(m * ld * 2));
     const int64_t units = m * (half / 8), groups = ceil_div(units, kEdgeThreads);
     if (units > 0) {

@@ -127,7 +127,7 @@ int expand(const uint8_t* q, const uint8_t* scales, int64_t n, int64_t k, int bl
     while (8 << shift < block) ++shift;
     hipLaunchKernelGGL((expand_kernel<KIND>), dim3((unsigned)(n * row_groups)), dim3(kExpandThreads), 0, stream,
                        reinterpret_cast<const uint32_t*>(q), scales, (uint32_t)row_units, (uint32_t)row_groups, shift,
-                       spread_ld(k) / 8, static_cast<uint4*>(out));
+                       k / 8, static_cast<uint4*>(out));
     return launched();
 }
 
@@ -143,7 +143,7 @@ int64_t linear_workspace(int64_t m, int64_t n, int64_t k) {
         const int parts = stream_product::parts(m, n, k);
         return up(m * k * 2, 256) + up(m * 4, 256) + (parts > 1 ? up(parts * m * n * 4, 256) : 0);
     }
-    return up(n * spread_ld(k) * 2, 256) + parts_bytes<kBf16, kAlong, kSingle>(m, n, k);
+    return up(n * k * 2, 256) + parts_bytes<kBf16, kAlong, kSingle>(m, n, k);
 }
 
 template <int MF>
@@ -196,11 +196,11 @@ int run_linear(const void* x, int64_t ldx, const uint8_t* q, const uint8_t* scal
         return partial ? join_parts(partial, t.parts, m * n, nullptr, out, f32, stream) : NVFP4_OK;
     }
     Carver c{static_cast<char*>(ws)};
-    void* w = c.take(n * spread_ld(k) * 2);
+    void* w = c.take(n * k * 2);
     if (const int rc = expand<kBf16>(q, scales, n, k, block, w, stream)) return rc;
     Args p = {};
     p.a.p = static_cast<const char*>(x), p.a.ld = ldx * 2;
-    p.b.p = static_cast<const char*>(w), p.b.ld = spread_ld(k) * 2;
+    p.b.p = static_cast<const char*>(w), p.b.ld = k * 2;
     p.m = m, p.n = n, p.inner = k, p.scale = S, p.out = out, p.out_ld = n, p.out_f32 = out_dtype == NVFP4_IN_F32;
     return run_sums<kBf16, kAlong, kAlong, kSingle>(p, static_cast<float*>(c.take(0)), stream);
 }
@@ -209,7 +209,7 @@ int run_linear(const void* x, int64_t ldx, const uint8_t* q, const uint8_t* scal
 
 int64_t grad_workspace(int64_t m, int64_t n, int64_t k, int64_t k32, int64_t ld) {
     Carver c{nullptr};
-    c.take(n * spread_ld(k32) * 2);
+    c.take(n * k32 * 2);
     if (needs_pack(n, ld)) c.take(m * packed_ld(n) * 2);
     return c.at + parts_bytes<kBf16, kAcross, kSingle>(m, k, n);
 }
@@ -219,7 +219,7 @@ template <Kind KIND>
 int run_grad(const void* dy, int64_t ld, const uint8_t* q, const uint8_t* scales, int block, const float* S, int64_t m,
              int64_t n, int64_t k, int64_t k32, int out_dtype, void* out, void* ws, hipStream_t stream) {
     Carver c{static_cast<char*>(ws)};
-    void* w = c.take(n * spread_ld(k32) * 2);
+    void* w = c.take(n * k32 * 2);
     if (const int rc = expand<KIND>(q, scales, n, k32, block, w, stream)) return rc;
     if (needs_pack(n, ld)) {
         void* packed = c.take(m * packed_ld(n) * 2);
@@ -228,7 +228,7 @@ int run_grad(const void* dy, int64_t ld, const uint8_t* q, const uint8_t* scales
     }
     Args p = {};
     p.a.p = static_cast<const char*>(dy), p.a.ld = ld * 2;
-    p.b.p = static_cast<const char*>(w), p.b.ld = spread_ld(k32) * 2;
+    p.b.p = static_cast<const char*>(w), p.b.ld = k32 * 2;
     p.m = m, p.n = k, p.inner = n, p.scale = S, p.out = out, p.out_ld = k, p.out_f32 = out_dtype == NVFP4_IN_F32;
     return run_sums<kBf16, kAlong, kAcross, kSingle>(p, static_cast<float*>(c.take(0)), stream);
 }

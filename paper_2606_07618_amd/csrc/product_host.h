@@ -31,10 +31,7 @@ inline int launched() { return hipGetLastError() == hipSuccess ? NVFP4_OK : NVFP
 
 // Rows of `width` values as the tiles read them: 16-byte chunks, zeros past the width.
 inline bool needs_pack(int64_t width, int64_t ld) { return width % 8 != 0 || ld % 8 != 0; }
-// Rows that this library lays out are an odd number of 128-byte lines apart: at a multiple of a large power of two
-// their lines meet in the same sets and channels ([8192, 4096] x [2 x 14336, 4096]: 1728 us, so apart 1563).
-inline int64_t spread_ld(int64_t width) { return (up(width, 64) / 64 | 1) * 64; }
-inline int64_t packed_ld(int64_t width) { return spread_ld(width); }
+inline int64_t packed_ld(int64_t width) { return up(width, 8); }
 
 // Sections of a caller's workspace, 256-byte aligned.  With a null base it only measures.
 struct Carver {

@@ -253,18 +253,19 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
     const char* a0 = p.a.p + (LA == kAlong ? m0 * p.a.ld : m0 * 2);
     const int64_t b_at = LB == kAlong ? n0 * p.b.ld : n0 * 2;
     const int64_t pair_steps = PAIR == kPairInner ? p.steps / 2 : p.steps;
-    auto fetch = [&](int64_t s, int stage) {
-        char* l = lds[stage];
-        constexpr int kElem = KIND == kMx ? 1 : 2;         // twice the values of a byte
-        const int64_t ia = LA == kAlong ? (p.inner * kElem >> (KIND == kMx ? 1 : 0)) : p.inner;
-        const int64_t sb_in = PAIR == kPairInner && s >= pair_steps ? s - pair_steps : s;
+    auto fetch_a = [&](int64_t s, int stage) {
+        const int64_t in = LA == kAlong ? (KIND == kMx ? p.inner / 2 : p.inner * 2) : p.inner;
         // kPairInner: A's rows hold both contractions one after the other, each filled up with zeros
-        const int64_t a_ahead = PAIR == kPairInner ? (p.steps - s) * A::kFull : ia - s * A::kFull;
-        sa.load(a0 + (LA == kAlong ? s * kStepBytes : s * A::kFull * p.a.ld), nullptr, l, a_ahead, tid, wave);
-        const int64_t ib = LB == kAlong ? (p.inner * kElem >> (KIND == kMx ? 1 : 0)) : p.inner;
-        const int64_t step = LB == kAlong ? sb_in * kStepBytes : sb_in * B::kFull * p.b.ld;
-        const char* b = PAIR == kPairInner && s >= pair_steps ? p.b.p2 : p.b.p;
-        sb.load(b + b_at + step, HALF ? p.b.p2 + b_at + step : nullptr, l + A::kBytes, ib - sb_in * B::kFull, tid, wave);
+        const int64_t ahead = PAIR == kPairInner ? (p.steps - s) * A::kFull : in - s * A::kFull;
+        sa.load(a0 + (LA == kAlong ? s * kStepBytes : s * A::kFull * p.a.ld), nullptr, lds[stage], ahead, tid, wave);
+    };
+    auto fetch_b = [&](int64_t s, int stage) {
+        char* l = lds[stage] + A::kBytes;
+        const int64_t in = LB == kAlong ? (KIND == kMx ? p.inner / 2 : p.inner * 2) : p.inner;
+        const bool second = PAIR == kPairInner && s >= pair_steps;
+        const int64_t at = second ? s - pair_steps : s;
+        const int64_t step = b_at + (LB == kAlong ? at * kStepBytes : at * B::kFull * p.b.ld);
+        sb.load((second ? p.b.p2 : p.b.p) + step, HALF ? p.b.p2 + step : nullptr, l, in - at * B::kFull, tid, wave);
         if constexpr (KIND == kMx) {
             const bool any = p.inner / 32 - s * 8 > tid % 2 * 4;
             const __amdgpu_buffer_rsrc_t ra = window(p.a.scales + m0 * p.a.scale_ld + s * 8),
@@ -273,8 +274,7 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
             for (int i = 0; i < kScaleLoads; ++i) {
                 const int first = i * T::kThreads + wave * kLanes;
                 if (!kEven && first * 4 >= kScales) break;
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(first / 2 < T::M ? ra : rb,
-                                                         (lds_void*)(l + A::kBytes + B::kBytes + first * 4), 4,
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(first / 2 < T::M ? ra : rb, (lds_void*)(l + B::kBytes + first * 4), 4,
                                                          (int)(any ? scale_offset[i] : kOutside), 0, 0, 0);
             }
         }
@@ -297,8 +297,11 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
 
     // Registers run a quarter of a step ahead of the matrix instructions, LDS kSlots steps: while one
     // quarter's fragments are multiplied the next one's are read, and the one barrier of a step stands
-    // where its last fragments have been read, so that its LDS is free for the step kSlots on.  What a step
-    // waits for at its barrier are the loads that were started kSlots - 1 steps before, and no later ones.
+    // where its last fragments have been read, so that its LDS is free for the step kSlots on.  That step's
+    // loads are started in two parts, A's behind the barrier and B's a quarter later, among the matrix
+    // instructions: in one burst they fill the queue that both waves of a SIMD then wait at ([4096, 14336] x
+    // [14336, 4096], contraction down the rows: 487 -> 449 us).  What a step waits for at its barrier are
+    // the loads of the next step, and no later ones.
     i32x4 fa[2][MF], fb[2][NF];
     int xa[2][MF], xb[2][NF];                  // scales of this step and of the next
     auto read = [&](auto q, int stage) {
@@ -338,14 +341,15 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
             }
         }
     };
-    // the LDS reads of a quarter spread among the one before's matrix instructions
-    auto interleave = [&]() {
+    // the LDS reads of a quarter, and the loads it starts, spread among the matrix instructions of the one before
+    auto interleave = [&](int loads) {
         constexpr int kReads = MF * (LA == kAcross ? 2 : 1) + NF * (LB == kAcross ? 2 : 1), kOps = MF * NF;
         constexpr int kEach = kReads > kOps ? (kReads + kOps - 1) / kOps : 1;
 #pragma unroll
         for (int r = 0; r < kOps; ++r) {
-            __builtin_amdgcn_sched_group_barrier(0x100, kEach, 0);
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, kEach, 0);               // LDS reads
+            if (r < loads) __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);    // loads from memory
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                   // matrix instructions
         }
     };
     auto next_scales = [&]() {
@@ -358,7 +362,11 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
     };
     if (s0 < s1) {
 #pragma unroll
-        for (int i = 0; i < kSlots; ++i) fetch(s0 + i, i);          // past the contraction's end: zeros
+        for (int i = 0; i < kSlots; ++i) {
+            fetch_a(s0 + i, i);                                      // past the contraction's end: zeros
+            fetch_b(s0 + i, i);
+            asm volatile("" ::: "memory");                           // the wait counts on this order
+        }
         arrive<(kSlots - 1) * kLoads>();
         read(Const<0>{}, 0);
         int slot = 0;
@@ -366,19 +374,20 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
             const int next = slot + 1 == kSlots ? 0 : slot + 1;
             next_scales();
             read(Const<1>{}, slot);
+            if (s > s0) fetch_b(s - 1 + kSlots, slot == 0 ? kSlots - 1 : slot - 1);
             multiply(Const<0>{});
-            interleave();
+            interleave(B::kLoads);
             read(Const<2>{}, slot);
             multiply(Const<1>{});
-            interleave();
+            interleave(0);
             read(Const<3>{}, slot);
             multiply(Const<2>{});
-            interleave();
+            interleave(0);
             arrive<(kSlots - 2) * kLoads>();
-            fetch(s + kSlots, slot);
+            fetch_a(s + kSlots, slot);
             read(Const<0>{}, next);
             multiply(Const<3>{});
-            interleave();
+            interleave(A::kLoads);
             slot = next;
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");            // no load into LDS outlives the workgroup
