@@ -5,7 +5,9 @@
 //
 // Both element types share one geometry: a step takes 128 bytes of every row of the tile (64
 // bfloat16 values, 256 FP4 ones), and a lane's operand of one matrix instruction is 16 of them (8
-// values of 32x32x16, 32 of 32x32x64), so staging, LDS layout and register tiles are the same.
+// values of 16x16x32, 32 of 16x16x128), so staging, LDS layout and register tiles are the same.
+// (On random values the card's power holds 16x16 instructions at 2.13 PFLOP/s bfloat16 and 7.5 FP4, the
+// 32x32 ones at 1.86 and 6.3.)
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -28,7 +30,6 @@ typedef __attribute__((address_space(3))) char lds_char;
 
 constexpr int kLanes = 64;
 constexpr int kStepBytes = 128;                  // of a row, a step of the contraction
-constexpr int kQuarters = kStepBytes / 32;      // matrix instructions a step along the contraction
 constexpr int kChunk = 16;                       // bytes of a lane's load
 constexpr uint32_t kOutside = 0x80000000u;       // an offset that the buffer's size excludes: reads as zero
 
@@ -102,12 +103,12 @@ struct Side {
 
     // LDS holds a step as rows of chunks.  A chunk's place in its row is exchanged by the row, so that
     // the lanes of a read hit all banks: along, 16 lanes read one chunk of 16 rows, and the row's
-    // parity and the exchanged place cover the 256 bytes of the banks; across, 32 lanes read four
-    // contraction rows by 64 bytes, and the place of a 64-byte unit is exchanged by those rows.
+    // parity and the exchanged place cover the 256 bytes of the banks; across, 32 lanes read eight
+    // contraction rows by 32 bytes, and the place of a 32-byte unit is exchanged by those rows.
     __device__ static __forceinline__ int exchange(int row) {
         if constexpr (LAYOUT == kAlong) return (row >> 1) & 7;
-        constexpr int kUnits = R / 32 < 4 ? R / 32 : 4;
-        return (row & (kUnits - 1)) << 2;
+        constexpr int kUnits = R / 16 < 8 ? R / 16 : 8;
+        return (((row & 3) | (((row >> 3) & 1) << 2)) & (kUnits - 1)) << 1;
     }
 
     uint32_t offset[kLoads];             // of this thread's loads from the step's base
@@ -143,20 +144,20 @@ struct Side {
         }
     }
 
-    // This lane's 16 bytes of the operand at outer indexes row0 .. row0 + 31 of the tile, quarter Q of the step.
-    // bfloat16: values 16 Q + 8 (lane / 32) on.  Microscaled: the 32-value block 4 (lane / 32) + Q, so that the
-    // quarters' scales are the bytes of one word.
-    template <int Q>
+    // This lane's 16 bytes of the operand at outer indexes row0 .. row0 + 15 of the tile, half H of the step.
+    // bfloat16: values 32 H + 8 (lane / 16) on.  Microscaled: the 32-value block 2 (lane / 16) + H, so that the
+    // halves' scales are neighbours.
+    template <int H>
     __device__ static __forceinline__ i32x4 read(const char* lds, int row0, int lane) {
-        const int g = lane / 32;
+        const int g = lane / 16, i = lane % 16;
         if constexpr (LAYOUT == kAlong) {
-            const int row = row0 + lane % 32, chunk = KIND == kMx ? kQuarters * g + Q : 2 * Q + g;
+            const int row = row0 + i, chunk = KIND == kMx ? 2 * g + H : 4 * H + g;
             return *reinterpret_cast<const i32x4*>(lds + row * kStepBytes + ((chunk ^ exchange(row)) * kChunk));
         } else {
             // ds_read_b64_tr_b16: 16 lanes read four rows of 16 values, four each, and get a column each
-            const int i = lane % 16, row = 16 * Q + 8 * g + (i >> 2);
-            const int chunk = (row0 / 8 + lane / 16 % 2 * 2 + ((i & 3) >> 1)) ^ exchange(row);
-            const char* at = lds + row * (R * 2) + chunk * kChunk + (i & 1) * 8;
+            const int row = 32 * H + 8 * g + (i >> 2);
+            const int unit = (row0 / 16) ^ (exchange(row) >> 1);
+            const char* at = lds + row * (R * 2) + unit * 32 + (i & 3) * 8;
             typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
             const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
             const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 4 * R * 2));
@@ -171,7 +172,7 @@ struct Tile {
     static constexpr int kSlots = SLOTS;                             // steps of the contraction in LDS
     static constexpr int M = M_, N = N_, WM = WM_, WN = WN_, kThreads = WM_ * WN_ * kLanes;
     static constexpr int kWavesPerSimd = M_ * N_ / (WM_ * WN_) > 8192 ? 1 : 2;   // 512 or 256 registers
-    static constexpr int MF = M_ / WM_ / 32, NF = N_ / WN_ / 32;     // a wave's matrix instructions
+    static constexpr int MF = M_ / WM_ / 16, NF = N_ / WN_ / 16;     // a wave's matrix instructions
 };
 
 // What happens to the sums.
@@ -218,7 +219,7 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
     constexpr bool HALF = PAIR == kPairOuter;
     using A = Side<KIND, LA, T::M, T::kThreads, false>;
     using B = Side<KIND, LB, T::N, T::kThreads, HALF>;
-    constexpr int kScales = KIND == kMx ? (T::M + T::N) * 2 * kQuarters : 0;   // eight bytes a row and step
+    constexpr int kScales = KIND == kMx ? (T::M + T::N) * 8 : 0;           // eight bytes a row and step
     constexpr int kScaleLoads = (kScales + T::kThreads * 4 - 1) / (T::kThreads * 4);
     constexpr bool kEven = kScales % (T::kThreads * 4) == 0;               // else the last waves' last load is not one
     constexpr int kStage = A::kBytes + B::kBytes + kScales;
@@ -242,13 +243,21 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
     B sb;
     sa.init(p.m - m0, p.a.ld, tid);
     sb.init(p.n - n0, p.b.ld, tid);
-    // the scales of A's rows, then of B's; a load is of one operand's rows
+    // Scales: a word holds four blocks' codes of a row, a row two.  LDS holds them wave by wave, A's then B's, by row
+    // in the fragment, word, fragment, so that a lane reads its word of all its wave's fragments at once.
     uint32_t scale_offset[kScaleLoads + 1];
+    int scale_left[kScaleLoads + 1];               // bytes of the step ahead of the word
 #pragma unroll
     for (int i = 0; i < kScaleLoads; ++i) {
-        const int row = (i * T::kThreads + tid) / 2, rb = row - T::M, word = tid % 2 * 4;
-        scale_offset[i] = row < T::M ? (row < p.m - m0 ? (uint32_t)row * (uint32_t)p.a.scale_ld + word : kOutside)
-                                     : (rb < p.n - n0 ? (uint32_t)rb * (uint32_t)p.b.scale_ld + word : kOutside);
+        int word = i * T::kThreads + tid;
+        const bool of_a = word < T::M * 2;
+        const int frags = of_a ? MF : NF;
+        word -= of_a ? 0 : T::M * 2;
+        const int w = word / (32 * frags), in = word % (32 * frags), f = in % frags;
+        const int row = (of_a ? w * (T::M / T::WM) + f * 16 : w * (T::N / T::WN) + f * 16) + in / (2 * frags);
+        const uint32_t at = (uint32_t)(in / frags % 2) * 4;
+        scale_offset[i] = row < (of_a ? p.m - m0 : p.n - n0) ? (uint32_t)row * (uint32_t)(of_a ? p.a.scale_ld : p.b.scale_ld) + at : kOutside;
+        scale_left[i] = (int)at;
     }
     const char* a0 = p.a.p + (LA == kAlong ? m0 * p.a.ld : m0 * 2);
     const int64_t b_at = LB == kAlong ? n0 * p.b.ld : n0 * 2;
@@ -267,7 +276,7 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
         const int64_t step = b_at + (LB == kAlong ? at * kStepBytes : at * B::kFull * p.b.ld);
         sb.load((second ? p.b.p2 : p.b.p) + step, HALF ? p.b.p2 + step : nullptr, l, in - at * B::kFull, tid, wave);
         if constexpr (KIND == kMx) {
-            const bool any = p.inner / 32 - s * 8 > tid % 2 * 4;
+            const int64_t left = p.inner / 32 - s * 8;
             const __amdgpu_buffer_rsrc_t ra = window(p.a.scales + m0 * p.a.scale_ld + s * 8),
                                          rb = window(p.b.scales + n0 * p.b.scale_ld + s * 8);
 #pragma unroll
@@ -275,89 +284,99 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
                 const int first = i * T::kThreads + wave * kLanes;
                 if (!kEven && first * 4 >= kScales) break;
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(first / 2 < T::M ? ra : rb, (lds_void*)(l + B::kBytes + first * 4), 4,
-                                                         (int)(any ? scale_offset[i] : kOutside), 0, 0, 0);
+                                                         (int)(scale_left[i] < left ? scale_offset[i] : kOutside), 0, 0, 0);
             }
         }
     };
 
     // first rows of this wave's fragments in the tile
-    auto a_row = [&](int i) { return wm * (T::M / T::WM) + i * 32; };
+    auto a_row = [&](int i) { return wm * (T::M / T::WM) + i * 16; };
     auto b_row = [&](int j) {
-        if constexpr (!HALF) return wn * (T::N / T::WN) + j * 32;
-        return (j < NF / 2 ? 0 : T::N / 2) + wn * (T::N / 2 / T::WN) + j % (NF / 2) * 32;
+        if constexpr (!HALF) return wn * (T::N / T::WN) + j * 16;
+        return (j < NF / 2 ? 0 : T::N / 2) + wn * (T::N / 2 / T::WN) + j % (NF / 2) * 16;
     };
 
-    f32x16 acc[MF][NF];
+    f32x4 acc[MF][NF];
 #pragma unroll
     for (int i = 0; i < MF; ++i)
 #pragma unroll
-        for (int j = 0; j < NF; ++j)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+        for (int j = 0; j < NF; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-    // Registers run a quarter of a step ahead of the matrix instructions, LDS kSlots steps: while one
-    // quarter's fragments are multiplied the next one's are read, and the one barrier of a step stands
-    // where its last fragments have been read, so that its LDS is free for the step kSlots on.  That step's
-    // loads are started in two parts, A's behind the barrier and B's a quarter later, among the matrix
-    // instructions: in one burst they fill the queue that both waves of a SIMD then wait at ([4096, 14336] x
-    // [14336, 4096], contraction down the rows: 487 -> 449 us).  What a step waits for at its barrier are
-    // the loads of the next step, and no later ones.
-    i32x4 fa[2][MF], fb[2][NF];
-    int xa[2][MF], xb[2][NF];                  // scales of this step and of the next
-    auto read = [&](auto q, int stage) {
-        constexpr int Q = decltype(q)::value;
-        const char* la = lds[stage];
-        const char* lb = la + A::kBytes;
-#pragma unroll
-        for (int j = 0; j < NF; ++j) fb[Q % 2][j] = B::template read<Q>(lb, b_row(j), lane);
-#pragma unroll
-        for (int i = 0; i < MF; ++i) fa[Q % 2][i] = A::template read<Q>(la, a_row(i), lane);
-        if constexpr (KIND == kMx && Q == 0) {
-            const char* ls = lb + B::kBytes + lane / 32 * 4;
-#pragma unroll
-            for (int j = 0; j < NF; ++j)
-                xb[1][j] = *reinterpret_cast<const int*>(ls + (T::M + b_row(j) + lane % 32) * 8);
-#pragma unroll
-            for (int i = 0; i < MF; ++i)
-                xa[1][i] = *reinterpret_cast<const int*>(ls + (a_row(i) + lane % 32) * 8);
-        }
+    // A step is 2 MF groups of NF matrix instructions, a fragment of A against a half's fragments of B.
+    // Registers run kLead groups ahead of them (a whole half for B), LDS kSlots steps: while a group is
+    // multiplied a later one's fragment is read, and the one barrier of a step stands where its last fragments
+    // have been read, so that its LDS is free for the step kSlots on.  That step's loads are started in two
+    // parts, A's behind the barrier and B's in the next step, among the matrix instructions: in one burst
+    // they fill the queue that both waves of a SIMD then wait at ([4096, 14336] x [14336, 4096], contraction
+    // down the rows: 487 -> 449 us).  What a step waits for at its barrier are the loads of the next step, and
+    // no later ones.
+    constexpr int kLead = MF >= 8 ? 3 : MF >= 4 ? 2 : 1, kRing = 4, kGroups = 2 * MF;
+    constexpr int kOneA = LA == kAcross ? 2 : 1, kOneB = LB == kAcross ? 2 : 1;     // LDS reads of a fragment
+    i32x4 fa[kRing], fb[2][NF];
+    int xa[MF], xb[NF], ya[MF], yb[NF];        // scales of this step, and the next one's words
+    auto read_a = [&](auto gc, int stage) {    // the fragment of group g of a step
+        constexpr int g = decltype(gc)::value;
+        fa[g % kRing] = A::template read<g / MF>(lds[stage], a_row(g % MF), lane);
     };
-    auto multiply = [&](auto q) {
-        constexpr int Q = decltype(q)::value;
+    auto read_b = [&](auto hc, int stage, int from, int to) {
+        constexpr int H = decltype(hc)::value;
 #pragma unroll
-        for (int i = 0; i < MF; ++i) {
-#pragma unroll
-            for (int j = 0; j < NF; ++j) {
-                // B's values as the instruction's rows: a lane gets runs of four neighbouring outputs of a row of D
-                const i32x4 b = fb[Q % 2][j], a = fa[Q % 2][i];
-                if constexpr (KIND == kBf16) {
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, b),
-                                                                        __builtin_bit_cast(bf16x8, a), acc[i][j], 0, 0, 0);
-                } else {
-                    const i32x8 wb = {b[0], b[1], b[2], b[3], 0, 0, 0, 0}, wa = {a[0], a[1], a[2], a[3], 0, 0, 0, 0};
-                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wb, wa, acc[i][j], 4, 4, Q, xb[0][j], Q,
-                                                                                xa[0][i]);
-                }
-            }
-        }
+        for (int j = from; j < to; ++j) fb[H][j] = B::template read<H>(lds[stage] + A::kBytes, b_row(j), lane);
     };
-    // the LDS reads of a quarter, and the loads it starts, spread among the matrix instructions of the one before
-    auto interleave = [&](int loads) {
-        constexpr int kReads = MF * (LA == kAcross ? 2 : 1) + NF * (LB == kAcross ? 2 : 1), kOps = MF * NF;
-        constexpr int kEach = kReads > kOps ? (kReads + kOps - 1) / kOps : 1;
+    auto read_scales = [&](int stage) {
+        if constexpr (KIND == kMx) {
+            const int* la = reinterpret_cast<const int*>(lds[stage] + A::kBytes + B::kBytes);
+            const int at = lane % 16 * 2 + lane / 32;
 #pragma unroll
-        for (int r = 0; r < kOps; ++r) {
-            __builtin_amdgcn_sched_group_barrier(0x100, kEach, 0);               // LDS reads
-            if (r < loads) __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);    // loads from memory
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                   // matrix instructions
+            for (int i = 0; i < MF; ++i) ya[i] = la[(wm * 32 + at) * MF + i];
+#pragma unroll
+            for (int j = 0; j < NF; ++j) yb[j] = la[T::M * 2 + (wn * 32 + at) * NF + j];
         }
     };
     auto next_scales = [&]() {
         if constexpr (KIND == kMx) {
+            const int shift = lane / 16 % 2 * 16;      // two codes of this lane's word
 #pragma unroll
-            for (int i = 0; i < MF; ++i) xa[0][i] = xa[1][i];
+            for (int i = 0; i < MF; ++i) xa[i] = (int)((uint32_t)ya[i] >> shift);
 #pragma unroll
-            for (int j = 0; j < NF; ++j) xb[0][j] = xb[1][j];
+            for (int j = 0; j < NF; ++j) xb[j] = (int)((uint32_t)yb[j] >> shift);
+        }
+    };
+    auto group = [&](int64_t s, int slot, int next, auto gc) {
+        constexpr int g = decltype(gc)::value, H = g / MF, i = g % MF, ahead = g + kLead;
+        constexpr bool first = ahead == kGroups;       // the first group whose reads ahead are the next step's
+        // the second half's fragments of B: one in each of the first groups, or what is left in the last that may
+        constexpr bool more_b = g < NF && g < MF - 1;
+        constexpr int b_to = g == MF - 2 ? NF : g + 1;
+        constexpr int kReads = kOneA + (more_b ? (b_to - g) * kOneB : 0) + (first ? NF * kOneB + (KIND == kMx ? (MF + NF) / 4 : 0) : 0);
+        constexpr int kStarts = first ? A::kLoads : g == 0 ? B::kLoads : 0;
+        if constexpr (first) {
+            arrive<(kSlots - 2) * kLoads>();
+            fetch_a(s + kSlots, slot);
+            read_b(Const<0>{}, next, 0, NF);
+            read_scales(next);
+        }
+        read_a(Const<ahead % kGroups>{}, ahead < kGroups ? slot : next);
+        if constexpr (more_b) read_b(Const<1>{}, slot, g, b_to);
+        if constexpr (g == 0) if (s > s0) fetch_b(s - 1 + kSlots, slot == 0 ? kSlots - 1 : slot - 1);
+#pragma unroll
+        for (int j = 0; j < NF; ++j) {
+            // B's values as the instruction's rows: a lane gets four neighbouring outputs of a row of D
+            const i32x4 b = fb[H][j], a = fa[g % kRing];
+            if constexpr (KIND == kBf16) {
+                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, b), __builtin_bit_cast(bf16x8, a),
+                                                                    acc[i][j], 0, 0, 0);
+            } else {
+                const i32x8 wb = {b[0], b[1], b[2], b[3], 0, 0, 0, 0}, wa = {a[0], a[1], a[2], a[3], 0, 0, 0, 0};
+                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wb, wa, acc[i][j], 4, 4, H, xb[j], H, xa[i]);
+            }
+        }
+        // the order of a group: its LDS reads and its loads among its matrix instructions
+#pragma unroll
+        for (int r = 0; r < NF; ++r) {
+            __builtin_amdgcn_sched_group_barrier(0x100, (kReads + NF - 1) / NF, 0);                          // LDS reads
+            if constexpr (kStarts > 0) __builtin_amdgcn_sched_group_barrier(0x010, (kStarts + NF - 1) / NF, 0);  // loads from memory
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                                               // matrix instructions
         }
     };
     if (s0 < s1) {
@@ -368,43 +387,44 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
             asm volatile("" ::: "memory");                           // the wait counts on this order
         }
         arrive<(kSlots - 1) * kLoads>();
-        read(Const<0>{}, 0);
+        read_b(Const<0>{}, 0, 0, NF);
+        read_scales(0);
+        read_a(Const<0>{}, 0);
+        if constexpr (kLead > 1) read_a(Const<1>{}, 0);
+        if constexpr (kLead > 2) read_a(Const<2>{}, 0);
         int slot = 0;
         for (int64_t s = s0; s < s1; ++s) {
             const int next = slot + 1 == kSlots ? 0 : slot + 1;
             next_scales();
-            read(Const<1>{}, slot);
-            if (s > s0) fetch_b(s - 1 + kSlots, slot == 0 ? kSlots - 1 : slot - 1);
-            multiply(Const<0>{});
-            interleave(B::kLoads);
-            read(Const<2>{}, slot);
-            multiply(Const<1>{});
-            interleave(0);
-            read(Const<3>{}, slot);
-            multiply(Const<2>{});
-            interleave(0);
-            arrive<(kSlots - 2) * kLoads>();
-            fetch_a(s + kSlots, slot);
-            read(Const<0>{}, next);
-            multiply(Const<3>{});
-            interleave(A::kLoads);
+            group(s, slot, next, Const<0>{}), group(s, slot, next, Const<1>{});
+            group(s, slot, next, Const<2>{}), group(s, slot, next, Const<3>{});
+            if constexpr (MF >= 4) {
+                group(s, slot, next, Const<4>{}), group(s, slot, next, Const<5>{});
+                group(s, slot, next, Const<6>{}), group(s, slot, next, Const<7>{});
+            }
+            if constexpr (MF >= 8) {
+                group(s, slot, next, Const<8>{}), group(s, slot, next, Const<9>{});
+                group(s, slot, next, Const<10>{}), group(s, slot, next, Const<11>{});
+                group(s, slot, next, Const<12>{}), group(s, slot, next, Const<13>{});
+                group(s, slot, next, Const<14>{}), group(s, slot, next, Const<15>{});
+            }
+            static_assert(MF == 2 || MF == 4 || MF == 8, "groups of a step");
             slot = next;
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");            // no load into LDS outlives the workgroup
     }
 
-    // a lane holds, of row lane % 32 of D, the runs of four columns from 4 (lane / 32) on, eight apart
+    // a lane holds four neighbouring columns of row lane % 16 of D
     const bool vec = p.out_ld % 4 == 0;
     const float scale = OUT == kSums && p.scale ? *p.scale : 1.0f;
 #pragma unroll
     for (int i = 0; i < MF; ++i) {
-        const int64_t m = m0 + a_row(i) + lane % 32;
+        const int64_t m = m0 + a_row(i) + lane % 16;
         if (m >= p.m) continue;
 #pragma unroll
-        for (int jr = 0; jr < (HALF ? NF / 2 : NF) * 4; ++jr) {
-            const int j = jr / 4, r = jr % 4 * 4;
-            const int64_t n = n0 + b_row(j) + r * 2 + lane / 32 * 4, left = p.n - n;
-            const f32x4 v = {acc[i][j][r], acc[i][j][r + 1], acc[i][j][r + 2], acc[i][j][r + 3]};
+        for (int j = 0; j < (HALF ? NF / 2 : NF); ++j) {
+            const int64_t n = n0 + b_row(j) + lane / 16 * 4, left = p.n - n;
+            const f32x4 v = acc[i][j];
             if constexpr (OUT == kSums) {
                 store4(p.out, p.out_f32, m * p.out_ld + n, left, vec, v * scale);
             } else if constexpr (OUT == kPartial) {
@@ -415,7 +435,7 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
                     store4(m < p.half_rows ? p.out : p.out2, 0, row * p.out_ld + n, left, vec, v);
             } else {
                 constexpr int H = HALF ? NF / 2 : 0;
-                const f32x4 u = {acc[i][H + j][r], acc[i][H + j][r + 1], acc[i][H + j][r + 2], acc[i][H + j][r + 3]};
+                const f32x4 u = acc[i][H + j];
                 f32x4 h;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) h[e] = silu(v[e]) * u[e];
