@@ -145,13 +145,12 @@ struct Side {
     }
 
     // This lane's 16 bytes of the operand at outer indexes row0 .. row0 + 15 of the tile, half H of the step.
-    // bfloat16: values 32 H + 8 (lane / 16) on.  Microscaled: the 32-value block 2 (lane / 16) + H, so that the
-    // halves' scales are neighbours.
+    // bfloat16: values 32 H + 8 (lane / 16) on.  Microscaled: the 32-value block 4 H + lane / 16.
     template <int H>
     __device__ static __forceinline__ i32x4 read(const char* lds, int row0, int lane) {
         const int g = lane / 16, i = lane % 16;
         if constexpr (LAYOUT == kAlong) {
-            const int row = row0 + i, chunk = KIND == kMx ? 2 * g + H : 4 * H + g;
+            const int row = row0 + i, chunk = 4 * H + g;
             return *reinterpret_cast<const i32x4*>(lds + row * kStepBytes + ((chunk ^ exchange(row)) * kChunk));
         } else {
             // ds_read_b64_tr_b16: 16 lanes read four rows of 16 values, four each, and get a column each
@@ -243,8 +242,8 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
     B sb;
     sa.init(p.m - m0, p.a.ld, tid);
     sb.init(p.n - n0, p.b.ld, tid);
-    // Scales: a word holds four blocks' codes of a row, a row two.  LDS holds them wave by wave, A's then B's, by row
-    // in the fragment, word, fragment, so that a lane reads its word of all its wave's fragments at once.
+    // Scales: a word holds a half's four codes of a row.  LDS holds them wave by wave, A's then B's, by row
+    // in the fragment, half, fragment, so that a lane reads the words of all its wave's fragments at once.
     uint32_t scale_offset[kScaleLoads + 1];
     int scale_left[kScaleLoads + 1];               // bytes of the step ahead of the word
 #pragma unroll
@@ -310,10 +309,14 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
     // they fill the queue that both waves of a SIMD then wait at ([4096, 14336] x [14336, 4096], contraction
     // down the rows: 487 -> 449 us).  What a step waits for at its barrier are the loads of the next step, and
     // no later ones.
-    constexpr int kLead = MF >= 8 ? 3 : MF >= 4 ? 2 : 1, kRing = 4, kGroups = 2 * MF;
+    // Down the rows a fragment of B is two reads: the barrier stands earlier there, and the next step's are read two a
+    // group behind it (450 -> 437 us in the same product; along the rows, where they are one each, 400 -> 410).
+    constexpr bool kSlowB = MF >= 8 && LB == kAcross;
+    constexpr int kLead = kSlowB ? (LA == kAcross ? 5 : 6) : MF >= 8 ? 3 : MF >= 4 ? 2 : 1;
+    constexpr int kRing = kLead > 3 ? 8 : 4, kGroups = 2 * MF, kBehind = kSlowB ? 2 : NF;
     constexpr int kOneA = LA == kAcross ? 2 : 1, kOneB = LB == kAcross ? 2 : 1;     // LDS reads of a fragment
     i32x4 fa[kRing], fb[2][NF];
-    int xa[MF], xb[NF], ya[MF], yb[NF];        // scales of this step, and the next one's words
+    int xa[MF], xb[NF], ya[2][MF], yb[2][NF];  // codes of this step, and the next one's words
     auto read_a = [&](auto gc, int stage) {    // the fragment of group g of a step
         constexpr int g = decltype(gc)::value;
         fa[g % kRing] = A::template read<g / MF>(lds[stage], a_row(g % MF), lane);
@@ -326,20 +329,23 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
     auto read_scales = [&](int stage) {
         if constexpr (KIND == kMx) {
             const int* la = reinterpret_cast<const int*>(lds[stage] + A::kBytes + B::kBytes);
-            const int at = lane % 16 * 2 + lane / 32;
 #pragma unroll
-            for (int i = 0; i < MF; ++i) ya[i] = la[(wm * 32 + at) * MF + i];
+            for (int h = 0; h < 2; ++h) {
 #pragma unroll
-            for (int j = 0; j < NF; ++j) yb[j] = la[T::M * 2 + (wn * 32 + at) * NF + j];
+                for (int i = 0; i < MF; ++i) ya[h][i] = la[((wm * 16 + lane % 16) * 2 + h) * MF + i];
+#pragma unroll
+                for (int j = 0; j < NF; ++j) yb[h][j] = la[T::M * 2 + ((wn * 16 + lane % 16) * 2 + h) * NF + j];
+            }
         }
     };
     auto next_scales = [&]() {
         if constexpr (KIND == kMx) {
-            const int shift = lane / 16 % 2 * 16;      // two codes of this lane's word
+            // this lane's code of the first half, then of the second
+            const uint32_t pick = 0x0C0C0400u + (uint32_t)(lane / 16) * 0x0101u;
 #pragma unroll
-            for (int i = 0; i < MF; ++i) xa[i] = (int)((uint32_t)ya[i] >> shift);
+            for (int i = 0; i < MF; ++i) xa[i] = (int)__builtin_amdgcn_perm((uint32_t)ya[1][i], (uint32_t)ya[0][i], pick);
 #pragma unroll
-            for (int j = 0; j < NF; ++j) xb[j] = (int)((uint32_t)yb[j] >> shift);
+            for (int j = 0; j < NF; ++j) xb[j] = (int)__builtin_amdgcn_perm((uint32_t)yb[1][j], (uint32_t)yb[0][j], pick);
         }
     };
     auto group = [&](int64_t s, int slot, int next, auto gc) {
@@ -348,14 +354,18 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
         // the second half's fragments of B: one in each of the first groups, or what is left in the last that may
         constexpr bool more_b = g < NF && g < MF - 1;
         constexpr int b_to = g == MF - 2 ? NF : g + 1;
-        constexpr int kReads = kOneA + (more_b ? (b_to - g) * kOneB : 0) + (first ? NF * kOneB + (KIND == kMx ? (MF + NF) / 4 : 0) : 0);
+        // the next step's first ones, kBehind a group from the barrier on
+        constexpr int b_next = (ahead - kGroups) * kBehind;
+        constexpr bool next_b = ahead >= kGroups && b_next < NF;
+        constexpr int kReads = kOneA + (more_b ? (b_to - g) * kOneB : 0) + (next_b ? kBehind * kOneB : 0) +
+                               (first && KIND == kMx ? (MF + NF) / 2 : 0);
         constexpr int kStarts = first ? A::kLoads : g == 0 ? B::kLoads : 0;
         if constexpr (first) {
             arrive<(kSlots - 2) * kLoads>();
             fetch_a(s + kSlots, slot);
-            read_b(Const<0>{}, next, 0, NF);
             read_scales(next);
         }
+        if constexpr (next_b) read_b(Const<0>{}, next, b_next, b_next + kBehind);
         read_a(Const<ahead % kGroups>{}, ahead < kGroups ? slot : next);
         if constexpr (more_b) read_b(Const<1>{}, slot, g, b_to);
         if constexpr (g == 0) if (s > s0) fetch_b(s - 1 + kSlots, slot == 0 ? kSlots - 1 : slot - 1);
@@ -392,6 +402,8 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
         read_a(Const<0>{}, 0);
         if constexpr (kLead > 1) read_a(Const<1>{}, 0);
         if constexpr (kLead > 2) read_a(Const<2>{}, 0);
+        if constexpr (kLead > 3) read_a(Const<3>{}, 0), read_a(Const<4>{}, 0);
+        if constexpr (kLead > 5) read_a(Const<5>{}, 0);
         int slot = 0;
         for (int64_t s = s0; s < s1; ++s) {
             const int next = slot + 1 == kSlots ? 0 : slot + 1;
@@ -414,16 +426,67 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");            // no load into LDS outlives the workgroup
     }
 
-    // a lane holds four neighbouring columns of row lane % 16 of D
-    const bool vec = p.out_ld % 4 == 0;
+    // A lane holds four neighbouring columns of row lane % 16 of D.  Stored from here, an instruction would write
+    // 32 bytes of 16 rows; bfloat16 outputs go through LDS instead and leave as whole rows of the tile, 16 bytes a
+    // lane ([8192, 4096] x [14336, 4096] microscaled, where the contraction is short: 338 -> 305 us).
     const float scale = OUT == kSums && p.scale ? *p.scale : 1.0f;
+    auto column = [&](int j) { return HALF ? wn * (kOutN / T::WN) + j * 16 : b_row(j); };
+    if (OUT != kPartial && !p.out_f32 && p.out_ld % 8 == 0) {
+        constexpr int kOutChunks = kOutN / 8, kMask = kOutChunks < 16 ? kOutChunks - 1 : 15;
+        static_assert(T::M * kOutN * 2 <= kSlots * kStage, "the tile in LDS");
+        char* tile = lds[0];
+        auto write = [&](auto value, auto row_of) {      // value(i, j): of a fragment; row_of(m): where row m goes
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < MF; ++i)
+#pragma unroll
+                for (int j = 0; j < (HALF ? NF / 2 : NF); ++j) {
+                    const f32x4 v = value(i, j);
+                    const int row = a_row(i) + lane % 16, col = column(j) + lane / 16 * 4;
+                    *reinterpret_cast<uint2*>(tile + (row * kOutChunks + ((col / 8) ^ (row & kMask))) * kChunk + col % 8 * 2) =
+                        make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+                }
+            __syncthreads();
+#pragma unroll 4
+            for (int c = tid; c < T::M * kOutChunks; c += T::kThreads) {
+                const int row = c / kOutChunks, chunk = c % kOutChunks;
+                const int64_t m = m0 + row, n = n0 + chunk * 8;
+                uint16_t* to = m < p.m && n < p.n ? row_of(m) : nullptr;
+                if (to) *reinterpret_cast<uint4*>(to + n) = *reinterpret_cast<const uint4*>(tile + (row * kOutChunks + (chunk ^ (row & kMask))) * kChunk);
+            }
+        };
+        auto rows_of = [&](void* out) { return [=](int64_t m) { return static_cast<uint16_t*>(out) + m * p.out_ld; }; };
+        if constexpr (OUT == kSums) {
+            write([&](int i, int j) { return acc[i][j] * scale; }, rows_of(p.out));
+        } else if constexpr (OUT == kTwoRows) {
+            write([&](int i, int j) { return acc[i][j]; }, [&](int64_t m) {
+                const int64_t row = m < p.half_rows ? m : m - p.half_rows;
+                void* out = m < p.half_rows ? p.out : p.out2;
+                return row < p.out_rows ? static_cast<uint16_t*>(out) + row * p.out_ld : nullptr;
+            });
+        } else if constexpr (OUT == kGate) {
+            constexpr int H = NF / 2;
+            write([&](int i, int j) {
+                f32x4 h;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) h[e] = silu(acc[i][j][e]) * acc[i][H + j][e];
+                return h;
+            }, rows_of(p.out));
+            if (p.out2) {
+                write([&](int i, int j) { return acc[i][j]; }, rows_of(p.out2));
+                write([&](int i, int j) { return acc[i][H + j]; }, rows_of(p.out3));
+            }
+        }
+        return;
+    }
+    const bool vec = p.out_ld % 4 == 0;
 #pragma unroll
     for (int i = 0; i < MF; ++i) {
         const int64_t m = m0 + a_row(i) + lane % 16;
         if (m >= p.m) continue;
 #pragma unroll
         for (int j = 0; j < (HALF ? NF / 2 : NF); ++j) {
-            const int64_t n = n0 + b_row(j) + lane / 16 * 4, left = p.n - n;
+            const int64_t n = n0 + column(j) + lane / 16 * 4, left = p.n - n;
             const f32x4 v = acc[i][j];
             if constexpr (OUT == kSums) {
                 store4(p.out, p.out_f32, m * p.out_ld + n, left, vec, v * scale);
