@@ -131,6 +131,62 @@ int expand(const uint8_t* q, const uint8_t* scales, int64_t n, int64_t k, int bl
     return launched();
 }
 
+// The same transposed, [k, ld] with zeros from n to ld: as rows of the gradient's contraction.  A workgroup turns 64
+// by 128 values in LDS, whose rows are two words longer than their values so that a wave's writes, 16 weight rows
+// by four rows of the tile 16 apart, meet in no bank.
+constexpr int kTurnN = 64, kTurnK = 128;
+
+template <Kind KIND>
+__global__ __launch_bounds__(kExpandThreads) void expand_turned_kernel(const uint8_t* __restrict__ q,
+                                                                       const uint8_t* __restrict__ scales, int64_t n,
+                                                                       uint32_t k, uint32_t tiles_k, int shift, int64_t ld,
+                                                                       uint16_t* __restrict__ out) {
+    __shared__ uint32_t tile[kTurnK][kTurnN / 2 + 1];
+    const int64_t n0 = (int64_t)(blockIdx.x / tiles_k) * kTurnN;
+    const uint32_t k0 = blockIdx.x % tiles_k * kTurnK;
+    const int row = threadIdx.x / 4, part = threadIdx.x % 4;             // 16 values of a weight row, 64 apart
+    const uint64_t row_at = (uint64_t)(n0 + row) * k;
+    constexpr int kPieces = kTurnK / 64;
+    uint2 w[kPieces];
+    uint32_t code[kPieces];
+#pragma unroll
+    for (int p = 0; p < kPieces; ++p) {
+        const uint32_t at = k0 + p * 64 + part * 16;                     // k is a multiple of 16
+        const bool in = n0 + row < n && at < k;
+        w[p] = in ? *reinterpret_cast<const uint2*>(q + (row_at + at) / 2) : make_uint2(0u, 0u);
+        code[p] = in ? scales[(row_at + at) >> shift] : 0u;
+    }
+#pragma unroll
+    for (int p = 0; p < kPieces; ++p) {
+        const uint4 a = expand8<KIND>(w[p].x, code[p]), b = expand8<KIND>(w[p].y, code[p]);
+        const uint32_t v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            reinterpret_cast<uint16_t*>(tile[p * 64 + part * 16 + j])[row] = (uint16_t)(v[j / 2] >> (j % 2 * 16));
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kTurnK * kTurnN / 8 / kExpandThreads; ++i) {
+        const int c = i * kExpandThreads + threadIdx.x, r = c / (kTurnN / 8), chunk = c % (kTurnN / 8);
+        if (k0 + r < k && n0 + chunk * 8 < ld)
+            *reinterpret_cast<uint4*>(out + (int64_t)(k0 + r) * ld + n0 + chunk * 8) =
+                make_uint4(tile[r][chunk * 4], tile[r][chunk * 4 + 1], tile[r][chunk * 4 + 2], tile[r][chunk * 4 + 3]);
+    }
+}
+
+template <Kind KIND>
+int expand_turned(const uint8_t* q, const uint8_t* scales, int64_t n, int64_t k, int block, int64_t ld, void* out,
+                  hipStream_t stream) {
+    const int64_t tiles_k = ceil_div(k, kTurnK), tiles = ceil_div(n, kTurnN) * tiles_k;
+    if (tiles == 0) return NVFP4_OK;
+    if (tiles > 0x7FFFFFFF) return NVFP4_ERR_SHAPE;
+    int shift = 4;
+    while (1 << shift < block) ++shift;
+    hipLaunchKernelGGL((expand_turned_kernel<KIND>), dim3((unsigned)tiles), dim3(kExpandThreads), 0, stream, q, scales, n,
+                       (uint32_t)k, (uint32_t)tiles_k, shift, ld, static_cast<uint16_t*>(out));
+    return launched();
+}
+
 bool valid_out(int dtype) { return dtype == NVFP4_IN_F32 || dtype == NVFP4_IN_BF16; }
 
 // ---- y = x W^T ------------------------------------------------------------------------------
@@ -206,12 +262,14 @@ int run_linear(const void* x, int64_t ldx, const uint8_t* q, const uint8_t* scal
 }
 
 // ---- dx = dy W ------------------------------------------------------------------------------
+// The weights are expanded with their rows turned, so that both operands hold the contraction along their rows
+// ([4096, 14336] x [14336, 4096]: 438 us with the weights as they lie, 365 so).
 
 int64_t grad_workspace(int64_t m, int64_t n, int64_t k, int64_t k32, int64_t ld) {
     Carver c{nullptr};
-    c.take(n * k32 * 2);
+    c.take(k32 * packed_ld(n) * 2);
     if (needs_pack(n, ld)) c.take(m * packed_ld(n) * 2);
-    return c.at + parts_bytes<kBf16, kAcross, kSingle>(m, k, n);
+    return c.at + parts_bytes<kBf16, kAlong, kSingle>(m, k, n);
 }
 
 // k32: the width of the weights' rows (k filled up to whole blocks); dx has k columns.
@@ -219,8 +277,8 @@ template <Kind KIND>
 int run_grad(const void* dy, int64_t ld, const uint8_t* q, const uint8_t* scales, int block, const float* S, int64_t m,
              int64_t n, int64_t k, int64_t k32, int out_dtype, void* out, void* ws, hipStream_t stream) {
     Carver c{static_cast<char*>(ws)};
-    void* w = c.take(n * k32 * 2);
-    if (const int rc = expand<KIND>(q, scales, n, k32, block, w, stream)) return rc;
+    void* w = c.take(k32 * packed_ld(n) * 2);
+    if (const int rc = expand_turned<KIND>(q, scales, n, k32, block, packed_ld(n), w, stream)) return rc;
     if (needs_pack(n, ld)) {
         void* packed = c.take(m * packed_ld(n) * 2);
         if (const int rc = pack_bf16_rows(dy, m, n, ld, packed, stream)) return rc;
@@ -228,9 +286,9 @@ int run_grad(const void* dy, int64_t ld, const uint8_t* q, const uint8_t* scales
     }
     Args p = {};
     p.a.p = static_cast<const char*>(dy), p.a.ld = ld * 2;
-    p.b.p = static_cast<const char*>(w), p.b.ld = k32 * 2;
+    p.b.p = static_cast<const char*>(w), p.b.ld = packed_ld(n) * 2;
     p.m = m, p.n = k, p.inner = n, p.scale = S, p.out = out, p.out_ld = k, p.out_f32 = out_dtype == NVFP4_IN_F32;
-    return run_sums<kBf16, kAlong, kAcross, kSingle>(p, static_cast<float*>(c.take(0)), stream);
+    return run_sums<kBf16, kAlong, kAlong, kSingle>(p, static_cast<float*>(c.take(0)), stream);
 }
 
 // ---- y = A B^T, both microscaled --------------------------------------------------------------
