@@ -1,7 +1,8 @@
-// NVFP4 products with one to four activation rows (a decode step): reading the weights is all there is to do, and
-// what stands in its way are instructions, so each weight pair costs one conversion and one two-way dot product
-// a row.  A wave's lanes lie along the contraction, 32 values each; a lane holds its activations in registers and
-// goes down eight weight rows, whose loads are all in flight at once.  The values of a block are summed as they
+// Products with one to four activation rows (a decode step): reading the weights is all there is to do, so a wave
+// reads whole stretches of a row, its lanes along the contraction, and has many rows in flight.
+//
+// NVFP4: what else stands in its way are instructions, so each weight pair costs one conversion and one two-way dot
+// product a row.  A lane holds 32 values' activations in registers and goes down eight weight rows, whose loads are all in flight at once.  The values of a block are summed as they
 // are and the sum is multiplied by the block's scale, so scales cost an instruction a block.
 //   y[m][n] = S sum_blocks s sum_j q_j x_j, sums in binary32.
 // [14336, 4096] for one row: see the table of the measured cases; a matrix instruction would need the weights
@@ -150,6 +151,100 @@ __global__ __launch_bounds__(kWaves * kLanes) void dot_kernel(Args p) {
     v *= *p.scale;
     if (p.out_f32) static_cast<float*>(p.out)[m * p.n + n] = v;
     else static_cast<uint16_t*>(p.out)[m * p.n + n] = (uint16_t)pack_bf16(v, v);
+}
+
+// The gated block in the same way, bfloat16 weights: a lane holds eight values of the contraction and goes down
+// kGatedRows rows of both matrices.
+constexpr int kGatedRows = 8, kGatedSpan = kLanes * 8;
+
+struct GatedArgs {
+    const char *wg, *wu;                         // [n, ldw bytes]
+    const char* x;                               // [m, ldx bytes]
+    int64_t ldw, ldx, n, k;
+    int along;
+    void *h, *gate, *up;
+};
+
+template <int M>
+__global__ __launch_bounds__(kWaves * kLanes) void gated_dot_kernel(GatedArgs p) {
+    __shared__ float sums[kWaves][2][M][kGatedRows];
+    const int tid = threadIdx.x, lane = tid % kLanes;
+    const int wave = __builtin_amdgcn_readfirstlane(tid / kLanes);
+    const int along = p.along, part = wave % along, group = wave / along;
+    const int64_t rows = kGatedRows * (kWaves / along), n0 = blockIdx.x * rows + group * kGatedRows, left = p.n - n0;
+    const __amdgpu_buffer_rsrc_t rw[2] = {window(p.wg + n0 * p.ldw), window(p.wu + n0 * p.ldw)}, rx = window(p.x);
+    const uint32_t k = (uint32_t)p.k;
+
+    float acc[2][M][kGatedRows];
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int m = 0; m < M; ++m)
+#pragma unroll
+            for (int r = 0; r < kGatedRows; ++r) acc[b][m][r] = 0.0f;
+
+    for (uint32_t at = (uint32_t)part * kGatedSpan; at < k; at += (uint32_t)along * kGatedSpan) {
+        const uint32_t v = at + lane * 8;        // rows hold whole groups of eight, zeros past k
+        i32x4 x[M], w[2][kGatedRows];
+#pragma unroll
+        for (int m = 0; m < M; ++m) x[m] = load16(rx, v < k ? (uint32_t)m * (uint32_t)p.ldx + v * 2 : kOutside);
+#pragma unroll
+        for (int r = 0; r < kGatedRows; ++r)
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+                w[b][r] = load16(rw[b], r < left && v < k ? (uint32_t)r * (uint32_t)p.ldw + v * 2 : kOutside);
+#pragma unroll
+        for (int r = 0; r < kGatedRows; ++r)
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int m = 0; m < M; ++m)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[b][m][r] = dot2((uint32_t)w[b][r][j], (uint32_t)x[m][j], acc[b][m][r]);
+    }
+
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+            static_assert(kGatedRows == 8, "two folds and a pair");
+            const float* a = acc[b][m];
+            const float lo = sum16(fold16(fold32(a[0], a[2]), fold32(a[1], a[3])));
+            const float hi = sum16(fold16(fold32(a[4], a[6]), fold32(a[5], a[7])));
+            if (lane % 16 == 0) {
+                sums[wave][b][m][lane / 16] = lo;
+                sums[wave][b][m][4 + lane / 16] = hi;
+            }
+        }
+    __syncthreads();
+    if (tid >= M * kGatedRows * (kWaves / along)) return;
+    const int r = tid % kGatedRows, m = tid / kGatedRows % M, of = tid / (kGatedRows * M);
+    const int64_t n = blockIdx.x * rows + of * kGatedRows + r;
+    if (n >= p.n) return;
+    float g = 0.0f, u = 0.0f;
+    for (int a = 0; a < along; ++a) {
+        g += sums[of * along + a][0][m][r];
+        u += sums[of * along + a][1][m][r];
+    }
+    const float h = silu(g) * u;
+    static_cast<uint16_t*>(p.h)[m * p.n + n] = (uint16_t)pack_bf16(h, h);
+    if (p.gate) {
+        static_cast<uint16_t*>(p.gate)[m * p.n + n] = (uint16_t)pack_bf16(g, g);
+        static_cast<uint16_t*>(p.up)[m * p.n + n] = (uint16_t)pack_bf16(u, u);
+    }
+}
+
+// Waves of a workgroup along the contraction, for spans of `span` values.
+inline int waves_along(int64_t k, int span) {
+    int along = 1;
+    while (along < kWaves && (int64_t)along * span < k) along *= 2;
+    return along;
+}
+
+template <int M>
+void launch_gated_dot(const GatedArgs& p, hipStream_t stream) {
+    const int64_t rows = kGatedRows * (kWaves / p.along);
+    hipLaunchKernelGGL((gated_dot_kernel<M>), dim3((unsigned)((p.n + rows - 1) / rows)), dim3(kWaves * kLanes), 0, stream, p);
 }
 
 template <int M>

@@ -2,6 +2,7 @@
 // h = silu(g) u, silu(g) = g / (1 + e^-g), in bfloat16 with sums in binary32, and its backward pass
 //   s = 1 / (1 + e^-g),  dg = dh u s (1 + g (1 - s)),  du = dh g s,
 //   dx = dg Wg + du Wu,  dWg = dg^T x,  dWu = du^T x.
+#include "dot_product.h"
 #include "product_host.h"
 #include "thin_product.h"
 
@@ -122,6 +123,20 @@ int nvfp4_swiglu_ffn(const void* x, int64_t ldx, const void* w_gate, const void*
     if (const int rc = packed(c, rx, m, k, needs_pack(k, ldx), st)) return rc;
     if (const int rc = packed(c, rg, n, k, pw, st)) return rc;
     if (const int rc = packed(c, ru, n, k, pw, st)) return rc;
+    if (m <= dot_product::kMostRows) {
+        dot_product::GatedArgs t = {};
+        t.wg = static_cast<const char*>(rg.p), t.wu = static_cast<const char*>(ru.p), t.ldw = rg.ld * 2;
+        t.x = static_cast<const char*>(rx.p), t.ldx = rx.ld * 2, t.n = n, t.k = k;
+        t.along = dot_product::waves_along(k, dot_product::kGatedSpan);
+        t.h = h, t.gate = gate, t.up = up_out;
+        switch (m) {
+            case 1: dot_product::launch_gated_dot<1>(t, st); break;
+            case 2: dot_product::launch_gated_dot<2>(t, st); break;
+            case 3: dot_product::launch_gated_dot<3>(t, st); break;
+            default: dot_product::launch_gated_dot<4>(t, st);
+        }
+        return launched();
+    }
     if (m <= thin_product::kRows) {
         thin_product::Args t = {};
         t.w = static_cast<const char*>(rg.p), t.w2 = static_cast<const char*>(ru.p), t.ldw = rg.ld * 2;

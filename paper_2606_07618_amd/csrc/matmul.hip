@@ -220,7 +220,7 @@ int run_linear(const void* x, int64_t ldx, const uint8_t* q, const uint8_t* scal
         dot_product::Args t = {};
         t.q = reinterpret_cast<const char*>(q), t.scales = scales, t.x = static_cast<const char*>(x), t.ldx = ldx * 2;
         t.n = n, t.k = k, t.shift = shift, t.scale = S, t.out = out, t.out_f32 = f32;
-        for (t.along = 1; t.along < dot_product::kWaves && t.along * dot_product::kSpan < k;) t.along *= 2;
+        t.along = dot_product::waves_along(k, dot_product::kSpan);
         switch (m) {
             case 1: dot_product::launch_dot<1>(t, stream); break;
             case 2: dot_product::launch_dot<2>(t, stream); break;
