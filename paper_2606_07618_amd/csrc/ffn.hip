@@ -12,51 +12,136 @@ using namespace product_host;
 
 constexpr int kEdgeThreads = 256;
 
-__device__ __forceinline__ float bf16_f32(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }
+// The backward products' contractions run over the tokens (dW) and over the weights' rows (dx), so dg and du are
+// written as they lie and turned, and x and the weights are turned: all four products then read whole rows.
+// [4000, 4096] -> 14336: 1830 us with the operands as they lie, 1636 so.  The two products take nine tenths of it at
+// 1.25 PFLOP/s; this kernel moves 800 MB in 142 us and turning a weight matrix 235 MB in 48 (5.6 and 4.9 TB/s).
+//
+// Turning: a workgroup takes 64 rows by 128 columns.  A thread holds two rows by eight columns of either half and
+// writes pairs of rows, a word each, to LDS; LDS rows are a word longer than their 64 values, so that the eight row
+// pairs by eight groups of columns of a wave meet in no bank.  Then each row of LDS leaves in 16-byte pieces.
+constexpr int kTurnRows = 64, kTurnColumns = 128;
+typedef uint32_t TurnTile[kTurnColumns][kTurnRows / 2 + 1];
 
-// dg and du, side by side: d [m, ld], du from column `half` on, zeros from n to half.  Their rounding to
+constexpr int kTurnHalf = kTurnColumns / 2;
+__device__ __forceinline__ int turn_pair() { return threadIdx.x / 8; }
+__device__ __forceinline__ int turn_column() { return threadIdx.x % 8 * 8; }
+
+// Words of two rows' eight values to columns c .. c + 7.
+__device__ __forceinline__ void turn8(TurnTile& tile, int c, const uint4& a, const uint4& b) {
+    const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        tile[c + 2 * j][turn_pair()] = __builtin_amdgcn_perm(y[j], x[j], 0x05040100u);
+        tile[c + 2 * j + 1][turn_pair()] = __builtin_amdgcn_perm(y[j], x[j], 0x07060302u);
+    }
+}
+
+// Columns c0 .. of the source as rows of dst, values r0 .. r0 + 63 of each, as far as they lie in [rows, fill].
+__device__ __forceinline__ void turn_out(const TurnTile& tile, int64_t c0, int64_t rows, int64_t r0, int64_t fill,
+                                         int64_t to_ld, uint16_t* dst) {
+#pragma unroll
+    for (int i = 0; i < kTurnColumns * kTurnRows / 8 / kEdgeThreads; ++i) {
+        const int at = i * kEdgeThreads + threadIdx.x, c = at / (kTurnRows / 8), chunk = at % (kTurnRows / 8);
+        if (c0 + c < rows && r0 + chunk * 8 < fill)
+            *reinterpret_cast<uint4*>(dst + (c0 + c) * to_ld + r0 + chunk * 8) =
+                make_uint4(tile[c][chunk * 4], tile[c][chunk * 4 + 1], tile[c][chunk * 4 + 2], tile[c][chunk * 4 + 3]);
+    }
+}
+
+// Values c .. c + 7 of row r of a [rows, width] matrix, zeros outside.  VEC: its rows are whole 16-byte pieces.
+template <bool VEC>
+__device__ __forceinline__ uint4 eight(const uint16_t* src, int64_t r, int64_t rows, int64_t c, int64_t width, int64_t ld) {
+    if (r >= rows || c >= width) return make_uint4(0, 0, 0, 0);
+    if constexpr (VEC) return *reinterpret_cast<const uint4*>(src + r * ld + c);
+    uint32_t v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = c + j < width ? src[r * ld + c + j] : 0u;
+    return make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+}
+
+// src [rows, width] turned: dst [width, to_ld], values from rows to fill zero.
+template <bool VEC>
+__global__ __launch_bounds__(kEdgeThreads) void turn_kernel(const uint16_t* __restrict__ src, int64_t rows, int64_t width,
+                                                            int64_t ld, int64_t tiles_c, int64_t fill,
+                                                            uint16_t* __restrict__ dst, int64_t to_ld) {
+    __shared__ TurnTile tile;
+    const int64_t r0 = blockIdx.x / tiles_c * kTurnRows, c0 = blockIdx.x % tiles_c * kTurnColumns;
+    const int64_t r = r0 + turn_pair() * 2, c = c0 + turn_column();
+    uint4 v[2][2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) v[h][e] = eight<VEC>(src, r + e, rows, c + h * kTurnHalf, width, ld);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) turn8(tile, turn_column() + h * kTurnHalf, v[h][0], v[h][1]);
+    __syncthreads();
+    turn_out(tile, c0, width, r0, fill, to_ld, dst);
+}
+
+int turn(const uint16_t* src, int64_t rows, int64_t width, int64_t ld, int64_t fill, uint16_t* dst, int64_t to_ld,
+         hipStream_t stream) {
+    const int64_t tiles_c = ceil_div(width, kTurnColumns), tiles = ceil_div(fill, kTurnRows) * tiles_c;
+    if (tiles == 0) return NVFP4_OK;
+    if (tiles > 0x7FFFFFFF) return NVFP4_ERR_SHAPE;
+    hipLaunchKernelGGL((width % 8 == 0 && ld % 8 == 0 ? turn_kernel<true> : turn_kernel<false>), dim3((unsigned)tiles),
+                       dim3(kEdgeThreads), 0, stream, src, rows, width, ld, tiles_c, fill, dst, to_ld);
+    return launched();
+}
+
+// dg and du side by side, d [m, 2 half], du from column `half` on, zeros from n to half; and turned, one below the
+// other, t [2 n, ld], zeros from m to ld.  Either is left out where its pointer is NULL.  Their rounding to
 // bfloat16 is what the matrix cores take; the products' sums stay in binary32.
 template <bool VEC>
 __global__ __launch_bounds__(kEdgeThreads) void gate_grad_kernel(const uint16_t* __restrict__ dh,
                                                                  const uint16_t* __restrict__ gate,
                                                                  const uint16_t* __restrict__ up_, int64_t m, int64_t n,
-                                                                 int64_t half, int64_t ld, uint16_t* __restrict__ d) {
-    const int64_t row_units = half / 8, units = m * row_units;
-    for (int64_t i = (int64_t)blockIdx.x * kEdgeThreads + threadIdx.x; i < units;
-         i += (int64_t)gridDim.x * kEdgeThreads) {
-        const int64_t r = i / row_units, c = i % row_units * 8;
-        uint16_t a[8], g[8], u[8];
-        if (VEC && c < n) {
-            *reinterpret_cast<uint4*>(a) = *reinterpret_cast<const uint4*>(dh + r * n + c);
-            *reinterpret_cast<uint4*>(g) = *reinterpret_cast<const uint4*>(gate + r * n + c);
-            *reinterpret_cast<uint4*>(u) = *reinterpret_cast<const uint4*>(up_ + r * n + c);
-        } else {
+                                                                 int64_t tiles_n, int64_t half, uint16_t* __restrict__ d,
+                                                                 int64_t ld, uint16_t* __restrict__ t) {
+    __shared__ TurnTile tg, tu;
+    const int64_t r0 = blockIdx.x / tiles_n * kTurnRows, c0 = blockIdx.x % tiles_n * kTurnColumns;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const bool in = c + j < n;
-                a[j] = in ? dh[r * n + c + j] : 0;
-                g[j] = in ? gate[r * n + c + j] : 0;
-                u[j] = in ? up_[r * n + c + j] : 0;
+    for (int h = 0; h < 2; ++h) {
+        const int64_t r = r0 + turn_pair() * 2, c = c0 + turn_column() + h * kTurnHalf;
+        uint4 og[2], ou[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const uint4 va = eight<VEC>(dh, r + e, m, c, n, n), vg = eight<VEC>(gate, r + e, m, c, n, n),
+                        vu = eight<VEC>(up_, r + e, m, c, n, n);
+            const uint32_t a[4] = {va.x, va.y, va.z, va.w}, g[4] = {vg.x, vg.y, vg.z, vg.w}, u[4] = {vu.x, vu.y, vu.z, vu.w};
+            uint32_t wg[4], wu[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float dg[2], du[2];
+#pragma unroll
+                for (int o = 0; o < 2; ++o) {
+                    const int shift = o ? 0 : 16;
+                    const float G = __uint_as_float(g[j] << shift & 0xFFFF0000u), U = __uint_as_float(u[j] << shift & 0xFFFF0000u),
+                                H = __uint_as_float(a[j] << shift & 0xFFFF0000u);
+                    const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(G * -1.44269504f));
+                    const float silu = G * s;
+                    du[o] = H * silu;
+                    dg[o] = H * U * fmaf(silu, 1.0f - s, s);
+                }
+                wg[j] = pack_bf16(dg[0], dg[1]);
+                wu[j] = pack_bf16(du[0], du[1]);
+            }
+            og[e] = make_uint4(wg[0], wg[1], wg[2], wg[3]);
+            ou[e] = make_uint4(wu[0], wu[1], wu[2], wu[3]);
+            if (d && r + e < m && c < half) {
+                *reinterpret_cast<uint4*>(d + (r + e) * 2 * half + c) = og[e];
+                *reinterpret_cast<uint4*>(d + (r + e) * 2 * half + half + c) = ou[e];
             }
         }
-        uint32_t og[4], ou[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            float dg[2], du[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const float G = bf16_f32(g[2 * j + e]), U = bf16_f32(u[2 * j + e]), H = bf16_f32(a[2 * j + e]);
-                const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(G * -1.44269504f));
-                const float silu = G * s;
-                du[e] = H * silu;
-                dg[e] = H * U * fmaf(silu, 1.0f - s, s);
-            }
-            og[j] = pack_bf16(dg[0], dg[1]);
-            ou[j] = pack_bf16(du[0], du[1]);
+        if (t) {
+            turn8(tg, turn_column() + h * kTurnHalf, og[0], og[1]);
+            turn8(tu, turn_column() + h * kTurnHalf, ou[0], ou[1]);
         }
-        *reinterpret_cast<uint4*>(d + r * ld + c) = make_uint4(og[0], og[1], og[2], og[3]);
-        *reinterpret_cast<uint4*>(d + r * ld + half + c) = make_uint4(ou[0], ou[1], ou[2], ou[3]);
     }
+    if (!t) return;
+    __syncthreads();
+    turn_out(tg, c0, n, r0, ld, ld, t);
+    turn_out(tu, c0, n, r0, ld, ld, t + n * ld);
 }
 
 struct Rows { const void* p; int64_t ld; };
@@ -80,10 +165,21 @@ int64_t pack_workspace(int64_t m, int64_t n, int64_t k, int64_t ldx, int64_t ldw
     return c.at;
 }
 
-int64_t half_of(int64_t n) { return up(n, 64); }       // whole steps of the contraction
+// Sections of the backward pass's workspace: d, and what each product reads besides.
+struct Backward { int64_t half, ld; char *d, *wt, *dt, *xt, *parts; };
 
-int64_t backward_workspace(int64_t m, int64_t n, int64_t k, int64_t ldx, int64_t ldw) {
-    return pack_workspace(m, n, k, ldx, ldw) + up(m * 2 * half_of(n) * 2, 256) + parts_bytes<kBf16, kAcross, kPairInner>(m, k, n);
+int64_t backward_sections(void* workspace, int64_t m, int64_t n, int64_t k, Backward& b) {
+    Carver c{static_cast<char*>(workspace)};
+    // Whole lines of memory, and whole steps of the products: dW of [4000, 4096] -> 14336 took 842 us with rows
+    // filled up to eights only, 770 so.
+    b.half = up(n, 64), b.ld = up(m, 64);
+    b.d = static_cast<char*>(c.take(m * 2 * b.half * 2));
+    b.dt = static_cast<char*>(c.take(2 * n * b.ld * 2));
+    Carver x = c, w = c;                         // dx is done before x is turned
+    b.wt = static_cast<char*>(x.take(k * 2 * b.half * 2));
+    b.parts = static_cast<char*>(x.take(parts_bytes<kBf16>(m, k, 2 * b.half)));
+    b.xt = static_cast<char*>(w.take(k * b.ld * 2));
+    return x.at > w.at ? x.at : w.at;
 }
 
 int check_call(int64_t m, int64_t n, int64_t k, int64_t ldx, int64_t ldw) {
@@ -142,7 +238,7 @@ int nvfp4_swiglu_ffn(const void* x, int64_t ldx, const void* w_gate, const void*
         t.w = static_cast<const char*>(rg.p), t.w2 = static_cast<const char*>(ru.p), t.ldw = rg.ld * 2;
         t.x = static_cast<const char*>(rx.p), t.ldx = rx.ld * 2, t.m = (int)m, t.n = n, t.k = k;
         t.out = h, t.out2 = gate, t.out3 = up_out;
-        thin_product::launch_thin<thin_product::kGated, 8, 4, true>(t, st);
+        thin_product::launch_thin<thin_product::kGated, 8, 4>(t, st);
         return launched();
     }
     Args p = {};
@@ -150,12 +246,13 @@ int nvfp4_swiglu_ffn(const void* x, int64_t ldx, const void* w_gate, const void*
     p.b.p = static_cast<const char*>(rg.p), p.b.p2 = static_cast<const char*>(ru.p), p.b.ld = rg.ld * 2;
     p.m = m, p.n = n, p.inner = k, p.out = h, p.out2 = gate, p.out3 = up_out, p.out_ld = n;
     p.parts = 1;
-    return launch_product<kBf16, kAlong, kAlong, kPairOuter, kGate>(p, plan_product<kBf16, kAlong, kPairOuter>(m, n, k, false).tile, st);
+    return launch_product<kBf16, kGate>(p, plan_product<kBf16, kGate>(m, n, k).tile, st);
 }
 
 int64_t nvfp4_swiglu_ffn_backward_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t ldx, int64_t ldw) {
     if (const int rc = check_call(m, n, k, ldx, ldw)) return rc;
-    return backward_workspace(m, n, k, ldx, ldw);
+    Backward b;
+    return backward_sections(nullptr, m, n, k, b);
 }
 
 int nvfp4_swiglu_ffn_backward(const void* dh, const void* x, int64_t ldx, const void* w_gate, const void* w_up,
@@ -171,41 +268,35 @@ int nvfp4_swiglu_ffn_backward(const void* dh, const void* x, int64_t ldx, const 
     if (inputs && (!dh || !gate || !up_in || (want_x && (!w_gate || !w_up)) || (want_w && !x))) return NVFP4_ERR_NULL;
     for (const void* p : {dh, x, w_gate, w_up, gate, up_in, (const void*)dx, (const void*)dw_gate, (const void*)dw_up})
         if (!aligned(p, 16)) return NVFP4_ERR_ALIGN;
-    if (const int rc = check_ws(workspace, workspace_bytes, backward_workspace(m, n, k, ldx, ldw))) return rc;
+    if (want_w && m > kMaxLd) return NVFP4_ERR_SHAPE;              // a row of the turned operands
+    Backward b;
+    if (const int rc = check_ws(workspace, workspace_bytes, backward_sections(workspace, m, n, k, b))) return rc;
     hipStream_t st = (hipStream_t)stream;
-    Carver c{static_cast<char*>(workspace)};
-    const int64_t half = half_of(n);
-    const int64_t ld = 2 * half;
-    uint16_t* d = static_cast<uint16_t*>(c.take(m * ld * 2));
-    const int64_t units = m * (half / 8), groups = ceil_div(units, kEdgeThreads);
-    if (units > 0) {
-        hipLaunchKernelGGL((n % 8 == 0 ? gate_grad_kernel<true> : gate_grad_kernel<false>),
-                           dim3((unsigned)(groups < 16384 ? groups : 16384)), dim3(kEdgeThreads), 0, st,
-                           static_cast<const uint16_t*>(dh), static_cast<const uint16_t*>(gate),
-                           static_cast<const uint16_t*>(up_in), m, n, half, ld, d);
+    const auto values = [](const void* p) { return static_cast<const uint16_t*>(p); };
+    const auto turned = [](char* p) { return reinterpret_cast<uint16_t*>(p); };
+    const int64_t tiles_n = ceil_div(n, kTurnColumns), tiles = ceil_div(m, kTurnRows) * tiles_n;
+    if (tiles > 0x7FFFFFFF) return NVFP4_ERR_SHAPE;
+    if (tiles > 0) {
+        hipLaunchKernelGGL((n % 8 == 0 ? gate_grad_kernel<true> : gate_grad_kernel<false>), dim3((unsigned)tiles),
+                           dim3(kEdgeThreads), 0, st, values(dh), values(gate), values(up_in), m, n, tiles_n, b.half,
+                           want_x ? turned(b.d) : nullptr, b.ld, want_w ? turned(b.dt) : nullptr);
         if (const int rc = launched()) return rc;
     }
-    Rows rx{x, ldx}, rg{w_gate, ldw}, ru{w_up, ldw};
     if (want_x) {
-        const bool pw = needs_pack(k, ldw);
-        if (const int rc = packed(c, rg, n, k, pw, st)) return rc;
-        if (const int rc = packed(c, ru, n, k, pw, st)) return rc;
+        if (const int rc = turn(values(w_gate), n, k, ldw, b.half, turned(b.wt), 2 * b.half, st)) return rc;
+        if (const int rc = turn(values(w_up), n, k, ldw, b.half, turned(b.wt) + b.half, 2 * b.half, st)) return rc;
         Args p = {};
-        p.a.p = reinterpret_cast<const char*>(d), p.a.ld = ld * 2;
-        p.b.p = static_cast<const char*>(rg.p), p.b.p2 = static_cast<const char*>(ru.p), p.b.ld = rg.ld * 2;
-        p.m = m, p.n = k, p.inner = n, p.out = dx, p.out_ld = k;
-        if (const int rc = run_sums<kBf16, kAlong, kAcross, kPairInner>(p, static_cast<float*>(c.take(0)), st)) return rc;
+        p.a.p = b.d, p.a.ld = p.b.ld = 2 * b.half * 2, p.b.p = b.wt;
+        p.m = m, p.n = k, p.inner = 2 * b.half, p.out = dx, p.out_ld = k;
+        if (const int rc = run_sums<kBf16>(p, reinterpret_cast<float*>(b.parts), st)) return rc;
     }
     if (want_w) {
-        if (const int rc = packed(c, rx, m, k, needs_pack(k, ldx), st)) return rc;
+        if (const int rc = turn(values(x), m, k, ldx, b.ld, turned(b.xt), b.ld, st)) return rc;
         Args p = {};
-        p.a.p = reinterpret_cast<const char*>(d), p.a.ld = ld * 2;
-        p.b.p = static_cast<const char*>(rx.p), p.b.ld = rx.ld * 2;
-        p.m = 2 * half, p.n = k, p.inner = m, p.half_rows = half, p.out_rows = n;
-        p.out = dw_gate, p.out2 = dw_up, p.out_ld = k;
-        p.parts = 1;
-        const int tile = plan_product<kBf16, kAcross, kSingle>(p.m, k, m, false).tile;
-        if (const int rc = launch_product<kBf16, kAcross, kAcross, kSingle, kTwoRows>(p, tile, st)) return rc;
+        p.a.p = b.dt, p.a.ld = p.b.ld = b.ld * 2, p.b.p = b.xt;
+        p.m = 2 * n, p.n = k, p.inner = m, p.half_rows = n;
+        p.out = dw_gate, p.out2 = dw_up, p.out_ld = k, p.parts = 1;
+        if (const int rc = launch_product<kBf16, kTwoRows>(p, plan_product<kBf16, kTwoRows>(2 * n, k, m).tile, st)) return rc;
     }
     return NVFP4_OK;
 }

@@ -65,7 +65,6 @@ int pack_scale_rows(const uint8_t* src, int64_t rows, int64_t width, uint8_t* ds
     return pack(src, rows, width, width, dst, dst_ld, stream);
 }
 
-
 int join_parts(const float* part, int parts, int64_t count, const float* scale, void* out, int f32, hipStream_t stream) {
     const bool vec = count % 4 == 0;
     const int64_t groups = ceil_div(vec ? count / 4 : count, kJoinThreads);
@@ -80,7 +79,6 @@ int join_parts(const float* part, int parts, int64_t count, const float* scale, 
 namespace {
 
 using namespace product_host;
-typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 // ---- weights expanded to bfloat16 -----------------------------------------------------------
 
@@ -89,45 +87,35 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 // microscaled blocks of codes under 2 hold).
 template <Kind KIND>
 __device__ __forceinline__ uint4 expand8(uint32_t n, uint32_t code) {
-    f32x2 d[4];
-    if constexpr (KIND == kMx) {
-        const float s = __uint_as_float(code << 23);
-        d[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(n, s, 0);
-        d[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(n, s, 1);
-        d[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(n, s, 2);
-        d[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(n, s, 3);
-        if (code == 255) d[0] = d[1] = d[2] = d[3] = f32x2{__uint_as_float(0x7FC00000u), __uint_as_float(0x7FC00000u)};
-    } else {
-        return __builtin_bit_cast(uint4, thin_product::expand8(n, thin_product::e4m3_f32(code)));
-    }
-    return make_uint4(pack_bf16(d[0][0], d[0][1]), pack_bf16(d[1][0], d[1][1]), pack_bf16(d[2][0], d[2][1]),
-                      pack_bf16(d[3][0], d[3][1]));
+    const float s = KIND == kMx ? __uint_as_float(code << 23) : 1.0f, t = KIND == kMx ? 1.0f : e4m3_f32(code);
+    f32x2 d[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(n, s, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(n, s, 1),
+                  __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(n, s, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(n, s, 3)};
+    if (KIND == kMx && code == 255) d[0] = d[1] = d[2] = d[3] = f32x2{__uint_as_float(0x7FC00000u), __uint_as_float(0x7FC00000u)};
+    return make_uint4(pack_bf16(d[0][0] * t, d[0][1] * t), pack_bf16(d[1][0] * t, d[1][1] * t),
+                      pack_bf16(d[2][0] * t, d[2][1] * t), pack_bf16(d[3][0] * t, d[3][1] * t));
 }
 
 constexpr int kExpandThreads = 256;
 
 // Rows of row_units units of 8 values, a scale for each 2^shift of them; a workgroup expands a piece of one row.
-template <Kind KIND>
 __global__ __launch_bounds__(kExpandThreads) void expand_kernel(const uint32_t* __restrict__ q,
                                                                 const uint8_t* __restrict__ scales, uint32_t row_units,
-                                                                uint32_t row_groups, int shift, int64_t ld_units,
-                                                                uint4* __restrict__ out) {
+                                                                uint32_t row_groups, int shift, uint4* __restrict__ out) {
     const uint32_t row = blockIdx.x / row_groups, u = blockIdx.x % row_groups * kExpandThreads + threadIdx.x;
     if (u >= row_units) return;
     const int64_t at = (int64_t)row * row_units + u;
-    out[row * ld_units + u] = expand8<KIND>(q[at], scales[at >> shift]);
+    out[at] = expand8<kBf16>(q[at], scales[at >> shift]);
 }
 
-template <Kind KIND>
 int expand(const uint8_t* q, const uint8_t* scales, int64_t n, int64_t k, int block, void* out, hipStream_t stream) {
     const int64_t row_units = k / 8, row_groups = ceil_div(row_units, kExpandThreads);
     if (n * row_units == 0) return NVFP4_OK;
     if (n * row_groups > 0x7FFFFFFF) return NVFP4_ERR_SHAPE;
     int shift = 1;
     while (8 << shift < block) ++shift;
-    hipLaunchKernelGGL((expand_kernel<KIND>), dim3((unsigned)(n * row_groups)), dim3(kExpandThreads), 0, stream,
+    hipLaunchKernelGGL(expand_kernel, dim3((unsigned)(n * row_groups)), dim3(kExpandThreads), 0, stream,
                        reinterpret_cast<const uint32_t*>(q), scales, (uint32_t)row_units, (uint32_t)row_groups, shift,
-                       k / 8, static_cast<uint4*>(out));
+                       static_cast<uint4*>(out));
     return launched();
 }
 
@@ -199,7 +187,7 @@ int64_t linear_workspace(int64_t m, int64_t n, int64_t k) {
         const int parts = stream_product::parts(m, n, k);
         return up(m * k * 2, 256) + up(m * 4, 256) + (parts > 1 ? up(parts * m * n * 4, 256) : 0);
     }
-    return up(n * k * 2, 256) + parts_bytes<kBf16, kAlong, kSingle>(m, n, k);
+    return up(n * k * 2, 256) + parts_bytes<kBf16>(m, n, k);
 }
 
 template <int MF>
@@ -253,12 +241,12 @@ int run_linear(const void* x, int64_t ldx, const uint8_t* q, const uint8_t* scal
     }
     Carver c{static_cast<char*>(ws)};
     void* w = c.take(n * k * 2);
-    if (const int rc = expand<kBf16>(q, scales, n, k, block, w, stream)) return rc;
+    if (const int rc = expand(q, scales, n, k, block, w, stream)) return rc;
     Args p = {};
     p.a.p = static_cast<const char*>(x), p.a.ld = ldx * 2;
     p.b.p = static_cast<const char*>(w), p.b.ld = k * 2;
     p.m = m, p.n = n, p.inner = k, p.scale = S, p.out = out, p.out_ld = n, p.out_f32 = out_dtype == NVFP4_IN_F32;
-    return run_sums<kBf16, kAlong, kAlong, kSingle>(p, static_cast<float*>(c.take(0)), stream);
+    return run_sums<kBf16>(p, static_cast<float*>(c.take(0)), stream);
 }
 
 // ---- dx = dy W ------------------------------------------------------------------------------
@@ -269,7 +257,7 @@ int64_t grad_workspace(int64_t m, int64_t n, int64_t k, int64_t k32, int64_t ld)
     Carver c{nullptr};
     c.take(k32 * packed_ld(n) * 2);
     if (needs_pack(n, ld)) c.take(m * packed_ld(n) * 2);
-    return c.at + parts_bytes<kBf16, kAlong, kSingle>(m, k, n);
+    return c.at + parts_bytes<kBf16>(m, k, n);
 }
 
 // k32: the width of the weights' rows (k filled up to whole blocks); dx has k columns.
@@ -288,7 +276,7 @@ int run_grad(const void* dy, int64_t ld, const uint8_t* q, const uint8_t* scales
     p.a.p = static_cast<const char*>(dy), p.a.ld = ld * 2;
     p.b.p = static_cast<const char*>(w), p.b.ld = packed_ld(n) * 2;
     p.m = m, p.n = k, p.inner = n, p.scale = S, p.out = out, p.out_ld = k, p.out_f32 = out_dtype == NVFP4_IN_F32;
-    return run_sums<kBf16, kAlong, kAlong, kSingle>(p, static_cast<float*>(c.take(0)), stream);
+    return run_sums<kBf16>(p, static_cast<float*>(c.take(0)), stream);
 }
 
 // ---- y = A B^T, both microscaled --------------------------------------------------------------
@@ -300,7 +288,7 @@ int64_t mx_workspace(int64_t m, int64_t n, int64_t blocks) {
         c.take(m * up(blocks, 8));
         c.take(n * up(blocks, 8));
     }
-    return c.at + (m > thin_product::kRows ? parts_bytes<kMx, kAlong, kSingle>(m, n, blocks * 32) : 0);
+    return c.at + (m > thin_product::kRows ? parts_bytes<kMx>(m, n, blocks * 32) : 0);
 }
 
 int run_mx(const uint8_t* aq, const uint8_t* as, const uint8_t* bq, const uint8_t* bs, int64_t m, int64_t n,
@@ -310,7 +298,7 @@ int run_mx(const uint8_t* aq, const uint8_t* as, const uint8_t* bq, const uint8_
         t.w = reinterpret_cast<const char*>(bq), t.ldw = blocks * 16, t.w_scales = bs, t.w_scale_ld = blocks;
         t.x = reinterpret_cast<const char*>(aq), t.ldx = blocks * 16, t.x_scales = as, t.m = (int)m, t.n = n, t.k = blocks * 32;
         t.out = out, t.out_f32 = out_dtype == NVFP4_IN_F32;
-        thin_product::launch_thin<thin_product::kMicroscaled, 8, 4, true>(t, stream);
+        thin_product::launch_thin<thin_product::kMicroscaled, 8, 4>(t, stream);
         return launched();
     }
     int64_t scale_ld = blocks;
@@ -327,7 +315,7 @@ int run_mx(const uint8_t* aq, const uint8_t* as, const uint8_t* bq, const uint8_
     p.a.p = reinterpret_cast<const char*>(aq), p.a.ld = blocks * 16, p.a.scales = as, p.a.scale_ld = scale_ld;
     p.b.p = reinterpret_cast<const char*>(bq), p.b.ld = blocks * 16, p.b.scales = bs, p.b.scale_ld = scale_ld;
     p.m = m, p.n = n, p.inner = blocks * 32, p.out = out, p.out_ld = n, p.out_f32 = out_dtype == NVFP4_IN_F32;
-    return run_sums<kMx, kAlong, kAlong, kSingle>(p, static_cast<float*>(c.take(0)), stream);
+    return run_sums<kMx>(p, static_cast<float*>(c.take(0)), stream);
 }
 
 int check_ws(const void* ws, size_t bytes, int64_t need) {

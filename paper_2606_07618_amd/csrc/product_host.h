@@ -58,28 +58,27 @@ struct TileCost { int m, n; float alone, among; };
 constexpr int kTiles = 4, kMostParts = 16;
 constexpr float kJoinUs = 5.0f, kJoinBytesUs = 4e6f;     // a second launch; bytes a microsecond
 
-// outputs of a tile: kPairOuter's are half its columns
-template <Kind KIND, Layout LB>
+template <Kind KIND>
 inline const TileCost* tile_costs() {
     static constexpr TileCost mx[kTiles] = {{256, 256, 1.9f, 2.4f}, {128, 128, 1.05f, 0.92f}, {64, 128, 0.75f, 0.60f}, {64, 64, 0.52f, 0.41f}};
-    static constexpr TileCost along[kTiles] = {{256, 256, 1.25f, 1.72f}, {128, 128, 0.83f, 0.54f}, {64, 128, 0.48f, 0.34f}, {64, 64, 0.40f, 0.25f}};
-    static constexpr TileCost across[kTiles] = {{256, 256, 1.5f, 2.0f}, {128, 128, 0.79f, 0.62f}, {64, 128, 0.66f, 0.40f}, {64, 64, 0.56f, 0.31f}};
-    return KIND == kMx ? mx : LB == kAlong ? along : across;
+    static constexpr TileCost bf16[kTiles] = {{256, 256, 1.25f, 1.72f}, {128, 128, 0.83f, 0.54f}, {64, 128, 0.48f, 0.34f}, {64, 64, 0.40f, 0.25f}};
+    return KIND == kMx ? mx : bf16;
 }
 
 struct Plan { int tile, parts; };
 
-template <Kind KIND, Layout LB, Pair PAIR>
-Plan plan_product(int64_t m, int64_t n, int64_t inner, bool split) {
-    constexpr int kStepValues = KIND == kMx ? 256 : 64, kHalf = PAIR == kPairOuter ? 2 : 1;
-    const int64_t steps = ceil_div(inner, kStepValues) * (PAIR == kPairInner ? 2 : 1);
-    const TileCost* costs = tile_costs<KIND, LB>();
+// A sum is split (kPartial, then joined); kGate's and kTwoRows' are not.
+template <Kind KIND, Out OUT>
+Plan plan_product(int64_t m, int64_t n, int64_t inner) {
+    constexpr int kStepValues = KIND == kMx ? 256 : 64, kHalf = OUT == kGate ? 2 : 1, kMost = OUT == kSums ? kMostParts : 1;
+    const int64_t steps = ceil_div(inner, kStepValues);
+    const TileCost* costs = tile_costs<KIND>();
     Plan best = {0, 1};
     float least = 3e38f;
     for (int t = 0; t < kTiles; ++t) {
-        if (PAIR == kPairOuter && costs[t].n < 128) continue;        // a wave holds both products of 32 columns
+        if (OUT == kGate && costs[t].n < 128) continue;        // a wave holds both products of 32 columns
         const float tiles = (float)ceil_div(m, costs[t].m) * (float)ceil_div(n * kHalf, costs[t].n);
-        for (int parts = 1; parts <= (split ? kMostParts : 1) && (parts == 1 || steps / parts >= 8); parts *= 2) {
+        for (int parts = 1; parts <= kMost && (parts == 1 || steps / parts >= 8); parts *= 2) {
             const float rounds = tiles * parts <= 256.0f ? 1.0f : (float)(int64_t)((tiles * parts + 255.0f) / 256.0f);
             const float step = rounds * costs[t].among > costs[t].alone ? rounds * costs[t].among : costs[t].alone;
             float us = (float)ceil_div(steps, parts) * step;
@@ -91,35 +90,35 @@ Plan plan_product(int64_t m, int64_t n, int64_t inner, bool split) {
 }
 
 // Bytes of the parts' sums, 0 where the product is not split.
-template <Kind KIND, Layout LB, Pair PAIR>
+template <Kind KIND>
 int64_t parts_bytes(int64_t m, int64_t n, int64_t inner) {
-    const Plan p = plan_product<KIND, LB, PAIR>(m, n, inner, true);
+    const Plan p = plan_product<KIND, kSums>(m, n, inner);
     return p.parts > 1 ? up(p.parts * m * n * 4, 256) : 0;
 }
 
 // Fills in the tiles and steps of p and launches; p's operands, outer indexes and outputs are set.
-template <Kind KIND, Layout LA, Layout LB, Pair PAIR, Out OUT, class T>
+template <Kind KIND, Out OUT, class T>
 int launch_tiles(Args p, hipStream_t stream) {
     constexpr int kStepValues = KIND == kMx ? 256 : 64;
-    p.steps = ceil_div(p.inner, kStepValues) * (PAIR == kPairInner ? 2 : 1);
+    p.steps = ceil_div(p.inner, kStepValues);
     p.tiles_m = ceil_div(p.m, T::M);
-    p.tiles_n = ceil_div(p.n, PAIR == kPairOuter ? T::N / 2 : T::N);
+    p.tiles_n = ceil_div(p.n, OUT == kGate ? T::N / 2 : T::N);
     p.split_steps = ceil_div(p.steps, p.parts);
     if (p.tiles_m > 0x7FFFFFFF || p.tiles_m * p.tiles_n > 0x7FFFFFFF / p.parts) return NVFP4_ERR_SHAPE;
     if (p.tiles_m * p.tiles_n == 0) return NVFP4_OK;
-    hipLaunchKernelGGL((product_kernel<KIND, LA, LB, PAIR, OUT, T>), dim3((unsigned)(p.tiles_m * p.tiles_n * p.parts)),
+    hipLaunchKernelGGL((product_kernel<KIND, OUT, T>), dim3((unsigned)(p.tiles_m * p.tiles_n * p.parts)),
                        dim3(T::kThreads), 0, stream, p);
     return launched();
 }
 
-template <Kind KIND, Layout LA, Layout LB, Pair PAIR, Out OUT>
+template <Kind KIND, Out OUT>
 int launch_product(const Args& p, int tile, hipStream_t stream) {
     switch (tile) {
-        case 0: return launch_tiles<KIND, LA, LB, PAIR, OUT, Tile<256, 256, 2, 4>>(p, stream);
-        case 1: return launch_tiles<KIND, LA, LB, PAIR, OUT, Tile<128, 128, 2, 2>>(p, stream);
-        case 2: return launch_tiles<KIND, LA, LB, PAIR, OUT, Tile<64, 128, 2, 2, 3>>(p, stream);
+        case 0: return launch_tiles<KIND, OUT, Tile<256, 256, 2, 4>>(p, stream);
+        case 1: return launch_tiles<KIND, OUT, Tile<128, 128, 2, 2>>(p, stream);
+        case 2: return launch_tiles<KIND, OUT, Tile<64, 128, 2, 2, 3>>(p, stream);
         default:
-            if constexpr (PAIR != kPairOuter) return launch_tiles<KIND, LA, LB, PAIR, OUT, Tile<64, 64, 2, 2, 4>>(p, stream);
+            if constexpr (OUT != kGate) return launch_tiles<KIND, OUT, Tile<64, 64, 2, 2, 4>>(p, stream);
             return NVFP4_ERR_SHAPE;                                  // no plan chooses it
     }
 }
@@ -128,14 +127,14 @@ int launch_product(const Args& p, int tile, hipStream_t stream) {
 int join_parts(const float* part, int parts, int64_t count, const float* scale, void* out, int f32, hipStream_t stream);
 
 // A product whose sums are stored: split where the plan says so, the parts' sums in `partial`.
-template <Kind KIND, Layout LA, Layout LB, Pair PAIR>
+template <Kind KIND>
 int run_sums(Args p, float* partial, hipStream_t stream) {
-    const Plan plan = plan_product<KIND, LB, PAIR>(p.m, p.n, p.inner, true);
+    const Plan plan = plan_product<KIND, kSums>(p.m, p.n, p.inner);
     p.parts = plan.parts;
-    if (plan.parts == 1) return launch_product<KIND, LA, LB, PAIR, kSums>(p, plan.tile, stream);
+    if (plan.parts == 1) return launch_product<KIND, kSums>(p, plan.tile, stream);
     void* out = p.out;
     p.out = partial;
-    if (const int rc = launch_product<KIND, LA, LB, PAIR, kPartial>(p, plan.tile, stream)) return rc;
+    if (const int rc = launch_product<KIND, kPartial>(p, plan.tile, stream)) return rc;
     return join_parts(partial, plan.parts, p.m * p.n, p.scale, out, p.out_f32, stream);
 }
 

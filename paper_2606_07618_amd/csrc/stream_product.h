@@ -16,15 +16,11 @@
 // Few weight rows: the contraction is split over workgroups as well, whose sums a second kernel adds in order.
 #pragma once
 
-#include "thin_product.h"
+#include "tile_product.h"
 
 namespace stream_product {
 
 using namespace tile_product;
-using thin_product::i32x2;
-using thin_product::load1;
-using thin_product::load16;
-using thin_product::load8;
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 

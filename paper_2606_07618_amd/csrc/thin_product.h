@@ -11,13 +11,10 @@
 namespace thin_product {
 
 using namespace tile_product;
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef int i32x2 __attribute__((ext_vector_type(2)));
-
 constexpr int kRows = 16;                        // of the activations, at most
 
-// What multiplies: bfloat16 weights (two matrices, gated), NVFP4 weights, or both sides microscaled.
-enum Weights { kGated, kNvfp4, kMicroscaled };
+// What multiplies: bfloat16 weights (two matrices, gated), or both sides microscaled.
+enum Weights { kGated, kMicroscaled };
 
 struct Args {
     const char *w, *w2;                          // [n, ldw bytes]
@@ -27,38 +24,12 @@ struct Args {
     const uint8_t* x_scales;
     int64_t ldx;
     int64_t n, k;                                // k: values
-    int m, shift;                                // shift: log2 of the NVFP4 block
-    const float* scale;
+    int m;
     void *out, *out2, *out3;
     int out_f32;
 };
 
-__device__ __forceinline__ i32x4 load16(__amdgpu_buffer_rsrc_t r, uint32_t at) {
-    return __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)at, 0, 0));
-}
-__device__ __forceinline__ i32x2 load8(__amdgpu_buffer_rsrc_t r, uint32_t at) {
-    return __builtin_bit_cast(i32x2, __builtin_amdgcn_raw_buffer_load_b64(r, (int)at, 0, 0));
-}
-__device__ __forceinline__ uint32_t load1(__amdgpu_buffer_rsrc_t r, uint32_t at) {
-    return (uint32_t)__builtin_amdgcn_raw_buffer_load_b8(r, (int)at, 0, 0);
-}
-
-__device__ __forceinline__ float e4m3_f32(uint32_t c) {
-    // the code's fields as those of a binary32 number 2^120 times too small; the product is exact
-    return __uint_as_float((c & 0x7Fu) << 20) * 0x1p120f;
-}
-
-// Eight E2M1 values times a binary32 scale with at most four significand bits, exact in bfloat16.
-__device__ __forceinline__ bf16x8 expand8(uint32_t n, float s) {
-    const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(n, 1.0f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(n, 1.0f, 1),
-                c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(n, 1.0f, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(n, 1.0f, 3);
-    const i32x4 v = {(int)pack_bf16(a[0] * s, a[1] * s), (int)pack_bf16(b[0] * s, b[1] * s),
-                     (int)pack_bf16(c[0] * s, c[1] * s), (int)pack_bf16(d[0] * s, d[1] * s)};
-    return __builtin_bit_cast(bf16x8, v);
-}
-
-// EVEN (NVFP4): k is a multiple of 32, so that a lane's 16 bytes are all inside or all outside.
-template <Weights W, int WAVES, int kUnroll, bool EVEN>
+template <Weights W, int WAVES, int kUnroll>
 __global__ __launch_bounds__(WAVES * kLanes) void thin_kernel(Args p) {
     constexpr int kAcc = W == kGated ? 2 : 1;
     __shared__ f32x4 sums[WAVES][kAcc][kLanes];
@@ -90,38 +61,6 @@ __global__ __launch_bounds__(WAVES * kLanes) void thin_kernel(Args p) {
                 const bf16x8 xv = __builtin_bit_cast(bf16x8, x[u]);
                 acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a[u]), xv, acc[0], 0, 0, 0);
                 acc[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, b[u]), xv, acc[1], 0, 0, 0);
-            }
-        }
-    } else if constexpr (W == kNvfp4) {
-        const __amdgpu_buffer_rsrc_t rs = window(p.w_scales + n0 * p.w_scale_ld);
-        const uint32_t s_row = (uint32_t)i * (uint32_t)p.w_scale_ld;
-        constexpr uint32_t kPiece = 128;
-        for (uint32_t at = (uint32_t)wave * kUnroll * kPiece; at < k; at += WAVES * kUnroll * kPiece) {
-            i32x4 a[kUnroll], x[kUnroll][4];
-            uint32_t s[kUnroll][2];
-#pragma unroll
-            for (int u = 0; u < kUnroll; ++u) {
-                const uint32_t v = at + u * kPiece + g * 32;   // this lane's 32 values
-                const bool in0 = row_in && v < k, in1 = EVEN ? in0 : row_in && v + 16 < k;
-                if constexpr (EVEN) {
-                    a[u] = load16(rw, in0 ? w_row + v / 2 : kOutside);
-                } else {
-                    const i32x2 lo = load8(rw, in0 ? w_row + v / 2 : kOutside), hi = load8(rw, in1 ? w_row + v / 2 + 8 : kOutside);
-                    a[u] = i32x4{lo[0], lo[1], hi[0], hi[1]};
-                }
-                s[u][0] = load1(rs, in0 ? s_row + (v >> p.shift) : kOutside);
-                s[u][1] = p.shift == 4 ? load1(rs, in1 ? s_row + (v >> 4) + 1 : kOutside) : s[u][0];
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    x[u][j] = load16(rx, m_in && v + j * 8 < k ? x_row + v * 2 + j * 16 : kOutside);
-            }
-#pragma unroll
-            for (int u = 0; u < kUnroll; ++u) {
-                const float s0 = e4m3_f32(s[u][0]), s1 = e4m3_f32(s[u][1]);
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(expand8((uint32_t)a[u][j], j < 2 ? s0 : s1),
-                                                                     __builtin_bit_cast(bf16x8, x[u][j]), acc[0], 0, 0, 0);
             }
         }
     } else {
@@ -173,13 +112,13 @@ __global__ __launch_bounds__(WAVES * kLanes) void thin_kernel(Args p) {
             store4(p.out3, 0, to, left, vec, v[1]);
         }
     } else {
-        store4(p.out, p.out_f32, to, left, vec, v[0] * (p.scale ? *p.scale : 1.0f));
+        store4(p.out, p.out_f32, to, left, vec, v[0]);
     }
 }
 
-template <Weights W, int WAVES, int kUnroll, bool EVEN>
+template <Weights W, int WAVES, int kUnroll>
 void launch_thin(const Args& p, hipStream_t stream) {
-    hipLaunchKernelGGL((thin_kernel<W, WAVES, kUnroll, EVEN>), dim3((unsigned)((p.n + 15) / 16)), dim3(WAVES * kLanes), 0, stream, p);
+    hipLaunchKernelGGL((thin_kernel<W, WAVES, kUnroll>), dim3((unsigned)((p.n + 15) / 16)), dim3(WAVES * kLanes), 0, stream, p);
 }
 
 }  // namespace thin_product

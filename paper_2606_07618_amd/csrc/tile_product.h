@@ -1,7 +1,9 @@
 // Tiled matrix product on the matrix cores of gfx950, D[m][n] = sum_k A[m][k] B[n][k], sums in
 // binary32, for bfloat16 operands and for microscaled FP4 ones (E2M1 nibbles with an E8M0 scale
-// for each 32 values of a row).  The kernels built from it differ in where their operands lie and
-// in what is done with the sums; both are template arguments.
+// for each 32 values of a row).  Both operands' rows hold the contraction; what is done with the sums is a
+// template argument.  (A contraction that runs down an operand's rows is turned before: with the matrix
+// turned inside the product, by transposing reads of LDS, a step took 1.5 us in place of 1.0, and a
+// gradient of [4096, 14336] x [14336, 4096] 438 us in place of 343 and 38 for the turning.)
 //
 // Both element types share one geometry: a step takes 128 bytes of every row of the tile (64
 // bfloat16 values, 256 FP4 ones), and a lane's operand of one matrix instruction is 16 of them (8
@@ -16,17 +18,16 @@
 
 namespace tile_product {
 
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef int i32x2 __attribute__((ext_vector_type(2)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 typedef __attribute__((address_space(3))) void lds_void;
-typedef __attribute__((address_space(3))) char lds_char;
 
 constexpr int kLanes = 64;
 constexpr int kStepBytes = 128;                  // of a row, a step of the contraction
@@ -38,25 +39,33 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t window(const void* base) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, (int)kOutside, 0x00020000);
 }
 
+// Loads at such offsets into registers.
+__device__ __forceinline__ i32x4 load16(__amdgpu_buffer_rsrc_t r, uint32_t at) {
+    return __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)at, 0, 0));
+}
+__device__ __forceinline__ i32x2 load8(__amdgpu_buffer_rsrc_t r, uint32_t at) {
+    return __builtin_bit_cast(i32x2, __builtin_amdgcn_raw_buffer_load_b64(r, (int)at, 0, 0));
+}
+__device__ __forceinline__ uint32_t load1(__amdgpu_buffer_rsrc_t r, uint32_t at) {
+    return (uint32_t)__builtin_amdgcn_raw_buffer_load_b8(r, (int)at, 0, 0);
+}
+
+__device__ __forceinline__ float e4m3_f32(uint32_t c) {
+    // the code's fields as those of a binary32 number 2^120 times too small; the product is exact
+    return __uint_as_float((c & 0x7Fu) << 20) * 0x1p120f;
+}
+
 template <int V> struct Const { static constexpr int value = V; };
 
 enum Kind { kBf16, kMx };
-// How an operand lies in memory: its rows hold the contraction (kAlong), or the contraction runs down
-// its rows and a row holds the operand's outer index (kAcross; bfloat16 only).
-enum Layout { kAlong, kAcross };
 
 struct Operand {
     const char* p;              // element (0, 0)
-    const char* p2;             // the second matrix of a pair (see Pair)
+    const char* p2;             // the second matrix (B of kGate)
     int64_t ld;                 // bytes from row to row
     const uint8_t* scales;      // microscaled: E8M0 codes [outer, scale_ld]
     int64_t scale_ld;
 };
-
-// Where operand B is two matrices.  kPairOuter: the tile's outer indexes are taken half from each, so
-// that both products of one output meet in one lane.  kPairInner: the contraction runs over the first,
-// then over the second.
-enum Pair { kSingle, kPairOuter, kPairInner };
 
 __device__ __forceinline__ float silu(float g) {
     // g / (1 + e^-g): e^-g overflows to infinity below -88, where the quotient's reciprocal is zero.
@@ -91,25 +100,17 @@ __device__ __forceinline__ TileIndex tile_of(int64_t id, int64_t count, int64_t 
 }
 
 // One operand's side of a tile: R outer indexes, staged by THREADS threads.
-template <Kind KIND, Layout LAYOUT, int R, int THREADS, bool HALF>
+template <int R, int THREADS, bool HALF>
 struct Side {
-    static_assert(LAYOUT == kAlong || KIND == kBf16, "microscaled operands lie along their rows");
     static constexpr int kBytes = R * kStepBytes;
     static constexpr int kLoads = kBytes / (THREADS * kChunk);
     static_assert(kBytes % (THREADS * kChunk) == 0, "whole loads");
-    static constexpr int kRowChunks = LAYOUT == kAlong ? kStepBytes / kChunk : R / 8;
-    // what a step takes of the contraction: bytes of a row, or rows
-    static constexpr int kFull = LAYOUT == kAlong ? kStepBytes : kStepBytes / 2;
+    static constexpr int kRowChunks = kStepBytes / kChunk;
 
     // LDS holds a step as rows of chunks.  A chunk's place in its row is exchanged by the row, so that
-    // the lanes of a read hit all banks: along, 16 lanes read one chunk of 16 rows, and the row's
-    // parity and the exchanged place cover the 256 bytes of the banks; across, 32 lanes read eight
-    // contraction rows by 32 bytes, and the place of a 32-byte unit is exchanged by those rows.
-    __device__ static __forceinline__ int exchange(int row) {
-        if constexpr (LAYOUT == kAlong) return (row >> 1) & 7;
-        constexpr int kUnits = R / 16 < 8 ? R / 16 : 8;
-        return (((row & 3) | (((row >> 3) & 1) << 2)) & (kUnits - 1)) << 1;
-    }
+    // the lanes of a read hit all banks: 16 lanes read one chunk of 16 rows, and the row's parity and the
+    // exchanged place cover the 256 bytes of the banks.
+    __device__ static __forceinline__ int exchange(int row) { return (row >> 1) & 7; }
 
     uint32_t offset[kLoads];             // of this thread's loads from the step's base
 
@@ -121,22 +122,21 @@ struct Side {
             const int id = i * THREADS + tid, row = id / kRowChunks;
             const int chunk = (id % kRowChunks) ^ exchange(row);
             const int r = HALF ? row % (R / 2) : row;
-            const bool in = LAYOUT == kAlong ? r < left : chunk * 8 < left;
-            offset[i] = in ? (uint32_t)r * (uint32_t)ld + chunk * kChunk : kOutside;
+            offset[i] = r < left ? (uint32_t)r * (uint32_t)ld + chunk * kChunk : kOutside;
         }
     }
 
-    // Starts the loads of one step into LDS.  ahead: what is left of the contraction from the step's
-    // first value on, in units of kFull; beyond it LDS gets zeros.
+    // Starts the loads of one step into LDS.  ahead: bytes of a row from the step's first one on; beyond
+    // them LDS gets zeros.
     __device__ __forceinline__ void load(const char* base, const char* base2, char* lds, int64_t ahead, int tid,
                                          int wave) const {
         const __amdgpu_buffer_rsrc_t w = window(base), w2 = HALF ? window(base2) : w;
-        const int left = ahead > kFull ? kFull : ahead > 0 ? (int)ahead : 0;
+        const int left = ahead > kStepBytes ? kStepBytes : ahead > 0 ? (int)ahead : 0;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const bool second = HALF && i * THREADS / kRowChunks >= R / 2;
             const int id = i * THREADS + tid, row = id / kRowChunks;
-            const int at = LAYOUT == kAlong ? ((id % kRowChunks) ^ exchange(row)) * kChunk : row;
+            const int at = ((id % kRowChunks) ^ exchange(row)) * kChunk;
             const uint32_t off = at < left ? offset[i] : kOutside;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(second ? w2 : w,
                                                      (lds_void*)(lds + (i * THREADS + wave * kLanes) * kChunk), kChunk,
@@ -148,20 +148,8 @@ struct Side {
     // bfloat16: values 32 H + 8 (lane / 16) on.  Microscaled: the 32-value block 4 H + lane / 16.
     template <int H>
     __device__ static __forceinline__ i32x4 read(const char* lds, int row0, int lane) {
-        const int g = lane / 16, i = lane % 16;
-        if constexpr (LAYOUT == kAlong) {
-            const int row = row0 + i, chunk = 4 * H + g;
-            return *reinterpret_cast<const i32x4*>(lds + row * kStepBytes + ((chunk ^ exchange(row)) * kChunk));
-        } else {
-            // ds_read_b64_tr_b16: 16 lanes read four rows of 16 values, four each, and get a column each
-            const int row = 32 * H + 8 * g + (i >> 2);
-            const int unit = (row0 / 16) ^ (exchange(row) >> 1);
-            const char* at = lds + row * (R * 2) + unit * 32 + (i & 3) * 8;
-            typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
-            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 4 * R * 2));
-            return __builtin_bit_cast(i32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-        }
+        const int row = row0 + lane % 16, chunk = 4 * H + lane / 16;
+        return *reinterpret_cast<const i32x4*>(lds + row * kStepBytes + ((chunk ^ exchange(row)) * kChunk));
     }
 };
 
@@ -178,21 +166,22 @@ struct Tile {
 enum Out {
     kSums,        // scale * sum, as bfloat16 or binary32
     kPartial,     // the sum of this part of the contraction, binary32, for a later reduction
-    kGate,        // silu(sum of the first matrix) * sum of the second, and both sums where asked for
+    kGate,        // B is two matrices: silu(sum of the first) * sum of the second, and both sums where asked for;
+                  // a tile's outer indexes of B are taken half from each, so that an output's two sums meet in one lane
     kTwoRows      // rows below `half_rows` to the first output, those from there on to the second
 };
 
 struct Args {
     Operand a, b;
-    int64_t m, n;               // outer indexes of A and of B (kPairOuter: of each of B's two)
-    int64_t inner;              // values of the contraction (kPairInner: of each of B's two)
+    int64_t m, n;               // outer indexes of A and of B (kGate: of each of B's two)
+    int64_t inner;              // values of the contraction
     int64_t steps, split_steps; // of the whole contraction, and of one part of it
     int64_t tiles_m, tiles_n;
     int parts;
     int out_f32;
     const float* scale;         // NULL: 1
     void *out, *out2, *out3;
-    int64_t half_rows, out_rows;   // kTwoRows
+    int64_t half_rows;          // kTwoRows
     int64_t out_ld;
 };
 
@@ -213,11 +202,11 @@ __device__ __forceinline__ void store4(void* out, int f32, int64_t at, int64_t l
     }
 }
 
-template <Kind KIND, Layout LA, Layout LB, Pair PAIR, Out OUT, class T>
+template <Kind KIND, Out OUT, class T>
 __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(Args p) {
-    constexpr bool HALF = PAIR == kPairOuter;
-    using A = Side<KIND, LA, T::M, T::kThreads, false>;
-    using B = Side<KIND, LB, T::N, T::kThreads, HALF>;
+    constexpr bool HALF = OUT == kGate;
+    using A = Side<T::M, T::kThreads, false>;
+    using B = Side<T::N, T::kThreads, HALF>;
     constexpr int kScales = KIND == kMx ? (T::M + T::N) * 8 : 0;           // eight bytes a row and step
     constexpr int kScaleLoads = (kScales + T::kThreads * 4 - 1) / (T::kThreads * 4);
     constexpr bool kEven = kScales % (T::kThreads * 4) == 0;               // else the last waves' last load is not one
@@ -258,22 +247,15 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
         scale_offset[i] = row < (of_a ? p.m - m0 : p.n - n0) ? (uint32_t)row * (uint32_t)(of_a ? p.a.scale_ld : p.b.scale_ld) + at : kOutside;
         scale_left[i] = (int)at;
     }
-    const char* a0 = p.a.p + (LA == kAlong ? m0 * p.a.ld : m0 * 2);
-    const int64_t b_at = LB == kAlong ? n0 * p.b.ld : n0 * 2;
-    const int64_t pair_steps = PAIR == kPairInner ? p.steps / 2 : p.steps;
+    const char* a0 = p.a.p + m0 * p.a.ld;
+    const int64_t b_at = n0 * p.b.ld, row_bytes = KIND == kMx ? p.inner / 2 : p.inner * 2;
     auto fetch_a = [&](int64_t s, int stage) {
-        const int64_t in = LA == kAlong ? (KIND == kMx ? p.inner / 2 : p.inner * 2) : p.inner;
-        // kPairInner: A's rows hold both contractions one after the other, each filled up with zeros
-        const int64_t ahead = PAIR == kPairInner ? (p.steps - s) * A::kFull : in - s * A::kFull;
-        sa.load(a0 + (LA == kAlong ? s * kStepBytes : s * A::kFull * p.a.ld), nullptr, lds[stage], ahead, tid, wave);
+        sa.load(a0 + s * kStepBytes, nullptr, lds[stage], row_bytes - s * kStepBytes, tid, wave);
     };
     auto fetch_b = [&](int64_t s, int stage) {
         char* l = lds[stage] + A::kBytes;
-        const int64_t in = LB == kAlong ? (KIND == kMx ? p.inner / 2 : p.inner * 2) : p.inner;
-        const bool second = PAIR == kPairInner && s >= pair_steps;
-        const int64_t at = second ? s - pair_steps : s;
-        const int64_t step = b_at + (LB == kAlong ? at * kStepBytes : at * B::kFull * p.b.ld);
-        sb.load((second ? p.b.p2 : p.b.p) + step, HALF ? p.b.p2 + step : nullptr, l, in - at * B::kFull, tid, wave);
+        const int64_t at = b_at + s * kStepBytes;
+        sb.load(p.b.p + at, HALF ? p.b.p2 + at : nullptr, l, row_bytes - s * kStepBytes, tid, wave);
         if constexpr (KIND == kMx) {
             const int64_t left = p.inner / 32 - s * 8;
             const __amdgpu_buffer_rsrc_t ra = window(p.a.scales + m0 * p.a.scale_ld + s * 8),
@@ -306,15 +288,10 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
     // multiplied a later one's fragment is read, and the one barrier of a step stands where its last fragments
     // have been read, so that its LDS is free for the step kSlots on.  That step's loads are started in two
     // parts, A's behind the barrier and B's in the next step, among the matrix instructions: in one burst
-    // they fill the queue that both waves of a SIMD then wait at ([4096, 14336] x [14336, 4096], contraction
-    // down the rows: 487 -> 449 us).  What a step waits for at its barrier are the loads of the next step, and
-    // no later ones.
-    // Down the rows a fragment of B is two reads: the barrier stands earlier there, and the next step's are read two a
-    // group behind it (450 -> 437 us in the same product; along the rows, where they are one each, 400 -> 410).
-    constexpr bool kSlowB = MF >= 8 && LB == kAcross;
-    constexpr int kLead = kSlowB ? (LA == kAcross ? 5 : 6) : MF >= 8 ? 3 : MF >= 4 ? 2 : 1;
-    constexpr int kRing = kLead > 3 ? 8 : 4, kGroups = 2 * MF, kBehind = kSlowB ? 2 : NF;
-    constexpr int kOneA = LA == kAcross ? 2 : 1, kOneB = LB == kAcross ? 2 : 1;     // LDS reads of a fragment
+    // they fill the queue that both waves of a SIMD then wait at.  What a step waits for at its barrier are the
+    // loads of the next step, and no later ones.
+    constexpr int kLead = MF >= 8 ? 3 : MF >= 4 ? 2 : 1;
+    constexpr int kRing = 4, kGroups = 2 * MF;
     i32x4 fa[kRing], fb[2][NF];
     int xa[MF], xb[NF], ya[2][MF], yb[2][NF];  // codes of this step, and the next one's words
     auto read_a = [&](auto gc, int stage) {    // the fragment of group g of a step
@@ -354,18 +331,14 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
         // the second half's fragments of B: one in each of the first groups, or what is left in the last that may
         constexpr bool more_b = g < NF && g < MF - 1;
         constexpr int b_to = g == MF - 2 ? NF : g + 1;
-        // the next step's first ones, kBehind a group from the barrier on
-        constexpr int b_next = (ahead - kGroups) * kBehind;
-        constexpr bool next_b = ahead >= kGroups && b_next < NF;
-        constexpr int kReads = kOneA + (more_b ? (b_to - g) * kOneB : 0) + (next_b ? kBehind * kOneB : 0) +
-                               (first && KIND == kMx ? (MF + NF) / 2 : 0);
+        constexpr int kReads = 1 + (more_b ? b_to - g : 0) + (first ? NF + (KIND == kMx ? (MF + NF) / 2 : 0) : 0);
         constexpr int kStarts = first ? A::kLoads : g == 0 ? B::kLoads : 0;
         if constexpr (first) {
             arrive<(kSlots - 2) * kLoads>();
             fetch_a(s + kSlots, slot);
             read_scales(next);
+            read_b(Const<0>{}, next, 0, NF);
         }
-        if constexpr (next_b) read_b(Const<0>{}, next, b_next, b_next + kBehind);
         read_a(Const<ahead % kGroups>{}, ahead < kGroups ? slot : next);
         if constexpr (more_b) read_b(Const<1>{}, slot, g, b_to);
         if constexpr (g == 0) if (s > s0) fetch_b(s - 1 + kSlots, slot == 0 ? kSlots - 1 : slot - 1);
@@ -402,8 +375,6 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
         read_a(Const<0>{}, 0);
         if constexpr (kLead > 1) read_a(Const<1>{}, 0);
         if constexpr (kLead > 2) read_a(Const<2>{}, 0);
-        if constexpr (kLead > 3) read_a(Const<3>{}, 0), read_a(Const<4>{}, 0);
-        if constexpr (kLead > 5) read_a(Const<5>{}, 0);
         int slot = 0;
         for (int64_t s = s0; s < s1; ++s) {
             const int next = slot + 1 == kSlots ? 0 : slot + 1;
@@ -451,8 +422,9 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
             for (int c = tid; c < T::M * kOutChunks; c += T::kThreads) {
                 const int row = c / kOutChunks, chunk = c % kOutChunks;
                 const int64_t m = m0 + row, n = n0 + chunk * 8;
-                uint16_t* to = m < p.m && n < p.n ? row_of(m) : nullptr;
-                if (to) *reinterpret_cast<uint4*>(to + n) = *reinterpret_cast<const uint4*>(tile + (row * kOutChunks + (chunk ^ (row & kMask))) * kChunk);
+                if (m < p.m && n < p.n)
+                    *reinterpret_cast<uint4*>(row_of(m) + n) =
+                        *reinterpret_cast<const uint4*>(tile + (row * kOutChunks + (chunk ^ (row & kMask))) * kChunk);
             }
         };
         auto rows_of = [&](void* out) { return [=](int64_t m) { return static_cast<uint16_t*>(out) + m * p.out_ld; }; };
@@ -460,9 +432,8 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
             write([&](int i, int j) { return acc[i][j] * scale; }, rows_of(p.out));
         } else if constexpr (OUT == kTwoRows) {
             write([&](int i, int j) { return acc[i][j]; }, [&](int64_t m) {
-                const int64_t row = m < p.half_rows ? m : m - p.half_rows;
-                void* out = m < p.half_rows ? p.out : p.out2;
-                return row < p.out_rows ? static_cast<uint16_t*>(out) + row * p.out_ld : nullptr;
+                return m < p.half_rows ? static_cast<uint16_t*>(p.out) + m * p.out_ld
+                                       : static_cast<uint16_t*>(p.out2) + (m - p.half_rows) * p.out_ld;
             });
         } else if constexpr (OUT == kGate) {
             constexpr int H = NF / 2;
@@ -493,9 +464,8 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
             } else if constexpr (OUT == kPartial) {
                 store4(p.out, 1, (part * p.m + m) * p.out_ld + n, left, vec, v);
             } else if constexpr (OUT == kTwoRows) {
-                const int64_t row = m < p.half_rows ? m : m - p.half_rows;
-                if (row < p.out_rows)
-                    store4(m < p.half_rows ? p.out : p.out2, 0, row * p.out_ld + n, left, vec, v);
+                const bool first = m < p.half_rows;
+                store4(first ? p.out : p.out2, 0, (first ? m : m - p.half_rows) * p.out_ld + n, left, vec, v);
             } else {
                 constexpr int H = HALF ? NF / 2 : 0;
                 const f32x4 u = acc[i][H + j];
