@@ -12,22 +12,12 @@ namespace {
 
 constexpr int kPackThreads = 256;
 
-template <typename V>
-__global__ __launch_bounds__(kPackThreads) void pack_kernel(const V* __restrict__ src, int64_t count, int64_t width,
-                                                            int64_t ld, V* __restrict__ dst, int64_t dst_ld) {
+__global__ __launch_bounds__(kPackThreads) void pack_kernel(const uint16_t* __restrict__ src, int64_t count, int64_t width,
+                                                            int64_t ld, uint16_t* __restrict__ dst, int64_t dst_ld) {
     for (int64_t i = (int64_t)blockIdx.x * kPackThreads + threadIdx.x; i < count; i += (int64_t)gridDim.x * kPackThreads) {
         const int64_t r = i / dst_ld, c = i % dst_ld;
-        dst[i] = c < width ? src[r * ld + c] : V(0);
+        dst[i] = c < width ? src[r * ld + c] : (uint16_t)0;
     }
-}
-
-template <typename V>
-int pack(const V* src, int64_t rows, int64_t width, int64_t ld, V* dst, int64_t dst_ld, hipStream_t stream) {
-    const int64_t count = rows * dst_ld, groups = ceil_div(count, kPackThreads);
-    if (count == 0) return NVFP4_OK;
-    hipLaunchKernelGGL((pack_kernel<V>), dim3((unsigned)(groups < 8192 ? groups : 8192)), dim3(kPackThreads), 0, stream,
-                       src, count, width, ld, dst, dst_ld);
-    return launched();
 }
 
 // Sums of parts of the contraction.
@@ -58,11 +48,11 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(const float* __restr
 }  // namespace
 
 int pack_bf16_rows(const void* src, int64_t rows, int64_t width, int64_t ld, void* dst, hipStream_t stream) {
-    return pack(static_cast<const uint16_t*>(src), rows, width, ld, static_cast<uint16_t*>(dst), packed_ld(width), stream);
-}
-
-int pack_scale_rows(const uint8_t* src, int64_t rows, int64_t width, uint8_t* dst, int64_t dst_ld, hipStream_t stream) {
-    return pack(src, rows, width, width, dst, dst_ld, stream);
+    const int64_t count = rows * packed_ld(width), groups = ceil_div(count, kPackThreads);
+    if (count == 0) return NVFP4_OK;
+    hipLaunchKernelGGL(pack_kernel, dim3((unsigned)(groups < 8192 ? groups : 8192)), dim3(kPackThreads), 0, stream,
+                       static_cast<const uint16_t*>(src), count, width, ld, static_cast<uint16_t*>(dst), packed_ld(width));
+    return launched();
 }
 
 int join_parts(const float* part, int parts, int64_t count, const float* scale, void* out, int f32, hipStream_t stream) {
@@ -281,14 +271,67 @@ int run_grad(const void* dy, int64_t ld, const uint8_t* q, const uint8_t* scales
 
 // ---- y = A B^T, both microscaled --------------------------------------------------------------
 
-// The tiles read a row's scales four at a time: rows of another width are copied to one of eights.
-int64_t mx_workspace(int64_t m, int64_t n, int64_t blocks) {
-    Carver c{nullptr};
-    if (blocks % 4 && m > thin_product::kRows) {
-        c.take(m * up(blocks, 8));
-        c.take(n * up(blocks, 8));
+constexpr int kScaleThreads = 256;
+
+struct Scales { const uint8_t* from; uint8_t* to; int64_t rows, groups; int fragments; };
+
+// Both operands' scales as scale_at() lays them out, zeros outside.  A thread takes a step's eight codes of the F rows
+// r, 16 + r, .. of a group, and writes them to four lanes.  WORDS: rows are whole words.
+template <bool WORDS>
+__global__ __launch_bounds__(kScaleThreads) void lay_scales_kernel(Scales a, Scales b, int64_t blocks, int64_t steps) {
+    const uint32_t pieces = ((uint32_t)steps * 16 + kScaleThreads - 1) / kScaleThreads;   // of a group's steps
+    const uint32_t at = blockIdx.x % pieces * kScaleThreads + threadIdx.x, of = blockIdx.x / pieces;
+    const Scales p = of < a.groups ? a : b;
+    const int64_t group = of < a.groups ? of : of - a.groups;
+    const int r = (int)(at % 16);
+    const int64_t step = at / 16;
+    if (step >= steps) return;
+    const int64_t row0 = group * p.fragments * 16;
+    const __amdgpu_buffer_rsrc_t from = window(p.from + row0 * blocks);
+    uint32_t code[8][2];                         // of blocks 0 .. 3 and 4 .. 7 of the step
+#pragma unroll
+    for (int f = 0; f < 8; ++f) {
+        const int64_t left = f < p.fragments && row0 + f * 16 + r < p.rows ? blocks - step * 8 : 0;
+        const uint32_t offset = (uint32_t)(f * 16 + r) * (uint32_t)blocks + (uint32_t)step * 8;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if constexpr (WORDS) {
+                code[f][h] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(from, (int)(h * 4 < left ? offset + h * 4 : kOutside), 0, 0);
+            } else {
+                code[f][h] = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) code[f][h] |= load1(from, h * 4 + i < left ? offset + h * 4 + i : kOutside) << i * 8;
+            }
+        }
     }
-    return c.at + (m > thin_product::kRows ? parts_bytes<kMx>(m, n, blocks * 32) : 0);
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        uint32_t* to = reinterpret_cast<uint32_t*>(p.to + scale_at(group, steps, step, g * 16 + r, p.fragments));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t pick = 0x0C0C0400u + g * 0x0101u;
+            if (i < p.fragments / 2)
+                to[i] = __builtin_amdgcn_perm(code[2 * i][1], code[2 * i][0], pick) |
+                        __builtin_amdgcn_perm(code[2 * i + 1][1], code[2 * i + 1][0], pick) << 16;
+        }
+    }
+}
+
+int64_t scale_bytes(int64_t rows, int64_t blocks) { return up(rows, 128) * ceil_div(blocks, 8) * 8; }
+
+// The largest tile takes its scales laid out, and so do the others where rows of scales are no whole words.
+bool lays_scales(int64_t m, int64_t n, int64_t blocks) {
+    return blocks % 4 != 0 || plan_product<kMx, kSums>(m, n, blocks * 32).tile == 0;
+}
+
+int64_t mx_workspace(int64_t m, int64_t n, int64_t blocks) {
+    if (m <= thin_product::kRows) return 0;
+    Carver c{nullptr};
+    if (lays_scales(m, n, blocks)) {
+        c.take(scale_bytes(m, blocks));
+        c.take(scale_bytes(n, blocks));
+    }
+    return c.at + parts_bytes<kMx>(m, n, blocks * 32);
 }
 
 int run_mx(const uint8_t* aq, const uint8_t* as, const uint8_t* bq, const uint8_t* bs, int64_t m, int64_t n,
@@ -301,21 +344,26 @@ int run_mx(const uint8_t* aq, const uint8_t* as, const uint8_t* bq, const uint8_
         thin_product::launch_thin<thin_product::kMicroscaled, 8, 4>(t, stream);
         return launched();
     }
-    int64_t scale_ld = blocks;
     Carver c{static_cast<char*>(ws)};
-    if (blocks % 4) {
-        scale_ld = up(blocks, 8);
-        uint8_t* pa = static_cast<uint8_t*>(c.take(m * scale_ld));
-        uint8_t* pb = static_cast<uint8_t*>(c.take(n * scale_ld));
-        if (const int rc = pack_scale_rows(as, m, blocks, pa, scale_ld, stream)) return rc;
-        if (const int rc = pack_scale_rows(bs, n, blocks, pb, scale_ld, stream)) return rc;
-        as = pa, bs = pb;
-    }
     Args p = {};
-    p.a.p = reinterpret_cast<const char*>(aq), p.a.ld = blocks * 16, p.a.scales = as, p.a.scale_ld = scale_ld;
-    p.b.p = reinterpret_cast<const char*>(bq), p.b.ld = blocks * 16, p.b.scales = bs, p.b.scale_ld = scale_ld;
+    p.a.p = reinterpret_cast<const char*>(aq), p.a.ld = blocks * 16, p.a.scales = as, p.a.scale_ld = blocks;
+    p.b.p = reinterpret_cast<const char*>(bq), p.b.ld = blocks * 16, p.b.scales = bs, p.b.scale_ld = blocks;
     p.m = m, p.n = n, p.inner = blocks * 32, p.out = out, p.out_ld = n, p.out_f32 = out_dtype == NVFP4_IN_F32;
-    return run_sums<kMx>(p, static_cast<float*>(c.take(0)), stream);
+    if (!lays_scales(m, n, blocks)) return run_sums<kMx>(p, static_cast<float*>(c.take(0)), stream);
+    const int* fragments = kFragments[plan_product<kMx, kSums>(m, n, blocks * 32).tile];
+    const int64_t steps = ceil_div(blocks, 8);
+    const auto scales = [&](const uint8_t* from, int64_t rows, int f) {
+        return Scales{from, static_cast<uint8_t*>(c.take(scale_bytes(rows, blocks))), rows, ceil_div(rows, 16 * f), f};
+    };
+    const Scales a = scales(as, m, fragments[0]), b = scales(bs, n, fragments[1]);
+    const int64_t groups = (a.groups + b.groups) * ceil_div(steps * 16, kScaleThreads);
+    if (groups > 0x7FFFFFFF) return NVFP4_ERR_SHAPE;
+    if (groups > 0) {
+        hipLaunchKernelGGL((blocks % 4 == 0 ? lay_scales_kernel<true> : lay_scales_kernel<false>), dim3((unsigned)groups), dim3(kScaleThreads), 0, stream, a, b, blocks, steps);
+        if (const int rc = launched()) return rc;
+    }
+    p.a.scales = a.to, p.b.scales = b.to;
+    return run_sums<kMxLaid>(p, static_cast<float*>(c.take(0)), stream);
 }
 
 int check_ws(const void* ws, size_t bytes, int64_t need) {

@@ -45,7 +45,6 @@ struct Carver {
 };
 
 int pack_bf16_rows(const void* src, int64_t rows, int64_t width, int64_t ld, void* dst, hipStream_t stream);
-int pack_scale_rows(const uint8_t* src, int64_t rows, int64_t width, uint8_t* dst, int64_t dst_ld, hipStream_t stream);
 
 // ---- the tile and the split of a product --------------------------------------------------------
 // Four tiles, from the one that moves least through LDS for what it computes to the one that gives the most
@@ -62,15 +61,18 @@ template <Kind KIND>
 inline const TileCost* tile_costs() {
     static constexpr TileCost mx[kTiles] = {{256, 256, 1.9f, 2.4f}, {128, 128, 1.05f, 0.92f}, {64, 128, 0.75f, 0.60f}, {64, 64, 0.52f, 0.41f}};
     static constexpr TileCost bf16[kTiles] = {{256, 256, 1.25f, 1.72f}, {128, 128, 0.83f, 0.54f}, {64, 128, 0.48f, 0.34f}, {64, 64, 0.40f, 0.25f}};
-    return KIND == kMx ? mx : bf16;
+    return KIND != kBf16 ? mx : bf16;
 }
+
+// Fragments of a wave's rows of A and of B.
+constexpr int kFragments[kTiles][2] = {{8, 4}, {4, 4}, {2, 4}, {2, 2}};
 
 struct Plan { int tile, parts; };
 
 // A sum is split (kPartial, then joined); kGate's and kTwoRows' are not.
 template <Kind KIND, Out OUT>
 Plan plan_product(int64_t m, int64_t n, int64_t inner) {
-    constexpr int kStepValues = KIND == kMx ? 256 : 64, kHalf = OUT == kGate ? 2 : 1, kMost = OUT == kSums ? kMostParts : 1;
+    constexpr int kStepValues = KIND != kBf16 ? 256 : 64, kHalf = OUT == kGate ? 2 : 1, kMost = OUT == kSums ? kMostParts : 1;
     const int64_t steps = ceil_div(inner, kStepValues);
     const TileCost* costs = tile_costs<KIND>();
     Plan best = {0, 1};
@@ -99,7 +101,7 @@ int64_t parts_bytes(int64_t m, int64_t n, int64_t inner) {
 // Fills in the tiles and steps of p and launches; p's operands, outer indexes and outputs are set.
 template <Kind KIND, Out OUT, class T>
 int launch_tiles(Args p, hipStream_t stream) {
-    constexpr int kStepValues = KIND == kMx ? 256 : 64;
+    constexpr int kStepValues = KIND != kBf16 ? 256 : 64;
     p.steps = ceil_div(p.inner, kStepValues);
     p.tiles_m = ceil_div(p.m, T::M);
     p.tiles_n = ceil_div(p.n, OUT == kGate ? T::N / 2 : T::N);
@@ -111,15 +113,25 @@ int launch_tiles(Args p, hipStream_t stream) {
     return launched();
 }
 
+using Tile0 = Tile<256, 256, 2, 4>;
+using Tile1 = Tile<128, 128, 2, 2>;
+using Tile2 = Tile<64, 128, 2, 2, 3>;
+using Tile3 = Tile<64, 64, 2, 2, 4>;
+template <class T, int I>
+constexpr bool kAgrees = T::MF == kFragments[I][0] && T::NF == kFragments[I][1];
+static_assert(kAgrees<Tile0, 0> && kAgrees<Tile1, 1> && kAgrees<Tile2, 2> && kAgrees<Tile3, 3>, "the scales' layout");
+
 template <Kind KIND, Out OUT>
 int launch_product(const Args& p, int tile, hipStream_t stream) {
     switch (tile) {
-        case 0: return launch_tiles<KIND, OUT, Tile<256, 256, 2, 4>>(p, stream);
-        case 1: return launch_tiles<KIND, OUT, Tile<128, 128, 2, 2>>(p, stream);
-        case 2: return launch_tiles<KIND, OUT, Tile<64, 128, 2, 2, 3>>(p, stream);
+        case 0:
+            if constexpr (KIND != kMx) return launch_tiles<KIND, OUT, Tile0>(p, stream);
+            return NVFP4_ERR_SHAPE;                                  // takes its scales laid out
+        case 1: return launch_tiles<KIND, OUT, Tile1>(p, stream);
+        case 2: return launch_tiles<KIND, OUT, Tile2>(p, stream);
         default:
-            if constexpr (OUT != kGate) return launch_tiles<KIND, OUT, Tile<64, 64, 2, 2, 4>>(p, stream);
-            return NVFP4_ERR_SHAPE;                                  // no plan chooses it
+            if constexpr (OUT != kGate) return launch_tiles<KIND, OUT, Tile3>(p, stream);
+            return NVFP4_ERR_SHAPE;                                  // kGate has no plan with it
     }
 }
 

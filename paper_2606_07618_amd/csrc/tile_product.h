@@ -57,14 +57,15 @@ __device__ __forceinline__ float e4m3_f32(uint32_t c) {
 
 template <int V> struct Const { static constexpr int value = V; };
 
-enum Kind { kBf16, kMx };
+// Microscaled operands' scales as the rows lie (kMx, rows of whole words), or laid out by scale_at() (kMxLaid).
+enum Kind { kBf16, kMx, kMxLaid };
 
 struct Operand {
     const char* p;              // element (0, 0)
     const char* p2;             // the second matrix (B of kGate)
     int64_t ld;                 // bytes from row to row
-    const uint8_t* scales;      // microscaled: E8M0 codes [outer, scale_ld]
-    int64_t scale_ld;
+    const uint8_t* scales;      // microscaled: E8M0 codes
+    int64_t scale_ld;           // kMx: bytes from row to row
 };
 
 __device__ __forceinline__ float silu(float g) {
@@ -76,6 +77,16 @@ __device__ __forceinline__ float silu(float g) {
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
     bf16x2 v = {(__bf16)a, (__bf16)b};
     return __builtin_bit_cast(uint32_t, v);
+}
+
+// E8M0 codes in the order in which lanes take them: for the 16 F rows of a wave's fragments and for a step, each lane's
+// codes of its F fragments, two neighbouring bytes a fragment (blocks lane / 16 and 4 + lane / 16 of the step), so that
+// an instruction picks its byte from a word as it was read.  As the rows lie, a step takes eight bytes of each row's
+// scales, whose lines, fetched again for each step, are as many bytes as the values themselves: with a chip full of
+// the largest tiles this costs more than laying the scales out ([8192, 4096] x [14336, 4096]: 313 us as they lie,
+// 275 laid out, 7 of them for that; [64, 4096] x [14336, 4096]: 14.5 and 16).
+__device__ __forceinline__ int64_t scale_at(int64_t group, int64_t steps, int64_t step, int lane, int fragments) {
+    return ((group * steps + step) * kLanes + lane) * fragments * 2;
 }
 
 // All but this wave's last LEFT loads into LDS have arrived and its reads of LDS are done, then all waves'.
@@ -207,7 +218,8 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
     constexpr bool HALF = OUT == kGate;
     using A = Side<T::M, T::kThreads, false>;
     using B = Side<T::N, T::kThreads, HALF>;
-    constexpr int kScales = KIND == kMx ? (T::M + T::N) * 8 : 0;           // eight bytes a row and step
+    constexpr bool kScaled = KIND != kBf16, kLaid = KIND == kMxLaid;
+    constexpr int kScales = kScaled ? (T::M + T::N) * 8 : 0;           // eight bytes a row and step
     constexpr int kScaleLoads = (kScales + T::kThreads * 4 - 1) / (T::kThreads * 4);
     constexpr bool kEven = kScales % (T::kThreads * 4) == 0;               // else the last waves' last load is not one
     constexpr int kStage = A::kBytes + B::kBytes + kScales;
@@ -231,24 +243,28 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
     B sb;
     sa.init(p.m - m0, p.a.ld, tid);
     sb.init(p.n - n0, p.b.ld, tid);
-    // Scales: a word holds a half's four codes of a row.  LDS holds them wave by wave, A's then B's, by row
-    // in the fragment, half, fragment, so that a lane reads the words of all its wave's fragments at once.
+    // Scales: LDS holds a step's wave by wave, A's then B's.  Laid out, as they lie in memory; else a word holds a half's
+    // four codes of a row, by row in the fragment, half, fragment, so that a lane reads its fragments' words at once.
     uint32_t scale_offset[kScaleLoads + 1];
-    int scale_left[kScaleLoads + 1];               // bytes of the step ahead of the word
+    int scale_left[kScaleLoads + 1];               // kMx: bytes of the step ahead of the word
 #pragma unroll
     for (int i = 0; i < kScaleLoads; ++i) {
         int word = i * T::kThreads + tid;
         const bool of_a = word < T::M * 2;
-        const int frags = of_a ? MF : NF;
         word -= of_a ? 0 : T::M * 2;
-        const int w = word / (32 * frags), in = word % (32 * frags), f = in % frags;
-        const int row = (of_a ? w * (T::M / T::WM) + f * 16 : w * (T::N / T::WN) + f * 16) + in / (2 * frags);
-        const uint32_t at = (uint32_t)(in / frags % 2) * 4;
-        scale_offset[i] = row < (of_a ? p.m - m0 : p.n - n0) ? (uint32_t)row * (uint32_t)(of_a ? p.a.scale_ld : p.b.scale_ld) + at : kOutside;
-        scale_left[i] = (int)at;
+        const int fragments = of_a ? MF : NF, group = word / (32 * fragments), in = word % (32 * fragments);
+        const int64_t left = of_a ? p.m - m0 : p.n - n0;
+        if constexpr (kLaid) {
+            scale_offset[i] = group * 16 * fragments < left ? (uint32_t)scale_at(group, p.steps, 0, 0, fragments) + in * 4 : kOutside;
+            scale_left[i] = 0;
+        } else {
+            const int row = (group * fragments + in % fragments) * 16 + in / (2 * fragments);
+            scale_left[i] = in / fragments % 2 * 4;
+            scale_offset[i] = row < left ? (uint32_t)row * (uint32_t)(of_a ? p.a.scale_ld : p.b.scale_ld) + scale_left[i] : kOutside;
+        }
     }
     const char* a0 = p.a.p + m0 * p.a.ld;
-    const int64_t b_at = n0 * p.b.ld, row_bytes = KIND == kMx ? p.inner / 2 : p.inner * 2;
+    const int64_t b_at = n0 * p.b.ld, row_bytes = kScaled ? p.inner / 2 : p.inner * 2;
     auto fetch_a = [&](int64_t s, int stage) {
         sa.load(a0 + s * kStepBytes, nullptr, lds[stage], row_bytes - s * kStepBytes, tid, wave);
     };
@@ -256,10 +272,11 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
         char* l = lds[stage] + A::kBytes;
         const int64_t at = b_at + s * kStepBytes;
         sb.load(p.b.p + at, HALF ? p.b.p2 + at : nullptr, l, row_bytes - s * kStepBytes, tid, wave);
-        if constexpr (KIND == kMx) {
+        if constexpr (kScaled) {
             const int64_t left = p.inner / 32 - s * 8;
-            const __amdgpu_buffer_rsrc_t ra = window(p.a.scales + m0 * p.a.scale_ld + s * 8),
-                                         rb = window(p.b.scales + n0 * p.b.scale_ld + s * 8);
+            const __amdgpu_buffer_rsrc_t
+                ra = window(p.a.scales + (kLaid ? scale_at(m0 / (16 * MF), p.steps, s, 0, MF) : m0 * p.a.scale_ld + s * 8)),
+                rb = window(p.b.scales + (kLaid ? scale_at(n0 / (16 * NF), p.steps, s, 0, NF) : n0 * p.b.scale_ld + s * 8));
 #pragma unroll
             for (int i = 0; i < kScaleLoads; ++i) {
                 const int first = i * T::kThreads + wave * kLanes;
@@ -293,7 +310,10 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
     constexpr int kLead = MF >= 8 ? 3 : MF >= 4 ? 2 : 1;
     constexpr int kRing = 4, kGroups = 2 * MF;
     i32x4 fa[kRing], fb[2][NF];
-    int xa[MF], xb[NF], ya[2][MF], yb[2][NF];  // codes of this step, and the next one's words
+    // Codes of this step and the next step's words.  Laid out, a word is two fragments' codes of both halves; else a
+    // half's of one fragment, and a lane picks its own.
+    constexpr int kPer = kLaid ? 2 : 1, kHalves = kLaid ? 1 : 2;
+    int xa[MF / kPer], xb[NF / kPer], ya[kHalves][MF / kPer], yb[kHalves][NF / kPer];
     auto read_a = [&](auto gc, int stage) {    // the fragment of group g of a step
         constexpr int g = decltype(gc)::value;
         fa[g % kRing] = A::template read<g / MF>(lds[stage], a_row(g % MF), lane);
@@ -304,25 +324,26 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
         for (int j = from; j < to; ++j) fb[H][j] = B::template read<H>(lds[stage] + A::kBytes, b_row(j), lane);
     };
     auto read_scales = [&](int stage) {
-        if constexpr (KIND == kMx) {
+        if constexpr (kScaled) {
             const int* la = reinterpret_cast<const int*>(lds[stage] + A::kBytes + B::kBytes);
+            const int at = kLaid ? lane : lane % 16 * 2, per = kLaid ? kLanes : 32;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+            for (int h = 0; h < kHalves; ++h) {
 #pragma unroll
-                for (int i = 0; i < MF; ++i) ya[h][i] = la[((wm * 16 + lane % 16) * 2 + h) * MF + i];
+                for (int i = 0; i < MF / kPer; ++i) ya[h][i] = la[(wm * per + at + h) * (MF / kPer) + i];
 #pragma unroll
-                for (int j = 0; j < NF; ++j) yb[h][j] = la[T::M * 2 + ((wn * 16 + lane % 16) * 2 + h) * NF + j];
+                for (int j = 0; j < NF / kPer; ++j) yb[h][j] = la[T::M * 2 + (wn * per + at + h) * (NF / kPer) + j];
             }
         }
     };
     auto next_scales = [&]() {
-        if constexpr (KIND == kMx) {
-            // this lane's code of the first half, then of the second
-            const uint32_t pick = 0x0C0C0400u + (uint32_t)(lane / 16) * 0x0101u;
+        if constexpr (kScaled) {
+            const uint32_t pick = 0x0C0C0400u + (uint32_t)(lane / 16) * 0x0101u;   // this lane's code of either half
+            auto codes = [&](int first, int second) { return kLaid ? first : (int)__builtin_amdgcn_perm((uint32_t)second, (uint32_t)first, pick); };
 #pragma unroll
-            for (int i = 0; i < MF; ++i) xa[i] = (int)__builtin_amdgcn_perm((uint32_t)ya[1][i], (uint32_t)ya[0][i], pick);
+            for (int i = 0; i < MF / kPer; ++i) xa[i] = codes(ya[0][i], ya[kHalves - 1][i]);
 #pragma unroll
-            for (int j = 0; j < NF; ++j) xb[j] = (int)__builtin_amdgcn_perm((uint32_t)yb[1][j], (uint32_t)yb[0][j], pick);
+            for (int j = 0; j < NF / kPer; ++j) xb[j] = codes(yb[0][j], yb[kHalves - 1][j]);
         }
     };
     auto group = [&](int64_t s, int slot, int next, auto gc) {
@@ -331,7 +352,7 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
         // the second half's fragments of B: one in each of the first groups, or what is left in the last that may
         constexpr bool more_b = g < NF && g < MF - 1;
         constexpr int b_to = g == MF - 2 ? NF : g + 1;
-        constexpr int kReads = 1 + (more_b ? b_to - g : 0) + (first ? NF + (KIND == kMx ? (MF + NF) / 2 : 0) : 0);
+        constexpr int kReads = 1 + (more_b ? b_to - g : 0) + (first ? NF + (kLaid ? 2 : kScaled ? (MF + NF) / 2 : 0) : 0);
         constexpr int kStarts = first ? A::kLoads : g == 0 ? B::kLoads : 0;
         if constexpr (first) {
             arrive<(kSlots - 2) * kLoads>();
@@ -346,12 +367,14 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
         for (int j = 0; j < NF; ++j) {
             // B's values as the instruction's rows: a lane gets four neighbouring outputs of a row of D
             const i32x4 b = fb[H][j], a = fa[g % kRing];
-            if constexpr (KIND == kBf16) {
+            if constexpr (!kScaled) {
                 acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, b), __builtin_bit_cast(bf16x8, a),
                                                                     acc[i][j], 0, 0, 0);
             } else {
                 const i32x8 wb = {b[0], b[1], b[2], b[3], 0, 0, 0, 0}, wa = {a[0], a[1], a[2], a[3], 0, 0, 0, 0};
-                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wb, wa, acc[i][j], 4, 4, H, xb[j], H, xa[i]);
+                constexpr int kOdd = kLaid ? 2 : 0, kCode = i % 2 * kOdd + H;
+                acc[i][j] = j % 2 ? __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wb, wa, acc[i][j], 4, 4, kOdd + H, xb[j / kPer], kCode, xa[i / kPer])
+                                  : __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wb, wa, acc[i][j], 4, 4, H, xb[j / kPer], kCode, xa[i / kPer]);
             }
         }
         // the order of a group: its LDS reads and its loads among its matrix instructions
