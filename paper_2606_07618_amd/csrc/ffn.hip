@@ -4,7 +4,6 @@
 //   dx = dg Wg + du Wu,  dWg = dg^T x,  dWu = du^T x.
 #include "dot_product.h"
 #include "product_host.h"
-#include "thin_product.h"
 
 namespace {
 
@@ -155,14 +154,40 @@ int packed(Carver& c, Rows& r, int64_t rows, int64_t width, bool pack, hipStream
     return NVFP4_OK;
 }
 
-int64_t pack_workspace(int64_t m, int64_t n, int64_t k, int64_t ldx, int64_t ldw) {
+// h, and both pre-activations where asked for, from the sums of parts of the contraction, added in order.
+template <bool VEC>
+__global__ __launch_bounds__(kEdgeThreads) void join_gate_kernel(const float* __restrict__ part, int parts, int64_t count,
+                                                                 void* __restrict__ h, void* __restrict__ gate,
+                                                                 void* __restrict__ up_) {
+    constexpr int kPer = VEC ? 4 : 1;
+    const int64_t at = ((int64_t)blockIdx.x * kEdgeThreads + threadIdx.x) * kPer;
+    if (at >= count) return;
+    f32x4 v[2] = {};
+    for (int p = 0; p < parts; ++p)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const float* from = part + (p * 2 + b) * count + at;
+            if constexpr (VEC) v[b] += *reinterpret_cast<const f32x4*>(from);
+            else v[b][0] += *from;
+        }
+    f32x4 out;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) out[e] = silu(v[0][e]) * v[1][e];
+    store4(h, 0, at, kPer, VEC, out);
+    if (gate) {
+        store4(gate, 0, at, kPer, VEC, v[0]);
+        store4(up_, 0, at, kPer, VEC, v[1]);
+    }
+}
+
+int64_t forward_workspace(int64_t m, int64_t n, int64_t k, int64_t ldx, int64_t ldw) {
     Carver c{nullptr};
     if (needs_pack(k, ldx)) c.take(m * packed_ld(k) * 2);
     if (needs_pack(k, ldw)) {
         c.take(n * packed_ld(k) * 2);
         c.take(n * packed_ld(k) * 2);
     }
-    return c.at;
+    return c.at + (m > dot_product::kMostRows ? parts_bytes<kBf16, kGate>(m, n, k) : 0);
 }
 
 // Sections of the backward pass's workspace: d, and what each product reads besides.
@@ -199,7 +224,7 @@ extern "C" {
 
 int64_t nvfp4_swiglu_ffn_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t ldx, int64_t ldw) {
     if (const int rc = check_call(m, n, k, ldx, ldw)) return rc;
-    return pack_workspace(m, n, k, ldx, ldw);
+    return forward_workspace(m, n, k, ldx, ldw);
 }
 
 int nvfp4_swiglu_ffn(const void* x, int64_t ldx, const void* w_gate, const void* w_up, int64_t ldw, int64_t m,
@@ -211,7 +236,7 @@ int nvfp4_swiglu_ffn(const void* x, int64_t ldx, const void* w_gate, const void*
     if (!aligned(x, 16) || !aligned(w_gate, 16) || !aligned(w_up, 16) || !aligned(h, 16) || !aligned(gate, 16) ||
         !aligned(up_out, 16))
         return NVFP4_ERR_ALIGN;
-    if (const int rc = check_ws(workspace, workspace_bytes, pack_workspace(m, n, k, ldx, ldw))) return rc;
+    if (const int rc = check_ws(workspace, workspace_bytes, forward_workspace(m, n, k, ldx, ldw))) return rc;
     hipStream_t st = (hipStream_t)stream;
     Carver c{static_cast<char*>(workspace)};
     Rows rx{x, ldx}, rg{w_gate, ldw}, ru{w_up, ldw};
@@ -233,20 +258,21 @@ int nvfp4_swiglu_ffn(const void* x, int64_t ldx, const void* w_gate, const void*
         }
         return launched();
     }
-    if (m <= thin_product::kRows) {
-        thin_product::Args t = {};
-        t.w = static_cast<const char*>(rg.p), t.w2 = static_cast<const char*>(ru.p), t.ldw = rg.ld * 2;
-        t.x = static_cast<const char*>(rx.p), t.ldx = rx.ld * 2, t.m = (int)m, t.n = n, t.k = k;
-        t.out = h, t.out2 = gate, t.out3 = up_out;
-        thin_product::launch_thin<thin_product::kGated, 8, 4>(t, st);
-        return launched();
-    }
     Args p = {};
     p.a.p = static_cast<const char*>(rx.p), p.a.ld = rx.ld * 2;
     p.b.p = static_cast<const char*>(rg.p), p.b.p2 = static_cast<const char*>(ru.p), p.b.ld = rg.ld * 2;
     p.m = m, p.n = n, p.inner = k, p.out = h, p.out2 = gate, p.out3 = up_out, p.out_ld = n;
-    p.parts = 1;
-    return launch_product<kBf16, kGate>(p, plan_product<kBf16, kGate>(m, n, k).tile, st);
+    const Plan plan = plan_product<kBf16, kGate>(m, n, k);
+    p.parts = plan.parts;
+    if (plan.parts == 1) return launch_product<kBf16, kGate>(p, plan.tile, st);
+    float* parts = static_cast<float*>(p.out = c.take(0));
+    if (const int rc = launch_product<kBf16, kGatePartial>(p, plan.tile, st)) return rc;
+    const bool vec = n % 4 == 0;
+    const int64_t groups = ceil_div(vec ? m * n / 4 : m * n, kEdgeThreads);
+    if (groups > 0x7FFFFFFF) return NVFP4_ERR_SHAPE;
+    hipLaunchKernelGGL((vec ? join_gate_kernel<true> : join_gate_kernel<false>), dim3((unsigned)groups), dim3(kEdgeThreads), 0, st,
+                       parts, plan.parts, m * n, h, gate, up_out);
+    return launched();
 }
 
 int64_t nvfp4_swiglu_ffn_backward_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t ldx, int64_t ldw) {

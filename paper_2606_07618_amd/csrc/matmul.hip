@@ -319,13 +319,18 @@ __global__ __launch_bounds__(kScaleThreads) void lay_scales_kernel(Scales a, Sca
 
 int64_t scale_bytes(int64_t rows, int64_t blocks) { return up(rows, 128) * ceil_div(blocks, 8) * 8; }
 
+// Few rows, and no tiles to keep the chip busy with whole contractions.
+bool thin(int64_t m, int64_t n, int64_t blocks) {
+    return m <= thin_product::kRows && plan_product<kMx, kSums>(m, n, blocks * 32).parts > 1;
+}
+
 // The largest tile takes its scales laid out, and so do the others where rows of scales are no whole words.
 bool lays_scales(int64_t m, int64_t n, int64_t blocks) {
     return blocks % 4 != 0 || plan_product<kMx, kSums>(m, n, blocks * 32).tile == 0;
 }
 
 int64_t mx_workspace(int64_t m, int64_t n, int64_t blocks) {
-    if (m <= thin_product::kRows) return 0;
+    if (thin(m, n, blocks)) return 0;
     Carver c{nullptr};
     if (lays_scales(m, n, blocks)) {
         c.take(scale_bytes(m, blocks));
@@ -336,12 +341,11 @@ int64_t mx_workspace(int64_t m, int64_t n, int64_t blocks) {
 
 int run_mx(const uint8_t* aq, const uint8_t* as, const uint8_t* bq, const uint8_t* bs, int64_t m, int64_t n,
            int64_t blocks, int out_dtype, void* out, void* ws, hipStream_t stream) {
-    if (m <= thin_product::kRows) {
+    if (thin(m, n, blocks)) {
         thin_product::Args t = {};
-        t.w = reinterpret_cast<const char*>(bq), t.ldw = blocks * 16, t.w_scales = bs, t.w_scale_ld = blocks;
-        t.x = reinterpret_cast<const char*>(aq), t.ldx = blocks * 16, t.x_scales = as, t.m = (int)m, t.n = n, t.k = blocks * 32;
-        t.out = out, t.out_f32 = out_dtype == NVFP4_IN_F32;
-        thin_product::launch_thin<thin_product::kMicroscaled, 8, 4>(t, stream);
+        t.w = reinterpret_cast<const char*>(bq), t.w_scales = bs, t.x = reinterpret_cast<const char*>(aq), t.x_scales = as;
+        t.m = (int)m, t.n = n, t.k = blocks * 32, t.out = out, t.out_f32 = out_dtype == NVFP4_IN_F32;
+        thin_product::launch_thin(t, stream);
         return launched();
     }
     Carver c{static_cast<char*>(ws)};

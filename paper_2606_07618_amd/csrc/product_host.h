@@ -59,7 +59,7 @@ constexpr float kJoinUs = 5.0f, kJoinBytesUs = 4e6f;     // a second launch; byt
 
 template <Kind KIND>
 inline const TileCost* tile_costs() {
-    static constexpr TileCost mx[kTiles] = {{256, 256, 1.9f, 2.4f}, {128, 128, 1.05f, 0.92f}, {64, 128, 0.75f, 0.60f}, {64, 64, 0.52f, 0.41f}};
+    static constexpr TileCost mx[kTiles] = {{256, 256, 1.8f, 2.05f}, {128, 128, 1.05f, 0.92f}, {64, 128, 0.75f, 0.60f}, {64, 64, 0.52f, 0.41f}};
     static constexpr TileCost bf16[kTiles] = {{256, 256, 1.25f, 1.72f}, {128, 128, 0.83f, 0.54f}, {64, 128, 0.48f, 0.34f}, {64, 64, 0.40f, 0.25f}};
     return KIND != kBf16 ? mx : bf16;
 }
@@ -69,10 +69,10 @@ constexpr int kFragments[kTiles][2] = {{8, 4}, {4, 4}, {2, 4}, {2, 2}};
 
 struct Plan { int tile, parts; };
 
-// A sum is split (kPartial, then joined); kGate's and kTwoRows' are not.
+// kSums and kGate may be split (kPartial and kGatePartial, then joined), kTwoRows is not.
 template <Kind KIND, Out OUT>
 Plan plan_product(int64_t m, int64_t n, int64_t inner) {
-    constexpr int kStepValues = KIND != kBf16 ? 256 : 64, kHalf = OUT == kGate ? 2 : 1, kMost = OUT == kSums ? kMostParts : 1;
+    constexpr int kStepValues = KIND != kBf16 ? 256 : 64, kHalf = OUT == kGate ? 2 : 1, kMost = OUT == kTwoRows ? 1 : kMostParts;
     const int64_t steps = ceil_div(inner, kStepValues);
     const TileCost* costs = tile_costs<KIND>();
     Plan best = {0, 1};
@@ -84,7 +84,7 @@ Plan plan_product(int64_t m, int64_t n, int64_t inner) {
             const float rounds = tiles * parts <= 256.0f ? 1.0f : (float)(int64_t)((tiles * parts + 255.0f) / 256.0f);
             const float step = rounds * costs[t].among > costs[t].alone ? rounds * costs[t].among : costs[t].alone;
             float us = (float)ceil_div(steps, parts) * step;
-            if (parts > 1) us += kJoinUs + (float)m * (float)n * (float)(8 * parts) / kJoinBytesUs;
+            if (parts > 1) us += kJoinUs + (float)m * (float)n * (float)(8 * kHalf * parts) / kJoinBytesUs;
             if (us < least) least = us, best = {t, parts};
         }
     }
@@ -92,10 +92,10 @@ Plan plan_product(int64_t m, int64_t n, int64_t inner) {
 }
 
 // Bytes of the parts' sums, 0 where the product is not split.
-template <Kind KIND>
+template <Kind KIND, Out OUT = kSums>
 int64_t parts_bytes(int64_t m, int64_t n, int64_t inner) {
-    const Plan p = plan_product<KIND, kSums>(m, n, inner);
-    return p.parts > 1 ? up(p.parts * m * n * 4, 256) : 0;
+    const Plan p = plan_product<KIND, OUT>(m, n, inner);
+    return p.parts > 1 ? up(p.parts * m * n * (OUT == kGate ? 8 : 4), 256) : 0;
 }
 
 // Fills in the tiles and steps of p and launches; p's operands, outer indexes and outputs are set.
@@ -104,7 +104,7 @@ int launch_tiles(Args p, hipStream_t stream) {
     constexpr int kStepValues = KIND != kBf16 ? 256 : 64;
     p.steps = ceil_div(p.inner, kStepValues);
     p.tiles_m = ceil_div(p.m, T::M);
-    p.tiles_n = ceil_div(p.n, OUT == kGate ? T::N / 2 : T::N);
+    p.tiles_n = ceil_div(p.n, OUT == kGate || OUT == kGatePartial ? T::N / 2 : T::N);
     p.split_steps = ceil_div(p.steps, p.parts);
     if (p.tiles_m > 0x7FFFFFFF || p.tiles_m * p.tiles_n > 0x7FFFFFFF / p.parts) return NVFP4_ERR_SHAPE;
     if (p.tiles_m * p.tiles_n == 0) return NVFP4_OK;
@@ -130,7 +130,7 @@ int launch_product(const Args& p, int tile, hipStream_t stream) {
         case 1: return launch_tiles<KIND, OUT, Tile1>(p, stream);
         case 2: return launch_tiles<KIND, OUT, Tile2>(p, stream);
         default:
-            if constexpr (OUT != kGate) return launch_tiles<KIND, OUT, Tile3>(p, stream);
+            if constexpr (OUT != kGate && OUT != kGatePartial) return launch_tiles<KIND, OUT, Tile3>(p, stream);
             return NVFP4_ERR_SHAPE;                                  // kGate has no plan with it
     }
 }

@@ -179,6 +179,7 @@ enum Out {
     kPartial,     // the sum of this part of the contraction, binary32, for a later reduction
     kGate,        // B is two matrices: silu(sum of the first) * sum of the second, and both sums where asked for;
                   // a tile's outer indexes of B are taken half from each, so that an output's two sums meet in one lane
+    kGatePartial, // both sums of this part of the contraction, [part][2][m][n] in binary32
     kTwoRows      // rows below `half_rows` to the first output, those from there on to the second
 };
 
@@ -215,7 +216,7 @@ __device__ __forceinline__ void store4(void* out, int f32, int64_t at, int64_t l
 
 template <Kind KIND, Out OUT, class T>
 __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(Args p) {
-    constexpr bool HALF = OUT == kGate;
+    constexpr bool HALF = OUT == kGate || OUT == kGatePartial;
     using A = Side<T::M, T::kThreads, false>;
     using B = Side<T::N, T::kThreads, HALF>;
     constexpr bool kScaled = KIND != kBf16, kLaid = KIND == kMxLaid;
@@ -425,7 +426,7 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
     // lane ([8192, 4096] x [14336, 4096] microscaled, where the contraction is short: 338 -> 305 us).
     const float scale = OUT == kSums && p.scale ? *p.scale : 1.0f;
     auto column = [&](int j) { return HALF ? wn * (kOutN / T::WN) + j * 16 : b_row(j); };
-    if (OUT != kPartial && !p.out_f32 && p.out_ld % 8 == 0) {
+    if (OUT != kPartial && OUT != kGatePartial && !p.out_f32 && p.out_ld % 8 == 0) {
         constexpr int kOutChunks = kOutN / 8, kMask = kOutChunks < 16 ? kOutChunks - 1 : 15;
         static_assert(T::M * kOutN * 2 <= kSlots * kStage, "the tile in LDS");
         char* tile = lds[0];
@@ -486,6 +487,9 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
                 store4(p.out, p.out_f32, m * p.out_ld + n, left, vec, v * scale);
             } else if constexpr (OUT == kPartial) {
                 store4(p.out, 1, (part * p.m + m) * p.out_ld + n, left, vec, v);
+            } else if constexpr (OUT == kGatePartial) {
+                store4(p.out, 1, (part * 2 * p.m + m) * p.out_ld + n, left, vec, v);
+                store4(p.out, 1, ((part * 2 + 1) * p.m + m) * p.out_ld + n, left, vec, acc[i][NF / 2 + j]);
             } else if constexpr (OUT == kTwoRows) {
                 const bool first = m < p.half_rows;
                 store4(first ? p.out : p.out2, 0, (first ? m : m - p.half_rows) * p.out_ld + n, left, vec, v);
