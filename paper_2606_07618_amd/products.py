@@ -52,19 +52,22 @@ def _rows(t, what):
 
 
 def _same_device(t, *others):
-    if any(o is not None and o.device != t.device for o in others):
-        raise ValueError("all tensors must be on one device")
+    index = t.get_device()
+    for o in others:
+        if o is not None and o.get_device() != index:
+            raise ValueError("all tensors must be on one device")
 
 
 def _plain(t, shape, dtype, what):
-    if not (t.is_cuda and t.dtype == dtype and t.is_contiguous() and tuple(t.shape) == tuple(shape)):
+    if not (t.is_cuda and t.dtype == dtype and t.shape == shape and t.is_contiguous()):
         raise ValueError(f"{what} must be a contiguous {dtype} device tensor {list(shape)}")
 
 
-def _output(out, shape, dtype, device, what="out"):
+def _output(out, shape, dtype, like, what="out"):
     if out is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
     _plain(out, shape, dtype, what)
+    _same_device(like, out)
     return out
 
 
@@ -98,8 +101,8 @@ def mx_quantize(x: torch.Tensor, out=None):
     rows, cols = x.shape
     kb = -(-cols // MX_BLOCK)
     q, sc = (None, None) if out is None else out
-    q = _output(q, (rows, 16 * kb), torch.uint8, x.device, "q")
-    sc = _output(sc, (rows, kb), torch.uint8, x.device, "scales")
+    q = _output(q, (rows, 16 * kb), torch.uint8, x, "q")
+    sc = _output(sc, (rows, kb), torch.uint8, x, "scales")
     _check(mxfp4_quant(_ptr(x), dt, rows, cols, _ptr(q), _ptr(sc), _stream(x)), "mxfp4_quant")
     return q, sc
 
@@ -122,7 +125,7 @@ def mx_dequant(q: torch.Tensor, scales: torch.Tensor, cols: int | None = None,
     cols = MX_BLOCK * kb if cols is None else cols
     if -(-cols // MX_BLOCK) != kb:
         raise ValueError(f"cols must lie in the last of the {kb} blocks of a row")
-    out = _output(out, (rows, cols), out_dtype, q.device)
+    out = _output(out, (rows, cols), out_dtype, q)
     _check(mxfp4_dequant(_ptr(q), _ptr(scales), rows, cols, dt, _ptr(out), _stream(q)), "mxfp4_dequant")
     return out
 
@@ -138,8 +141,7 @@ def mx_matmul(a, b, out_dtype: torch.dtype = torch.bfloat16, out: torch.Tensor |
     if kb != kb2:
         raise ValueError("a and b must have rows of the same number of blocks")
     _same_device(aq, bq)
-    out = _output(out, (m, n), out_dtype, aq.device)
-    _same_device(aq, out)
+    out = _output(out, (m, n), out_dtype, aq)
     k = MX_BLOCK * kb
     ws, nbytes = _workspace(mxfp4_matmul_workspace_bytes(m, n, k), ws, aq.device, "mxfp4_matmul_workspace_bytes")
     _check(mxfp4_matmul(_ptr(aq), _ptr(asc), _ptr(bq), _ptr(bsc), m, n, k, dt, _ptr(out), _ptr(ws), nbytes,
@@ -161,8 +163,8 @@ def mx_matmul_grad_input(dy: torch.Tensor, q: torch.Tensor, scales: torch.Tensor
     cols = MX_BLOCK * kb if cols is None else cols
     if -(-cols // MX_BLOCK) != kb:
         raise ValueError(f"cols must lie in the last of the {kb} blocks of a row")
-    out = _output(out, (m, cols), out_dtype, dy.device)
-    _same_device(dy, q, out)
+    out = _output(out, (m, cols), out_dtype, dy)
+    _same_device(dy, q)
     ws, nbytes = _workspace(mxfp4_matmul_grad_input_workspace_bytes(m, n, cols, ld), ws, dy.device,
                             "mxfp4_matmul_grad_input_workspace_bytes")
     _check(mxfp4_matmul_grad_input(_ptr(dy), ld, _ptr(q), _ptr(scales), m, n, cols, dt, _ptr(out), _ptr(ws), nbytes,
@@ -197,8 +199,7 @@ def matmul(x: torch.Tensor, q: torch.Tensor, scales: torch.Tensor, S: torch.Tens
     m = x.shape[0]
     if x.shape[1] != k:
         raise ValueError("x must be [m, k] for weights [n, k]")
-    out = _output(out, (m, n), out_dtype, x.device)
-    _same_device(x, out)
+    out = _output(out, (m, n), out_dtype, x)
     ws, nbytes = _workspace(nvfp4_matmul_workspace_bytes(m, n, k), ws, x.device, "nvfp4_matmul_workspace_bytes")
     _check(nvfp4_matmul(_ptr(x), ldx, _ptr(q), _ptr(scales), block, _ptr(S), m, n, k, dt, _ptr(out), _ptr(ws), nbytes,
                         _stream(x)), "nvfp4_matmul")
@@ -215,8 +216,7 @@ def matmul_grad_input(dy: torch.Tensor, q: torch.Tensor, scales: torch.Tensor, S
     m = dy.shape[0]
     if dy.shape[1] != n:
         raise ValueError("dy must be [m, n] for weights [n, k]")
-    out = _output(out, (m, k), out_dtype, dy.device)
-    _same_device(dy, out)
+    out = _output(out, (m, k), out_dtype, dy)
     ws, nbytes = _workspace(nvfp4_matmul_grad_input_workspace_bytes(m, n, k, ld), ws, dy.device,
                             "nvfp4_matmul_grad_input_workspace_bytes")
     _check(nvfp4_matmul_grad_input(_ptr(dy), ld, _ptr(q), _ptr(scales), block, _ptr(S), m, n, k, dt, _ptr(out),
@@ -243,11 +243,10 @@ def swiglu_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, save: 
     swiglu_ffn_backward takes.  ``out`` may pass preallocated outputs in the same form."""
     m, n, k, ldx, ldw = _ffn_operands(x, w_gate, w_up)
     h, gate, up = (out if save else (out, None, None)) if out is not None else (None, None, None)
-    h = _output(h, (m, n), torch.bfloat16, x.device, "h")
+    h = _output(h, (m, n), torch.bfloat16, x, "h")
     if save:
-        gate = _output(gate, (m, n), torch.bfloat16, x.device, "gate")
-        up = _output(up, (m, n), torch.bfloat16, x.device, "up")
-    _same_device(x, h, gate, up)
+        gate = _output(gate, (m, n), torch.bfloat16, x, "gate")
+        up = _output(up, (m, n), torch.bfloat16, x, "up")
     ws, nbytes = _workspace(nvfp4_swiglu_ffn_workspace_bytes(m, n, k, ldx, ldw), ws, x.device,
                             "nvfp4_swiglu_ffn_workspace_bytes")
     _check(nvfp4_swiglu_ffn(_ptr(x), ldx, _ptr(w_gate), _ptr(w_up), ldw, m, n, k, _ptr(h), _ptr(gate), _ptr(up),
@@ -267,10 +266,10 @@ def swiglu_ffn_backward(dh: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor,
     if not (need_x or need_w):
         return None, None, None
     dx, dwg, dwu = out if out is not None else (None, None, None)
-    dx = _output(dx, (m, k), torch.bfloat16, x.device, "dx") if need_x else None
-    dwg = _output(dwg, (n, k), torch.bfloat16, x.device, "dw_gate") if need_w else None
-    dwu = _output(dwu, (n, k), torch.bfloat16, x.device, "dw_up") if need_w else None
-    _same_device(x, dh, gate, up, dx, dwg, dwu)
+    dx = _output(dx, (m, k), torch.bfloat16, x, "dx") if need_x else None
+    dwg = _output(dwg, (n, k), torch.bfloat16, x, "dw_gate") if need_w else None
+    dwu = _output(dwu, (n, k), torch.bfloat16, x, "dw_up") if need_w else None
+    _same_device(x, dh, gate, up)
     ws, nbytes = _workspace(nvfp4_swiglu_ffn_backward_workspace_bytes(m, n, k, ldx, ldw), ws, x.device,
                             "nvfp4_swiglu_ffn_backward_workspace_bytes")
     _check(nvfp4_swiglu_ffn_backward(_ptr(dh), _ptr(x), ldx, _ptr(w_gate), _ptr(w_up), ldw, _ptr(gate), _ptr(up), m, n,
