@@ -52,12 +52,12 @@ typedef enum { NVFP4_IN_F32 = 0, NVFP4_IN_BF16 = 1 } nvfp4_dtype;
 typedef enum {
     NVFP4_OK = 0,
     NVFP4_ERR_NULL = -1,      /* a required pointer is NULL */
-    NVFP4_ERR_SHAPE = -2,     /* rows < 0, cols < 0, or cols % block != 0 */
+    NVFP4_ERR_SHAPE = -2,     /* rows < 0, cols < 0, or cols % block != 0; a size or stride out of a product's range */
     NVFP4_ERR_BLOCK = -3,     /* block not in {16, 32, 64, 128} */
     NVFP4_ERR_DTYPE = -4,     /* dtype / out_dtype not supported */
     NVFP4_ERR_ARG = -5,       /* fp8_range, static_scale or a window out of range */
-    NVFP4_ERR_WORKSPACE = -6, /* dynamic scale requested without a large enough workspace */
-    NVFP4_ERR_ALIGN = -7,     /* x, col_weight or workspace not 16-byte aligned, q not 8 */
+    NVFP4_ERR_WORKSPACE = -6, /* dynamic scale or product requested without a large enough workspace */
+    NVFP4_ERR_ALIGN = -7,     /* x, col_weight or workspace not 16-byte aligned, q not 8; products: see there */
     NVFP4_ERR_HIP = -8,       /* a kernel launch failed */
     NVFP4_ERR_LIMIT = -10     /* more than the no-allocation entry point's fixed scratch holds */
 } nvfp4_status;
@@ -375,7 +375,8 @@ int mxfp4_dequant(const uint8_t* q, const uint8_t* scales, int64_t rows, int64_t
 
 /* y = x W^T S of bfloat16 x [m, k] and NVFP4 weights (q, scales, *tensor_scale) of `block` (16, 32, 64 or 128;
  * k % block == 0), scales row-major.  The weights' values q s enter exactly, the sums are multiplied
- * by S.  ldx % 8 == 0, else NVFP4_ERR_ALIGN. */
+ * by S.  Calls of 5 to 512 rows take the activations in binary16, each row scaled by a power of two: values down to
+ * 2^-31 of the row's largest enter exactly, smaller ones to 2^-39 of it.  ldx % 8 == 0, else NVFP4_ERR_ALIGN. */
 int64_t nvfp4_matmul_workspace_bytes(int64_t m, int64_t n, int64_t k);
 int nvfp4_matmul(const void* x, int64_t ldx, const uint8_t* q, const uint8_t* scales, int block,
                  const float* tensor_scale, int64_t m, int64_t n, int64_t k, int out_dtype, void* out, void* workspace,
@@ -400,7 +401,7 @@ int mxfp4_matmul_grad_input(const void* dy, int64_t ld, const uint8_t* q, const 
                             int64_t k, int out_dtype, void* dx, void* workspace, size_t workspace_bytes,
                             void* stream);
 
-/* The gated feed-forward block in one kernel: g = x Wg^T, u = x Wu^T, h = silu(g) u with
+/* The gated feed-forward block, without g and u in memory: g = x Wg^T, u = x Wu^T, h = silu(g) u with
  * silu(g) = g / (1 + e^-g), all bfloat16 with sums in binary32; h is formed from the unrounded sums.
  * x [m, k] (rows ldx apart), w_gate and w_up [n, k] (rows ldw apart), any k.  h [m, n]; gate and up
  * [m, n] receive g and u for a backward pass, or are both NULL. */
@@ -412,7 +413,8 @@ int nvfp4_swiglu_ffn(const void* x, int64_t ldx, const void* w_gate, const void*
 /* Its gradients from dh [m, n] and the forward's gate and up [m, n] (contiguous): with s = 1 / (1 + e^-g),
  *   dg = dh u s (1 + g (1 - s)),  du = dh g s  (rounded to bfloat16 for the products),
  *   dx [m, k] = dg Wg + du Wu,  dw_gate [n, k] = dg^T x,  dw_up [n, k] = du^T x.
- * dx, or both dw_gate and dw_up, may be NULL: not computed. */
+ * dx, or both dw_gate and dw_up, may be NULL: not computed.  The weights' gradients take m <= 2^21, else
+ * NVFP4_ERR_SHAPE. */
 int64_t nvfp4_swiglu_ffn_backward_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t ldx, int64_t ldw);
 int nvfp4_swiglu_ffn_backward(const void* dh, const void* x, int64_t ldx, const void* w_gate, const void* w_up,
                               int64_t ldw, const void* gate, const void* up, int64_t m, int64_t n, int64_t k,

@@ -4,8 +4,9 @@
 // The instructions of the expansion are what bounds it (each costs 4.8 cycles of a SIMD's four), so it is done in
 // binary16: q s has six significand bits and lies in 2^-10 .. 2688, exact there, and takes one conversion and
 // one packed product a pair; in bfloat16 it would take four instructions.  The activations are converted once,
-// each row scaled by a power of two so that its largest value lies in [2^14, 2^15): values down to 2^-29 of it
-// stay exact, and what is lost of smaller ones is below 2^-40 of it, far under the sums' own rounding.
+// each row scaled by a power of two so that its largest value lies in [2^14, 2^15): values down to 2^-31 of it
+// stay exact (eight significant bits above binary16's smallest 2^-24), and smaller ones lose 2^-39 of it at most, far
+// under the sums' own rounding.
 //
 // A workgroup owns 128 weight rows and up to 128 activation rows.  Its waves are four times 32 weight rows by the
 // two halves of its contraction; a wave loads its weights (32 rows by two lanes of 16 bytes) into
