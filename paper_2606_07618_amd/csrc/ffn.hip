@@ -12,9 +12,10 @@ using namespace product_host;
 constexpr int kEdgeThreads = 256;
 
 // The backward products' contractions run over the tokens (dW) and over the weights' rows (dx), so dg and du are
-// written as they lie and turned, and x and the weights are turned: all four products then read whole rows.
-// [4000, 4096] -> 14336: 1830 us with the operands as they lie, 1636 so.  The two products take nine tenths of it at
-// 1.25 PFLOP/s; this kernel moves 800 MB in 142 us and turning a weight matrix 235 MB in 48 (5.6 and 4.9 TB/s).
+// written as they lie and turned, and x and the weights are turned: all four products then read whole rows.  One launch
+// does all of it (prepare_kernel): with six launches a gradient of [237, 176] -> 112 took 31 us, with three 22.
+// [4000, 4096] -> 14336: 1830 us with the operands as they lie, 1615 so.  The two products take 1.35 ms of it (1.4
+// PFLOP/s), the preparation 254 us for the 1.34 GB it has to move (5.3 TB/s).
 //
 // Turning: a workgroup takes 64 rows by 128 columns.  A thread holds two rows by eight columns of either half and
 // writes pairs of rows, a word each, to LDS; LDS rows are a word longer than their 64 values, so that the eight row
@@ -48,65 +49,53 @@ __device__ __forceinline__ void turn_out(const TurnTile& tile, int64_t c0, int64
     }
 }
 
-// Values c .. c + 7 of row r of a [rows, width] matrix, zeros outside.  VEC: its rows are whole 16-byte pieces.
-template <bool VEC>
-__device__ __forceinline__ uint4 eight(const uint16_t* src, int64_t r, int64_t rows, int64_t c, int64_t width, int64_t ld) {
+// Values c .. c + 7 of row r of a [rows, width] matrix, zeros outside.  vec: its rows are whole 16-byte pieces.
+__device__ __forceinline__ uint4 eight(bool vec, const uint16_t* src, int64_t r, int64_t rows, int64_t c, int64_t width,
+                                       int64_t ld) {
     if (r >= rows || c >= width) return make_uint4(0, 0, 0, 0);
-    if constexpr (VEC) return *reinterpret_cast<const uint4*>(src + r * ld + c);
+    if (vec) return *reinterpret_cast<const uint4*>(src + r * ld + c);
     uint32_t v[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = c + j < width ? src[r * ld + c + j] : 0u;
     return make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
 }
 
-// src [rows, width] turned: dst [width, to_ld], values from rows to fill zero.
-template <bool VEC>
-__global__ __launch_bounds__(kEdgeThreads) void turn_kernel(const uint16_t* __restrict__ src, int64_t rows, int64_t width,
-                                                            int64_t ld, int64_t tiles_c, int64_t fill,
-                                                            uint16_t* __restrict__ dst, int64_t to_ld) {
-    __shared__ TurnTile tile;
-    const int64_t r0 = blockIdx.x / tiles_c * kTurnRows, c0 = blockIdx.x % tiles_c * kTurnColumns;
+// src [rows, width] turned: dst [width, to_ld], values from rows to fill zero.  vec: rows are whole 16-byte pieces.
+struct Turn { const uint16_t* src; int64_t rows, width, ld, fill; uint16_t* dst; int64_t to_ld; uint32_t tiles_c, tiles; int vec; };
+
+__device__ __forceinline__ void turn(TurnTile& tile, const Turn& p, uint32_t at) {
+    const int64_t r0 = (int64_t)(at / p.tiles_c) * kTurnRows, c0 = (int64_t)(at % p.tiles_c) * kTurnColumns;
     const int64_t r = r0 + turn_pair() * 2, c = c0 + turn_column();
     uint4 v[2][2];
 #pragma unroll
     for (int e = 0; e < 2; ++e)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) v[h][e] = eight<VEC>(src, r + e, rows, c + h * kTurnHalf, width, ld);
+        for (int h = 0; h < 2; ++h)
+            v[h][e] = eight(p.vec, p.src, r + e, p.rows, c + h * kTurnHalf, p.width, p.ld);
 #pragma unroll
     for (int h = 0; h < 2; ++h) turn8(tile, turn_column() + h * kTurnHalf, v[h][0], v[h][1]);
     __syncthreads();
-    turn_out(tile, c0, width, r0, fill, to_ld, dst);
-}
-
-int turn(const uint16_t* src, int64_t rows, int64_t width, int64_t ld, int64_t fill, uint16_t* dst, int64_t to_ld,
-         hipStream_t stream) {
-    const int64_t tiles_c = ceil_div(width, kTurnColumns), tiles = ceil_div(fill, kTurnRows) * tiles_c;
-    if (tiles == 0) return NVFP4_OK;
-    if (tiles > 0x7FFFFFFF) return NVFP4_ERR_SHAPE;
-    hipLaunchKernelGGL((width % 8 == 0 && ld % 8 == 0 ? turn_kernel<true> : turn_kernel<false>), dim3((unsigned)tiles),
-                       dim3(kEdgeThreads), 0, stream, src, rows, width, ld, tiles_c, fill, dst, to_ld);
-    return launched();
+    turn_out(tile, c0, p.width, r0, p.fill, p.to_ld, p.dst);
 }
 
 // dg and du side by side, d [m, 2 half], du from column `half` on, zeros from n to half; and turned, one below the
 // other, t [2 n, ld], zeros from m to ld.  Either is left out where its pointer is NULL.  Their rounding to
 // bfloat16 is what the matrix cores take; the products' sums stay in binary32.
-template <bool VEC>
-__global__ __launch_bounds__(kEdgeThreads) void gate_grad_kernel(const uint16_t* __restrict__ dh,
-                                                                 const uint16_t* __restrict__ gate,
-                                                                 const uint16_t* __restrict__ up_, int64_t m, int64_t n,
-                                                                 int64_t tiles_n, int64_t half, uint16_t* __restrict__ d,
-                                                                 int64_t ld, uint16_t* __restrict__ t) {
-    __shared__ TurnTile tg, tu;
-    const int64_t r0 = blockIdx.x / tiles_n * kTurnRows, c0 = blockIdx.x % tiles_n * kTurnColumns;
+struct Gates { const uint16_t *dh, *gate, *up; int64_t m, n, half; uint16_t* d; int64_t ld; uint16_t* t; uint32_t tiles_n, tiles; };
+
+__device__ __forceinline__ void gate_grad(TurnTile& tg, TurnTile& tu, const Gates& p, uint32_t at) {
+    const int64_t m = p.m, n = p.n, half = p.half, ld = p.ld;
+    uint16_t *d = p.d, *t = p.t;
+    const bool vec = n % 8 == 0;
+    const int64_t r0 = (int64_t)(at / p.tiles_n) * kTurnRows, c0 = (int64_t)(at % p.tiles_n) * kTurnColumns;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const int64_t r = r0 + turn_pair() * 2, c = c0 + turn_column() + h * kTurnHalf;
         uint4 og[2], ou[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            const uint4 va = eight<VEC>(dh, r + e, m, c, n, n), vg = eight<VEC>(gate, r + e, m, c, n, n),
-                        vu = eight<VEC>(up_, r + e, m, c, n, n);
+            const uint4 va = eight(vec, p.dh, r + e, m, c, n, n), vg = eight(vec, p.gate, r + e, m, c, n, n),
+                        vu = eight(vec, p.up, r + e, m, c, n, n);
             const uint32_t a[4] = {va.x, va.y, va.z, va.w}, g[4] = {vg.x, vg.y, vg.z, vg.w}, u[4] = {vu.x, vu.y, vu.z, vu.w};
             uint32_t wg[4], wu[4];
 #pragma unroll
@@ -141,6 +130,38 @@ __global__ __launch_bounds__(kEdgeThreads) void gate_grad_kernel(const uint16_t*
     __syncthreads();
     turn_out(tg, c0, n, r0, ld, ld, t);
     turn_out(tu, c0, n, r0, ld, ld, t + n * ld);
+}
+
+// Everything that the products wait for, in one launch: workgroups of dg and du first, then those of the turned operands.
+struct Prepare { Gates gates; Turn turns[3]; };
+
+__global__ __launch_bounds__(kEdgeThreads) void prepare_kernel(Prepare p) {
+    __shared__ TurnTile tile[2];
+    uint32_t at = blockIdx.x;
+    if (at < p.gates.tiles) return gate_grad(tile[0], tile[1], p.gates, at);
+    at -= p.gates.tiles;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+        if (at < p.turns[i].tiles) return turn(tile[0], p.turns[i], at);
+        at -= p.turns[i].tiles;
+    }
+}
+
+int prepare(Prepare p, hipStream_t stream) {
+    int64_t tiles = 0;
+    const auto count = [&](int64_t rows, int64_t columns, uint32_t& across, uint32_t& all) {
+        const int64_t a = ceil_div(columns, kTurnColumns), n = a * ceil_div(rows, kTurnRows);
+        across = (uint32_t)a, all = (uint32_t)n, tiles += n;
+        return tiles <= 0x7FFFFFFF;
+    };
+    if (!count(p.gates.m, p.gates.n, p.gates.tiles_n, p.gates.tiles)) return NVFP4_ERR_SHAPE;
+    for (Turn& t : p.turns) {
+        t.vec = t.width % 8 == 0 && t.ld % 8 == 0;
+        if (!count(t.fill, t.width, t.tiles_c, t.tiles)) return NVFP4_ERR_SHAPE;
+    }
+    if (tiles == 0) return NVFP4_OK;
+    hipLaunchKernelGGL(prepare_kernel, dim3((unsigned)tiles), dim3(kEdgeThreads), 0, stream, p);
+    return launched();
 }
 
 struct Rows { const void* p; int64_t ld; };
@@ -200,11 +221,11 @@ int64_t backward_sections(void* workspace, int64_t m, int64_t n, int64_t k, Back
     b.half = up(n, 64), b.ld = up(m, 64);
     b.d = static_cast<char*>(c.take(m * 2 * b.half * 2));
     b.dt = static_cast<char*>(c.take(2 * n * b.ld * 2));
-    Carver x = c, w = c;                         // dx is done before x is turned
-    b.wt = static_cast<char*>(x.take(k * 2 * b.half * 2));
-    b.parts = static_cast<char*>(x.take(parts_bytes<kBf16>(m, k, 2 * b.half)));
-    b.xt = static_cast<char*>(w.take(k * b.ld * 2));
-    return x.at > w.at ? x.at : w.at;
+    b.wt = static_cast<char*>(c.take(k * 2 * b.half * 2));
+    b.xt = static_cast<char*>(c.take(k * b.ld * 2));
+    const int64_t px = parts_bytes<kBf16>(m, k, 2 * b.half), pw = parts_bytes<kBf16, kTwoRows>(2 * n, k, m);
+    b.parts = static_cast<char*>(c.take(px > pw ? px : pw));     // of one product after the other
+    return c.at;
 }
 
 int check_call(int64_t m, int64_t n, int64_t k, int64_t ldx, int64_t ldw) {
@@ -300,29 +321,27 @@ int nvfp4_swiglu_ffn_backward(const void* dh, const void* x, int64_t ldx, const 
     hipStream_t st = (hipStream_t)stream;
     const auto values = [](const void* p) { return static_cast<const uint16_t*>(p); };
     const auto turned = [](char* p) { return reinterpret_cast<uint16_t*>(p); };
-    const int64_t tiles_n = ceil_div(n, kTurnColumns), tiles = ceil_div(m, kTurnRows) * tiles_n;
-    if (tiles > 0x7FFFFFFF) return NVFP4_ERR_SHAPE;
-    if (tiles > 0) {
-        hipLaunchKernelGGL((n % 8 == 0 ? gate_grad_kernel<true> : gate_grad_kernel<false>), dim3((unsigned)tiles),
-                           dim3(kEdgeThreads), 0, st, values(dh), values(gate), values(up_in), m, n, tiles_n, b.half,
-                           want_x ? turned(b.d) : nullptr, b.ld, want_w ? turned(b.dt) : nullptr);
-        if (const int rc = launched()) return rc;
-    }
+    Prepare ready = {};
+    ready.gates = {values(dh), values(gate), values(up_in), m, n, b.half, want_x ? turned(b.d) : nullptr, b.ld,
+                   want_w ? turned(b.dt) : nullptr};
     if (want_x) {
-        if (const int rc = turn(values(w_gate), n, k, ldw, b.half, turned(b.wt), 2 * b.half, st)) return rc;
-        if (const int rc = turn(values(w_up), n, k, ldw, b.half, turned(b.wt) + b.half, 2 * b.half, st)) return rc;
+        ready.turns[0] = {values(w_gate), n, k, ldw, b.half, turned(b.wt), 2 * b.half};
+        ready.turns[1] = {values(w_up), n, k, ldw, b.half, turned(b.wt) + b.half, 2 * b.half};
+    }
+    if (want_w) ready.turns[2] = {values(x), m, k, ldx, b.ld, turned(b.xt), b.ld};
+    if (const int rc = prepare(ready, st)) return rc;
+    if (want_x) {
         Args p = {};
         p.a.p = b.d, p.a.ld = p.b.ld = 2 * b.half * 2, p.b.p = b.wt;
         p.m = m, p.n = k, p.inner = 2 * b.half, p.out = dx, p.out_ld = k;
         if (const int rc = run_sums<kBf16>(p, reinterpret_cast<float*>(b.parts), st)) return rc;
     }
     if (want_w) {
-        if (const int rc = turn(values(x), m, k, ldx, b.ld, turned(b.xt), b.ld, st)) return rc;
         Args p = {};
         p.a.p = b.dt, p.a.ld = p.b.ld = b.ld * 2, p.b.p = b.xt;
         p.m = 2 * n, p.n = k, p.inner = m, p.half_rows = n;
-        p.out = dw_gate, p.out2 = dw_up, p.out_ld = k, p.parts = 1;
-        if (const int rc = launch_product<kBf16, kTwoRows>(p, plan_product<kBf16, kTwoRows>(2 * n, k, m).tile, st)) return rc;
+        p.out = dw_gate, p.out2 = dw_up, p.out_ld = k;
+        if (const int rc = run_sums<kBf16, kTwoRows>(p, reinterpret_cast<float*>(b.parts), st)) return rc;
     }
     return NVFP4_OK;
 }

@@ -26,7 +26,7 @@ constexpr int kJoinThreads = 256;
 template <bool VEC>
 __global__ __launch_bounds__(kJoinThreads) void join_kernel(const float* __restrict__ part, int parts, int64_t count,
                                                             const float* __restrict__ scale, void* __restrict__ out,
-                                                            int f32) {
+                                                            int f32, int64_t first, void* __restrict__ out2) {
     constexpr int kPer = VEC ? 4 : 1;
     const int64_t at = ((int64_t)blockIdx.x * kJoinThreads + threadIdx.x) * kPer;
     if (at >= count) return;
@@ -41,8 +41,10 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(const float* __restr
         }
     }
     const float s = scale ? *scale : 1.0f;
-    if constexpr (VEC) store4(out, f32, at, 4, true, f32x4{v[0], v[1], v[2], v[3]} * s);
-    else store4(out, f32, at, 1, false, f32x4{v[0] * s, 0.0f, 0.0f, 0.0f});
+    void* to = at < first ? out : out2;
+    const int64_t place = at < first ? at : at - first;
+    if constexpr (VEC) store4(to, f32, place, 4, true, f32x4{v[0], v[1], v[2], v[3]} * s);
+    else store4(to, f32, place, 1, false, f32x4{v[0] * s, 0.0f, 0.0f, 0.0f});
 }
 
 }  // namespace
@@ -55,12 +57,13 @@ int pack_bf16_rows(const void* src, int64_t rows, int64_t width, int64_t ld, voi
     return launched();
 }
 
-int join_parts(const float* part, int parts, int64_t count, const float* scale, void* out, int f32, hipStream_t stream) {
-    const bool vec = count % 4 == 0;
+int join_parts(const float* part, int parts, int64_t count, const float* scale, void* out, int f32, int64_t first, void* out2,
+               hipStream_t stream) {
+    const bool vec = count % 4 == 0 && first % 4 == 0;
     const int64_t groups = ceil_div(vec ? count / 4 : count, kJoinThreads);
     if (groups > 0x7FFFFFFF) return NVFP4_ERR_SHAPE;
     hipLaunchKernelGGL((vec ? join_kernel<true> : join_kernel<false>), dim3((unsigned)groups), dim3(kJoinThreads), 0, stream,
-                       part, parts, count, scale, out, f32);
+                       part, parts, count, scale, out, f32, first, out2);
     return launched();
 }
 
@@ -227,7 +230,7 @@ int run_linear(const void* x, int64_t ldx, const uint8_t* q, const uint8_t* scal
             default: launch_stream<4>(t, stream);
         }
         if (const int rc = launched()) return rc;
-        return partial ? join_parts(partial, t.parts, m * n, nullptr, out, f32, stream) : NVFP4_OK;
+        return partial ? join_parts(partial, t.parts, m * n, nullptr, out, f32, m * n, nullptr, stream) : NVFP4_OK;
     }
     Carver c{static_cast<char*>(ws)};
     void* w = c.take(n * k * 2);

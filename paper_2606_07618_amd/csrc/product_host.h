@@ -49,18 +49,24 @@ int pack_bf16_rows(const void* src, int64_t rows, int64_t width, int64_t ld, voi
 // ---- the tile and the split of a product --------------------------------------------------------
 // Four tiles, from the one that moves least through LDS for what it computes to the one that gives the most
 // workgroups; and the contraction may be split over workgroups, whose sums a second kernel adds.  The rule takes the
-// least estimated time, from what a step of each tile took on this card: `alone`, microseconds of one workgroup on a
-// compute unit (latency), and `among`, microseconds a unit spends on each of many (throughput).
-//   measured, [2048, 8192] x [28672, 8192] microscaled: 315 us with the largest tile, 411, 541, 727 with the next;
-//   [64, 14336] x [4096, 14336] microscaled: 100, 60, 45, 35 us, and 17 with the smallest one split in four.
-struct TileCost { int m, n; float alone, among; };
+// least estimated time, from what each tile took on this card with contractions of 128 to 4096 values: with a workgroup
+// on few of the 256 compute units `start` + steps * `alone` microseconds, and with many workgroups `fixed` (filling
+// the pipeline, storing the tile) + steps * `among` for each 256 of them.
+//   measured, bfloat16, contraction 384: [8192, 8192] outputs 70 us with the largest tile, 86, 118, 159 with the
+//   next; [256, 2048] outputs 16.1, 9.8, 7.0, 5.5 us.
+struct TileCost { int m, n; float start, alone, fixed, among; };
 constexpr int kTiles = 4, kMostParts = 16;
-constexpr float kJoinUs = 5.0f, kJoinBytesUs = 4e6f;     // a second launch; bytes a microsecond
+constexpr float kLaunchUs = 2.0f;
+constexpr float kJoinUs = 6.0f, kJoinBytesUs = 8e6f;     // a second launch; bytes a microsecond
+constexpr float kSmaller = 0.93f;                        // a smaller tile reads more: taken where it is clearly faster
+constexpr float kLayUs = 6.0f;                           // a launch that lays scales out
 
 template <Kind KIND>
 inline const TileCost* tile_costs() {
-    static constexpr TileCost mx[kTiles] = {{256, 256, 1.8f, 2.05f}, {128, 128, 1.05f, 0.92f}, {64, 128, 0.75f, 0.60f}, {64, 64, 0.52f, 0.41f}};
-    static constexpr TileCost bf16[kTiles] = {{256, 256, 1.25f, 1.72f}, {128, 128, 0.83f, 0.54f}, {64, 128, 0.48f, 0.34f}, {64, 64, 0.40f, 0.25f}};
+    static constexpr TileCost mx[kTiles] = {{256, 256, 7.0f, 1.5f, 9.0f, 1.7f}, {128, 128, 6.3f, 1.1f, 1.9f, 0.75f},
+                                            {64, 128, 5.1f, 0.64f, 1.4f, 0.48f}, {64, 64, 4.4f, 0.40f, 1.3f, 0.31f}};
+    static constexpr TileCost bf16[kTiles] = {{256, 256, 9.8f, 1.05f, 8.5f, 1.54f}, {128, 128, 5.1f, 0.77f, 2.5f, 0.51f},
+                                              {64, 128, 4.7f, 0.38f, 1.7f, 0.34f}, {64, 64, 3.7f, 0.31f, 1.3f, 0.23f}};
     return KIND != kBf16 ? mx : bf16;
 }
 
@@ -69,10 +75,9 @@ constexpr int kFragments[kTiles][2] = {{8, 4}, {4, 4}, {2, 4}, {2, 2}};
 
 struct Plan { int tile, parts; };
 
-// kSums and kGate may be split (kPartial and kGatePartial, then joined), kTwoRows is not.
 template <Kind KIND, Out OUT>
 Plan plan_product(int64_t m, int64_t n, int64_t inner) {
-    constexpr int kStepValues = KIND != kBf16 ? 256 : 64, kHalf = OUT == kGate ? 2 : 1, kMost = OUT == kTwoRows ? 1 : kMostParts;
+    constexpr int kStepValues = KIND != kBf16 ? 256 : 64, kHalf = OUT == kGate ? 2 : 1;
     const int64_t steps = ceil_div(inner, kStepValues);
     const TileCost* costs = tile_costs<KIND>();
     Plan best = {0, 1};
@@ -80,12 +85,15 @@ Plan plan_product(int64_t m, int64_t n, int64_t inner) {
     for (int t = 0; t < kTiles; ++t) {
         if (OUT == kGate && costs[t].n < 128) continue;        // a wave holds both products of 32 columns
         const float tiles = (float)ceil_div(m, costs[t].m) * (float)ceil_div(n * kHalf, costs[t].n);
-        for (int parts = 1; parts <= kMost && (parts == 1 || steps / parts >= 8); parts *= 2) {
-            const float rounds = tiles * parts <= 256.0f ? 1.0f : (float)(int64_t)((tiles * parts + 255.0f) / 256.0f);
-            const float step = rounds * costs[t].among > costs[t].alone ? rounds * costs[t].among : costs[t].alone;
-            float us = (float)ceil_div(steps, parts) * step;
+        for (int parts = 1; parts <= kMostParts && (parts == 1 || steps / parts >= 8); parts *= 2) {
+            const float load = tiles * parts / 256.0f, own = (float)ceil_div(steps, parts);
+            const float share = load < 1.0f && costs[t].among > costs[t].alone ? (costs[t].among - costs[t].alone) * load : 0.0f;
+            const float few = costs[t].start + own * (costs[t].alone + share);
+            const float many = load > 1.0f ? kLaunchUs + (float)(int64_t)(load + 0.999f) * (costs[t].fixed + own * costs[t].among) : 0.0f;
+            float us = few > many ? few : many;
+            if (KIND != kBf16 && t == 0) us += kLayUs;
             if (parts > 1) us += kJoinUs + (float)m * (float)n * (float)(8 * kHalf * parts) / kJoinBytesUs;
-            if (us < least) least = us, best = {t, parts};
+            if (us < least * (t > best.tile ? kSmaller : 1.0f)) least = us, best = {t, parts};
         }
     }
     return best;
@@ -135,19 +143,21 @@ int launch_product(const Args& p, int tile, hipStream_t stream) {
     }
 }
 
-// out = scale * (the parts' sums [parts, count], added in order)
-int join_parts(const float* part, int parts, int64_t count, const float* scale, void* out, int f32, hipStream_t stream);
+// out = scale * (the parts' sums [parts, count], added in order); values from `first` on go to out2.
+int join_parts(const float* part, int parts, int64_t count, const float* scale, void* out, int f32, int64_t first, void* out2,
+               hipStream_t stream);
 
-// A product whose sums are stored: split where the plan says so, the parts' sums in `partial`.
-template <Kind KIND>
+// A product whose sums are stored (kSums, kTwoRows): split where the plan says so, the parts' sums in `partial`.
+template <Kind KIND, Out OUT = kSums>
 int run_sums(Args p, float* partial, hipStream_t stream) {
-    const Plan plan = plan_product<KIND, kSums>(p.m, p.n, p.inner);
+    const Plan plan = plan_product<KIND, OUT>(p.m, p.n, p.inner);
     p.parts = plan.parts;
-    if (plan.parts == 1) return launch_product<KIND, kSums>(p, plan.tile, stream);
+    if (plan.parts == 1) return launch_product<KIND, OUT>(p, plan.tile, stream);
     void* out = p.out;
     p.out = partial;
     if (const int rc = launch_product<KIND, kPartial>(p, plan.tile, stream)) return rc;
-    return join_parts(partial, plan.parts, p.m * p.n, p.scale, out, p.out_f32, stream);
+    return join_parts(partial, plan.parts, p.m * p.n, p.scale, out, p.out_f32, OUT == kTwoRows ? p.half_rows * p.n : p.m * p.n,
+                      p.out2, stream);
 }
 
 }  // namespace product_host
