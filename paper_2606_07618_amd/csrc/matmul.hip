@@ -172,10 +172,14 @@ bool valid_out(int dtype) { return dtype == NVFP4_IN_F32 || dtype == NVFP4_IN_BF
 
 // ---- y = x W^T ------------------------------------------------------------------------------
 
-constexpr int64_t kStreamRows = 512;             // see run_linear
+// Up to this many rows the weights are expanded in registers, on their way into the matrix instructions, once for each
+// 128 rows; beyond, once and for all, and multiplied as bfloat16 tiles.  Measured, expanded in registers and beforehand:
+// [14336, 4096] 16 rows 20 and 51 us, 128 rows 34 and 58, 512 rows 82 and 86, 640 rows 121 and 104;
+// [28672, 8192] 512 rows 290 and 304, 1024 rows 510 and 466.
+constexpr int64_t kStreamRows = 512;
 
 int64_t linear_workspace(int64_t m, int64_t n, int64_t k) {
-    if (m <= dot_product::kMostRows) return 0;
+    if (m <= dot_product::kMostRows) return 0;       // one launch, no workspace
     if (m <= kStreamRows) {
         const int parts = stream_product::parts(m, n, k);
         return up(m * k * 2, 256) + up(m * 4, 256) + (parts > 1 ? up(parts * m * n * 4, 256) : 0);

@@ -292,19 +292,27 @@ __global__ __launch_bounds__(256 * kWavesK, kWavesK) void stream_kernel(Args p) 
 
 inline int rows_of(int64_t m) { return m <= 32 ? 1 : m <= 64 ? 2 : 4; }
 inline int tiles_m(int64_t m) { return (int)((m + 127) / 128); }
-// A workgroup takes a compute unit's LDS: parts of the contraction, of at least 1024 values, until 256 units
-// have work.
-inline int parts(int64_t m, int64_t n, int64_t k) {
-    const int64_t groups = (n + kRowsN - 1) / kRowsN * tiles_m(m);
-    int64_t want = (256 + groups / 2) / (groups ? groups : 1);
-    if (want > k / 1024) want = k / 1024;
-    if (want > 16) want = 16;
-    return want < 1 ? 1 : (int)want;
-}
+
 // Values of a part: halves of whole groups.
 inline int part_values(int64_t k, int parts) {
     constexpr int64_t kUnit = kGroup * kWavesK;
     return (int)(((k + parts - 1) / parts + kUnit - 1) / kUnit * kUnit);
+}
+
+// A workgroup takes a compute unit's LDS, so 256 of them work at a time, and a value of the contraction takes each 5.3, 7
+// or 10 ns (32, 64 or 128 rows).  Parts of it, of at least 1024 values, where rounds and the parts' sums then take less
+// ([384, 14336] x [4096, 14336]: 102 us in three parts of 288 workgroups together, 80 in two of 192).
+inline int parts(int64_t m, int64_t n, int64_t k) {
+    const int64_t groups = (n + kRowsN - 1) / kRowsN * tiles_m(m);
+    const float us = (rows_of(m) == 1 ? 0.0053f : rows_of(m) == 2 ? 0.007f : 0.01f);
+    int best = 1;
+    float least = 3e38f;
+    for (int p = 1; p <= 16 && (p == 1 || k / p >= 1024); ++p) {
+        const float took = (float)((groups * p + 255) / 256) * (float)part_values(k, p) * us +
+                           (p > 1 ? 6.0f + (float)m * (float)n * (float)(8 * p) / 4e6f : 0.0f);
+        if (took < least) least = took, best = p;
+    }
+    return best;
 }
 
 }  // namespace stream_product
