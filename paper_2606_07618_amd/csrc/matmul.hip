@@ -326,9 +326,9 @@ __global__ __launch_bounds__(kScaleThreads) void lay_scales_kernel(Scales a, Sca
 
 int64_t scale_bytes(int64_t rows, int64_t blocks) { return up(rows, 128) * ceil_div(blocks, 8) * 8; }
 
-// Few rows, and no tiles to keep the chip busy with whole contractions.
+// Few rows: the kernel for them where tiles, which must be many or be split to keep the chip busy, would take longer.
 bool thin(int64_t m, int64_t n, int64_t blocks) {
-    return m <= thin_product::kRows && plan_product<kMx, kSums>(m, n, blocks * 32).parts > 1;
+    return m <= thin_product::kRows && thin_product::us(m, n, blocks * 32) < plan_product<kMx, kSums>(m, n, blocks * 32).us;
 }
 
 // The largest tile takes its scales laid out, and so do the others where rows of scales are no whole words.

@@ -73,15 +73,14 @@ inline const TileCost* tile_costs() {
 // Fragments of a wave's rows of A and of B.
 constexpr int kFragments[kTiles][2] = {{8, 4}, {4, 4}, {2, 4}, {2, 2}};
 
-struct Plan { int tile, parts; };
+struct Plan { int tile, parts; float us; };
 
 template <Kind KIND, Out OUT>
 Plan plan_product(int64_t m, int64_t n, int64_t inner) {
     constexpr int kStepValues = KIND != kBf16 ? 256 : 64, kHalf = OUT == kGate ? 2 : 1;
     const int64_t steps = ceil_div(inner, kStepValues);
     const TileCost* costs = tile_costs<KIND>();
-    Plan best = {0, 1};
-    float least = 3e38f;
+    Plan best = {0, 1, 3e38f};
     for (int t = 0; t < kTiles; ++t) {
         if (OUT == kGate && costs[t].n < 128) continue;        // a wave holds both products of 32 columns
         const float tiles = (float)ceil_div(m, costs[t].m) * (float)ceil_div(n * kHalf, costs[t].n);
@@ -93,7 +92,7 @@ Plan plan_product(int64_t m, int64_t n, int64_t inner) {
             float us = few > many ? few : many;
             if (KIND != kBf16 && t == 0) us += kLayUs;
             if (parts > 1) us += kJoinUs + (float)m * (float)n * (float)(8 * kHalf * parts) / kJoinBytesUs;
-            if (us < least * (t > best.tile ? kSmaller : 1.0f)) least = us, best = {t, parts};
+            if (us < best.us * (t > best.tile ? kSmaller : 1.0f)) best = {t, parts, us};
         }
     }
     return best;

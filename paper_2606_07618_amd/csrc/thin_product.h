@@ -1,9 +1,10 @@
-// Microscaled products with few rows of activations, where the tiles' contraction would have to be split and joined by
-// a second launch: nothing is staged and nothing waits for a neighbour.  A workgroup owns 16 weight rows; its waves
+// Microscaled products with few rows of activations and weights too small to keep the chip busy with tiles: nothing is
+// staged and nothing waits for a neighbour.  A workgroup owns 16 weight rows; its waves
 // take turns along the contraction, each loading weights straight into the registers of its matrix instructions (16
 // rows by four lanes of 16 bytes), the activations' side of the instruction from the caches, kUnroll such pieces in
-// flight; one exchange through LDS adds the waves' sums, in a fixed order.  [4096, 14336], four rows: 11.5 us, 16.3 with
-// tiles; with tiles enough, [28672, 8192], 39 and 31.
+// flight; one exchange through LDS adds the waves' sums, in a fixed order.  One row, [4096, 4096]: 5.2 us (1.7 TB/s,
+// most of it the way to memory and back), 11.2 with tiles; [4096, 14336] 10.9 (2.9 TB/s) and 15; with tiles enough,
+// [28672, 8192], 36 and 31.
 // Lanes past the operands' ends load nothing (kOutside) and multiply zeros.
 #pragma once
 
@@ -64,6 +65,9 @@ __global__ __launch_bounds__(kWaves * kLanes) void thin_kernel(Args p) {
     const int64_t n = n0 + g * 4;
     if (m_in) store4(p.out, p.out_f32, (int64_t)i * p.n + n, p.n - n, p.n % 4 == 0, acc);
 }
+
+// Estimated microseconds, from the times above and 16 rows' (6.7, 16.5 and 55).
+inline float us(int64_t m, int64_t n, int64_t k) { return 2.0f + (float)n * (float)k * (1.6e-7f + 0.7e-8f * (float)m); }
 
 inline void launch_thin(const Args& p, hipStream_t stream) {
     hipLaunchKernelGGL(thin_kernel, dim3((unsigned)((p.n + 15) / 16)), dim3(kWaves * kLanes), 0, stream, p);
