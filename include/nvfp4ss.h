@@ -364,7 +364,7 @@ int mxfp4_dequant(const uint8_t* q, const uint8_t* scales, int64_t rows, int64_t
  * product; weights are [n, k] row-major as the quantizers take them.  Sums are held in binary32
  * and rounded once to the output, [m, n] or [m, k] contiguous, bfloat16 or binary32 (out_dtype).
  * The order of a sum depends on the sizes alone, so results are deterministic.
- *   - m, n or k may be 0 (a sum over nothing is 0).  n, k <= 2^20, row strides <= 2^21, else
+ *   - m, n or k may be 0 (a sum over nothing is 0).  m <= 2^36, n, k <= 2^20, row strides <= 2^21, else
  *     NVFP4_ERR_SHAPE.
  *   - x, dy: bfloat16, rows ldx / ld elements apart (>= their width).
  *   - Pointers to values and outputs are 16-byte aligned, E8M0 scales 4-byte, the workspace 256-byte;

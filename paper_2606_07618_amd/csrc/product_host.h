@@ -16,7 +16,7 @@ using namespace tile_product;
 // A tile's loads take 32-bit offsets from its first row: 256 rows of this many bfloat16 values stay
 // below the 2 GiB window.
 constexpr int64_t kMaxWidth = (int64_t)1 << 20, kMaxLd = (int64_t)1 << 21;
-constexpr int64_t kMaxRows = (int64_t)1 << 40;
+constexpr int64_t kMaxRows = (int64_t)1 << 36;      // workspace sizes stay within 63 bits
 
 inline bool aligned(const void* p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 inline int64_t up(int64_t v, int64_t unit) { return (v + unit - 1) / unit * unit; }
