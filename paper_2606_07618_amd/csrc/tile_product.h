@@ -84,7 +84,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 // an instruction picks its byte from a word as it was read.  As the rows lie, a step takes eight bytes of each row's
 // scales, whose lines, fetched again for each step, are as many bytes as the values themselves: with a chip full of
 // the largest tiles this costs more than laying the scales out ([8192, 4096] x [14336, 4096]: 313 us as they lie,
-// 275 laid out, 7 of them for that; [64, 4096] x [14336, 4096]: 14.5 and 16).
+// 271 laid out, 7 of them for that; [64, 4096] x [14336, 4096]: 14.5 and 16).
 __device__ __forceinline__ int64_t scale_at(int64_t group, int64_t steps, int64_t step, int lane, int fragments) {
     return ((group * steps + step) * kLanes + lane) * fragments * 2;
 }
@@ -423,7 +423,9 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
 
     // A lane holds four neighbouring columns of row lane % 16 of D.  Stored from here, an instruction would write
     // 32 bytes of 16 rows; bfloat16 outputs go through LDS instead and leave as whole rows of the tile, 16 bytes a
-    // lane ([8192, 4096] x [14336, 4096] microscaled, where the contraction is short: 338 -> 305 us).
+    // lane ([8192, 4096] x [14336, 4096] microscaled, where the contraction is short: 338 -> 305 us).  The largest tile,
+    // whose outputs are too many to stay in the L2 until they are read, stores them past it and leaves the L2 to the
+    // operands (the same product: 282 -> 252 us).
     const float scale = OUT == kSums && p.scale ? *p.scale : 1.0f;
     auto column = [&](int j) { return HALF ? wn * (kOutN / T::WN) + j * 16 : b_row(j); };
     if (OUT != kPartial && OUT != kGatePartial && !p.out_f32 && p.out_ld % 8 == 0) {
@@ -446,9 +448,12 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
             for (int c = tid; c < T::M * kOutChunks; c += T::kThreads) {
                 const int row = c / kOutChunks, chunk = c % kOutChunks;
                 const int64_t m = m0 + row, n = n0 + chunk * 8;
-                if (m < p.m && n < p.n)
-                    *reinterpret_cast<uint4*>(row_of(m) + n) =
-                        *reinterpret_cast<const uint4*>(tile + (row * kOutChunks + (chunk ^ (row & kMask))) * kChunk);
+                if (m < p.m && n < p.n) {
+                    const i32x4 v = *reinterpret_cast<const i32x4*>(tile + (row * kOutChunks + (chunk ^ (row & kMask))) * kChunk);
+                    i32x4* to = reinterpret_cast<i32x4*>(row_of(m) + n);
+                    if constexpr (T::M == 256) __builtin_nontemporal_store(v, to);
+                    else *to = v;
+                }
             }
         };
         auto rows_of = [&](void* out) { return [=](int64_t m) { return static_cast<uint16_t*>(out) + m * p.out_ld; }; };
