@@ -7,7 +7,7 @@
 // scale, so scales cost an instruction a block.
 //   y[m][n] = S sum_blocks s sum_j q_j x_j, sums in binary32.
 // (A matrix instruction would need the weights times their scales, twice the conversions, and of its 16 columns 12
-// to 15 would be empty: one row, [14336, 4096], 14.8 us in place of 9.9.)
+// to 15 would be empty: one row, [4096, 14336], 14.8 us in place of 9.0, 3.7 TB/s.)
 #pragma once
 
 #include "tile_product.h"

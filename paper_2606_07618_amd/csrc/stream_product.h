@@ -15,7 +15,7 @@
 // Weights are loaded by groups of 256 values of a row, whole lines of 128 bytes, and so are the group's scales
 // where their rows allow it: visited in smaller pieces, a line would have left the L1 between two visits.
 // Few weight rows: the contraction is split over workgroups as well, whose sums a second kernel adds in order.
-// [48, 8192] x [28672, 8192]: 52 us in the kernel and 5 in scaling the rows (2.6 TB/s, 0.43 PFLOP/s); 231 us with the
+// [48, 8192] x [28672, 8192]: 57 us, 5 of them scaling the rows (2.4 TB/s, 0.39 PFLOP/s); 231 us with the
 // weights expanded beforehand.
 #pragma once
 
