@@ -71,13 +71,18 @@ def _output(out, shape, dtype, like, what="out"):
     return out
 
 
-def _workspace(nbytes, ws, device, where):
-    """(pointer owner, bytes) of a workspace of at least nbytes; a caller's own is passed on as it is."""
+def _workspace(nbytes, ws, like, where):
+    """(pointer owner, bytes) of a workspace of at least nbytes on like's device.  The kernels write a caller's
+    own from its first byte on, so it must be a run of that device's memory."""
     if nbytes < 0:
         raise NVFP4Error(int(nbytes), where)
-    if ws is None and nbytes:
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    return ws, 0 if ws is None else ws.numel() * ws.element_size()
+    if nbytes == 0:
+        return None, 0
+    if ws is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=like.device), nbytes
+    if not (ws.is_cuda and ws.is_contiguous() and ws.get_device() == like.get_device()):
+        raise ValueError("ws must be a contiguous tensor on the operands' device")
+    return ws, ws.numel() * ws.element_size()
 
 
 def _check(rc, where):
@@ -143,7 +148,7 @@ def mx_matmul(a, b, out_dtype: torch.dtype = torch.bfloat16, out: torch.Tensor |
     _same_device(aq, bq)
     out = _output(out, (m, n), out_dtype, aq)
     k = MX_BLOCK * kb
-    ws, nbytes = _workspace(mxfp4_matmul_workspace_bytes(m, n, k), ws, aq.device, "mxfp4_matmul_workspace_bytes")
+    ws, nbytes = _workspace(mxfp4_matmul_workspace_bytes(m, n, k), ws, aq, "mxfp4_matmul_workspace_bytes")
     _check(mxfp4_matmul(_ptr(aq), _ptr(asc), _ptr(bq), _ptr(bsc), m, n, k, dt, _ptr(out), _ptr(ws), nbytes,
                         _stream(aq)), "mxfp4_matmul")
     return out
@@ -165,7 +170,7 @@ def mx_matmul_grad_input(dy: torch.Tensor, q: torch.Tensor, scales: torch.Tensor
         raise ValueError(f"cols must lie in the last of the {kb} blocks of a row")
     out = _output(out, (m, cols), out_dtype, dy)
     _same_device(dy, q)
-    ws, nbytes = _workspace(mxfp4_matmul_grad_input_workspace_bytes(m, n, cols, ld), ws, dy.device,
+    ws, nbytes = _workspace(mxfp4_matmul_grad_input_workspace_bytes(m, n, cols, ld), ws, dy,
                             "mxfp4_matmul_grad_input_workspace_bytes")
     _check(mxfp4_matmul_grad_input(_ptr(dy), ld, _ptr(q), _ptr(scales), m, n, cols, dt, _ptr(out), _ptr(ws), nbytes,
                                    _stream(dy)), "mxfp4_matmul_grad_input")
@@ -200,7 +205,7 @@ def matmul(x: torch.Tensor, q: torch.Tensor, scales: torch.Tensor, S: torch.Tens
     if x.shape[1] != k:
         raise ValueError("x must be [m, k] for weights [n, k]")
     out = _output(out, (m, n), out_dtype, x)
-    ws, nbytes = _workspace(nvfp4_matmul_workspace_bytes(m, n, k), ws, x.device, "nvfp4_matmul_workspace_bytes")
+    ws, nbytes = _workspace(nvfp4_matmul_workspace_bytes(m, n, k), ws, x, "nvfp4_matmul_workspace_bytes")
     _check(nvfp4_matmul(_ptr(x), ldx, _ptr(q), _ptr(scales), block, _ptr(S), m, n, k, dt, _ptr(out), _ptr(ws), nbytes,
                         _stream(x)), "nvfp4_matmul")
     return out
@@ -217,7 +222,7 @@ def matmul_grad_input(dy: torch.Tensor, q: torch.Tensor, scales: torch.Tensor, S
     if dy.shape[1] != n:
         raise ValueError("dy must be [m, n] for weights [n, k]")
     out = _output(out, (m, k), out_dtype, dy)
-    ws, nbytes = _workspace(nvfp4_matmul_grad_input_workspace_bytes(m, n, k, ld), ws, dy.device,
+    ws, nbytes = _workspace(nvfp4_matmul_grad_input_workspace_bytes(m, n, k, ld), ws, dy,
                             "nvfp4_matmul_grad_input_workspace_bytes")
     _check(nvfp4_matmul_grad_input(_ptr(dy), ld, _ptr(q), _ptr(scales), block, _ptr(S), m, n, k, dt, _ptr(out),
                                    _ptr(ws), nbytes, _stream(dy)), "nvfp4_matmul_grad_input")
@@ -247,7 +252,7 @@ def swiglu_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, save: 
     if save:
         gate = _output(gate, (m, n), torch.bfloat16, x, "gate")
         up = _output(up, (m, n), torch.bfloat16, x, "up")
-    ws, nbytes = _workspace(nvfp4_swiglu_ffn_workspace_bytes(m, n, k, ldx, ldw), ws, x.device,
+    ws, nbytes = _workspace(nvfp4_swiglu_ffn_workspace_bytes(m, n, k, ldx, ldw), ws, x,
                             "nvfp4_swiglu_ffn_workspace_bytes")
     _check(nvfp4_swiglu_ffn(_ptr(x), ldx, _ptr(w_gate), _ptr(w_up), ldw, m, n, k, _ptr(h), _ptr(gate), _ptr(up),
                             _ptr(ws), nbytes, _stream(x)), "nvfp4_swiglu_ffn")
@@ -270,7 +275,7 @@ def swiglu_ffn_backward(dh: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor,
     dwg = _output(dwg, (n, k), torch.bfloat16, x, "dw_gate") if need_w else None
     dwu = _output(dwu, (n, k), torch.bfloat16, x, "dw_up") if need_w else None
     _same_device(x, dh, gate, up)
-    ws, nbytes = _workspace(nvfp4_swiglu_ffn_backward_workspace_bytes(m, n, k, ldx, ldw), ws, x.device,
+    ws, nbytes = _workspace(nvfp4_swiglu_ffn_backward_workspace_bytes(m, n, k, ldx, ldw), ws, x,
                             "nvfp4_swiglu_ffn_backward_workspace_bytes")
     _check(nvfp4_swiglu_ffn_backward(_ptr(dh), _ptr(x), ldx, _ptr(w_gate), _ptr(w_up), ldw, _ptr(gate), _ptr(up), m, n,
                                      k, _ptr(dx), _ptr(dwg), _ptr(dwu), _ptr(ws), nbytes, _stream(x)),
