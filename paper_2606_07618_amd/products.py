@@ -184,9 +184,10 @@ def _nvfp4_weights(x, q, scales, S, block):
         raise ValueError("q must be 2-D [n, k/2]")
     n, k = q.shape[0], q.shape[1] * 2
     _plain(q, (n, k // 2), torch.uint8, "q")
+    # by shape: a flat buffer of swizzled scales may hold as many bytes
     if not (scales.is_cuda and scales.dtype == torch.uint8 and scales.is_contiguous()
-            and (block <= 0 or scales.numel() == n * (k // block))):
-        raise ValueError("scales must be a contiguous uint8 device tensor [n, k/block]")
+            and (block <= 0 or scales.shape == (n, k // block))):
+        raise ValueError("scales must be a contiguous uint8 device tensor [n, k/block], row-major")
     if not (S.is_cuda and S.dtype == torch.float32 and S.numel() >= 1):
         raise ValueError("S must be a float32 device tensor")
     _same_device(x, q, scales, S)
