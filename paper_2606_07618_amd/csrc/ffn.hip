@@ -310,7 +310,7 @@ int nvfp4_swiglu_ffn_backward(const void* dh, const void* x, int64_t ldx, const 
     const bool inputs = m > 0 && n > 0;
     const bool want_x = dx && m > 0 && k > 0, want_w = dw_gate && n > 0 && k > 0;
     if (!dw_gate != !dw_up) return NVFP4_ERR_NULL;
-    if (!dx && !dw_gate && m * n * k > 0) return NVFP4_ERR_NULL;
+    if (!dx && !dw_gate && m > 0 && n > 0 && k > 0) return NVFP4_ERR_NULL;
     if (!want_x && !want_w) return NVFP4_OK;
     if (inputs && (!dh || !gate || !up_in || (want_x && (!w_gate || !w_up)) || (want_w && !x))) return NVFP4_ERR_NULL;
     for (const void* p : {dh, x, w_gate, w_up, gate, up_in, (const void*)dx, (const void*)dw_gate, (const void*)dw_up})
