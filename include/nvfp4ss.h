@@ -351,11 +351,12 @@ int nvfp4_sum_f64(const double* v, int64_t n, double* out, void* workspace,
 /* scale = 2^E, E = floor(log2 max|x|) - 2 over the block, clamped to -127 .. 127 (code 0 for a block
  * of zeros); q = RNE_E2M1(x / 2^E), saturating at 6, the sign kept.  A block that holds an infinity
  * or a NaN gets code 255 (its nibbles are unspecified).  x: [rows, cols] contiguous, binary32 or
- * bfloat16, 16-byte aligned, any cols.  No workspace; one kernel. */
+ * bfloat16, 16-byte aligned, any cols, at most 2^35 - 2^11
+ * values in whole blocks (what one launch holds), else NVFP4_ERR_SHAPE.  No workspace; one kernel. */
 int mxfp4_quant(const void* x, int dtype, int64_t rows, int64_t cols, uint8_t* q, uint8_t* scales, void* stream);
 
 /* x_hat = q 2^E into out [rows, cols], binary32 or bfloat16 (both exact; above their range infinity),
- * 16-byte aligned. */
+ * 16-byte aligned.  As many values as mxfp4_quant. */
 int mxfp4_dequant(const uint8_t* q, const uint8_t* scales, int64_t rows, int64_t cols, int out_dtype, void* out,
                   void* stream);
 
@@ -364,8 +365,8 @@ int mxfp4_dequant(const uint8_t* q, const uint8_t* scales, int64_t rows, int64_t
  * product; weights are [n, k] row-major as the quantizers take them.  Sums are held in binary32
  * and rounded once to the output, [m, n] or [m, k] contiguous, bfloat16 or binary32 (out_dtype).
  * The order of a sum depends on the sizes alone, so results are deterministic.
- *   - m, n or k may be 0 (a sum over nothing is 0).  m <= 2^36, n, k <= 2^20, row strides <= 2^21, else
- *     NVFP4_ERR_SHAPE.
+ *   - m, n or k may be 0 (a sum over nothing is 0).  m <= 2^36, n, k <= 2^20, row strides <= 2^21, and
+ *     what one launch holds (2^32 threads: from 2^36 outputs or 2^35 weights on it may not do); else NVFP4_ERR_SHAPE.
  *   - x, dy: bfloat16, rows ldx / ld elements apart (>= their width).
  *   - Pointers to values and outputs are 16-byte aligned, E8M0 scales 4-byte, the workspace 256-byte;
  *     else NVFP4_ERR_ALIGN.

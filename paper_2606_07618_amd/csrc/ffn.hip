@@ -147,19 +147,27 @@ __global__ __launch_bounds__(kEdgeThreads) void prepare_kernel(Prepare p) {
     }
 }
 
-int prepare(Prepare p, hipStream_t stream) {
+int64_t turn_tiles(int64_t rows, int64_t columns) { return ceil_div(rows, kTurnRows) * ceil_div(columns, kTurnColumns); }
+
+// The tiles of p, all of them; a launch takes most_groups(kEdgeThreads) of them.
+int64_t count_tiles(Prepare& p) {
     int64_t tiles = 0;
     const auto count = [&](int64_t rows, int64_t columns, uint32_t& across, uint32_t& all) {
-        const int64_t a = ceil_div(columns, kTurnColumns), n = a * ceil_div(rows, kTurnRows);
-        across = (uint32_t)a, all = (uint32_t)n, tiles += n;
-        return tiles <= 0x7FFFFFFF;
+        across = (uint32_t)ceil_div(columns, kTurnColumns), all = (uint32_t)turn_tiles(rows, columns);
+        tiles += turn_tiles(rows, columns);
     };
-    if (!count(p.gates.m, p.gates.n, p.gates.tiles_n, p.gates.tiles)) return NVFP4_ERR_SHAPE;
+    count(p.gates.m, p.gates.n, p.gates.tiles_n, p.gates.tiles);
     for (Turn& t : p.turns) {
         t.vec = t.width % 8 == 0 && t.ld % 8 == 0;
-        if (!count(t.fill, t.width, t.tiles_c, t.tiles)) return NVFP4_ERR_SHAPE;
+        count(t.fill, t.width, t.tiles_c, t.tiles);
     }
+    return tiles;
+}
+
+int prepare(Prepare& p, hipStream_t stream) {
+    const int64_t tiles = count_tiles(p);
     if (tiles == 0) return NVFP4_OK;
+    if (!launchable(tiles, kEdgeThreads)) return NVFP4_ERR_SHAPE;
     hipLaunchKernelGGL(prepare_kernel, dim3((unsigned)tiles), dim3(kEdgeThreads), 0, stream, p);
     return launched();
 }
@@ -228,6 +236,17 @@ int64_t backward_sections(void* workspace, int64_t m, int64_t n, int64_t k, Back
     return c.at;
 }
 
+bool forward_launchable(int64_t m, int64_t n, int64_t k) {
+    return m <= dot_product::kMostRows || product_launchable<kBf16, kGate>(m, n, k);
+}
+
+bool backward_launchable(int64_t m, int64_t n, int64_t k, bool want_x, bool want_w) {
+    const int64_t half = up(n, 64);
+    const int64_t tiles = turn_tiles(m, n) + (want_x ? 2 * turn_tiles(half, k) : 0) + (want_w ? turn_tiles(up(m, 64), k) : 0);
+    return launchable(tiles, kEdgeThreads) && (!want_x || product_launchable<kBf16>(m, k, 2 * half)) &&
+           (!want_w || product_launchable<kBf16, kTwoRows>(2 * n, k, m));
+}
+
 int check_call(int64_t m, int64_t n, int64_t k, int64_t ldx, int64_t ldw) {
     if (const int rc = check_dims(m, n, k)) return rc;
     if (ldx < k || ldw < k || ldx > kMaxLd || ldw > kMaxLd) return NVFP4_ERR_SHAPE;
@@ -252,6 +271,7 @@ int nvfp4_swiglu_ffn(const void* x, int64_t ldx, const void* w_gate, const void*
                      int64_t n, int64_t k, void* h, void* gate, void* up_out, void* workspace,
                      size_t workspace_bytes, void* stream) {
     if (const int rc = check_call(m, n, k, ldx, ldw)) return rc;
+    if (!forward_launchable(m, n, k)) return NVFP4_ERR_SHAPE;
     if (m == 0 || n == 0) return NVFP4_OK;
     if (!h || (k > 0 && (!x || !w_gate || !w_up)) || !gate != !up_out) return NVFP4_ERR_NULL;
     if (!aligned(x, 16) || !aligned(w_gate, 16) || !aligned(w_up, 16) || !aligned(h, 16) || !aligned(gate, 16) ||
@@ -290,7 +310,7 @@ int nvfp4_swiglu_ffn(const void* x, int64_t ldx, const void* w_gate, const void*
     if (const int rc = launch_product<kBf16, kGatePartial>(p, plan.tile, st)) return rc;
     const bool vec = n % 4 == 0;
     const int64_t groups = ceil_div(vec ? m * n / 4 : m * n, kEdgeThreads);
-    if (groups > 0x7FFFFFFF) return NVFP4_ERR_SHAPE;
+    if (!launchable(groups, kEdgeThreads)) return NVFP4_ERR_SHAPE;
     hipLaunchKernelGGL((vec ? join_gate_kernel<true> : join_gate_kernel<false>), dim3((unsigned)groups), dim3(kEdgeThreads), 0, st,
                        parts, plan.parts, m * n, h, gate, up_out);
     return launched();
@@ -312,6 +332,7 @@ int nvfp4_swiglu_ffn_backward(const void* dh, const void* x, int64_t ldx, const 
     if (!dw_gate != !dw_up) return NVFP4_ERR_NULL;
     if (!dx && !dw_gate && m > 0 && n > 0 && k > 0) return NVFP4_ERR_NULL;
     if (!want_x && !want_w) return NVFP4_OK;
+    if (!backward_launchable(m, n, k, want_x, want_w)) return NVFP4_ERR_SHAPE;
     if (inputs && (!dh || !gate || !up_in || (want_x && (!w_gate || !w_up)) || (want_w && !x))) return NVFP4_ERR_NULL;
     for (const void* p : {dh, x, w_gate, w_up, gate, up_in, (const void*)dx, (const void*)dw_gate, (const void*)dw_up})
         if (!aligned(p, 16)) return NVFP4_ERR_ALIGN;

@@ -21,8 +21,6 @@ __global__ __launch_bounds__(kPackThreads) void pack_kernel(const uint16_t* __re
 }
 
 // Sums of parts of the contraction.
-constexpr int kJoinThreads = 256;
-
 template <bool VEC>
 __global__ __launch_bounds__(kJoinThreads) void join_kernel(const float* __restrict__ part, int parts, int64_t count,
                                                             const float* __restrict__ scale, void* __restrict__ out,
@@ -61,7 +59,7 @@ int join_parts(const float* part, int parts, int64_t count, const float* scale, 
                hipStream_t stream) {
     const bool vec = count % 4 == 0 && first % 4 == 0;
     const int64_t groups = ceil_div(vec ? count / 4 : count, kJoinThreads);
-    if (groups > 0x7FFFFFFF) return NVFP4_ERR_SHAPE;
+    if (!launchable(groups, kJoinThreads)) return NVFP4_ERR_SHAPE;
     hipLaunchKernelGGL((vec ? join_kernel<true> : join_kernel<false>), dim3((unsigned)groups), dim3(kJoinThreads), 0, stream,
                        part, parts, count, scale, out, f32, first, out2);
     return launched();
@@ -100,10 +98,11 @@ __global__ __launch_bounds__(kExpandThreads) void expand_kernel(const uint32_t* 
     out[at] = expand8<kBf16>(q[at], scales[at >> shift]);
 }
 
+int64_t expand_groups(int64_t n, int64_t k) { return n * ceil_div(k / 8, kExpandThreads); }
+
 int expand(const uint8_t* q, const uint8_t* scales, int64_t n, int64_t k, int block, void* out, hipStream_t stream) {
     const int64_t row_units = k / 8, row_groups = ceil_div(row_units, kExpandThreads);
     if (n * row_units == 0) return NVFP4_OK;
-    if (n * row_groups > 0x7FFFFFFF) return NVFP4_ERR_SHAPE;
     int shift = 1;
     while (8 << shift < block) ++shift;
     hipLaunchKernelGGL(expand_kernel, dim3((unsigned)(n * row_groups)), dim3(kExpandThreads), 0, stream,
@@ -155,12 +154,13 @@ __global__ __launch_bounds__(kExpandThreads) void expand_turned_kernel(const uin
     }
 }
 
+int64_t turned_groups(int64_t n, int64_t k) { return ceil_div(n, kTurnN) * ceil_div(k, kTurnK); }
+
 template <Kind KIND>
 int expand_turned(const uint8_t* q, const uint8_t* scales, int64_t n, int64_t k, int block, int64_t ld, void* out,
                   hipStream_t stream) {
-    const int64_t tiles_k = ceil_div(k, kTurnK), tiles = ceil_div(n, kTurnN) * tiles_k;
+    const int64_t tiles_k = ceil_div(k, kTurnK), tiles = turned_groups(n, k);
     if (tiles == 0) return NVFP4_OK;
-    if (tiles > 0x7FFFFFFF) return NVFP4_ERR_SHAPE;
     int shift = 4;
     while (1 << shift < block) ++shift;
     hipLaunchKernelGGL((expand_turned_kernel<KIND>), dim3((unsigned)tiles), dim3(kExpandThreads), 0, stream, q, scales, n,
@@ -185,6 +185,10 @@ int64_t linear_workspace(int64_t m, int64_t n, int64_t k) {
         return up(m * k * 2, 256) + up(m * 4, 256) + (parts > 1 ? up(parts * m * n * 4, 256) : 0);
     }
     return up(n * k * 2, 256) + parts_bytes<kBf16>(m, n, k);
+}
+
+bool linear_launchable(int64_t m, int64_t n, int64_t k) {
+    return m <= kStreamRows || (launchable(expand_groups(n, k), kExpandThreads) && product_launchable<kBf16>(m, n, k));
 }
 
 template <int MF>
@@ -257,6 +261,10 @@ int64_t grad_workspace(int64_t m, int64_t n, int64_t k, int64_t k32, int64_t ld)
     return c.at + parts_bytes<kBf16>(m, k, n);
 }
 
+bool grad_launchable(int64_t m, int64_t n, int64_t k, int64_t k32) {
+    return launchable(turned_groups(n, k32), kExpandThreads) && product_launchable<kBf16>(m, k, n);
+}
+
 // k32: the width of the weights' rows (k filled up to whole blocks); dx has k columns.
 template <Kind KIND>
 int run_grad(const void* dy, int64_t ld, const uint8_t* q, const uint8_t* scales, int block, const float* S, int64_t m,
@@ -324,6 +332,10 @@ __global__ __launch_bounds__(kScaleThreads) void lay_scales_kernel(Scales a, Sca
     }
 }
 
+int64_t lay_groups(int64_t m, int64_t n, int64_t blocks, const int* fragments) {
+    return (ceil_div(m, 16 * fragments[0]) + ceil_div(n, 16 * fragments[1])) * ceil_div(ceil_div(blocks, 8) * 16, kScaleThreads);
+}
+
 int64_t scale_bytes(int64_t rows, int64_t blocks) { return up(rows, 128) * ceil_div(blocks, 8) * 8; }
 
 // Few rows: the kernel for them where tiles, which must be many or be split to keep the chip busy, would take longer.
@@ -334,6 +346,12 @@ bool thin(int64_t m, int64_t n, int64_t blocks) {
 // The largest tile takes its scales laid out, and so do the others where rows of scales are no whole words.
 bool lays_scales(int64_t m, int64_t n, int64_t blocks) {
     return blocks % 4 != 0 || plan_product<kMx, kSums>(m, n, blocks * 32).tile == 0;
+}
+
+bool mx_launchable(int64_t m, int64_t n, int64_t blocks) {
+    const int* fragments = kFragments[plan_product<kMx, kSums>(m, n, blocks * 32).tile];
+    return thin(m, n, blocks) || (product_launchable<kMx>(m, n, blocks * 32) &&
+                                  (!lays_scales(m, n, blocks) || launchable(lay_groups(m, n, blocks, fragments), kScaleThreads)));
 }
 
 int64_t mx_workspace(int64_t m, int64_t n, int64_t blocks) {
@@ -367,8 +385,7 @@ int run_mx(const uint8_t* aq, const uint8_t* as, const uint8_t* bq, const uint8_
         return Scales{from, static_cast<uint8_t*>(c.take(scale_bytes(rows, blocks))), rows, ceil_div(rows, 16 * f), f};
     };
     const Scales a = scales(as, m, fragments[0]), b = scales(bs, n, fragments[1]);
-    const int64_t groups = (a.groups + b.groups) * ceil_div(steps * 16, kScaleThreads);
-    if (groups > 0x7FFFFFFF) return NVFP4_ERR_SHAPE;
+    const int64_t groups = lay_groups(m, n, blocks, fragments);
     if (groups > 0) {
         hipLaunchKernelGGL((blocks % 4 == 0 ? lay_scales_kernel<true> : lay_scales_kernel<false>), dim3((unsigned)groups), dim3(kScaleThreads), 0, stream, a, b, blocks, steps);
         if (const int rc = launched()) return rc;
@@ -402,7 +419,7 @@ int nvfp4_matmul(const void* x, int64_t ldx, const uint8_t* q, const uint8_t* sc
                  size_t workspace_bytes, void* stream) {
     if (!valid_out(out_dtype)) return NVFP4_ERR_DTYPE;
     if (const int rc = check_nvfp4(m, n, k, block)) return rc;
-    if (ldx < k || ldx > kMaxLd) return NVFP4_ERR_SHAPE;
+    if (ldx < k || ldx > kMaxLd || !linear_launchable(m, n, k)) return NVFP4_ERR_SHAPE;
     if (m == 0 || n == 0) return NVFP4_OK;
     if (!out || !tensor_scale || (k > 0 && (!x || !q || !scales))) return NVFP4_ERR_NULL;
     if (!aligned(x, 16) || ldx % 8 || !aligned(q, 16) || !aligned(out, 16) || !aligned(tensor_scale, 4))
@@ -421,7 +438,7 @@ int nvfp4_matmul_grad_input(const void* dy, int64_t ld, const uint8_t* q, const 
                             void* workspace, size_t workspace_bytes, void* stream) {
     if (!valid_out(out_dtype)) return NVFP4_ERR_DTYPE;
     if (const int rc = check_nvfp4(m, n, k, block)) return rc;
-    if (ld < n || ld > kMaxLd) return NVFP4_ERR_SHAPE;
+    if (ld < n || ld > kMaxLd || !grad_launchable(m, n, k, k)) return NVFP4_ERR_SHAPE;
     if (m == 0 || k == 0) return NVFP4_OK;
     if (!dx || !tensor_scale || (n > 0 && (!dy || !q || !scales))) return NVFP4_ERR_NULL;
     if (!aligned(dy, 16) || !aligned(q, 16) || !aligned(dx, 16) || !aligned(tensor_scale, 4)) return NVFP4_ERR_ALIGN;
@@ -440,6 +457,7 @@ int mxfp4_matmul(const uint8_t* a_q, const uint8_t* a_scales, const uint8_t* b_q
                  void* stream) {
     if (!valid_out(out_dtype)) return NVFP4_ERR_DTYPE;
     if (const int rc = check_dims(m, n, k)) return rc;
+    if (!mx_launchable(m, n, ceil_div(k, 32))) return NVFP4_ERR_SHAPE;
     if (m == 0 || n == 0) return NVFP4_OK;
     if (!out || (k > 0 && (!a_q || !a_scales || !b_q || !b_scales))) return NVFP4_ERR_NULL;
     if (!aligned(a_q, 16) || !aligned(b_q, 16) || !aligned(a_scales, 4) || !aligned(b_scales, 4) || !aligned(out, 16))
@@ -459,7 +477,7 @@ int mxfp4_matmul_grad_input(const void* dy, int64_t ld, const uint8_t* q, const 
                             void* stream) {
     if (!valid_out(out_dtype)) return NVFP4_ERR_DTYPE;
     if (const int rc = check_dims(m, n, k)) return rc;
-    if (ld < n || ld > kMaxLd) return NVFP4_ERR_SHAPE;
+    if (ld < n || ld > kMaxLd || !grad_launchable(m, n, k, up(k, 32))) return NVFP4_ERR_SHAPE;
     if (m == 0 || k == 0) return NVFP4_OK;
     if (!dx || (n > 0 && (!dy || !q || !scales))) return NVFP4_ERR_NULL;
     if (!aligned(dy, 16) || !aligned(q, 16) || !aligned(dx, 16)) return NVFP4_ERR_ALIGN;

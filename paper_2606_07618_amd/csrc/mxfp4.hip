@@ -9,6 +9,7 @@
 
 #include <stdint.h>
 
+#include "launch_limit.h"
 #include "nvfp4ss.h"
 #include "tile_product.h"
 
@@ -131,7 +132,7 @@ struct Shape { int64_t units, row_units, groups; };
 int shape_of(int64_t rows, int64_t cols, Shape& s) {
     if (rows < 0 || cols < 0 || cols > INT64_MAX / 2 - kBlock) return NVFP4_ERR_SHAPE;
     s.row_units = (cols + kBlock - 1) / kBlock * (kBlock / kPer);
-    if (s.row_units && rows > (int64_t)0x7FFFFFFF * kThreads / s.row_units) return NVFP4_ERR_SHAPE;
+    if (s.row_units && rows > most_groups(kThreads) * kThreads / s.row_units) return NVFP4_ERR_SHAPE;
     s.units = rows * s.row_units;
     s.groups = (s.units + kThreads - 1) / kThreads;
     return NVFP4_OK;

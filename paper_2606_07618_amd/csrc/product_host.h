@@ -6,6 +6,7 @@
 
 #include <stdint.h>
 
+#include "launch_limit.h"
 #include "nvfp4ss.h"
 #include "tile_product.h"
 
@@ -98,6 +99,18 @@ Plan plan_product(int64_t m, int64_t n, int64_t inner) {
     return best;
 }
 
+constexpr int kTileThreads[kTiles] = {512, 256, 256, 256}, kJoinThreads = 256;
+
+// Whether the launches of a product fit, all of them: asked before the first one of a call.
+template <Kind KIND, Out OUT = kSums>
+bool product_launchable(int64_t m, int64_t n, int64_t inner) {
+    const Plan p = plan_product<KIND, OUT>(m, n, inner);
+    const TileCost& tile = tile_costs<KIND>()[p.tile];
+    const int64_t tiles = ceil_div(m, tile.m) * ceil_div(n * (OUT == kGate ? 2 : 1), tile.n);
+    return launchable(tiles * p.parts, kTileThreads[p.tile]) &&
+           (p.parts == 1 || launchable(ceil_div(m * n, kJoinThreads), kJoinThreads));
+}
+
 // Bytes of the parts' sums, 0 where the product is not split.
 template <Kind KIND, Out OUT = kSums>
 int64_t parts_bytes(int64_t m, int64_t n, int64_t inner) {
@@ -113,7 +126,7 @@ int launch_tiles(Args p, hipStream_t stream) {
     p.tiles_m = ceil_div(p.m, T::M);
     p.tiles_n = ceil_div(p.n, OUT == kGate || OUT == kGatePartial ? T::N / 2 : T::N);
     p.split_steps = ceil_div(p.steps, p.parts);
-    if (p.tiles_m > 0x7FFFFFFF || p.tiles_m * p.tiles_n > 0x7FFFFFFF / p.parts) return NVFP4_ERR_SHAPE;
+    if (!launchable(p.tiles_m * p.tiles_n * p.parts, T::kThreads)) return NVFP4_ERR_SHAPE;
     if (p.tiles_m * p.tiles_n == 0) return NVFP4_OK;
     hipLaunchKernelGGL((product_kernel<KIND, OUT, T>), dim3((unsigned)(p.tiles_m * p.tiles_n * p.parts)),
                        dim3(T::kThreads), 0, stream, p);
@@ -125,8 +138,8 @@ using Tile1 = Tile<128, 128, 2, 2>;
 using Tile2 = Tile<64, 128, 2, 2, 3>;
 using Tile3 = Tile<64, 64, 2, 2, 4>;
 template <class T, int I>
-constexpr bool kAgrees = T::MF == kFragments[I][0] && T::NF == kFragments[I][1];
-static_assert(kAgrees<Tile0, 0> && kAgrees<Tile1, 1> && kAgrees<Tile2, 2> && kAgrees<Tile3, 3>, "the scales' layout");
+constexpr bool kAgrees = T::MF == kFragments[I][0] && T::NF == kFragments[I][1] && T::kThreads == kTileThreads[I];
+static_assert(kAgrees<Tile0, 0> && kAgrees<Tile1, 1> && kAgrees<Tile2, 2> && kAgrees<Tile3, 3>, "the scales' layout and the launch");
 
 template <Kind KIND, Out OUT>
 int launch_product(const Args& p, int tile, hipStream_t stream) {
