@@ -415,8 +415,11 @@ int nvfp4_swiglu_ffn(const void* x, int64_t ldx, const void* w_gate, const void*
  *   dg = dh u s (1 + g (1 - s)),  du = dh g s  (rounded to bfloat16 for the products),
  *   dx [m, k] = dg Wg + du Wu,  dw_gate [n, k] = dg^T x,  dw_up [n, k] = du^T x.
  * dx, or both dw_gate and dw_up, may be NULL: not computed.  The weights' gradients take m <= 2^21, else
- * NVFP4_ERR_SHAPE. */
+ * NVFP4_ERR_SHAPE.  A call that leaves some out needs a smaller workspace: nvfp4_ffn_gradients_workspace_bytes says
+ * how much for dx (want_x) and for dw_gate and dw_up (want_w). */
 int64_t nvfp4_swiglu_ffn_backward_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t ldx, int64_t ldw);
+int64_t nvfp4_ffn_gradients_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t ldx, int64_t ldw, int want_x,
+                                            int want_w);
 int nvfp4_swiglu_ffn_backward(const void* dh, const void* x, int64_t ldx, const void* w_gate, const void* w_up,
                               int64_t ldw, const void* gate, const void* up, int64_t m, int64_t n, int64_t k,
                               void* dx, void* dw_gate, void* dw_up, void* workspace, size_t workspace_bytes,

@@ -219,19 +219,22 @@ int64_t forward_workspace(int64_t m, int64_t n, int64_t k, int64_t ldx, int64_t 
     return c.at + (m > dot_product::kMostRows ? parts_bytes<kBf16, kGate>(m, n, k) : 0);
 }
 
-// Sections of the backward pass's workspace: d, and what each product reads besides.
+// Sections of the backward pass's workspace, of the gradients asked for: d and the turned weights for dx, the turned d
+// and x for the weights' gradients.
 struct Backward { int64_t half, ld; char *d, *wt, *dt, *xt, *parts; };
 
-int64_t backward_sections(void* workspace, int64_t m, int64_t n, int64_t k, Backward& b) {
+int64_t backward_sections(void* workspace, int64_t m, int64_t n, int64_t k, bool want_x, bool want_w, Backward& b) {
     Carver c{static_cast<char*>(workspace)};
     // Whole lines of memory, and whole steps of the products: dW of [4000, 4096] -> 14336 took 842 us with rows
     // filled up to eights only, 770 so.
     b.half = up(n, 64), b.ld = up(m, 64);
-    b.d = static_cast<char*>(c.take(m * 2 * b.half * 2));
-    b.dt = static_cast<char*>(c.take(2 * n * b.ld * 2));
-    b.wt = static_cast<char*>(c.take(k * 2 * b.half * 2));
-    b.xt = static_cast<char*>(c.take(k * b.ld * 2));
-    const int64_t px = parts_bytes<kBf16>(m, k, 2 * b.half), pw = parts_bytes<kBf16, kTwoRows>(2 * n, k, m);
+    const auto take = [&](bool want, int64_t bytes) { return want ? static_cast<char*>(c.take(bytes)) : nullptr; };
+    b.d = take(want_x, m * 2 * b.half * 2);
+    b.dt = take(want_w, 2 * n * b.ld * 2);
+    b.wt = take(want_x, k * 2 * b.half * 2);
+    b.xt = take(want_w, k * b.ld * 2);
+    const int64_t px = want_x ? parts_bytes<kBf16>(m, k, 2 * b.half) : 0,
+                  pw = want_w ? parts_bytes<kBf16, kTwoRows>(2 * n, k, m) : 0;
     b.parts = static_cast<char*>(c.take(px > pw ? px : pw));     // of one product after the other
     return c.at;
 }
@@ -317,9 +320,14 @@ int nvfp4_swiglu_ffn(const void* x, int64_t ldx, const void* w_gate, const void*
 }
 
 int64_t nvfp4_swiglu_ffn_backward_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t ldx, int64_t ldw) {
+    return nvfp4_ffn_gradients_workspace_bytes(m, n, k, ldx, ldw, 1, 1);
+}
+
+int64_t nvfp4_ffn_gradients_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t ldx, int64_t ldw, int want_x,
+                                            int want_w) {
     if (const int rc = check_call(m, n, k, ldx, ldw)) return rc;
     Backward b;
-    return backward_sections(nullptr, m, n, k, b);
+    return backward_sections(nullptr, m, n, k, want_x != 0, want_w != 0, b);
 }
 
 int nvfp4_swiglu_ffn_backward(const void* dh, const void* x, int64_t ldx, const void* w_gate, const void* w_up,
@@ -338,7 +346,7 @@ int nvfp4_swiglu_ffn_backward(const void* dh, const void* x, int64_t ldx, const 
         if (!aligned(p, 16)) return NVFP4_ERR_ALIGN;
     if (want_w && m > kMaxLd) return NVFP4_ERR_SHAPE;              // a row of the turned operands
     Backward b;
-    if (const int rc = check_ws(workspace, workspace_bytes, backward_sections(workspace, m, n, k, b))) return rc;
+    if (const int rc = check_ws(workspace, workspace_bytes, backward_sections(workspace, m, n, k, want_x, want_w, b))) return rc;
     hipStream_t st = (hipStream_t)stream;
     const auto values = [](const void* p) { return static_cast<const uint16_t*>(p); };
     const auto turned = [](char* p) { return reinterpret_cast<uint16_t*>(p); };

@@ -71,6 +71,7 @@ def _load():
         "nvfp4_swiglu_ffn_workspace_bytes": (I64, [I64, I64, I64, I64, I64]),
         "nvfp4_swiglu_ffn": (I, [P, I64, P, P, I64, I64, I64, I64, P, P, P, P, SZ, P]),
         "nvfp4_swiglu_ffn_backward_workspace_bytes": (I64, [I64, I64, I64, I64, I64]),
+        "nvfp4_ffn_gradients_workspace_bytes": (I64, [I64, I64, I64, I64, I64, I, I]),
         "nvfp4_swiglu_ffn_backward": (I, [P, P, I64, P, P, I64, P, P, I64, I64, I64, P, P, P, P, SZ, P]),
     }
     for name, (res, args) in sigs.items():

@@ -15,6 +15,7 @@ nvfp4_swiglu_ffn = lib.nvfp4_swiglu_ffn
 nvfp4_swiglu_ffn_workspace_bytes = lib.nvfp4_swiglu_ffn_workspace_bytes
 nvfp4_swiglu_ffn_backward = lib.nvfp4_swiglu_ffn_backward
 nvfp4_swiglu_ffn_backward_workspace_bytes = lib.nvfp4_swiglu_ffn_backward_workspace_bytes
+nvfp4_ffn_gradients_workspace_bytes = lib.nvfp4_ffn_gradients_workspace_bytes
 mxfp4_quant = lib.mxfp4_quant
 mxfp4_dequant = lib.mxfp4_dequant
 mxfp4_matmul = lib.mxfp4_matmul
@@ -276,8 +277,8 @@ def swiglu_ffn_backward(dh: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor,
     dwg = _output(dwg, (n, k), torch.bfloat16, x, "dw_gate") if need_w else None
     dwu = _output(dwu, (n, k), torch.bfloat16, x, "dw_up") if need_w else None
     _same_device(x, dh, gate, up)
-    ws, nbytes = _workspace(nvfp4_swiglu_ffn_backward_workspace_bytes(m, n, k, ldx, ldw), ws, x,
-                            "nvfp4_swiglu_ffn_backward_workspace_bytes")
+    ws, nbytes = _workspace(nvfp4_ffn_gradients_workspace_bytes(m, n, k, ldx, ldw, bool(need_x), bool(need_w)), ws, x,
+                            "nvfp4_ffn_gradients_workspace_bytes")
     _check(nvfp4_swiglu_ffn_backward(_ptr(dh), _ptr(x), ldx, _ptr(w_gate), _ptr(w_up), ldw, _ptr(gate), _ptr(up), m, n,
                                      k, _ptr(dx), _ptr(dwg), _ptr(dwu), _ptr(ws), nbytes, _stream(x)),
            "nvfp4_swiglu_ffn_backward")
