@@ -375,9 +375,8 @@ int mxfp4_dequant(const uint8_t* q, const uint8_t* scales, int64_t rows, int64_t
  */
 
 /* y = x W^T S of bfloat16 x [m, k] and NVFP4 weights (q, scales, *tensor_scale) of `block` (16, 32, 64 or 128;
- * k % block == 0), scales row-major.  The weights' values q s enter exactly, the sums are multiplied
- * by S.  Calls of 5 to 512 rows take the activations in binary16, each row scaled by a power of two: values down to
- * 2^-31 of the row's largest enter exactly, smaller ones to 2^-39 of it.  ldx % 8 == 0, else NVFP4_ERR_ALIGN. */
+ * k % block == 0), scales row-major.  The weights' values q s and x enter exactly, the sums are
+ * multiplied by S.  ldx % 8 == 0, else NVFP4_ERR_ALIGN. */
 int64_t nvfp4_matmul_workspace_bytes(int64_t m, int64_t n, int64_t k);
 int nvfp4_matmul(const void* x, int64_t ldx, const uint8_t* q, const uint8_t* scales, int block,
                  const float* tensor_scale, int64_t m, int64_t n, int64_t k, int out_dtype, void* out, void* workspace,

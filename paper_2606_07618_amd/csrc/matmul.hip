@@ -174,15 +174,15 @@ bool valid_out(int dtype) { return dtype == NVFP4_IN_F32 || dtype == NVFP4_IN_BF
 
 // Up to this many rows the weights are expanded in registers, on their way into the matrix instructions, once for each
 // 128 rows; beyond, once and for all, and multiplied as bfloat16 tiles.  Measured, expanded in registers and beforehand:
-// [14336, 4096] 16 rows 20 and 51 us, 128 rows 34 and 58, 512 rows 82 and 86, 640 rows 121 and 104;
-// [28672, 8192] 512 rows 290 and 304, 1024 rows 510 and 466.
+// [14336, 4096] 16 rows 18 and 50 us, 128 rows 31 and 56, 512 rows 81 and 89, 640 rows 118 and 106;
+// [28672, 8192] 512 rows 302 and 307, 1024 rows 525 and 468.
 constexpr int64_t kStreamRows = 512;
 
 int64_t linear_workspace(int64_t m, int64_t n, int64_t k) {
     if (m <= dot_product::kMostRows) return 0;       // one launch, no workspace
     if (m <= kStreamRows) {
         const int parts = stream_product::parts(m, n, k);
-        return up(m * k * 2, 256) + up(m * 4, 256) + (parts > 1 ? up(parts * m * n * 4, 256) : 0);
+        return parts > 1 ? up(parts * m * n * 4, 256) : 0;
     }
     return up(n * k * 2, 256) + parts_bytes<kBf16>(m, n, k);
 }
@@ -219,18 +219,12 @@ int run_linear(const void* x, int64_t ldx, const uint8_t* q, const uint8_t* scal
         return launched();
     }
     if (m <= kStreamRows) {
-        Carver c{static_cast<char*>(ws)};
-        uint16_t* x16 = static_cast<uint16_t*>(c.take(m * k * 2));
-        int* exponents = static_cast<int*>(c.take(m * 4));
-        hipLaunchKernelGGL(stream_product::scale_rows_kernel, dim3((unsigned)m), dim3(stream_product::kScaleThreads), 0, stream,
-                           static_cast<const uint16_t*>(x), ldx, (int)k, x16, exponents);
-        if (const int rc = launched()) return rc;
         stream_product::Args t = {};
-        t.q = reinterpret_cast<const char*>(q), t.scales = scales, t.x = reinterpret_cast<const char*>(x16), t.exponents = exponents;
+        t.q = reinterpret_cast<const char*>(q), t.scales = scales, t.x = static_cast<const char*>(x), t.ldx = ldx * 2;
         t.m = m, t.n = n, t.k = k, t.shift = shift, t.scale = S, t.out = out, t.out_f32 = f32;
         t.tiles_n = ceil_div(n, stream_product::kRowsN), t.tiles_m = stream_product::tiles_m(m);
         t.parts = stream_product::parts(m, n, k), t.part_values = stream_product::part_values(k, t.parts);
-        float* partial = t.parts > 1 ? static_cast<float*>(c.take(t.parts * m * n * 4)) : nullptr;
+        float* partial = t.parts > 1 ? static_cast<float*>(ws) : nullptr;
         if (partial) t.out = partial;
         switch (stream_product::rows_of(m)) {
             case 1: launch_stream<1>(t, stream); break;

@@ -1,12 +1,10 @@
 // NVFP4 products with some to some hundreds of activation rows: the weights are read once for each 128 rows and
 // expanded in registers, on their way into the matrix instructions, so no expanded copy of them is written.
 //
-// The instructions of the expansion are what bounds it (each costs 4.8 cycles of a SIMD's four), so it is done in
-// binary16: q s has six significand bits and lies in 2^-10 .. 2688, exact there, and takes one conversion and
-// one packed product a pair; in bfloat16 it would take four instructions.  The activations are converted once,
-// each row scaled by a power of two so that its largest value lies in [2^14, 2^15): values down to 2^-31 of it
-// stay exact (eight significant bits above binary16's smallest 2^-24), and smaller ones lose 2^-39 of it at most, far
-// under the sums' own rounding.
+// A weight q s has six significant bits and lies in 2^-10 .. 2688: exact in bfloat16, the activations' own type, which
+// the matrix instructions take as they are.  (Binary16 would take half of the expansion's instructions, but it spans
+// 40 powers of two: beside one large value of a row its small ones are lost.  It also needs a launch that scales the rows.
+// [48, 4096] x [14336, 4096]: 23.6 us so, 21.9 in bfloat16; [16, 8192] x [28672, 8192]: 48 and 49.)
 //
 // A workgroup owns 128 weight rows and up to 128 activation rows.  Its waves are four times 32 weight rows by the
 // two halves of its contraction; a wave loads its weights (32 rows by two lanes of 16 bytes) into
@@ -15,8 +13,7 @@
 // Weights are loaded by groups of 256 values of a row, whole lines of 128 bytes, and so are the group's scales
 // where their rows allow it: visited in smaller pieces, a line would have left the L1 between two visits.
 // Few weight rows: the contraction is split over workgroups as well, whose sums a second kernel adds in order.
-// [48, 8192] x [28672, 8192]: 57 us, 5 of them scaling the rows (2.4 TB/s, 0.39 PFLOP/s); 231 us with the
-// weights expanded beforehand.
+// [48, 8192] x [28672, 8192]: 61 us (2.2 TB/s, 0.37 PFLOP/s); 231 us with the weights expanded beforehand.
 #pragma once
 
 #include "tile_product.h"
@@ -24,8 +21,6 @@
 namespace stream_product {
 
 using namespace tile_product;
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kRowsN = 128;                      // weight rows of a workgroup, 32 a wave
 constexpr int kWavesK = 2;                       // waves along the contraction, a half each
@@ -35,9 +30,8 @@ constexpr int kGroup = 256;                      // values of a weight row whose
 struct Args {
     const char* q;
     const uint8_t* scales;
-    const char* x;                               // [m, k] binary16
-    const int* exponents;                        // of the rows' powers of two
-    int64_t m, n, k;
+    const char* x;                               // [m, ldx bytes]
+    int64_t ldx, m, n, k;
     int64_t tiles_n;
     int parts, tiles_m, shift, part_values;      // part_values: of the contraction, a part
     const float* scale;
@@ -45,58 +39,13 @@ struct Args {
     int out_f32;
 };
 
-// Rows of x in binary16 times 2^-e, and e.  A row of zeros has e = 0; one with an infinity or a NaN keeps it.
-constexpr int kScaleThreads = 256;
-__global__ __launch_bounds__(kScaleThreads) void scale_rows_kernel(const uint16_t* __restrict__ x, int64_t ldx, int k,
-                                                                   uint16_t* __restrict__ out, int* __restrict__ exponents) {
-    __shared__ uint32_t tops[kScaleThreads / kLanes];
-    const uint16_t* row = x + blockIdx.x * ldx;
-    uint32_t top = 0;
-    for (int c = threadIdx.x * 8; c < k; c += kScaleThreads * 8) {
-        const uint4 v = *reinterpret_cast<const uint4*>(row + c);
-        for (const uint32_t w : {v.x, v.y, v.z, v.w}) {
-            const uint32_t lo = w & 0x7FFFu, hi = w >> 16 & 0x7FFFu;
-            top = top > lo ? top : lo;
-            top = top > hi ? top : hi;
-        }
-    }
-#pragma unroll
-    for (int d = 1; d < kLanes; d *= 2) {
-        const uint32_t o = __shfl_xor(top, d);
-        top = top > o ? top : o;
-    }
-    if (threadIdx.x % kLanes == 0) tops[threadIdx.x / kLanes] = top;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kScaleThreads / kLanes; ++w) top = top > tops[w] ? top : tops[w];
-    int field = (int)(top >> 7);                 // 127 + floor(log2 max|x|)
-    field = field == 255 ? 254 : field < 1 ? 1 : field;
-    const int e = top == 0 ? 0 : field - 127 - 14;
-    if (threadIdx.x == 0) exponents[blockIdx.x] = e;
-    for (int c = threadIdx.x * 8; c < k; c += kScaleThreads * 8) {
-        const uint4 v = *reinterpret_cast<const uint4*>(row + c);
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-        uint32_t o[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const f16x2 h = {(_Float16)ldexpf(__uint_as_float(w[i] << 16), -e), (_Float16)ldexpf(__uint_as_float(w[i] & 0xFFFF0000u), -e)};
-            o[i] = __builtin_bit_cast(uint32_t, h);
-        }
-        *reinterpret_cast<uint4*>(out + blockIdx.x * (int64_t)k + c) = make_uint4(o[0], o[1], o[2], o[3]);
-    }
-}
-
-// An E4M3 code's fields as a binary16 number: the scale times 2^-8, subnormal codes included.
-__device__ __forceinline__ f16x2 e4m3_f16(uint32_t c) {
-    const uint32_t h = (c & 0x7Fu) << 7;
-    return __builtin_bit_cast(f16x2, h | h << 16);
-}
-
-// Eight values times 2^8 and a scale times 2^-8.
-__device__ __forceinline__ f16x8 expand8(uint32_t n, f16x2 s) {
-    const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(n, 256.0f, 0) * s, b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(n, 256.0f, 1) * s,
-                c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(n, 256.0f, 2) * s, d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(n, 256.0f, 3) * s;
-    return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+// Eight values times their scale, exact: the upper half of the binary32 product holds all of it.
+__device__ __forceinline__ bf16x8 expand8(uint32_t n, float s) {
+    const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(n, 1.0f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(n, 1.0f, 1),
+                c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(n, 1.0f, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(n, 1.0f, 3);
+    const auto top = [&](f32x2 p) { return (int)__builtin_amdgcn_perm(__float_as_uint(p[1] * s), __float_as_uint(p[0] * s), 0x07060302u); };
+    const i32x4 v = {top(a), top(b), top(c), top(d)};
+    return __builtin_bit_cast(bf16x8, v);
 }
 
 // How a lane gets its scales: those of a whole group of its row (blocks of 16: four words, of 32: two), or of its
@@ -129,7 +78,7 @@ __global__ __launch_bounds__(256 * kWavesK, kWavesK) void stream_kernel(Args p) 
     const int steps = ((half < k - begin ? half : k - begin) + kStep - 1) / kStep;   // the first half is the longer one
 
     const uint32_t q_ld = (uint32_t)k / 2, s_ld = (uint32_t)k >> p.shift;
-    const __amdgpu_buffer_rsrc_t rq = window(p.q + n0 * q_ld), rs = window(p.scales + n0 * s_ld), rx = window(p.x + m0 * k * 2);
+    const __amdgpu_buffer_rsrc_t rq = window(p.q + n0 * q_ld), rs = window(p.scales + n0 * s_ld), rx = window(p.x + m0 * p.ldx);
     const int row = r * 32 + i32;
     // offsets of rows that are not there stay outside with any column added
     const uint32_t q_row = n0 + row < p.n ? (uint32_t)row * q_ld : kOutside, s_row = n0 + row < p.n ? (uint32_t)row * s_ld : kOutside;
@@ -140,7 +89,7 @@ __global__ __launch_bounds__(256 * kWavesK, kWavesK) void stream_kernel(Args p) 
         // a chunk's place in its row is exchanged by the row: 16 lanes read one chunk of 16 rows
         const int id = i * kThreads + tid, xr = id / kChunks, chunk = id % kChunks ^ xr % 16;
         const int from = begin + chunk / (kStep / 8) * half, at = from + chunk % (kStep / 8) * 8;
-        x_row[i] = m0 + xr < p.m ? ((uint32_t)xr * (uint32_t)k + at) * 2 : kOutside;
+        x_row[i] = m0 + xr < p.m ? (uint32_t)xr * (uint32_t)p.ldx + at * 2 : kOutside;
         x_left[i] = (from + half < k ? from + half : k) - at;
     }
 
@@ -201,12 +150,12 @@ __global__ __launch_bounds__(256 * kWavesK, kWavesK) void stream_kernel(Args p) 
         for (int e = 0; e < 16; ++e) acc[i][e] = 0.0f;
 
     // Registers: the activations of four matrix instructions along the contraction, read two ahead of their use.
-    f16x8 xv[4][MF];
+    bf16x8 xv[4][MF];
     int x_lane = (i32 * kChunks + ((h * A * 8 + g * 4) ^ i32 % 16)) * kChunk;      // of piece 0, instruction 0
     auto read = [&](int slot, int a, int j) {
 #pragma unroll
         for (int i = 0; i < MF; ++i) {
-            xv[j][i] = *reinterpret_cast<const f16x8*>(lds[slot] + i * (32 * kChunks * kChunk) + (x_lane ^ (a * 8 + j) * kChunk));
+            xv[j][i] = *reinterpret_cast<const bf16x8*>(lds[slot] + i * (32 * kChunks * kChunk) + (x_lane ^ (a * 8 + j) * kChunk));
         }
     };
     // One step; past the last one it multiplies zeros.
@@ -220,7 +169,7 @@ __global__ __launch_bounds__(256 * kWavesK, kWavesK) void stream_kernel(Args p) 
             if constexpr (SCALES == kWide16) c = sc[d / G][piece] >> (g * 16);
             else if constexpr (SCALES == kWide32) c = sc[d / G][piece / 2] >> (piece % 2 * 16 + g * 8);
             else c = sc[d / G][piece];
-            const f16x2 f0 = e4m3_f16(c), f1 = PAIRS ? e4m3_f16(c >> 8) : f0;
+            const float f0 = e4m3_f32(c), f1 = PAIRS ? e4m3_f32(c >> 8) : f0;
             if (a == A - 1) {
                 // the next step's activations are here, the last one's are read; later loads: of the D - 3 steps before
                 constexpr int first = d + 3 - D + kTurn, last = d - 1 + kTurn;   // of the turn before, on
@@ -233,10 +182,12 @@ __global__ __launch_bounds__(256 * kWavesK, kWavesK) void stream_kernel(Args p) 
                 if (j < 2) read(slot, a, j + 2);
                 else read(a == A - 1 ? (d + 1) % D : slot, a == A - 1 ? 0 : a + 1, j - 2);
                 int n = w[d / G][piece][j];
-                asm volatile("" : "+v"(n));              // expanded here, where its registers are needed, not a step ahead
-                const f16x8 wv = expand8((uint32_t)n, j < 2 ? f0 : f1);
+                // with many accumulators: expanded here, where its registers are needed, not a step ahead
+                if constexpr (MF > 1) asm volatile("" : "+v"(n));
+                bf16x8 wv = expand8((uint32_t)n, j < 2 ? f0 : f1);
+                if constexpr (MF > 1) asm volatile("" : "+v"(wv));
 #pragma unroll
-                for (int i = 0; i < MF; ++i) acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(wv, xv[j][i], acc[i], 0, 0, 0);
+                for (int i = 0; i < MF; ++i) acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wv, xv[j][i], acc[i], 0, 0, 0);
             }
         }
     };
@@ -280,14 +231,11 @@ __global__ __launch_bounds__(256 * kWavesK, kWavesK) void stream_kernel(Args p) 
     for (int i = 0; i < MF; ++i) {
         const int64_t m = m0 + i * 32 + i32;
         if (m >= p.m) continue;
-        const int e = p.exponents[m];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            f32x4 v;
-#pragma unroll
-            for (int c = 0; c < 4; ++c) v[c] = ldexpf(acc[i][q * 4 + c] * scale, e);
+            const f32x4 v = {acc[i][q * 4], acc[i][q * 4 + 1], acc[i][q * 4 + 2], acc[i][q * 4 + 3]};
             const int64_t n = n0 + r * 32 + q * 8 + g * 4;
-            store4(p.out, p.parts > 1 || p.out_f32, ((p.parts > 1 ? part * p.m : 0) + m) * p.n + n, p.n - n, vec, v);
+            store4(p.out, p.parts > 1 || p.out_f32, ((p.parts > 1 ? part * p.m : 0) + m) * p.n + n, p.n - n, vec, v * scale);
         }
     }
 }
@@ -303,7 +251,7 @@ inline int part_values(int64_t k, int parts) {
 
 // A workgroup takes a compute unit's LDS, so 256 of them work at a time, and a value of the contraction takes each 5.3, 7
 // or 10 ns (32, 64 or 128 rows).  Parts of it, of at least 1024 values, where rounds and the parts' sums then take less
-// ([384, 14336] x [4096, 14336]: 102 us in three parts of 288 workgroups together, 80 in two of 192).
+// ([384, 14336] x [4096, 14336]: 102 us in three parts of 288 workgroups together, 79 in two of 192).
 inline int parts(int64_t m, int64_t n, int64_t k) {
     const int64_t groups = (n + kRowsN - 1) / kRowsN * tiles_m(m);
     const float us = (rows_of(m) == 1 ? 0.0053f : rows_of(m) == 2 ? 0.007f : 0.01f);

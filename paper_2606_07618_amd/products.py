@@ -199,7 +199,7 @@ def matmul(x: torch.Tensor, q: torch.Tensor, scales: torch.Tensor, S: torch.Tens
            out_dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None,
            ws: torch.Tensor | None = None) -> torch.Tensor:
     """y = x W^T [m, n] of a bfloat16 x [m, k] and the NVFP4 weights (q, scales, S) that quantize()
-    gives for W [n, k]; the weights enter exactly, sums in binary32, rounded once."""
+    gives for W [n, k]; weights and x enter exactly, sums in binary32, rounded once."""
     dt = _dtype_id(out_dtype, "out_dtype")
     ldx = _rows(x, "x")
     n, k = _nvfp4_weights(x, q, scales, S, block)
