@@ -4,6 +4,7 @@ device pointers and the current HIP stream."""
 from __future__ import annotations
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from .nvfp4 import BF16, F32, NVFP4Error, _ptr, _stream, lib
 
@@ -199,7 +200,10 @@ def matmul(x: torch.Tensor, q: torch.Tensor, scales: torch.Tensor, S: torch.Tens
            out_dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None,
            ws: torch.Tensor | None = None) -> torch.Tensor:
     """y = x W^T [m, n] of a bfloat16 x [m, k] and the NVFP4 weights (q, scales, S) that quantize()
-    gives for W [n, k]; weights and x enter exactly, sums in binary32, rounded once."""
+    gives for W [n, k]; weights and x enter exactly, sums in binary32, rounded once.  Recorded by autograd
+    where x requires a gradient (matmul_grad_input; q, scales and S are constants), unless ``out`` is given."""
+    if out is None and x.requires_grad and torch.is_grad_enabled():
+        return _Matmul.apply(x, q, scales, S, block, out_dtype, ws)
     dt = _dtype_id(out_dtype, "out_dtype")
     ldx = _rows(x, "x")
     n, k = _nvfp4_weights(x, q, scales, S, block)
@@ -231,6 +235,25 @@ def matmul_grad_input(dy: torch.Tensor, q: torch.Tensor, scales: torch.Tensor, S
     return out
 
 
+def _incoming(d):
+    """A gradient as the entry points take it; autograd hands over any type, layout and alignment."""
+    d = d.to(torch.bfloat16).contiguous()
+    return d if d.data_ptr() % 16 == 0 else d.clone()
+
+
+class _Matmul(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, q, scales, S, block, out_dtype, ws):
+        ctx.save_for_backward(q, scales, S)
+        ctx.block = block
+        return matmul(x, q, scales, S, block, out_dtype, ws=ws)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        return (matmul_grad_input(_incoming(dy), *ctx.saved_tensors, ctx.block),) + (None,) * 6
+
+
 # ---- the gated feed-forward block --------------------------------------------------------------
 
 def _ffn_operands(x, w_gate, w_up):
@@ -247,7 +270,12 @@ def swiglu_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, save: 
                ws: torch.Tensor | None = None):
     """h = silu(x Wg^T) (x Wu^T) [m, n] in bfloat16, x [m, k], w_gate and w_up [n, k] (rows may be
     strided, the weights alike).  With ``save`` returns (h, gate, up), the pre-activations that
-    swiglu_ffn_backward takes.  ``out`` may pass preallocated outputs in the same form."""
+    swiglu_ffn_backward takes.  ``out`` may pass preallocated outputs in the same form.  Recorded by
+    autograd where an operand requires a gradient, unless ``save`` (the caller's own backward) or
+    ``out`` is given."""
+    if out is None and not save and torch.is_grad_enabled() and (
+            x.requires_grad or w_gate.requires_grad or w_up.requires_grad):
+        return _SwigluFfn.apply(x, w_gate, w_up, ws)
     m, n, k, ldx, ldw = _ffn_operands(x, w_gate, w_up)
     h, gate, up = (out if save else (out, None, None)) if out is not None else (None, None, None)
     h = _output(h, (m, n), torch.bfloat16, x, "h")
@@ -266,7 +294,8 @@ def swiglu_ffn_backward(dh: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor,
                         ws: torch.Tensor | None = None):
     """Gradients (dx [m, k], dw_gate, dw_up [n, k]) of swiglu_ffn in bfloat16, from dh [m, n] and the
     pre-activations it saved.  need_x / need_w: a gradient that is not needed is None and not
-    computed.  ``out`` may pass preallocated gradients in the same form."""
+    computed.  ``out`` may pass preallocated gradients in the same form.  The pre-activations' gradients
+    are rounded to bfloat16 once, as operands of the products."""
     m, n, k, ldx, ldw = _ffn_operands(x, w_gate, w_up)
     for t, what in ((dh, "dh"), (gate, "gate"), (up, "up")):
         _plain(t, (m, n), torch.bfloat16, what)
@@ -283,3 +312,18 @@ def swiglu_ffn_backward(dh: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor,
                                      k, _ptr(dx), _ptr(dwg), _ptr(dwu), _ptr(ws), nbytes, _stream(x)),
            "nvfp4_swiglu_ffn_backward")
     return dx, dwg, dwu
+
+
+class _SwigluFfn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w_gate, w_up, ws):
+        h, gate, up = swiglu_ffn(x, w_gate, w_up, save=True, ws=ws)
+        ctx.save_for_backward(x, w_gate, w_up, gate, up)
+        return h
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dh):
+        x, gate, up = ctx.needs_input_grad[:3]
+        dx, dwg, dwu = swiglu_ffn_backward(_incoming(dh), *ctx.saved_tensors, need_x=x, need_w=gate or up)
+        return dx, dwg if gate else None, dwu if up else None, None
