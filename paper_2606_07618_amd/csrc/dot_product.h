@@ -17,7 +17,8 @@ namespace dot_product {
 using namespace tile_product;
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kMostRows = 4;
+using product_plan::kDotRows;
+constexpr int kMostRows = kDotRows;
 constexpr int kWaves = 8, kSpan = kLanes * 32;   // values of the contraction that a wave's lanes cover
 constexpr int kRows = 8;                         // weight rows a wave goes down
 

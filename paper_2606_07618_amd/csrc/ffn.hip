@@ -216,7 +216,7 @@ int64_t forward_workspace(int64_t m, int64_t n, int64_t k, int64_t ldx, int64_t 
         c.take(n * packed_ld(k) * 2);
         c.take(n * packed_ld(k) * 2);
     }
-    return c.at + (m > dot_product::kMostRows ? parts_bytes<kBf16, kGate>(m, n, k) : 0);
+    return c.at + (m > kDotRows ? parts_bytes<kBf16, kGate>(m, n, k) : 0);
 }
 
 // Sections of the backward pass's workspace, of the gradients asked for: d and the turned weights for dx, the turned d
@@ -240,7 +240,7 @@ int64_t backward_sections(void* workspace, int64_t m, int64_t n, int64_t k, bool
 }
 
 bool forward_launchable(int64_t m, int64_t n, int64_t k) {
-    return m <= dot_product::kMostRows || product_launchable<kBf16, kGate>(m, n, k);
+    return m <= kDotRows || product_launchable<kBf16, kGate>(m, n, k);
 }
 
 bool backward_launchable(int64_t m, int64_t n, int64_t k, bool want_x, bool want_w) {
@@ -288,7 +288,7 @@ int nvfp4_swiglu_ffn(const void* x, int64_t ldx, const void* w_gate, const void*
     if (const int rc = packed(c, rx, m, k, needs_pack(k, ldx), st)) return rc;
     if (const int rc = packed(c, rg, n, k, pw, st)) return rc;
     if (const int rc = packed(c, ru, n, k, pw, st)) return rc;
-    if (m <= dot_product::kMostRows) {
+    if (m <= kDotRows) {
         dot_product::GatedArgs t = {};
         t.wg = static_cast<const char*>(rg.p), t.wu = static_cast<const char*>(ru.p), t.ldw = rg.ld * 2;
         t.x = static_cast<const char*>(rx.p), t.ldx = rx.ld * 2, t.n = n, t.k = k;

@@ -172,16 +172,10 @@ bool valid_out(int dtype) { return dtype == NVFP4_IN_F32 || dtype == NVFP4_IN_BF
 
 // ---- y = x W^T ------------------------------------------------------------------------------
 
-// Up to this many rows the weights are expanded in registers, on their way into the matrix instructions, once for each
-// 128 rows; beyond, once and for all, and multiplied as bfloat16 tiles.  Measured, expanded in registers and beforehand:
-// [14336, 4096] 16 rows 18 and 50 us, 128 rows 31 and 56, 512 rows 81 and 89, 640 rows 118 and 106;
-// [28672, 8192] 512 rows 302 and 307, 1024 rows 525 and 468.
-constexpr int64_t kStreamRows = 512;
-
 int64_t linear_workspace(int64_t m, int64_t n, int64_t k) {
-    if (m <= dot_product::kMostRows) return 0;       // one launch, no workspace
+    if (m <= kDotRows) return 0;       // one launch, no workspace
     if (m <= kStreamRows) {
-        const int parts = stream_product::parts(m, n, k);
+        const int parts = stream_parts(m, n, k);
         return parts > 1 ? up(parts * m * n * 4, 256) : 0;
     }
     return up(n * k * 2, 256) + parts_bytes<kBf16>(m, n, k);
@@ -193,7 +187,7 @@ bool linear_launchable(int64_t m, int64_t n, int64_t k) {
 
 template <int MF>
 void launch_stream(const stream_product::Args& p, hipStream_t stream) {
-    const dim3 grid((unsigned)(p.tiles_n * p.tiles_m * p.parts)), threads(256 * stream_product::kWavesK);
+    const dim3 grid((unsigned)(p.tiles_n * p.tiles_m * p.parts)), threads(256 * kWavesK);
     using namespace stream_product;
     const bool wide = p.k % stream_product::kGroup == 0;   // whole groups, whose scales start on whole words
     auto kernel = p.shift == 4 ? (wide ? stream_kernel<MF, kWide16> : p.k % 32 == 0 ? stream_kernel<MF, kPair> : stream_kernel<MF, kOdd>)
@@ -205,7 +199,7 @@ int run_linear(const void* x, int64_t ldx, const uint8_t* q, const uint8_t* scal
                int64_t m, int64_t n, int64_t k, int out_dtype, void* out, void* ws, hipStream_t stream) {
     const int shift = block == 16 ? 4 : block == 32 ? 5 : block == 64 ? 6 : 7;
     const int f32 = out_dtype == NVFP4_IN_F32;
-    if (m <= dot_product::kMostRows) {
+    if (m <= kDotRows) {
         dot_product::Args t = {};
         t.q = reinterpret_cast<const char*>(q), t.scales = scales, t.x = static_cast<const char*>(x), t.ldx = ldx * 2;
         t.n = n, t.k = k, t.shift = shift, t.scale = S, t.out = out, t.out_f32 = f32;
@@ -222,11 +216,11 @@ int run_linear(const void* x, int64_t ldx, const uint8_t* q, const uint8_t* scal
         stream_product::Args t = {};
         t.q = reinterpret_cast<const char*>(q), t.scales = scales, t.x = static_cast<const char*>(x), t.ldx = ldx * 2;
         t.m = m, t.n = n, t.k = k, t.shift = shift, t.scale = S, t.out = out, t.out_f32 = f32;
-        t.tiles_n = ceil_div(n, stream_product::kRowsN), t.tiles_m = stream_product::tiles_m(m);
-        t.parts = stream_product::parts(m, n, k), t.part_values = stream_product::part_values(k, t.parts);
+        t.tiles_n = ceil_div(n, stream_product::kRowsN), t.tiles_m = stream_tiles_m(m);
+        t.parts = stream_parts(m, n, k), t.part_values = stream_part_values(k, t.parts);
         float* partial = t.parts > 1 ? static_cast<float*>(ws) : nullptr;
         if (partial) t.out = partial;
-        switch (stream_product::rows_of(m)) {
+        switch (stream_rows_of(m)) {
             case 1: launch_stream<1>(t, stream); break;
             case 2: launch_stream<2>(t, stream); break;
             default: launch_stream<4>(t, stream);
@@ -331,16 +325,6 @@ int64_t lay_groups(int64_t m, int64_t n, int64_t blocks, const int* fragments) {
 }
 
 int64_t scale_bytes(int64_t rows, int64_t blocks) { return up(rows, 128) * ceil_div(blocks, 8) * 8; }
-
-// Few rows: the kernel for them where tiles, which must be many or be split to keep the chip busy, would take longer.
-bool thin(int64_t m, int64_t n, int64_t blocks) {
-    return m <= thin_product::kRows && thin_product::us(m, n, blocks * 32) < plan_product<kMx, kSums>(m, n, blocks * 32).us;
-}
-
-// The largest tile takes its scales laid out, and so do the others where rows of scales are no whole words.
-bool lays_scales(int64_t m, int64_t n, int64_t blocks) {
-    return blocks % 4 != 0 || plan_product<kMx, kSums>(m, n, blocks * 32).tile == 0;
-}
 
 bool mx_launchable(int64_t m, int64_t n, int64_t blocks) {
     const int* fragments = kFragments[plan_product<kMx, kSums>(m, n, blocks * 32).tile];

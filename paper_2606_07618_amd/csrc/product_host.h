@@ -1,4 +1,4 @@
-// Host side of the matrix products: the checks that every product shares, the plan of its tiles, and
+// Host side of the matrix products: the checks that every product shares, the launch of its planned tiles, and
 // the kernels that bring an operand into the form the tiles read.
 #pragma once
 
@@ -6,12 +6,13 @@
 
 #include <stdint.h>
 
-#include "launch_limit.h"
 #include "nvfp4ss.h"
+#include "product_plan.h"
 #include "tile_product.h"
 
 namespace product_host {
 
+using namespace product_plan;
 using namespace tile_product;
 
 // A tile's loads take 32-bit offsets from its first row: 256 rows of this many bfloat16 values stay
@@ -20,8 +21,6 @@ constexpr int64_t kMaxWidth = (int64_t)1 << 20, kMaxLd = (int64_t)1 << 21;
 constexpr int64_t kMaxRows = (int64_t)1 << 36;      // workspace sizes stay within 63 bits
 
 inline bool aligned(const void* p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
-inline int64_t up(int64_t v, int64_t unit) { return (v + unit - 1) / unit * unit; }
-inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 inline int check_dims(int64_t m, int64_t n, int64_t k) {
     if (m < 0 || n < 0 || k < 0 || m > kMaxRows || n > kMaxWidth || k > kMaxWidth) return NVFP4_ERR_SHAPE;
@@ -46,77 +45,6 @@ struct Carver {
 };
 
 int pack_bf16_rows(const void* src, int64_t rows, int64_t width, int64_t ld, void* dst, hipStream_t stream);
-
-// ---- the tile and the split of a product --------------------------------------------------------
-// Four tiles, from the one that moves least through LDS for what it computes to the one that gives the most
-// workgroups; and the contraction may be split over workgroups, whose sums a second kernel adds.  The rule takes the
-// least estimated time, from what each tile took on this card with contractions of 128 to 4096 values: with a workgroup
-// on few of the 256 compute units `start` + steps * `alone` microseconds, and with many workgroups `fixed` (filling
-// the pipeline, storing the tile) + steps * `among` for each 256 of them.
-//   measured, bfloat16, contraction 384: [8192, 8192] outputs 70 us with the largest tile, 86, 118, 159 with the
-//   next; [256, 2048] outputs 16.1, 9.8, 7.0, 5.5 us.
-struct TileCost { int m, n; float start, alone, fixed, among; };
-constexpr int kTiles = 4, kMostParts = 16;
-constexpr float kLaunchUs = 2.0f;
-constexpr float kJoinUs = 6.0f, kJoinBytesUs = 8e6f;     // a second launch; bytes a microsecond
-constexpr float kSmaller = 0.93f;                        // a smaller tile reads more: taken where it is clearly faster
-constexpr float kLayUs = 6.0f;                           // a launch that lays scales out
-
-template <Kind KIND>
-inline const TileCost* tile_costs() {
-    static constexpr TileCost mx[kTiles] = {{256, 256, 7.0f, 1.5f, 9.0f, 1.7f}, {128, 128, 6.3f, 1.1f, 1.9f, 0.75f},
-                                            {64, 128, 5.1f, 0.64f, 1.4f, 0.48f}, {64, 64, 4.4f, 0.40f, 1.3f, 0.31f}};
-    static constexpr TileCost bf16[kTiles] = {{256, 256, 9.8f, 1.05f, 8.5f, 1.54f}, {128, 128, 5.1f, 0.77f, 2.5f, 0.51f},
-                                              {64, 128, 4.7f, 0.38f, 1.7f, 0.34f}, {64, 64, 3.7f, 0.31f, 1.3f, 0.23f}};
-    return KIND != kBf16 ? mx : bf16;
-}
-
-// Fragments of a wave's rows of A and of B.
-constexpr int kFragments[kTiles][2] = {{8, 4}, {4, 4}, {2, 4}, {2, 2}};
-
-struct Plan { int tile, parts; float us; };
-
-template <Kind KIND, Out OUT>
-Plan plan_product(int64_t m, int64_t n, int64_t inner) {
-    constexpr int kStepValues = KIND != kBf16 ? 256 : 64, kHalf = OUT == kGate ? 2 : 1;
-    const int64_t steps = ceil_div(inner, kStepValues);
-    const TileCost* costs = tile_costs<KIND>();
-    Plan best = {0, 1, 3e38f};
-    for (int t = 0; t < kTiles; ++t) {
-        if (OUT == kGate && costs[t].n < 128) continue;        // a wave holds both products of 32 columns
-        const float tiles = (float)ceil_div(m, costs[t].m) * (float)ceil_div(n * kHalf, costs[t].n);
-        for (int parts = 1; parts <= kMostParts && (parts == 1 || steps / parts >= 8); parts *= 2) {
-            const float load = tiles * parts / 256.0f, own = (float)ceil_div(steps, parts);
-            const float share = load < 1.0f && costs[t].among > costs[t].alone ? (costs[t].among - costs[t].alone) * load : 0.0f;
-            const float few = costs[t].start + own * (costs[t].alone + share);
-            const float many = load > 1.0f ? kLaunchUs + (float)(int64_t)(load + 0.999f) * (costs[t].fixed + own * costs[t].among) : 0.0f;
-            float us = few > many ? few : many;
-            if (KIND != kBf16 && t == 0) us += kLayUs;
-            if (parts > 1) us += kJoinUs + (float)m * (float)n * (float)(8 * kHalf * parts) / kJoinBytesUs;
-            if (us < best.us * (t > best.tile ? kSmaller : 1.0f)) best = {t, parts, us};
-        }
-    }
-    return best;
-}
-
-constexpr int kTileThreads[kTiles] = {512, 256, 256, 256}, kJoinThreads = 256;
-
-// Whether the launches of a product fit, all of them: asked before the first one of a call.
-template <Kind KIND, Out OUT = kSums>
-bool product_launchable(int64_t m, int64_t n, int64_t inner) {
-    const Plan p = plan_product<KIND, OUT>(m, n, inner);
-    const TileCost& tile = tile_costs<KIND>()[p.tile];
-    const int64_t tiles = ceil_div(m, tile.m) * ceil_div(n * (OUT == kGate ? 2 : 1), tile.n);
-    return launchable(tiles * p.parts, kTileThreads[p.tile]) &&
-           (p.parts == 1 || launchable(ceil_div(m * n, kJoinThreads), kJoinThreads));
-}
-
-// Bytes of the parts' sums, 0 where the product is not split.
-template <Kind KIND, Out OUT = kSums>
-int64_t parts_bytes(int64_t m, int64_t n, int64_t inner) {
-    const Plan p = plan_product<KIND, OUT>(m, n, inner);
-    return p.parts > 1 ? up(p.parts * m * n * (OUT == kGate ? 8 : 4), 256) : 0;
-}
 
 // Fills in the tiles and steps of p and launches; p's operands, outer indexes and outputs are set.
 template <Kind KIND, Out OUT, class T>

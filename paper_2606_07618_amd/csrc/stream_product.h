@@ -22,10 +22,9 @@ namespace stream_product {
 
 using namespace tile_product;
 
-constexpr int kRowsN = 128;                      // weight rows of a workgroup, 32 a wave
-constexpr int kWavesK = 2;                       // waves along the contraction, a half each
+using product_plan::kStreamRowsN, product_plan::kWavesK, product_plan::kGroup;
+constexpr int kRowsN = kStreamRowsN;             // weight rows of a workgroup, 32 a wave
 constexpr int kPiece = 64;                       // values of a weight row in one load of a wave
-constexpr int kGroup = 256;                      // values of a weight row whose scales are loaded together
 
 struct Args {
     const char* q;
@@ -238,31 +237,6 @@ __global__ __launch_bounds__(256 * kWavesK, kWavesK) void stream_kernel(Args p) 
             store4(p.out, p.parts > 1 || p.out_f32, ((p.parts > 1 ? part * p.m : 0) + m) * p.n + n, p.n - n, vec, v * scale);
         }
     }
-}
-
-inline int rows_of(int64_t m) { return m <= 32 ? 1 : m <= 64 ? 2 : 4; }
-inline int tiles_m(int64_t m) { return (int)((m + 127) / 128); }
-
-// Values of a part: halves of whole groups.
-inline int part_values(int64_t k, int parts) {
-    constexpr int64_t kUnit = kGroup * kWavesK;
-    return (int)(((k + parts - 1) / parts + kUnit - 1) / kUnit * kUnit);
-}
-
-// A workgroup takes a compute unit's LDS, so 256 of them work at a time, and a value of the contraction takes each 5.3, 7
-// or 10 ns (32, 64 or 128 rows).  Parts of it, of at least 1024 values, where rounds and the parts' sums then take less
-// ([384, 14336] x [4096, 14336]: 102 us in three parts of 288 workgroups together, 79 in two of 192).
-inline int parts(int64_t m, int64_t n, int64_t k) {
-    const int64_t groups = (n + kRowsN - 1) / kRowsN * tiles_m(m);
-    const float us = (rows_of(m) == 1 ? 0.0053f : rows_of(m) == 2 ? 0.007f : 0.01f);
-    int best = 1;
-    float least = 3e38f;
-    for (int p = 1; p <= 16 && (p == 1 || k / p >= 1024); ++p) {
-        const float took = (float)((groups * p + 255) / 256) * (float)part_values(k, p) * us +
-                           (p > 1 ? 6.0f + (float)m * (float)n * (float)(8 * p) / 4e6f : 0.0f);
-        if (took < least) least = took, best = p;
-    }
-    return best;
 }
 
 }  // namespace stream_product

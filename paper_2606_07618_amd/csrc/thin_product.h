@@ -13,7 +13,8 @@
 namespace thin_product {
 
 using namespace tile_product;
-constexpr int kRows = 16;                        // of the activations, at most
+using product_plan::kThinRows;
+constexpr int kRows = kThinRows;                 // of the activations, at most
 
 struct Args {
     const char *w, *x;                           // [n, k], [m, k] nibbles
@@ -65,9 +66,6 @@ __global__ __launch_bounds__(kWaves * kLanes) void thin_kernel(Args p) {
     const int64_t n = n0 + g * 4;
     if (m_in) store4(p.out, p.out_f32, (int64_t)i * p.n + n, p.n - n, p.n % 4 == 0, acc);
 }
-
-// Estimated microseconds, from the times above and 16 rows' (6.7, 16.5 and 55).
-inline float us(int64_t m, int64_t n, int64_t k) { return 2.0f + (float)n * (float)k * (1.6e-7f + 0.7e-8f * (float)m); }
 
 inline void launch_thin(const Args& p, hipStream_t stream) {
     hipLaunchKernelGGL(thin_kernel, dim3((unsigned)((p.n + 15) / 16)), dim3(kWaves * kLanes), 0, stream, p);

@@ -16,7 +16,13 @@
 
 #include <stdint.h>
 
+#include "product_plan.h"
+
 namespace tile_product {
+
+using product_plan::Kind, product_plan::kBf16, product_plan::kMx, product_plan::kMxLaid;
+using product_plan::Out, product_plan::kSums, product_plan::kPartial, product_plan::kGate, product_plan::kGatePartial,
+    product_plan::kTwoRows;
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -56,9 +62,6 @@ __device__ __forceinline__ float e4m3_f32(uint32_t c) {
 }
 
 template <int V> struct Const { static constexpr int value = V; };
-
-// Microscaled operands' scales as the rows lie (kMx, rows of whole words), or laid out by scale_at() (kMxLaid).
-enum Kind { kBf16, kMx, kMxLaid };
 
 struct Operand {
     const char* p;              // element (0, 0)
@@ -171,16 +174,6 @@ struct Tile {
     static constexpr int M = M_, N = N_, WM = WM_, WN = WN_, kThreads = WM_ * WN_ * kLanes;
     static constexpr int kWavesPerSimd = M_ * N_ / (WM_ * WN_) > 8192 ? 1 : 2;   // 512 or 256 registers
     static constexpr int MF = M_ / WM_ / 16, NF = N_ / WN_ / 16;     // a wave's matrix instructions
-};
-
-// What happens to the sums.
-enum Out {
-    kSums,        // scale * sum, as bfloat16 or binary32
-    kPartial,     // the sum of this part of the contraction, binary32, for a later reduction
-    kGate,        // B is two matrices: silu(sum of the first) * sum of the second, and both sums where asked for;
-                  // a tile's outer indexes of B are taken half from each, so that an output's two sums meet in one lane
-    kGatePartial, // both sums of this part of the contraction, [part][2][m][n] in binary32
-    kTwoRows      // rows below `half_rows` to the first output, those from there on to the second
 };
 
 struct Args {
