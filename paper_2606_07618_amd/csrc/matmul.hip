@@ -74,8 +74,8 @@ using namespace product_host;
 // ---- weights expanded to bfloat16 -----------------------------------------------------------
 
 // q s of NVFP4 (without S) or q 2^E of microscaled FP4, 8 values a lane, both exact: an E2M1 value has
-// two significand bits and an E4M3 scale four, bfloat16 eight (values below 2^-133 aside, which only
-// microscaled blocks of codes under 2 hold).
+// two significand bits and an E4M3 scale four, bfloat16 eight; the smallest microscaled value, 2^-128, is a
+// multiple of bfloat16's least, 2^-133, and the matrix instructions take such numbers as they are.
 template <Kind KIND>
 __device__ __forceinline__ uint4 expand8(uint32_t n, uint32_t code) {
     const float s = KIND == kMx ? __uint_as_float(code << 23) : 1.0f, t = KIND == kMx ? 1.0f : e4m3_f32(code);

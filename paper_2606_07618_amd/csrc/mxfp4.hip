@@ -51,7 +51,7 @@ __device__ __forceinline__ uint32_t quantize8(const float (&v)[kPer], int& code)
 }
 
 // WHOLE: cols % 32 == 0, so the tensor is a run of blocks and a lane's values are 8 aligned ones.
-// Otherwise a workgroup takes a row's units of 8, and values past cols are zeros.
+// Otherwise rows are taken as filled up to whole blocks, row_units units of 8 each, with zeros past cols.
 template <typename In, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void mx_quant_kernel(const In* __restrict__ x, int64_t units, int64_t cols,
                                                             int64_t row_units, uint32_t* __restrict__ q,
