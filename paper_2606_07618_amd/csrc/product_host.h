@@ -49,8 +49,7 @@ int pack_bf16_rows(const void* src, int64_t rows, int64_t width, int64_t ld, voi
 // Fills in the tiles and steps of p and launches; p's operands, outer indexes and outputs are set.
 template <Kind KIND, Out OUT, class T>
 int launch_tiles(Args p, hipStream_t stream) {
-    constexpr int kStepValues = KIND != kBf16 ? 256 : 64;
-    p.steps = ceil_div(p.inner, kStepValues);
+    p.steps = ceil_div(p.inner, kStepValues<KIND>);
     p.tiles_m = ceil_div(p.m, T::M);
     p.tiles_n = ceil_div(p.n, OUT == kGate || OUT == kGatePartial ? T::N / 2 : T::N);
     p.split_steps = ceil_div(p.steps, p.parts);

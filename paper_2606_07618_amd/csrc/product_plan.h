@@ -53,23 +53,35 @@ constexpr int kFragments[kTiles][2] = {{8, 4}, {4, 4}, {2, 4}, {2, 2}};
 
 struct Plan { int tile, parts; float us; };
 
+// Values of a step of the contraction, and outer indexes of B for an output.
+template <Kind KIND> constexpr int kStepValues = KIND != kBf16 ? 256 : 64;
+template <Out OUT> constexpr int kHalf = OUT == kGate ? 2 : 1;
+
+// Estimated microseconds with tile t and the contraction in `parts`.  Up to a workgroup a compute unit, what they take
+// of each other grows with their number ([1024, 4096] x [4096, 4096], where the largest tile in four parts makes 256
+// workgroups, estimated as if each were alone: 66 us; with a smaller tile, taken since, 57).
+template <Kind KIND, Out OUT>
+float product_us(int t, int parts, int64_t m, int64_t n, int64_t inner) {
+    const TileCost& cost = tile_costs<KIND>()[t];
+    const float tiles = (float)ceil_div(m, cost.m) * (float)ceil_div(n * kHalf<OUT>, cost.n);
+    const float load = tiles * parts / 256.0f, own = (float)ceil_div(ceil_div(inner, kStepValues<KIND>), parts);
+    const float share = load <= 1.0f && cost.among > cost.alone ? (cost.among - cost.alone) * load : 0.0f;
+    const float few = cost.start + own * (cost.alone + share);
+    const float many = load > 1.0f ? kLaunchUs + (float)(int64_t)(load + 0.999f) * (cost.fixed + own * cost.among) : 0.0f;
+    float us = few > many ? few : many;
+    if (KIND != kBf16 && t == 0) us += kLayUs;
+    if (parts > 1) us += kJoinUs + (float)m * (float)n * (float)(8 * kHalf<OUT> * parts) / kJoinBytesUs;
+    return us;
+}
+
 template <Kind KIND, Out OUT>
 Plan plan_product(int64_t m, int64_t n, int64_t inner) {
-    constexpr int kStepValues = KIND != kBf16 ? 256 : 64, kHalf = OUT == kGate ? 2 : 1;
-    const int64_t steps = ceil_div(inner, kStepValues);
-    const TileCost* costs = tile_costs<KIND>();
+    const int64_t steps = ceil_div(inner, kStepValues<KIND>);
     Plan best = {0, 1, 3e38f};
     for (int t = 0; t < kTiles; ++t) {
-        if (OUT == kGate && costs[t].n < 128) continue;        // a wave holds both products of 32 columns
-        const float tiles = (float)ceil_div(m, costs[t].m) * (float)ceil_div(n * kHalf, costs[t].n);
+        if (OUT == kGate && tile_costs<KIND>()[t].n < 128) continue;   // a wave holds both products of 32 columns
         for (int parts = 1; parts <= kMostParts && (parts == 1 || steps / parts >= 8); parts *= 2) {
-            const float load = tiles * parts / 256.0f, own = (float)ceil_div(steps, parts);
-            const float share = load < 1.0f && costs[t].among > costs[t].alone ? (costs[t].among - costs[t].alone) * load : 0.0f;
-            const float few = costs[t].start + own * (costs[t].alone + share);
-            const float many = load > 1.0f ? kLaunchUs + (float)(int64_t)(load + 0.999f) * (costs[t].fixed + own * costs[t].among) : 0.0f;
-            float us = few > many ? few : many;
-            if (KIND != kBf16 && t == 0) us += kLayUs;
-            if (parts > 1) us += kJoinUs + (float)m * (float)n * (float)(8 * kHalf * parts) / kJoinBytesUs;
+            const float us = product_us<KIND, OUT>(t, parts, m, n, inner);
             if (us < best.us * (t > best.tile ? kSmaller : 1.0f)) best = {t, parts, us};
         }
     }
@@ -83,7 +95,7 @@ template <Kind KIND, Out OUT = kSums>
 bool product_launchable(int64_t m, int64_t n, int64_t inner) {
     const Plan p = plan_product<KIND, OUT>(m, n, inner);
     const TileCost& tile = tile_costs<KIND>()[p.tile];
-    const int64_t tiles = ceil_div(m, tile.m) * ceil_div(n * (OUT == kGate ? 2 : 1), tile.n);
+    const int64_t tiles = ceil_div(m, tile.m) * ceil_div(n * kHalf<OUT>, tile.n);
     return launchable(tiles * p.parts, kTileThreads[p.tile]) &&
            (p.parts == 1 || launchable(ceil_div(m * n, kJoinThreads), kJoinThreads));
 }

@@ -20,6 +20,11 @@ int main() {
             if (m <= kDotRows) std::puts("dot");
             else if (m <= kStreamRows) std::printf("stream%d %s\n", stream_rows_of(m), stream_parts(m, n, k) > 1 ? "split" : "whole");
             else tiled<kBf16, kSums>("sums", m, n, k);
+        } else if (!std::strcmp(op, "times")) {            // estimated ones of m workgroups of each tile
+            for (int t = 0; t < kTiles; ++t)
+                std::printf("%.4f %.4f ", product_us<kBf16, kSums>(t, 1, m * tile_costs<kBf16>()[t].m, n, k),
+                            product_us<kMx, kSums>(t, 1, m * tile_costs<kMx>()[t].m, n, k));
+            std::puts("");
         } else if (!std::strcmp(op, "turns")) {            // of the stream kernel: rounds of 1024 values a workgroup
             std::printf("%lld\n", (long long)ceil_div(stream_part_values(k, stream_parts(m, n, k)), 1024));
         } else if (!std::strcmp(op, "grad") || !std::strcmp(op, "mxgrad")) {

@@ -43,3 +43,11 @@ def test_long_products_go_around(forms):
     shapes = [s[:3] for s in product_shapes.LONG]
     assert all(form.startswith("stream") for form in forms("linear", shapes))
     assert all(int(t) >= 3 for t in forms("turns", shapes))
+
+
+@pytest.mark.parametrize("k", [64, 1024, 14336])
+def test_estimates_grow_with_the_workgroups(forms, k):
+    """One more tile never makes a product faster: the estimates do not fall anywhere, full chip and more among them."""
+    rows = [list(map(float, line.split())) for line in forms("times", [(w, 64, k) for w in range(1, 600)])]
+    for lo, hi in zip(rows, rows[1:]):
+        assert all(b >= a for a, b in zip(lo, hi)), (lo, hi)
