@@ -14,8 +14,8 @@
 // where their rows allow it: visited in smaller pieces, a line would have left the L1 between two visits.
 // Few weight rows: the contraction is split over workgroups as well, whose sums a second kernel adds in order.
 // [48, 8192] x [28672, 8192]: 59 us (2.3 TB/s, 0.38 PFLOP/s); 231 us with the weights expanded beforehand.  Neither
-// the matrix instructions (27 % of the cycles) nor the vector ones (32 %) are what bounds it: with one group ahead and one
-// workgroup on each of 224 compute units, too few weights are on their way.
+// the matrix instructions (20 % of the chip's cycles) nor the vector ones (32 %) bound it, nor do the bytes: with one
+// group ahead and one workgroup on each of 224 compute units, too few weights are on their way.
 #pragma once
 
 #include "tile_product.h"
