@@ -3,8 +3,9 @@
 //
 // NVFP4: what else stands in its way are instructions, so each weight pair costs one conversion and one two-way dot
 // product a row.  A lane holds 32 values' activations in registers and goes down eight weight rows, whose loads are
-// all in flight at once.  The values of a block are summed as they are and the sum is multiplied by the block's
-// scale, so scales cost an instruction a block.
+// all in flight at once.  The values of a block are summed before the sum is multiplied by the block's
+// scale, so scales cost an instruction a block.  They enter 2^-7 as large, and the scale 2^7, both exact: so the sum of a
+// block of the largest activations stays within binary32 where the outputs do.
 //   y[m][n] = S sum_blocks s sum_j q_j x_j, sums in binary32.
 // (A matrix instruction would need the weights times their scales, twice the conversions, and of its 16 columns 12
 // to 15 would be empty: one row, [4096, 14336], 14.8 us in place of 9.0, 3.7 TB/s.)
@@ -37,12 +38,15 @@ __device__ __forceinline__ float dot2(uint32_t a, uint32_t b, float c) {
     return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, a), __builtin_bit_cast(bf16x2, b), c, false);
 }
 
-// Eight values of a word of nibbles against eight activations.
+constexpr int kUp = 7;                           // of a scale; 32 values of up to 6 make 1.5 2^kUp
+
+// Eight values of a word of nibbles, times 2^-kUp, against eight activations.
 __device__ __forceinline__ float dot8(uint32_t n, i32x4 x, float c) {
-    c = dot2(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(n, 1.0f, 0)), (uint32_t)x[0], c);
-    c = dot2(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(n, 1.0f, 1)), (uint32_t)x[1], c);
-    c = dot2(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(n, 1.0f, 2)), (uint32_t)x[2], c);
-    return dot2(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(n, 1.0f, 3)), (uint32_t)x[3], c);
+    constexpr float down = 1.0f / (1 << kUp);
+    c = dot2(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(n, down, 0)), (uint32_t)x[0], c);
+    c = dot2(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(n, down, 1)), (uint32_t)x[1], c);
+    c = dot2(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(n, down, 2)), (uint32_t)x[2], c);
+    return dot2(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(n, down, 3)), (uint32_t)x[3], c);
 }
 
 // Sums over the two halves of a wave (of its rows of 16) of two values at once: the first value's in the lower
@@ -112,7 +116,7 @@ __global__ __launch_bounds__(kWaves * kLanes) void dot_kernel(Args p) {
         }
 #pragma unroll
         for (int r = 0; r < kRows; ++r) {
-            const float s0 = e4m3_f32(s[r]), s1 = PAIRS ? e4m3_f32(s[r] >> 8) : s0;
+            const float s0 = e4m3_f32<kUp>(s[r]), s1 = PAIRS ? e4m3_f32<kUp>(s[r] >> 8) : s0;
 #pragma unroll
             for (int m = 0; m < M; ++m) {
                 const float lo = dot8((uint32_t)w[r][1], x[m][1], dot8((uint32_t)w[r][0], x[m][0], 0.0f));

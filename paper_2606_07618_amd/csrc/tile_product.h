@@ -56,9 +56,11 @@ __device__ __forceinline__ uint32_t load1(__amdgpu_buffer_rsrc_t r, uint32_t at)
     return (uint32_t)__builtin_amdgcn_raw_buffer_load_b8(r, (int)at, 0, 0);
 }
 
+// An E4M3 number times 2^UP.
+template <int UP = 0>
 __device__ __forceinline__ float e4m3_f32(uint32_t c) {
     // the code's fields as those of a binary32 number 2^120 times too small; the product is exact
-    return __uint_as_float((c & 0x7Fu) << 20) * 0x1p120f;
+    return __uint_as_float((c & 0x7Fu) << 20) * __builtin_ldexpf(0x1p120f, UP);
 }
 
 template <int V> struct Const { static constexpr int value = V; };

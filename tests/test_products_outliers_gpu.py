@@ -48,3 +48,20 @@ def test_rows_of_every_size(nv, m):
     want, bound = plain64.product(plain64.f64(x), plain64.nvfp4_values(q, sc, 16))
     # products below binary32's normal range may be lost, one quantum for each term
     plain64.check(nv.matmul(x, q, sc, S, out_dtype=torch.float32), want, bound + 2.0 ** -23 * want.abs() + k * 2.0 ** -126)
+
+
+@pytest.mark.parametrize("block,k", [(16, 256), (16, 272), (32, 256), (128, 256)])
+@pytest.mark.parametrize("m", [1, 2, 3, 4, 5, 40, 100, 513])
+def test_largest_activations(nv, m, block, k):
+    """Activations of 2^126 and small scales: no sum on the way leaves binary32 where the outputs lie within it."""
+    n, g = 72, workloads.generator(DEV, 533, m, block, k)
+    q = torch.randint(0, 256, (n, k // 2), generator=g, device=DEV, dtype=torch.uint8)
+    sc = torch.randint(0, 4, (n, k // block), generator=g, device=DEV, dtype=torch.uint8)
+    q[:, :block // 2], sc[:, 0] = 0x77, 3            # a block of the largest values
+    x = (torch.randn((m, k), generator=g, device=DEV) * 2.0 ** 123).bfloat16()
+    x[:, :block] = 2.0 ** (126 if block < 128 else 122)
+    S = torch.full((1,), 2.0 ** -20, device=DEV)
+    want, bound = plain64.product(plain64.f64(x), plain64.nvfp4_values(q, sc, block))
+    assert float(want.abs().max()) < 2.0 ** 127
+    plain64.check(nv.matmul(x, q, sc, S, block=block, out_dtype=torch.float32), want * 2.0 ** -20, bound * 2.0 ** -20
+                  + 2.0 ** -23 * want.abs() * 2.0 ** -20)
