@@ -401,6 +401,53 @@ int mxfp4_matmul_grad_input(const void* dy, int64_t ld, const uint8_t* q, const 
                             int64_t k, int out_dtype, void* dx, void* workspace, size_t workspace_bytes,
                             void* stream);
 
+/*
+ * Products of rows sorted by group with the weights of their own group: the tokens of each expert of a mixture.
+ *   offsets [experts + 1] device ints: group e has rows offsets[e] .. offsets[e + 1] - 1, any number of them.  They are
+ *           read on the device; what lies outside 0 .. rows counts as the nearest of these, and one that
+ *           descends as the largest before it, so no row is reached that is not there and none twice.
+ *   q, scales, tensor_scales: NVFP4 weights [n, k] of each group, one after the other, and their [experts]
+ *           global scales.
+ *   clear:  rows of no group (before offsets[0], from offsets[experts] on) become zero; 0: they are left as they were.
+ * As the products above else; rows <= 2^31 - 1, experts <= 2^20.  One launch (two where the gradient's rows are
+ * first copied to rows of whole 16 bytes). */
+
+/* y[i] = x[i] W_e^T S_e, x bfloat16 [rows, k], ldx % 8 == 0.  No workspace. */
+int nvfp4_grouped_product(const void* x, int64_t ldx, const int* offsets, const uint8_t* q, const uint8_t* scales, int block,
+                          const float* tensor_scales, int64_t rows, int64_t experts, int64_t n, int64_t k, int out_dtype,
+                          int clear, void* out, void* stream);
+
+/* Its gradient with respect to x: dx[i] = dy[i] W_e S_e, dy bfloat16 [rows, n], any ld >= n. */
+int64_t nvfp4_grouped_product_grad_input_workspace_bytes(int64_t rows, int64_t n, int64_t ld);
+int nvfp4_grouped_product_grad_input(const void* dy, int64_t ld, const int* offsets, const uint8_t* q, const uint8_t* scales,
+                                     int block, const float* tensor_scales, int64_t rows, int64_t experts, int64_t n, int64_t k,
+                                     int out_dtype, int clear, void* dx, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * 8-bit integers with a scale for each row: x_hat = s q, |q| <= 127.
+ *   q       [rows, 16 ceil(cols / 16)] bytes, zeros past the width, 16-byte aligned
+ *   scales  [rows] binary32
+ * Activations have a scale for each token so, weights [n, k] one for each output channel.
+ */
+
+/* s = max|x| / 127 of the row, rounded to binary32; q the whole number nearest to the quotient x / s, ties to the even
+ * one, at most 127 in magnitude; s = 0: q = 0.  A row that holds an infinity or a NaN gets s = NaN (and q = 0): its
+ * products are NaN.  x: [rows, cols], rows ldx elements apart, binary32 or bfloat16, aligned to its elements;
+ * cols < 2^17.  One kernel, no workspace. */
+int int8_quant(const void* x, int dtype, int64_t rows, int64_t cols, int64_t ldx, int8_t* q, float* scales, void* stream);
+
+/* y = A B^T of A [m, k] and B [n, k] quantized so: y[i][j] = s_a[i] s_b[j] sum q_a q_b, the sum exact (k < 2^17,
+ * else NVFP4_ERR_SHAPE), then rounded to binary32, times the product of the scales, and to the output.  q may hold -128. */
+int64_t int8_matmul_workspace_bytes(int64_t m, int64_t n, int64_t k);
+int int8_matmul(const int8_t* a_q, const float* a_scales, const int8_t* b_q, const float* b_scales, int64_t m, int64_t n,
+                int64_t k, int out_dtype, void* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* dx = dy B of bfloat16 dy [m, n] (any ld >= n) and B [n, k]: the gradient of the product above with respect to A,
+ * straight through A's quantization.  The weights s q are rounded to bfloat16 as operands. */
+int64_t int8_matmul_grad_input_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t ld);
+int int8_matmul_grad_input(const void* dy, int64_t ld, const int8_t* q, const float* scales, int64_t m, int64_t n, int64_t k,
+                           int out_dtype, void* dx, void* workspace, size_t workspace_bytes, void* stream);
+
 /* The gated feed-forward block, without g and u in memory: g = x Wg^T, u = x Wu^T, h = silu(g) u with
  * silu(g) = g / (1 + e^-g), all bfloat16 with sums in binary32; h is formed from the unrounded sums.
  * x [m, k] (rows ldx apart), w_gate and w_up [n, k] (rows ldw apart), any k.  h [m, n]; gate and up

@@ -10,7 +10,7 @@ ROOT = HERE.parent
 SRC = HERE / "csrc" / "nvfp4ss.hip"
 SOURCES = [SRC, HERE / "csrc" / "optimum.hip", HERE / "csrc" / "importance.hip",
            HERE / "csrc" / "gptq.hip", HERE / "csrc" / "mxfp4.hip", HERE / "csrc" / "matmul.hip",
-           HERE / "csrc" / "ffn.hip"]
+           HERE / "csrc" / "ffn.hip", HERE / "csrc" / "int8.hip", HERE / "csrc" / "grouped.hip"]
 LIB = HERE / "libnvfp4ss.so"
 
 HIPCC_FLAGS = [

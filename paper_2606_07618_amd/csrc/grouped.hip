@@ -1,0 +1,135 @@
+// Products of grouped rows with NVFP4 weights of each group's own: the experts of a mixture, y = x W_e^T and dx = dy W_e.
+#include "grouped_product.h"
+#include "product_host.h"
+
+namespace {
+
+using namespace product_host;
+using grouped_product::kPair, grouped_product::kOne, grouped_product::kOdd;
+using grouped_product::Scales;
+
+constexpr int64_t kMostGroupedRows = 0x7FFFFFFF, kMostExperts = (int64_t)1 << 20;
+
+// Which kernel: rows of a tile and outputs of it, by the rows that a group has on average.
+struct GroupedPlan { int height, width, threads; };
+
+using Large = grouped_product::Tile<256, 4, 64>;
+using Small = grouped_product::Tile<128, 2, 32>;
+
+constexpr int kFewThreads = grouped_product::kFewWaves * kLanes;
+
+GroupedPlan plan_grouped(int64_t rows, int64_t experts, int64_t outer, bool turned) {
+    const int64_t active = rows < experts ? rows : experts, each = active ? ceil_div(rows, active) : 0;
+    if (!turned && each <= 32) {
+        const int height = each <= 16 ? 16 : 32;
+        const int64_t tiles = active * ceil_div(each, height);
+        const int width = tiles * ceil_div(outer, 64) >= 512 ? 64 : tiles * ceil_div(outer, 32) >= 512 ? 32 : 16;
+        return {height, width, kFewThreads};
+    }
+    if (each > 128 && active * ceil_div(each, 256) * ceil_div(outer, 256) >= 192) return {Large::M, Large::N, Large::kThreads};
+    return {Small::M, Small::N, Small::kThreads};
+}
+
+// Row tiles that there may be, and one more, which finds rows of no group to clear.
+int64_t most_tiles(int64_t rows, int64_t experts, int height) {
+    return rows / height + (rows < experts ? rows : experts) + 1;
+}
+
+int check_grouped(int64_t rows, int64_t experts, int64_t n, int64_t k, int block) {
+    if (block != 16 && block != 32 && block != 64 && block != 128) return NVFP4_ERR_BLOCK;
+    if (const int rc = check_dims(rows, n, k)) return rc;
+    if (rows > kMostGroupedRows || experts < 0 || experts > kMostExperts || k % block) return NVFP4_ERR_SHAPE;
+    return NVFP4_OK;
+}
+
+bool grouped_launchable(int64_t rows, int64_t experts, int64_t outer, bool turned) {
+    const GroupedPlan plan = plan_grouped(rows, experts, outer, turned);
+    return launchable(most_tiles(rows, experts, plan.height) * ceil_div(outer, plan.width), plan.threads);
+}
+
+template <int R, int C>
+void launch_few(const grouped_product::Args& p, Scales scales, dim3 grid, hipStream_t stream) {
+    auto kernel = scales == kPair ? grouped_product::few_kernel<R, C, kPair>
+                  : scales == kOne ? grouped_product::few_kernel<R, C, kOne> : grouped_product::few_kernel<R, C, kOdd>;
+    hipLaunchKernelGGL(kernel, grid, dim3(kFewThreads), 0, stream, p);
+}
+
+template <class T>
+void launch_tiled(const grouped_product::Args& p, Scales scales, bool turned, dim3 grid, hipStream_t stream) {
+    auto kernel = turned ? grouped_product::grouped_kernel<T, true, kOne>
+                  : scales == kPair ? grouped_product::grouped_kernel<T, false, kPair>
+                  : scales == kOne ? grouped_product::grouped_kernel<T, false, kOne> : grouped_product::grouped_kernel<T, false, kOdd>;
+    hipLaunchKernelGGL(kernel, grid, dim3(T::kThreads), 0, stream, p);
+}
+
+int run_grouped(grouped_product::Args p, bool turned, int block, hipStream_t stream) {
+    const GroupedPlan plan = plan_grouped(p.rows, p.experts, p.outer, turned);
+    p.shift = block == 16 ? 4 : block == 32 ? 5 : block == 64 ? 6 : 7;
+    p.tiles_n = ceil_div(p.outer, plan.width);
+    const dim3 grid((unsigned)(most_tiles(p.rows, p.experts, plan.height) * p.tiles_n));
+    const Scales scales = p.shift > 4 ? kOne : p.k % 32 ? kOdd : kPair;
+    if (plan.threads == Large::kThreads && plan.height == Large::M) launch_tiled<Large>(p, scales, turned, grid, stream);
+    else if (plan.height == Small::M) launch_tiled<Small>(p, scales, turned, grid, stream);
+    else if (plan.height == 16) plan.width == 64 ? launch_few<4, 1>(p, scales, grid, stream) : plan.width == 32 ? launch_few<2, 1>(p, scales, grid, stream) : launch_few<1, 1>(p, scales, grid, stream);
+    else plan.width == 64 ? launch_few<4, 2>(p, scales, grid, stream) : plan.width == 32 ? launch_few<2, 2>(p, scales, grid, stream) : launch_few<1, 2>(p, scales, grid, stream);
+    return launched();
+}
+
+int check_workspace(const void* ws, size_t bytes, int64_t need) {
+    if (need > 0 && (!ws || (int64_t)bytes < need)) return NVFP4_ERR_WORKSPACE;
+    return aligned(ws, 256) || need == 0 ? NVFP4_OK : NVFP4_ERR_ALIGN;
+}
+
+int64_t grouped_grad_workspace(int64_t rows, int64_t n, int64_t ld) {
+    return needs_pack(n, ld) ? up(rows * packed_ld(n) * 2, 256) : 0;
+}
+
+}  // namespace
+
+extern "C" {
+
+int nvfp4_grouped_product(const void* x, int64_t ldx, const int* offsets, const uint8_t* q, const uint8_t* scales, int block,
+                          const float* tensor_scales, int64_t rows, int64_t experts, int64_t n, int64_t k, int out_dtype,
+                          int clear, void* out, void* stream) {
+    if (out_dtype != NVFP4_IN_F32 && out_dtype != NVFP4_IN_BF16) return NVFP4_ERR_DTYPE;
+    if (const int rc = check_grouped(rows, experts, n, k, block)) return rc;
+    if (ldx < k || ldx > kMaxLd || !grouped_launchable(rows, experts, n, false)) return NVFP4_ERR_SHAPE;
+    if (rows == 0 || n == 0 || (experts == 0 && !clear)) return NVFP4_OK;
+    if (!out || !offsets || (experts > 0 && (!tensor_scales || (k > 0 && (!x || !q || !scales))))) return NVFP4_ERR_NULL;
+    if (!aligned(x, 16) || ldx % 8 || !aligned(q, 16) || !aligned(out, 16) || !aligned(tensor_scales, 4) || !aligned(offsets, 4))
+        return NVFP4_ERR_ALIGN;
+    grouped_product::Args p = {};
+    p.x = static_cast<const char*>(x), p.ld = ldx * 2, p.rows = rows, p.offsets = offsets, p.experts = (int)experts;
+    p.q = reinterpret_cast<const char*>(q), p.scales = scales, p.S = tensor_scales, p.n = n, p.k = k, p.inner = k, p.outer = n;
+    p.out = out, p.out_f32 = out_dtype == NVFP4_IN_F32, p.clear = clear != 0;
+    return run_grouped(p, false, block, (hipStream_t)stream);
+}
+
+int64_t nvfp4_grouped_product_grad_input_workspace_bytes(int64_t rows, int64_t n, int64_t ld) {
+    if (const int rc = check_dims(rows, n, 0)) return rc;
+    return grouped_grad_workspace(rows, n, ld);
+}
+
+int nvfp4_grouped_product_grad_input(const void* dy, int64_t ld, const int* offsets, const uint8_t* q, const uint8_t* scales,
+                                     int block, const float* tensor_scales, int64_t rows, int64_t experts, int64_t n, int64_t k,
+                                     int out_dtype, int clear, void* dx, void* workspace, size_t workspace_bytes, void* stream) {
+    if (out_dtype != NVFP4_IN_F32 && out_dtype != NVFP4_IN_BF16) return NVFP4_ERR_DTYPE;
+    if (const int rc = check_grouped(rows, experts, n, k, block)) return rc;
+    if (ld < n || ld > kMaxLd || !grouped_launchable(rows, experts, k, true)) return NVFP4_ERR_SHAPE;
+    if (rows == 0 || k == 0 || (experts == 0 && !clear)) return NVFP4_OK;
+    if (!dx || !offsets || (experts > 0 && (!tensor_scales || (n > 0 && (!dy || !q || !scales))))) return NVFP4_ERR_NULL;
+    if (!aligned(dy, 16) || !aligned(q, 16) || !aligned(dx, 16) || !aligned(tensor_scales, 4) || !aligned(offsets, 4))
+        return NVFP4_ERR_ALIGN;
+    if (const int rc = check_workspace(workspace, workspace_bytes, grouped_grad_workspace(rows, n, ld))) return rc;
+    if (needs_pack(n, ld) && n > 0) {
+        if (const int rc = pack_bf16_rows(dy, rows, n, ld, workspace, (hipStream_t)stream)) return rc;
+        dy = workspace, ld = packed_ld(n);
+    }
+    grouped_product::Args p = {};
+    p.x = static_cast<const char*>(dy), p.ld = ld * 2, p.rows = rows, p.offsets = offsets, p.experts = (int)experts;
+    p.q = reinterpret_cast<const char*>(q), p.scales = scales, p.S = tensor_scales, p.n = n, p.k = k, p.inner = n, p.outer = k;
+    p.out = dx, p.out_f32 = out_dtype == NVFP4_IN_F32, p.clear = clear != 0;
+    return run_grouped(p, true, block, (hipStream_t)stream);
+}
+
+}  // extern "C"

@@ -11,8 +11,10 @@ namespace product_plan {
 inline int64_t up(int64_t v, int64_t unit) { return (v + unit - 1) / unit * unit; }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Microscaled operands' scales as the rows lie (kMx, rows of whole words), or laid out step by step (kMxLaid).
-enum Kind { kBf16, kMx, kMxLaid };
+// Microscaled operands' scales as the rows lie (kMx, rows of whole words), or laid out step by step (kMxLaid).  kInt8:
+// 8-bit integers, sums in 32 bits, exact, and a scale for each row of either operand.
+enum Kind { kBf16, kMx, kMxLaid, kInt8 };
+template <Kind KIND> constexpr bool kMicroscaled = KIND == kMx || KIND == kMxLaid;
 
 // What happens to the sums.
 enum Out {
@@ -45,7 +47,7 @@ inline const TileCost* tile_costs() {
                                             {64, 128, 5.1f, 0.64f, 1.4f, 0.48f}, {64, 64, 4.4f, 0.40f, 1.3f, 0.31f}};
     static constexpr TileCost bf16[kTiles] = {{256, 256, 9.8f, 1.05f, 8.5f, 1.54f}, {128, 128, 5.1f, 0.77f, 2.5f, 0.51f},
                                               {64, 128, 4.7f, 0.38f, 1.7f, 0.34f}, {64, 64, 3.7f, 0.31f, 1.3f, 0.23f}};
-    return KIND != kBf16 ? mx : bf16;
+    return kMicroscaled<KIND> ? mx : bf16;                   // kInt8: a step's bytes and instructions take what bfloat16's do
 }
 
 // Fragments of a wave's rows of A and of B.
@@ -54,7 +56,7 @@ constexpr int kFragments[kTiles][2] = {{8, 4}, {4, 4}, {2, 4}, {2, 2}};
 struct Plan { int tile, parts; float us; };
 
 // Values of a step of the contraction, and outer indexes of B for an output.
-template <Kind KIND> constexpr int kStepValues = KIND != kBf16 ? 256 : 64;
+template <Kind KIND> constexpr int kStepValues = kMicroscaled<KIND> ? 256 : KIND == kInt8 ? 128 : 64;
 template <Out OUT> constexpr int kHalf = OUT == kGate ? 2 : 1;
 
 // Estimated microseconds with tile t and the contraction in `parts`.  Up to a workgroup a compute unit, what they take
@@ -69,7 +71,7 @@ float product_us(int t, int parts, int64_t m, int64_t n, int64_t inner) {
     const float few = cost.start + own * (cost.alone + share);
     const float many = load > 1.0f ? kLaunchUs + (float)(int64_t)(load + 0.999f) * (cost.fixed + own * cost.among) : 0.0f;
     float us = few > many ? few : many;
-    if (KIND != kBf16 && t == 0) us += kLayUs;
+    if (kMicroscaled<KIND> && t == 0) us += kLayUs;
     if (parts > 1) us += kJoinUs + (float)m * (float)n * (float)(8 * kHalf<OUT> * parts) / kJoinBytesUs;
     return us;
 }

@@ -1,13 +1,13 @@
 // Tiled matrix product on the matrix cores of gfx950, D[m][n] = sum_k A[m][k] B[n][k], sums in
 // binary32, for bfloat16 operands and for microscaled FP4 ones (E2M1 nibbles with an E8M0 scale
-// for each 32 values of a row).  Both operands' rows hold the contraction; what is done with the sums is a
+// for each 32 values of a row); and for 8-bit integers, sums in 32-bit integers.  Both operands' rows hold the contraction; what is done with the sums is a
 // template argument.  (A contraction that runs down an operand's rows is turned before: with the matrix
 // turned inside the product, by transposing reads of LDS, a step took 1.5 us in place of 1.0, and a
 // gradient of [4096, 14336] x [14336, 4096] 438 us in place of 360, of which 37 for the turning.)
 //
-// Both element types share one geometry: a step takes 128 bytes of every row of the tile (64
-// bfloat16 values, 256 FP4 ones), and a lane's operand of one matrix instruction is 16 of them (8
-// values of 16x16x32, 32 of 16x16x128), so staging, LDS layout and register tiles are the same.
+// All element types share one geometry: a step takes 128 bytes of every row of the tile (64
+// bfloat16 values, 128 integers, 256 FP4 ones), and a lane's operand of one matrix instruction is 16 of them (8
+// values of 16x16x32, 16 of 16x16x64, 32 of 16x16x128), so staging, LDS layout and register tiles are the same.
 // (On random values the card's power holds 16x16 instructions at 2.13 PFLOP/s bfloat16 and 7.5 FP4, the
 // 32x32 ones at 1.86 and 6.3.)
 #pragma once
@@ -20,7 +20,7 @@
 
 namespace tile_product {
 
-using product_plan::Kind, product_plan::kBf16, product_plan::kMx, product_plan::kMxLaid;
+using product_plan::Kind, product_plan::kBf16, product_plan::kMx, product_plan::kMxLaid, product_plan::kInt8;
 using product_plan::Out, product_plan::kSums, product_plan::kPartial, product_plan::kGate, product_plan::kGatePartial,
     product_plan::kTwoRows;
 
@@ -187,6 +187,7 @@ struct Args {
     int parts;
     int out_f32;
     const float* scale;         // NULL: 1
+    const float *scale_m, *scale_n;      // kInt8: of the outer indexes of A and of B
     void *out, *out2, *out3;
     int64_t half_rows;          // kTwoRows
     int64_t out_ld;
@@ -209,12 +210,26 @@ __device__ __forceinline__ void store4(void* out, int f32, int64_t at, int64_t l
     }
 }
 
+// A lane's sums of a matrix instruction.  Integers leave as the nearest binary32 numbers times the two scales, or, as
+// parts, in the bits of a binary32 number.
+template <Kind KIND> struct SumsOf { typedef f32x4 type; };
+template <> struct SumsOf<kInt8> { typedef i32x4 type; };
+__device__ __forceinline__ f32x4 to_f32(i32x4 v) { return f32x4{(float)v[0], (float)v[1], (float)v[2], (float)v[3]}; }
+
+// The scales of n .. n + 3, those that there are.
+__device__ __forceinline__ f32x4 scales4(const float* s, int64_t n, int64_t left) {
+    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int r = 0; r < 4; ++r) if (r < left) v[r] = s[n + r];
+    return v;
+}
+
 template <Kind KIND, Out OUT, class T>
 __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(Args p) {
     constexpr bool HALF = OUT == kGate || OUT == kGatePartial;
     using A = Side<T::M, T::kThreads, false>;
     using B = Side<T::N, T::kThreads, HALF>;
-    constexpr bool kScaled = KIND != kBf16, kLaid = KIND == kMxLaid;
+    constexpr bool kScaled = product_plan::kMicroscaled<KIND>, kLaid = KIND == kMxLaid;
     constexpr int kScales = kScaled ? (T::M + T::N) * 8 : 0;           // eight bytes a row and step
     constexpr int kScaleLoads = (kScales + T::kThreads * 4 - 1) / (T::kThreads * 4);
     constexpr bool kEven = kScales % (T::kThreads * 4) == 0;               // else the last waves' last load is not one
@@ -260,7 +275,7 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
         }
     }
     const char* a0 = p.a.p + m0 * p.a.ld;
-    const int64_t b_at = n0 * p.b.ld, row_bytes = kScaled ? p.inner / 2 : p.inner * 2;
+    const int64_t b_at = n0 * p.b.ld, row_bytes = kScaled ? p.inner / 2 : KIND == kInt8 ? p.inner : p.inner * 2;
     auto fetch_a = [&](int64_t s, int stage) {
         sa.load(a0 + s * kStepBytes, nullptr, lds[stage], row_bytes - s * kStepBytes, tid, wave);
     };
@@ -290,11 +305,12 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
         return (j < NF / 2 ? 0 : T::N / 2) + wn * (T::N / 2 / T::WN) + j % (NF / 2) * 16;
     };
 
-    f32x4 acc[MF][NF];
+    using Sums = typename SumsOf<KIND>::type;
+    Sums acc[MF][NF];
 #pragma unroll
     for (int i = 0; i < MF; ++i)
 #pragma unroll
-        for (int j = 0; j < NF; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int j = 0; j < NF; ++j) acc[i][j] = Sums{0, 0, 0, 0};
 
     // A step is 2 MF groups of NF matrix instructions, a fragment of A against a half's fragments of B.
     // Registers run kLead groups ahead of them (a whole half for B), LDS kSlots steps: while a group is
@@ -363,7 +379,9 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
         for (int j = 0; j < NF; ++j) {
             // B's values as the instruction's rows: a lane gets four neighbouring outputs of a row of D
             const i32x4 b = fb[H][j], a = fa[g % kRing];
-            if constexpr (!kScaled) {
+            if constexpr (KIND == kInt8) {
+                acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(b, a, acc[i][j], 0, 0, 0);
+            } else if constexpr (!kScaled) {
                 acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, b), __builtin_bit_cast(bf16x8, a),
                                                                     acc[i][j], 0, 0, 0);
             } else {
@@ -422,6 +440,26 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
     // whose outputs are too many to stay in the L2 until they are read, stores them past it and leaves the L2 to the
     // operands (the same product: 282 -> 252 us).
     const float scale = OUT == kSums && p.scale ? *p.scale : 1.0f;
+    // integers: the scales of this lane's columns and of its rows
+    f32x4 scale_n[KIND == kInt8 && OUT == kSums ? NF : 1];
+    float scale_m[KIND == kInt8 && OUT == kSums ? MF : 1];
+    if constexpr (KIND == kInt8 && OUT == kSums) {
+#pragma unroll
+        for (int j = 0; j < NF; ++j) {
+            const int64_t n = n0 + b_row(j) + lane / 16 * 4;
+            scale_n[j] = scales4(p.scale_n, n, p.n - n);
+        }
+#pragma unroll
+        for (int i = 0; i < MF; ++i) {
+            const int64_t m = m0 + a_row(i) + lane % 16;
+            scale_m[i] = m < p.m ? p.scale_m[m] : 0.0f;
+        }
+    }
+    auto sums = [&](int i, int j) {
+        if constexpr (KIND != kInt8) return acc[i][j] * scale;
+        else if constexpr (OUT == kSums) return to_f32(acc[i][j]) * (scale_n[j] * scale_m[i]);
+        else return __builtin_bit_cast(f32x4, acc[i][j]);
+    };
     auto column = [&](int j) { return HALF ? wn * (kOutN / T::WN) + j * 16 : b_row(j); };
     if (OUT != kPartial && OUT != kGatePartial && !p.out_f32 && p.out_ld % 8 == 0) {
         constexpr int kOutChunks = kOutN / 8, kMask = kOutChunks < 16 ? kOutChunks - 1 : 15;
@@ -453,7 +491,7 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
         };
         auto rows_of = [&](void* out) { return [=](int64_t m) { return static_cast<uint16_t*>(out) + m * p.out_ld; }; };
         if constexpr (OUT == kSums) {
-            write([&](int i, int j) { return acc[i][j] * scale; }, rows_of(p.out));
+            write(sums, rows_of(p.out));
         } else if constexpr (OUT == kTwoRows) {
             write([&](int i, int j) { return acc[i][j]; }, [&](int64_t m) {
                 return m < p.half_rows ? static_cast<uint16_t*>(p.out) + m * p.out_ld
@@ -482,9 +520,11 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
 #pragma unroll
         for (int j = 0; j < (HALF ? NF / 2 : NF); ++j) {
             const int64_t n = n0 + column(j) + lane / 16 * 4, left = p.n - n;
-            const f32x4 v = acc[i][j];
+            f32x4 v;
+            if constexpr (KIND == kInt8) v = sums(i, j);
+            else v = acc[i][j];
             if constexpr (OUT == kSums) {
-                store4(p.out, p.out_f32, m * p.out_ld + n, left, vec, v * scale);
+                store4(p.out, p.out_f32, m * p.out_ld + n, left, vec, KIND == kInt8 ? v : v * scale);
             } else if constexpr (OUT == kPartial) {
                 store4(p.out, 1, (part * p.m + m) * p.out_ld + n, left, vec, v);
             } else if constexpr (OUT == kGatePartial) {

@@ -68,6 +68,14 @@ def _load():
         "nvfp4_matmul": (I, [P, I64, P, P, I, P, I64, I64, I64, I, P, P, SZ, P]),
         "nvfp4_matmul_grad_input_workspace_bytes": (I64, [I64, I64, I64, I64]),
         "nvfp4_matmul_grad_input": (I, [P, I64, P, P, I, P, I64, I64, I64, I, P, P, SZ, P]),
+        "nvfp4_grouped_product": (I, [P, I64, P, P, P, I, P, I64, I64, I64, I64, I, I, P, P]),
+        "nvfp4_grouped_product_grad_input_workspace_bytes": (I64, [I64, I64, I64]),
+        "nvfp4_grouped_product_grad_input": (I, [P, I64, P, P, P, I, P, I64, I64, I64, I64, I, I, P, P, SZ, P]),
+        "int8_quant": (I, [P, I, I64, I64, I64, P, P, P]),
+        "int8_matmul_workspace_bytes": (I64, [I64, I64, I64]),
+        "int8_matmul": (I, [P, P, P, P, I64, I64, I64, I, P, P, SZ, P]),
+        "int8_matmul_grad_input_workspace_bytes": (I64, [I64, I64, I64, I64]),
+        "int8_matmul_grad_input": (I, [P, I64, P, P, I64, I64, I64, I, P, P, SZ, P]),
         "nvfp4_swiglu_ffn_workspace_bytes": (I64, [I64, I64, I64, I64, I64]),
         "nvfp4_swiglu_ffn": (I, [P, I64, P, P, I64, I64, I64, I64, P, P, P, P, SZ, P]),
         "nvfp4_swiglu_ffn_backward_workspace_bytes": (I64, [I64, I64, I64, I64, I64]),

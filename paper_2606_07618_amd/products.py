@@ -24,7 +24,17 @@ mxfp4_matmul_workspace_bytes = lib.mxfp4_matmul_workspace_bytes
 mxfp4_matmul_grad_input = lib.mxfp4_matmul_grad_input
 mxfp4_matmul_grad_input_workspace_bytes = lib.mxfp4_matmul_grad_input_workspace_bytes
 
+nvfp4_grouped_product = lib.nvfp4_grouped_product
+nvfp4_grouped_product_grad_input = lib.nvfp4_grouped_product_grad_input
+nvfp4_grouped_product_grad_input_workspace_bytes = lib.nvfp4_grouped_product_grad_input_workspace_bytes
+int8_quant = lib.int8_quant
+int8_product = lib.int8_matmul
+int8_product_workspace_bytes = lib.int8_matmul_workspace_bytes
+int8_product_grad_input = lib.int8_matmul_grad_input
+int8_product_grad_input_workspace_bytes = lib.int8_matmul_grad_input_workspace_bytes
+
 MX_BLOCK = 32
+INT8_UNIT = 16                                   # rows of 8-bit integers hold whole ones
 
 
 def _dtype_id(dtype, what):
@@ -35,14 +45,14 @@ def _dtype_id(dtype, what):
     raise TypeError(f"{what} must be bfloat16 or float32")
 
 
-def _rows(t, what):
-    """The row stride of a bfloat16 device matrix whose rows are runs of values."""
+def _rows(t, what, dtypes=(torch.bfloat16,)):
+    """The row stride of a device matrix (bfloat16 unless said otherwise) whose rows are runs of values."""
     if t.dim() != 2:
         raise ValueError(f"{what} must be 2-D")
     if not t.is_cuda:
         raise ValueError(f"{what} must be a device tensor (the library runs on the GPU only)")
-    if t.dtype != torch.bfloat16:
-        raise TypeError(f"{what} must be bfloat16")
+    if t.dtype not in dtypes:
+        raise TypeError(f"{what} must be {' or '.join(str(d).split('.')[-1] for d in dtypes)}")
     rows, cols = t.shape
     if cols > 1 and t.stride(1) != 1:
         raise ValueError(f"{what}'s rows must be contiguous")
@@ -252,6 +262,147 @@ class _Matmul(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, dy):
         return (matmul_grad_input(_incoming(dy), *ctx.saved_tensors, ctx.block),) + (None,) * 6
+
+
+# ---- products of rows sorted by expert -----------------------------------------------------------
+
+def _grouped_weights(x, offsets, q, scales, S, block):
+    if q.dim() != 3:
+        raise ValueError("q must be 3-D [experts, n, k/2]")
+    experts, n, k = q.shape[0], q.shape[1], q.shape[2] * 2
+    _plain(q, (experts, n, k // 2), torch.uint8, "q")
+    if not (scales.is_cuda and scales.dtype == torch.uint8 and scales.is_contiguous()
+            and (block <= 0 or scales.shape == (experts, n, k // block))):
+        raise ValueError("scales must be a contiguous uint8 device tensor [experts, n, k/block], row-major")
+    _plain(S, (experts,), torch.float32, "S")
+    _plain(offsets, (experts + 1,), torch.int32, "offsets")
+    _same_device(x, offsets, q, scales, S)
+    return experts, n, k
+
+
+def grouped_matmul(x: torch.Tensor, offsets: torch.Tensor, q: torch.Tensor, scales: torch.Tensor, S: torch.Tensor,
+                   block: int = 16, out_dtype: torch.dtype = torch.bfloat16,
+                   out: torch.Tensor | None = None) -> torch.Tensor:
+    """y [rows, n]: each row of a bfloat16 x [rows, k], sorted by expert, times the NVFP4 weights of its own expert,
+    y[i] = x[i] W_e^T for offsets[e] <= i < offsets[e + 1] (device int32 [experts + 1]).  q [experts, n, k/2], scales
+    [experts, n, k/block] and S [experts] are what quantize() gives for each W_e, stacked.  Rows of no expert are zero, or
+    left as they were in a caller's ``out``.  Weights and x enter exactly, sums in binary32, rounded once.  Recorded by
+    autograd where x requires a gradient (grouped_matmul_grad_input; the weights are constants), unless ``out`` is given."""
+    if out is None and x.requires_grad and torch.is_grad_enabled():
+        return _GroupedMatmul.apply(x, offsets, q, scales, S, block, out_dtype)
+    dt = _dtype_id(out_dtype, "out_dtype")
+    ldx = _rows(x, "x")
+    experts, n, k = _grouped_weights(x, offsets, q, scales, S, block)
+    rows = x.shape[0]
+    if x.shape[1] != k:
+        raise ValueError("x must be [rows, k] for weights [experts, n, k]")
+    clear = out is None
+    out = _output(out, (rows, n), out_dtype, x)
+    _check(nvfp4_grouped_product(_ptr(x), ldx, _ptr(offsets), _ptr(q), _ptr(scales), block, _ptr(S), rows, experts, n, k, dt,
+                                 clear, _ptr(out), _stream(x)), "nvfp4_grouped_product")
+    return out
+
+
+def grouped_matmul_grad_input(dy: torch.Tensor, offsets: torch.Tensor, q: torch.Tensor, scales: torch.Tensor,
+                              S: torch.Tensor, block: int = 16, out_dtype: torch.dtype = torch.bfloat16,
+                              out: torch.Tensor | None = None, ws: torch.Tensor | None = None) -> torch.Tensor:
+    """dx [rows, k] of a bfloat16 dy [rows, n]: grouped_matmul()'s gradient with respect to x, dx[i] = dy[i] W_e; zero for
+    rows of no expert (a caller's ``out``: left as they were)."""
+    dt = _dtype_id(out_dtype, "out_dtype")
+    ld = _rows(dy, "dy")
+    experts, n, k = _grouped_weights(dy, offsets, q, scales, S, block)
+    rows = dy.shape[0]
+    if dy.shape[1] != n:
+        raise ValueError("dy must be [rows, n] for weights [experts, n, k]")
+    clear = out is None
+    out = _output(out, (rows, k), out_dtype, dy)
+    ws, nbytes = _workspace(nvfp4_grouped_product_grad_input_workspace_bytes(rows, n, ld), ws, dy,
+                            "nvfp4_grouped_product_grad_input_workspace_bytes")
+    _check(nvfp4_grouped_product_grad_input(_ptr(dy), ld, _ptr(offsets), _ptr(q), _ptr(scales), block, _ptr(S), rows,
+                                            experts, n, k, dt, clear, _ptr(out), _ptr(ws), nbytes, _stream(dy)),
+           "nvfp4_grouped_product_grad_input")
+    return out
+
+
+class _GroupedMatmul(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, offsets, q, scales, S, block, out_dtype):
+        ctx.save_for_backward(offsets, q, scales, S)
+        ctx.block = block
+        return grouped_matmul(x, offsets, q, scales, S, block, out_dtype)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        return (grouped_matmul_grad_input(_incoming(dy), *ctx.saved_tensors, ctx.block),) + (None,) * 6
+
+
+# ---- 8-bit integers ------------------------------------------------------------------------------
+
+def int8_quantize(x: torch.Tensor, out=None):
+    """8-bit integers of the rows of a bfloat16 or float32 device matrix [rows, cols] (rows may be strided):
+    (q [rows, 16 ceil(cols / 16)] int8, zeros past the width, scales [rows] float32), x about q * scale with
+    scale = max|x| / 127 of the row: a scale for each token of an activation, for each output channel of weights
+    [n, k].  See int8_quant."""
+    ldx = _rows(x, "x", (torch.bfloat16, torch.float32))
+    rows, cols = x.shape
+    q, sc = (None, None) if out is None else out
+    q = _output(q, (rows, -(-cols // INT8_UNIT) * INT8_UNIT), torch.int8, x, "q")
+    sc = _output(sc, (rows,), torch.float32, x, "scales")
+    _check(int8_quant(_ptr(x), _dtype_id(x.dtype, "x"), rows, cols, ldx, _ptr(q), _ptr(sc), _stream(x)), "int8_quant")
+    return q, sc
+
+
+def _int8_pair(q, scales, what):
+    if q.dim() != 2 or q.shape[1] % INT8_UNIT:
+        raise ValueError(f"{what} must be (q [rows, a multiple of {INT8_UNIT}], scales [rows])")
+    rows, k = q.shape
+    _plain(q, (rows, k), torch.int8, f"{what}'s q")
+    _plain(scales, (rows,), torch.float32, f"{what}'s scales")
+    _same_device(q, scales)
+    return rows, k
+
+
+def int8_matmul(a, b, out_dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None,
+                ws: torch.Tensor | None = None) -> torch.Tensor:
+    """y = A B^T [m, n] of two matrices in 8-bit integers (q, scales) as int8_quantize() gives them, A [m, k] and
+    B [n, k]: the integers' sum, exact, times the product of the two rows' scales."""
+    dt = _dtype_id(out_dtype, "out_dtype")
+    (aq, asc), (bq, bsc) = a, b
+    m, k = _int8_pair(aq, asc, "a")
+    n, k2 = _int8_pair(bq, bsc, "b")
+    if k != k2:
+        raise ValueError("a and b must have rows of the same length")
+    _same_device(aq, bq)
+    out = _output(out, (m, n), out_dtype, aq)
+    ws, nbytes = _workspace(int8_product_workspace_bytes(m, n, k), ws, aq, "int8_matmul_workspace_bytes")
+    _check(int8_product(_ptr(aq), _ptr(asc), _ptr(bq), _ptr(bsc), m, n, k, dt, _ptr(out), _ptr(ws), nbytes,
+                        _stream(aq)), "int8_matmul")
+    return out
+
+
+def int8_matmul_grad_input(dy: torch.Tensor, q: torch.Tensor, scales: torch.Tensor, cols: int | None = None,
+                           out_dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None,
+                           ws: torch.Tensor | None = None) -> torch.Tensor:
+    """dx = dy B [m, cols] of a bfloat16 dy [m, n] and B [n, cols] in 8-bit integers: the gradient of int8_matmul's A
+    (straight through its quantization).  B's values are rounded to bfloat16 as operands.  cols: whole rows of q by
+    default."""
+    dt = _dtype_id(out_dtype, "out_dtype")
+    ld = _rows(dy, "dy")
+    m = dy.shape[0]
+    n, k = _int8_pair(q, scales, "the weights")
+    if dy.shape[1] != n:
+        raise ValueError("dy must be [m, n] for weights of n rows")
+    cols = k if cols is None else cols
+    if -(-cols // INT8_UNIT) * INT8_UNIT != k:
+        raise ValueError(f"cols must lie in the last {INT8_UNIT} of a row's {k}")
+    out = _output(out, (m, cols), out_dtype, dy)
+    _same_device(dy, q)
+    ws, nbytes = _workspace(int8_product_grad_input_workspace_bytes(m, n, cols, ld), ws, dy,
+                            "int8_matmul_grad_input_workspace_bytes")
+    _check(int8_product_grad_input(_ptr(dy), ld, _ptr(q), _ptr(scales), m, n, cols, dt, _ptr(out), _ptr(ws), nbytes,
+                                   _stream(dy)), "int8_matmul_grad_input")
+    return out
 
 
 # ---- the gated feed-forward block --------------------------------------------------------------
