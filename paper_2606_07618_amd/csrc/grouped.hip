@@ -13,8 +13,8 @@ constexpr int64_t kMostGroupedRows = 0x7FFFFFFF, kMostExperts = (int64_t)1 << 20
 // Which kernel: rows of a tile and outputs of it, by the rows that a group has on average.
 struct GroupedPlan { int height, width, threads; };
 
-using Large = grouped_product::Tile<256, 4, 64>;
-using Small = grouped_product::Tile<128, 2, 32>;
+using Large = grouped_product::Tile<256, 4>;
+using Small = grouped_product::Tile<128, 2>;
 
 constexpr int kFewThreads = grouped_product::kFewWaves * kLanes;
 
@@ -55,10 +55,8 @@ void launch_few(const grouped_product::Args& p, Scales scales, dim3 grid, hipStr
 }
 
 template <class T>
-void launch_tiled(const grouped_product::Args& p, Scales scales, bool turned, dim3 grid, hipStream_t stream) {
-    auto kernel = turned ? grouped_product::grouped_kernel<T, true, kOne>
-                  : scales == kPair ? grouped_product::grouped_kernel<T, false, kPair>
-                  : scales == kOne ? grouped_product::grouped_kernel<T, false, kOne> : grouped_product::grouped_kernel<T, false, kOdd>;
+void launch_tiled(const grouped_product::Args& p, bool turned, dim3 grid, hipStream_t stream) {
+    auto kernel = turned ? grouped_product::grouped_kernel<T, true> : grouped_product::grouped_kernel<T, false>;
     hipLaunchKernelGGL(kernel, grid, dim3(T::kThreads), 0, stream, p);
 }
 
@@ -68,8 +66,8 @@ int run_grouped(grouped_product::Args p, bool turned, int block, hipStream_t str
     p.tiles_n = ceil_div(p.outer, plan.width);
     const dim3 grid((unsigned)(most_tiles(p.rows, p.experts, plan.height) * p.tiles_n));
     const Scales scales = p.shift > 4 ? kOne : p.k % 32 ? kOdd : kPair;
-    if (plan.threads == Large::kThreads && plan.height == Large::M) launch_tiled<Large>(p, scales, turned, grid, stream);
-    else if (plan.height == Small::M) launch_tiled<Small>(p, scales, turned, grid, stream);
+    if (plan.threads == Large::kThreads && plan.height == Large::M) launch_tiled<Large>(p, turned, grid, stream);
+    else if (plan.height == Small::M) launch_tiled<Small>(p, turned, grid, stream);
     else if (plan.height == 16) plan.width == 64 ? launch_few<4, 1>(p, scales, grid, stream) : plan.width == 32 ? launch_few<2, 1>(p, scales, grid, stream) : launch_few<1, 1>(p, scales, grid, stream);
     else plan.width == 64 ? launch_few<4, 2>(p, scales, grid, stream) : plan.width == 32 ? launch_few<2, 2>(p, scales, grid, stream) : launch_few<1, 2>(p, scales, grid, stream);
     return launched();

@@ -90,7 +90,7 @@ __device__ __forceinline__ void clear_rows(const Args& p, const Place& t, int64_
 
 // Row tile and columns from a workgroup's number: an XCD gets a run of the sequence, which walks kDeep row tiles at a
 // time, so that what it works on at one time shares rows and weights in its L2.
-constexpr int kDeep = 4;
+constexpr int kDeep = 8;
 struct Work { int64_t index, n; };
 __device__ __forceinline__ Work work_of(int64_t id, int64_t count, int64_t tiles_n) {
     const int64_t xcd = id % kXcds, each = count / kXcds, rest = count % kXcds, tiles_m = count / tiles_n;
@@ -203,174 +203,90 @@ __global__ __launch_bounds__(kFewWaves * kLanes) void few_kernel(Args p) {
 // A group's last tile computes as many rows as it needs, in halves.
 constexpr int kSteps = 2;                        // in LDS
 
-// A row's chunks of 16 bytes exchanged by the row: reads take one chunk of 16 neighbouring rows, turned writes one of
-// rows 8 apart.
+// Turned weights: a row's chunks of 16 bytes exchanged by the row, as reads take one chunk of 16 neighbouring rows and
+// writes one of rows 8 apart.
 __device__ __forceinline__ int exchange(int row) { return ((row >> 1) ^ (row >> 4)) & 7; }
 
-template <int M_, int WN_, int LEAST_>
+template <int M_, int WN_>
 struct Tile {
     static constexpr int M = M_, WM = 2, WN = WN_, N = WN_ * 64, kThreads = WM * WN_ * kLanes;
-    static constexpr int kMost = M_ / 32, kLeast = LEAST_ / 32;      // a wave's fragments of rows
+    static constexpr int kStage = (M + N) * kStepBytes;              // of LDS, a step of rows and turned weights; a power of two
+    static constexpr int kLds = kSteps * (kStage + N * 16);
+    static constexpr int kMost = M_ / 32;                            // a wave's fragments of rows
 };
 
-template <class T, bool TURNED, Scales SCALES>
-struct Weights {
-    // As they lie: 32 values of a row.  Turned: 8 columns of four rows.
-    static constexpr int kLoads = TURNED ? 8 : SCALES == kOdd ? 4 : 2;
-    i32x4 v;
-    uint32_t s[TURNED ? 4 : 1];
+// A window of at most 2 GiB over the `left` bytes from `base` on: loads past it return zero without an access.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t window_of(const void* base, int64_t left) {
+    // by halves, in scalar registers
+    const uint32_t high = (uint32_t)((uint64_t)left >> 32), low = (uint32_t)left, most = low < kOutside ? low : kOutside;
+    const uint32_t size = high == 0 ? most : (int)high < 0 ? 0u : kOutside;
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, (int)size, 0x00020000);
+}
 
-    // s0: the step's first value of the contraction
-    __device__ __forceinline__ void load(const Args& p, __amdgpu_buffer_rsrc_t rq, __amdgpu_buffer_rsrc_t rs, int64_t n0, int64_t s0, int tid) {
-        const uint32_t q_ld = (uint32_t)(p.k / 2), s_ld = (uint32_t)(p.k >> p.shift);
-        if constexpr (TURNED) {
+// Stores to LDS that wait for nothing: as ordinary ones they would wait for all LDS loads on their way, which go to other
+// places (the compiler cannot know).  arrive() waits for them.  at: an address in LDS.
+template <int OFFSET>
+__device__ __forceinline__ void put8(uint32_t at, i32x2 v) { asm volatile("ds_write_b64 %0, %1 offset:%2" ::"v"(at), "v"(v), "n"(OFFSET)); }
+
+// A thread's turned weights of a step, 8 columns of four rows, and where they lie from the step's first row on.  Past the
+// group's weights they are zero.
+template <class T>
+struct Turned {
+    static constexpr int kLoads = 8, kParts = 4;
+    struct From {
+        uint32_t q, s, q_ld, s_ld;
+        __device__ __forceinline__ void init(const Args& p, int64_t n0, int tid) {
+            q_ld = (uint32_t)(p.k / 2), s_ld = (uint32_t)(p.k >> p.shift);
             const int column = tid % (T::N / 8) * 8, row = tid / (T::N / 8) * 4;
             const bool in = n0 + column < p.k;
+            q = in ? (uint32_t)row * q_ld + (uint32_t)column / 2 : kOutside;
+            s = in ? (uint32_t)row * s_ld + (((uint32_t)n0 + column) >> p.shift) : kOutside;
+        }
+        __device__ __forceinline__ void remake() { asm volatile("" : "+v"(q), "+v"(s)); }
+    };
+    i32x4 v;
+    uint32_t s[4];
+
+    __device__ __forceinline__ void load(const From& at, __amdgpu_buffer_rsrc_t rq, __amdgpu_buffer_rsrc_t rs) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const bool here = in && s0 + row + r < p.n;
-                const uint32_t at = (uint32_t)(row + r);
-                v[r] = __builtin_amdgcn_raw_buffer_load_b32(rq, (int)(here ? at * q_ld + (uint32_t)column / 2 : kOutside), 0, 0);
-                s[r] = load1(rs, here ? at * s_ld + (((uint32_t)n0 + column) >> p.shift) : kOutside);
-            }
-        } else {
-            const int row = tid / 2;
-            const uint32_t at = (uint32_t)s0 + tid % 2 * 32, k = (uint32_t)p.k;
-            const bool here = n0 + row < p.n, in0 = here && at < k;
-            const uint32_t q_at = (uint32_t)row * q_ld + at / 2, s_at = (uint32_t)row * s_ld + (at >> p.shift);
-            if constexpr (SCALES == kOdd) {
-                const bool in1 = here && at + 16 < k;
-                const i32x2 lo = load8(rq, in0 ? q_at : kOutside), hi = load8(rq, in1 ? q_at + 8 : kOutside);
-                v = i32x4{lo[0], lo[1], hi[0], hi[1]};
-                s[0] = load1(rs, in0 ? s_at : kOutside) | load1(rs, in1 ? s_at + 1 : kOutside) << 8;
-            } else {
-                v = load16(rq, in0 ? q_at : kOutside);
-                if constexpr (SCALES == kPair) s[0] = (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rs, (int)(in0 ? s_at : kOutside), 0, 0);
-                else s[0] = load1(rs, in0 ? s_at : kOutside);
-            }
+        for (int r = 0; r < 4; ++r) {
+            v[r] = __builtin_amdgcn_raw_buffer_load_b32(rq, (int)(at.q + r * at.q_ld), 0, 0);
+            s[r] = load1(rs, at.s + r * at.s_ld);
         }
     }
 
-    // Part H of 2.
-    template <int H>
-    __device__ __forceinline__ void store(char* lds, int tid) const {
-        if constexpr (TURNED) {
-            const int column = tid % (T::N / 8) * 8, row = tid / (T::N / 8) * 4;
-            float f[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) f[r] = e4m3_f32(s[r]);
-            const auto pair = [&](int r, auto c) {
-                return __builtin_amdgcn_cvt_scalef32_pk_f32_fp4((uint32_t)v[r], 1.0f, decltype(c)::value) * f[r];
-            };
-            const auto columns = [&](auto c) {           // two of them
-                const f32x2 a = pair(0, c), b = pair(1, c), d = pair(2, c), e = pair(3, c);
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int to = column + 2 * decltype(c)::value + j;
-                    // the upper halves of the products hold all of them
-                    const uint2 w = {__builtin_amdgcn_perm(__float_as_uint(b[j]), __float_as_uint(a[j]), 0x07060302u),
-                                     __builtin_amdgcn_perm(__float_as_uint(e[j]), __float_as_uint(d[j]), 0x07060302u)};
-                    *reinterpret_cast<uint2*>(lds + to * kStepBytes + ((row / 8) ^ exchange(to)) * kChunk + row % 8 * 2) = w;
-                }
-            };
-            columns(Const<2 * H>{}), columns(Const<2 * H + 1>{});
-        } else {
-            const int row = tid / 2, chunk = tid % 2 * 4;
-            const float f = e4m3_f32(SCALES == kOne || H == 0 ? s[0] : s[0] >> 8);
-#pragma unroll
-            for (int j = 2 * H; j < 2 * H + 2; ++j)
-                *reinterpret_cast<bf16x8*>(lds + row * kStepBytes + ((chunk + j) ^ exchange(row)) * kChunk) = expand8((uint32_t)v[j], f);
-        }
+    // Where a thread's weights go in LDS: with its chunks' places exchanged, part Q lies at base ^ 16 Q, 256 Q on.
+    __device__ static __forceinline__ uint32_t base(int tid) {
+        const int column = tid % (T::N / 8) * 8, row = tid / (T::N / 8) * 4;
+        return column * kStepBytes + ((row / 8) ^ exchange(column)) * kChunk + row % 8 * 2;
+    }
+    // Part Q, two columns of the four rows, to LDS at base address `to`.
+    template <int Q>
+    __device__ __forceinline__ void store(uint32_t to) const {
+        const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4((uint32_t)v[0], 1.0f, Q) * e4m3_f32(s[0]),
+                    b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4((uint32_t)v[1], 1.0f, Q) * e4m3_f32(s[1]),
+                    c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4((uint32_t)v[2], 1.0f, Q) * e4m3_f32(s[2]),
+                    d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4((uint32_t)v[3], 1.0f, Q) * e4m3_f32(s[3]);
+        // the upper halves of the products hold all of them
+        const auto pair = [](float lo, float hi) { return (int)__builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u); };
+        put8<2 * Q * kStepBytes>(to ^ (Q * kChunk), i32x2{pair(a[0], b[0]), pair(c[0], d[0])});
+        put8<(2 * Q + 1) * kStepBytes>(to ^ (Q * kChunk), i32x2{pair(a[1], b[1]), pair(c[1], d[1])});
     }
 };
 
-// The product of one tile, MF fragments of 16 rows a wave.
-template <class T, bool TURNED, Scales SCALES, int MF>
-__device__ __forceinline__ void product(const Args& p, const Place& t, int64_t n0, char (*lds)[(T::M + T::N) * kStepBytes], int tid) {
+// The sums of a tile, times the global scale, to the rows that there are.  All waves are done with LDS' contents.
+template <class T, int MF>
+__device__ __forceinline__ void finish(const Args& p, const Place& t, int64_t n0, char* lds, int tid, const f32x4 (&acc)[MF][4]) {
     constexpr int NF = 4, kRows = MF * 32;
-    using A = Side<kRows, T::kThreads, false>;
-    using B = Weights<T, TURNED, SCALES>;
     const int lane = tid % kLanes, wave = __builtin_amdgcn_readfirstlane(tid / kLanes), wm = wave / T::WN, wn = wave % T::WN;
-    A sa;
-    sa.init(t.left, p.ld, tid);
-    const char* a0 = p.x + t.first * p.ld;
-    const int64_t row_bytes = p.inner * 2, q_ld = p.k / 2, s_ld = p.k >> p.shift;
-    const int64_t w_row = t.expert * p.n + (TURNED ? 0 : n0);
-    auto fetch_a = [&](int64_t s, int slot) {
-        sa.load(a0 + s * kStepBytes, nullptr, lds[slot], row_bytes - s * kStepBytes, tid, wave);
-    };
-    auto fetch_b = [&](int64_t s, B& b) {
-        // turned, the window moves down the rows; else a tile's rows stay within it
-        const int64_t row = w_row + (TURNED ? s * 64 : 0);
-        b.load(p, window(p.q + row * q_ld + (TURNED ? n0 / 2 : 0)), window(p.scales + row * s_ld), n0, s * 64, tid);
-    };
     auto a_row = [&](int i) { return wm * (MF * 16) + i * 16; };
     auto b_row = [&](int j) { return wn * 64 + j * 16; };
-    auto read_b = [&](const char* b, int j, int h) {
-        const int row = b_row(j) + lane % 16, chunk = 4 * h + lane / 16;
-        return *reinterpret_cast<const i32x4*>(b + row * kStepBytes + ((chunk ^ exchange(row)) * kChunk));
-    };
-
-    f32x4 acc[MF][NF];
-#pragma unroll
-    for (int i = 0; i < MF; ++i)
-#pragma unroll
-        for (int j = 0; j < NF; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-
-    const int64_t steps = (p.inner + 63) / 64;
-    B b[2];
-    auto in_order = [] { asm volatile("" ::: "memory"); };   // the waits count on it
-    auto step = [&](int64_t s, auto dc) {
-        constexpr int d = decltype(dc)::value;
-        const char *la = lds[d], *lb = lds[d] + T::M * kStepBytes;
-        char* next = lds[1 - d] + T::M * kStepBytes;
-        // the next step's weights, then those of the step two behind it
-        b[1 - d].template store<0>(next, tid);
-        b[1 - d].template store<1>(next, tid);
-        in_order();
-        fetch_b(s + 3, b[1 - d]);
-        in_order();
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            i32x4 fb[NF];
-#pragma unroll
-            for (int j = 0; j < NF; ++j) fb[j] = read_b(lb, j, h);
-#pragma unroll
-            for (int i = 0; i < MF; ++i) {
-                const i32x4 a = h == 0 ? A::template read<0>(la, a_row(i), lane) : A::template read<1>(la, a_row(i), lane);
-#pragma unroll
-                for (int j = 0; j < NF; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fb[j]), __builtin_bit_cast(bf16x8, a),
-                                                                        acc[i][j], 0, 0, 0);
-            }
-        }
-        arrive<B::kLoads>();                               // the next step's rows; the weights' loads go on
-        fetch_a(s + 2, d);
-        in_order();
-    };
-    fetch_b(0, b[0]);
-    fetch_b(1, b[1]);
-    b[0].template store<0>(lds[0] + T::M * kStepBytes, tid);
-    b[0].template store<1>(lds[0] + T::M * kStepBytes, tid);
-    fetch_b(2, b[0]);
-    in_order();
-    fetch_a(0, 0);
-    in_order();
-    fetch_a(1, 1);
-    in_order();
-    arrive<A::kLoads>();
-    for (int64_t s = 0; s < steps; s += 2) {               // past the last step: zeros
-        step(s, Const<0>{});
-        step(s + 1, Const<1>{});
-    }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // no load into LDS outlives the workgroup
-
     const float S = p.S[t.expert];
     if (!p.out_f32 && p.outer % 8 == 0) {
         // through LDS, as whole rows of the tile
         constexpr int kOutChunks = T::N / 8, kMask = 15;
-        static_assert(kRows * T::N * 2 <= kSteps * (T::M + T::N) * kStepBytes, "the tile in LDS");
-        char* tile = lds[0];
+        static_assert(kRows * T::N * 2 <= T::kLds, "the tile in LDS");
+        char* tile = lds;
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < MF; ++i)
@@ -386,9 +302,12 @@ __device__ __forceinline__ void product(const Args& p, const Place& t, int64_t n
         for (int c = tid; c < kRows * kOutChunks; c += T::kThreads) {
             const int row = c / kOutChunks, chunk = c % kOutChunks;
             const int64_t n = n0 + chunk * 8;
-            if (row < t.left && n < p.outer)
-                *reinterpret_cast<i32x4*>(static_cast<uint16_t*>(p.out) + (t.first + row) * p.outer + n) =
-                    *reinterpret_cast<const i32x4*>(tile + (row * kOutChunks + (chunk ^ (row & kMask))) * kChunk);
+            if (row < t.left && n < p.outer) {
+                const i32x4 v = *reinterpret_cast<const i32x4*>(tile + (row * kOutChunks + (chunk ^ (row & kMask))) * kChunk);
+                i32x4* to = reinterpret_cast<i32x4*>(static_cast<uint16_t*>(p.out) + (t.first + row) * p.outer + n);
+                if constexpr (T::M == 256) __builtin_nontemporal_store(v, to);      // past the L2, which the operands need
+                else *to = v;
+            }
         }
         return;
     }
@@ -404,18 +323,342 @@ __device__ __forceinline__ void product(const Args& p, const Place& t, int64_t n
     }
 }
 
-template <class T, bool TURNED, Scales SCALES>
+// The product of one tile with weights as they lie, MF fragments of 16 rows a wave.
+//
+// Weights go into LDS as they are, 256 values of each row (whole lines) at a time, and from there into the registers of
+// each wave, which expands the fragments that it multiplies, once for its 16 MF rows.  (Expanded once for the whole tile,
+// as turned ones are, each weight would be written to LDS, four times as wide: those stores took 0.45 of a step's 1.5 us,
+// more than expanding twice, which fits between the matrix instructions.)
+template <class T, int MF>
+__device__ __forceinline__ void product_raw(const Args& p, const Place& t, int64_t n0, char* lds, int tid) {
+    constexpr int NF = 4, kRows = MF * 32, kA = T::M * kStepBytes, kB = T::N * kStepBytes, kS = T::N * 16;
+    constexpr int kB0 = 2 * kA, kS0 = kB0 + 2 * kB;        // of LDS: rows, weights, scales, two of each
+    using A = Side<kRows, T::kThreads, false>;
+    using B = Side<T::N, T::kThreads, false>;              // 256 values in 128 bytes
+    static_assert(B::kLoads == 4 && T::kThreads == 2 * T::N, "the loads' order");
+    const int lane = tid % kLanes, wave = __builtin_amdgcn_readfirstlane(tid / kLanes), wm = wave / T::WN, wn = wave % T::WN;
+    A sa;
+    B sb;
+    sa.init(t.left, p.ld, tid);
+    const int64_t q_ld = p.k / 2, s_ld = p.k >> p.shift, w_row = t.expert * p.n + n0;
+    sb.init(p.n - n0, q_ld, tid);
+    const char *a0 = p.x + t.first * p.ld, *q0 = p.q + w_row * q_ld;
+    const uint8_t* s0 = p.scales + w_row * s_ld;
+    const int64_t q_left = (p.n - n0) * q_ld, s_left = (p.n - n0) * s_ld, row_bytes = p.k * 2;
+    auto fetch_a = [&](int s, int slot) {
+        sa.load(a0 + (int64_t)s * kStepBytes, nullptr, lds + slot * kA, row_bytes - (int64_t)s * kStepBytes, tid, wave);
+    };
+    // Half of a group's weights.  A row's last chunk may hold the next row's first values: they meet zeros.
+    auto fetch_q = [&](int group, int slot, auto hc) {
+        constexpr int H = decltype(hc)::value;
+        const int64_t done = (int64_t)group * kStepBytes, ahead = q_ld - done;
+        const int left = ahead > kStepBytes ? kStepBytes : ahead > 0 ? (int)ahead : 0;
+        const __amdgpu_buffer_rsrc_t w = window_of(q0 + done, q_left - done);
+#pragma unroll
+        for (int i = 2 * H; i < 2 * H + 2; ++i) {
+            const int row = (i * T::kThreads + tid) / 8, at = ((tid % 8) ^ B::exchange(row)) * kChunk;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(w, (lds_void*)(lds + kB0 + slot * kB + (i * T::kThreads + wave * kLanes) * kChunk), kChunk,
+                                                     (int)(at < left ? sb.offset[i] : kOutside), 0, 0, 0);
+        }
+    };
+    // A group's scales of a row, 16 at most, by two threads: as words where rows of them are whole words, else one by one.
+    const uint32_t s_at = n0 + tid / 2 < p.n ? (uint32_t)(tid / 2) * (uint32_t)s_ld + tid % 2 * 8 : kOutside;
+    const int group_scales = 256 >> p.shift;
+    const bool words = ((group_scales | (int)s_ld | (int)(uintptr_t)p.scales) & 3) == 0;
+    auto fetch_s = [&](int group) {
+        const int64_t done = (int64_t)group * group_scales;
+        const __amdgpu_buffer_rsrc_t w = window_of(s0 + done, s_left - done);
+        if (words) return load8(w, s_at);
+        uint32_t c[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) c[i] = load1(w, tid % 2 * 8 + i < group_scales ? s_at + i : kOutside);
+        return i32x2{(int)(c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24), (int)(c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24)};
+    };
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void*)lds;
+    auto put_s = [&](i32x2 v, int slot) { put8<0>(lds0 + kS0 + slot * kS + tid * 8, v); };
+
+    f32x4 acc[MF][NF];
+#pragma unroll
+    for (int i = 0; i < MF; ++i)
+#pragma unroll
+        for (int j = 0; j < NF; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+
+    // A lane of a fragment holds 16 values of a step, chunks 2 (lane / 16) and the one behind it of 8 values each, of its
+    // row: the contraction's order does not matter as long as both operands have the same.  Chunks' places are exchanged by
+    // their row.  Addresses are made in each step, not kept for all.
+    const int l16 = lane % 16, g4 = lane / 16;
+    struct {
+        uint32_t a, b, c;
+        __device__ __forceinline__ void remake() { asm volatile("" : "+v"(a), "+v"(b), "+v"(c)); }
+    } at = {(uint32_t)((wm * (MF * 16) + l16) * kStepBytes + ((2 * g4) ^ A::exchange(l16)) * kChunk),
+            (uint32_t)(kB0 + (wn * 64 + l16) * kStepBytes + ((g4 / 2) ^ B::exchange(l16)) * kChunk + g4 % 2 * 8),
+            (uint32_t)(kS0 + (wn * 64 + l16) * 16)};
+    const int down = p.shift - 4;
+
+    // A step is 2 MF groups of NF matrix instructions.  While one half's are multiplied the other half's weights are
+    // expanded: this step's second half, then the next step's first.
+    constexpr int kLead = MF >= 8 ? 3 : MF >= 4 ? 2 : 1, kRing = 4, kGroups = 2 * MF;
+    const int steps = (int)((p.k + 63) / 64);
+    i32x4 fa[kRing], fb[2][NF];
+    i32x2 raw[2][NF], scales = {0, 0};
+    float f[2][NF];
+    auto read_a = [&](auto gc, uint32_t from) {            // the fragment of group g of a step
+        constexpr int g = decltype(gc)::value;
+        fa[g % kRing] = *reinterpret_cast<const i32x4*>(lds + (from ^ (g / MF * kChunk)) + g % MF * (16 * kStepBytes));
+    };
+    auto read_b = [&](auto dc, auto uc, uint32_t slot) {   // step U of a group, to set D
+        constexpr int D = decltype(dc)::value, U = decltype(uc)::value;
+        const uint32_t c = at.c + (slot ? kS : 0) + ((4 * U + g4) >> down);
+#pragma unroll
+        for (int j = 0; j < NF; ++j) {
+            raw[D][j] = *reinterpret_cast<const i32x2*>(lds + ((at.b + (slot ? kB : 0)) ^ (U * 2 * kChunk)) + j * (16 * kStepBytes));
+            f[D][j] = __uint_as_float(*reinterpret_cast<const uint8_t*>(lds + c + j * 256));
+        }
+    };
+    auto scale_of = [&](auto dc) {
+        constexpr int D = decltype(dc)::value;
+#pragma unroll
+        for (int j = 0; j < NF; ++j) f[D][j] = e4m3_f32(__float_as_uint(f[D][j]));
+    };
+    auto expand = [&](auto dc, auto hc, auto jc, auto pc) {    // four values: half P of fragment J's half H of set D
+        constexpr int D = decltype(dc)::value, H = decltype(hc)::value, J = decltype(jc)::value, P = decltype(pc)::value;
+        const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4((uint32_t)raw[D][J][H], 1.0f, 2 * P) * f[D][J],
+                    b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4((uint32_t)raw[D][J][H], 1.0f, 2 * P + 1) * f[D][J];
+        // the upper halves of the products hold all of them
+        fb[H][J][2 * P] = (int)__builtin_amdgcn_perm(__float_as_uint(a[1]), __float_as_uint(a[0]), 0x07060302u);
+        fb[H][J][2 * P + 1] = (int)__builtin_amdgcn_perm(__float_as_uint(b[1]), __float_as_uint(b[0]), 0x07060302u);
+    };
+    auto in_order = [] { asm volatile("" ::: "memory"); };   // the waits count on it
+    auto group = [&](int s, int slot, auto uc, auto gc) {
+        constexpr int U = decltype(uc)::value, g = decltype(gc)::value, H = g / MF, i = g % MF, ahead = g + kLead, d = U % 2;
+        constexpr bool first = ahead == kGroups;       // the first group whose reads ahead are the next step's
+        constexpr int kFetch = MF == 8 ? 2 : 0, kRead = MF == 8 ? 4 : MF == 4 ? 2 : 1;
+        constexpr int kPer = MF == 8 ? 1 : MF == 4 ? 2 : 4;    // halves of fragments, a group
+        if constexpr (first) {
+            // what may still be on its way: loads of weights and scales begun behind the next step's rows
+            arrive<U == 0 ? 3 : U == 1 ? 2 : 0>();
+            fetch_a(s + 2, d);
+        }
+        read_a(Const<ahead % kGroups>{}, ahead < kGroups ? at.a ^ (d * kA) : at.a ^ ((1 - d) * kA));
+        if constexpr (U < 2 && g == kFetch) {
+            in_order();
+            fetch_q(s / 4 + 1, 1 - slot, Const<U>{});
+            if constexpr (U == 0) scales = fetch_s(s / 4 + 1);
+            in_order();
+        }
+        if constexpr (U == 2 && g == kFetch) put_s(scales, 1 - slot);
+        if constexpr (g == kRead) read_b(Const<1 - d>{}, Const<(U + 1) % 4>{}, U == 3 ? 1 - slot : slot);
+        if constexpr (g == MF) scale_of(Const<1 - d>{});
+        auto part = [&](auto ec) {
+            constexpr int e = g % MF * kPer + decltype(ec)::value;     // of the half's eight
+            if constexpr (H == 0) expand(Const<d>{}, Const<1>{}, Const<e / 2>{}, Const<e % 2>{});
+            else expand(Const<1 - d>{}, Const<0>{}, Const<e / 2>{}, Const<e % 2>{});
+        };
+        part(Const<0>{});
+        if constexpr (kPer >= 2) part(Const<1>{});
+        if constexpr (kPer >= 4) part(Const<2>{}), part(Const<3>{});
+#pragma unroll
+        for (int j = 0; j < NF; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fb[H][j]), __builtin_bit_cast(bf16x8, fa[g % kRing]),
+                                                                acc[i][j], 0, 0, 0);
+        // the order of a group: what else it does among its matrix instructions
+        constexpr int kReads = 1 + (g == kRead ? 2 * NF : 0), kStarts = first ? A::kLoads : U < 2 && g == kFetch ? 3 : 0;
+#pragma unroll
+        for (int r = 0; r < NF; ++r) {
+            __builtin_amdgcn_sched_group_barrier(0x100, (kReads + NF - 1) / NF, 0);                          // LDS reads
+            if constexpr (kStarts > 0) __builtin_amdgcn_sched_group_barrier(0x010, (kStarts + NF - 1) / NF, 0);  // loads from memory
+            __builtin_amdgcn_sched_group_barrier(0x002, 2 * kPer + (g == MF ? 3 : 0), 0);                    // vector instructions
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                                               // matrix instructions
+        }
+    };
+    static_assert(MF == 2 || MF == 4 || MF == 8, "groups of a step");
+    auto step = [&](int s, int slot, auto uc) {
+        group(s, slot, uc, Const<0>{}), group(s, slot, uc, Const<1>{}), group(s, slot, uc, Const<2>{}), group(s, slot, uc, Const<3>{});
+        if constexpr (MF >= 4) group(s, slot, uc, Const<4>{}), group(s, slot, uc, Const<5>{}), group(s, slot, uc, Const<6>{}), group(s, slot, uc, Const<7>{});
+        if constexpr (MF >= 8) {
+            group(s, slot, uc, Const<8>{}), group(s, slot, uc, Const<9>{}), group(s, slot, uc, Const<10>{}), group(s, slot, uc, Const<11>{});
+            group(s, slot, uc, Const<12>{}), group(s, slot, uc, Const<13>{}), group(s, slot, uc, Const<14>{}), group(s, slot, uc, Const<15>{});
+        }
+        at.remake();
+    };
+    if (steps > 0) {
+        scales = fetch_s(0);
+        fetch_q(0, 0, Const<0>{});
+        fetch_q(0, 0, Const<1>{});
+        fetch_a(0, 0);
+        fetch_a(1, 1);
+        put_s(scales, 0);
+        arrive<0>();
+        read_b(Const<0>{}, Const<0>{}, 0);
+        scale_of(Const<0>{});
+        auto whole = [&](auto jc) { expand(Const<0>{}, Const<0>{}, jc, Const<0>{}), expand(Const<0>{}, Const<0>{}, jc, Const<1>{}); };
+        whole(Const<0>{}), whole(Const<1>{}), whole(Const<2>{}), whole(Const<3>{});
+        read_a(Const<0>{}, at.a);
+        if constexpr (kLead > 1) read_a(Const<1>{}, at.a);
+        if constexpr (kLead > 2) read_a(Const<2>{}, at.a);
+        int slot = 0;
+        for (int s = 0; s < steps; s += 4, slot = 1 - slot) {
+            step(s, slot, Const<0>{});
+            if (s + 1 < steps) step(s + 1, slot, Const<1>{});
+            if (s + 2 < steps) step(s + 2, slot, Const<2>{});
+            if (s + 3 < steps) step(s + 3, slot, Const<3>{});
+        }
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // no load into LDS outlives the workgroup
+    finish<T, MF>(p, t, n0, lds, tid, acc);
+}
+
+// The product of one tile with turned weights.
+template <class T, int MF>
+__device__ __forceinline__ void product_turned(const Args& p, const Place& t, int64_t n0, char* lds, int tid) {
+    constexpr int NF = 4, kRows = MF * 32;
+    using A = Side<kRows, T::kThreads, false>;
+    using B = Turned<T>;
+    const int lane = tid % kLanes, wave = __builtin_amdgcn_readfirstlane(tid / kLanes), wm = wave / T::WN, wn = wave % T::WN;
+    A sa;
+    sa.init(t.left, p.ld, tid);
+    const char* a0 = p.x + t.first * p.ld;
+    const int64_t row_bytes = p.inner * 2, q_ld = p.k / 2, s_ld = p.k >> p.shift;
+    auto fetch_a = [&](int s, int slot) {
+        sa.load(a0 + (int64_t)s * kStepBytes, nullptr, lds + slot * T::kStage, row_bytes - (int64_t)s * kStepBytes, tid, wave);
+    };
+    typename B::From at;
+    at.init(p, n0, tid);
+    const char* q0 = p.q + t.expert * p.n * q_ld + n0 / 2;
+    const uint8_t* s0 = p.scales + t.expert * p.n * s_ld;
+    const int64_t q_left = p.n * q_ld - n0 / 2, s_left = p.n * s_ld;
+    auto fetch_b = [&](int s, B& b) {                      // the windows move down 64 rows a step
+        const int64_t dq = s * 64 * q_ld, ds = s * 64 * s_ld;
+        b.load(at, window_of(q0 + dq, q_left - dq), window_of(s0 + ds, s_left - ds));
+    };
+    auto a_row = [&](int i) { return wm * (MF * 16) + i * 16; };
+    auto b_row = [&](int j) { return wn * 64 + j * 16; };
+    f32x4 acc[MF][NF];
+#pragma unroll
+    for (int i = 0; i < MF; ++i)
+#pragma unroll
+        for (int j = 0; j < NF; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+
+    // A step is 2 MF groups of NF matrix instructions, a fragment of the rows against a half's fragments of the weights.
+    // Registers run kLead groups ahead of them (a whole half for the weights).  While a group is multiplied a later one's
+    // fragment is read, and in the first groups the next step's weights are expanded and written, a part at a time; then
+    // those of the step two behind it are loaded.  The one barrier of a step stands where its last fragments have been
+    // read: behind it lie the next step's rows and weights, and its own LDS is free.
+    constexpr int kLead = MF >= 8 ? 3 : MF >= 4 ? 2 : 1, kRing = 4, kGroups = 2 * MF;
+    constexpr int kFetch = MF >= 8 ? 9 : MF;               // the group that loads weights
+    const int steps = (int)((p.inner + 63) / 64);
+    // Where this lane reads its chunk of a fragment's first half, and where it writes: chunks' places are exchanged by
+    // their row, so other chunks and the next step's LDS are some bits away.  Made in each step, not kept for all.
+    const int l16 = lane % 16, chunk = lane / 16;
+    uint32_t a_at = (a_row(0) + l16) * kStepBytes + (chunk ^ A::exchange(l16)) * kChunk;
+    uint32_t b_at = (T::M + b_row(0) + l16) * kStepBytes + (chunk ^ exchange(b_row(0) + l16)) * kChunk;
+    uint32_t w_at = (uint32_t)(uintptr_t)(lds_void*)lds + T::M * kStepBytes + B::base(tid);   // the kernel's LDS begins with it
+    static_assert((T::kStage & (T::kStage - 1)) == 0 && T::M * kStepBytes >= 1024, "bits apart");
+    B b[2];
+    i32x4 fa[kRing], fb[2][NF];
+    auto read_a = [&](auto gc, uint32_t from) {            // the fragment of group g of a step
+        constexpr int g = decltype(gc)::value;
+        fa[g % kRing] = *reinterpret_cast<const i32x4*>(lds + (from ^ (g / MF * 64)) + g % MF * (16 * kStepBytes));
+    };
+    auto read_b = [&](auto hc, uint32_t stage, int from, int to) {
+        constexpr int H = decltype(hc)::value;
+#pragma unroll
+        for (int j = from; j < to; ++j)
+            fb[H][j] = *reinterpret_cast<const i32x4*>(lds + (stage ^ ((4 * H) ^ j) * kChunk) + j * (16 * kStepBytes));
+    };
+    auto in_order = [] { asm volatile("" ::: "memory"); };   // the waits count on it
+    auto group = [&](int s, auto dc, auto gc) {
+        constexpr int d = decltype(dc)::value, g = decltype(gc)::value, H = g / MF, i = g % MF, ahead = g + kLead;
+        constexpr bool first = ahead == kGroups;       // the first group whose reads ahead are the next step's
+        constexpr bool more_b = g < NF && g < MF - 1;  // the second half's weights: one in each of the first groups
+        constexpr int b_to = g == MF - 2 ? NF : g + 1;
+        constexpr int kReads = 1 + (more_b ? b_to - g : 0) + (first ? NF : 0);
+        constexpr int kPer = MF == 2 ? 2 : 1;          // parts of the next step's weights
+        constexpr bool stores = MF == 8 ? g % 2 == 1 && g < 8 : g * kPer < B::kParts;
+        constexpr int part = MF == 8 ? g / 2 : g * kPer;
+        if constexpr (first) {
+            arrive<B::kLoads>();                       // the weights' loads go on
+            fetch_a(s + 2, d);
+            read_b(Const<0>{}, b_at ^ T::kStage, 0, NF);
+        }
+        read_a(Const<ahead % kGroups>{}, ahead < kGroups ? a_at : a_at ^ T::kStage);
+        if constexpr (more_b) read_b(Const<1>{}, b_at, g, b_to);
+        if constexpr (stores) {
+            const uint32_t to = w_at ^ T::kStage;
+            b[1 - d].template store<part>(to);
+            if constexpr (kPer == 2) b[1 - d].template store<part + 1>(to);
+        }
+        if constexpr (g == kFetch) {
+            in_order();
+            fetch_b(s + 3, b[1 - d]);
+        }
+#pragma unroll
+        for (int j = 0; j < NF; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fb[H][j]), __builtin_bit_cast(bf16x8, fa[g % kRing]),
+                                                                acc[i][j], 0, 0, 0);
+        // the order of a group: what else it does among its matrix instructions
+#pragma unroll
+        for (int r = 0; r < NF; ++r) {
+            __builtin_amdgcn_sched_group_barrier(0x100, (kReads + NF - 1) / NF, 0);                          // LDS reads
+            if constexpr (first) __builtin_amdgcn_sched_group_barrier(0x010, (A::kLoads + NF - 1) / NF, 0);  // loads from memory
+            if constexpr (g == kFetch) __builtin_amdgcn_sched_group_barrier(0x010, (B::kLoads + NF - 1) / NF, 0);
+            if constexpr (stores) __builtin_amdgcn_sched_group_barrier(0x002, 5 * kPer, 0);                  // vector instructions
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                                               // matrix instructions
+        }
+    };
+    static_assert(MF == 2 || MF == 4 || MF == 8, "groups of a step");
+    auto step = [&](int s, auto dc) {
+        group(s, dc, Const<0>{}), group(s, dc, Const<1>{}), group(s, dc, Const<2>{}), group(s, dc, Const<3>{});
+        if constexpr (MF >= 4) group(s, dc, Const<4>{}), group(s, dc, Const<5>{}), group(s, dc, Const<6>{}), group(s, dc, Const<7>{});
+        if constexpr (MF >= 8) {
+            group(s, dc, Const<8>{}), group(s, dc, Const<9>{}), group(s, dc, Const<10>{}), group(s, dc, Const<11>{});
+            group(s, dc, Const<12>{}), group(s, dc, Const<13>{}), group(s, dc, Const<14>{}), group(s, dc, Const<15>{});
+        }
+        a_at ^= T::kStage, b_at ^= T::kStage, w_at ^= T::kStage;
+        asm volatile("" : "+v"(a_at), "+v"(b_at), "+v"(w_at));
+        at.remake();
+    };
+    if (steps > 0) {
+        fetch_b(0, b[0]);
+        fetch_b(1, b[1]);
+        in_order();
+        fetch_a(0, 0);
+        in_order();
+        fetch_a(1, 1);
+        in_order();
+        b[0].template store<0>(w_at), b[0].template store<1>(w_at), b[0].template store<2>(w_at), b[0].template store<3>(w_at);
+        fetch_b(2, b[0]);
+        in_order();
+        arrive<A::kLoads + B::kLoads>();
+        read_b(Const<0>{}, b_at, 0, NF);
+        read_a(Const<0>{}, a_at);
+        if constexpr (kLead > 1) read_a(Const<1>{}, a_at);
+        if constexpr (kLead > 2) read_a(Const<2>{}, a_at);
+        for (int s = 0; s < steps; s += 2) {               // past the last step: zeros
+            step(s, Const<0>{});
+            step(s + 1, Const<1>{});
+        }
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // no load into LDS outlives the workgroup
+    finish<T, MF>(p, t, n0, lds, tid, acc);
+}
+
+template <class T, bool TURNED>
 __global__ __launch_bounds__(T::kThreads, 2) void grouped_kernel(Args p) {
-    __shared__ __attribute__((aligned(1024))) char lds[kSteps][(T::M + T::N) * kStepBytes];
+    __shared__ __attribute__((aligned(1024))) char lds[TURNED ? kSteps * T::kStage : T::kLds];
     const int tid = threadIdx.x;
     const Work work = work_of(blockIdx.x, gridDim.x, p.tiles_n);
     const int64_t n0 = work.n * T::N;
     const Place t = place_of(p, work.index, T::M, tid % kLanes);
     if (t.expert < 0) return clear_rows(p, t, n0, T::N, gridDim.x / p.tiles_n - (work.index - t.index), tid, T::kThreads);
-    if constexpr (T::kLeast <= 1) if (t.left <= 32) return product<T, TURNED, SCALES, 1>(p, t, n0, lds, tid);
-    if constexpr (T::kLeast <= 2) if (t.left <= 64) return product<T, TURNED, SCALES, 2>(p, t, n0, lds, tid);
-    if constexpr (T::kMost > 4) if (t.left <= 128) return product<T, TURNED, SCALES, 4>(p, t, n0, lds, tid);
-    product<T, TURNED, SCALES, T::kMost>(p, t, n0, lds, tid);
+    auto product = [&](auto mc) {
+        constexpr int MF = decltype(mc)::value;
+        if constexpr (TURNED) product_turned<T, MF>(p, t, n0, lds, tid);
+        else product_raw<T, MF>(p, t, n0, lds, tid);
+    };
+    if (t.left <= 64) return product(Const<2>{});
+    if constexpr (T::kMost > 4) if (t.left <= 128) return product(Const<4>{});
+    product(Const<T::kMost>{});
 }
 
 }  // namespace grouped_product
