@@ -5,8 +5,7 @@
 namespace {
 
 using namespace product_host;
-using grouped_product::kPair, grouped_product::kOne, grouped_product::kOdd;
-using grouped_product::Scales;
+using grouped_product::kFewThreads;
 
 constexpr int64_t kMostGroupedRows = 0x7FFFFFFF, kMostExperts = (int64_t)1 << 20;
 
@@ -16,14 +15,12 @@ struct GroupedPlan { int height, width, threads; };
 using Large = grouped_product::Tile<256, 4>;
 using Small = grouped_product::Tile<128, 2>;
 
-constexpr int kFewThreads = grouped_product::kFewWaves * kLanes;
-
 GroupedPlan plan_grouped(int64_t rows, int64_t experts, int64_t outer, bool turned) {
     const int64_t active = rows < experts ? rows : experts, each = active ? ceil_div(rows, active) : 0;
-    if (!turned && each <= 32) {
+    if (!turned && each <= 64) {
         const int height = each <= 16 ? 16 : 32;
         const int64_t tiles = active * ceil_div(each, height);
-        const int width = tiles * ceil_div(outer, 64) >= 512 ? 64 : tiles * ceil_div(outer, 32) >= 512 ? 32 : 16;
+        const int width = tiles * ceil_div(outer, 128) >= 512 ? 128 : 64;
         return {height, width, kFewThreads};
     }
     if (each > 128 && active * ceil_div(each, 256) * ceil_div(outer, 256) >= 192) return {Large::M, Large::N, Large::kThreads};
@@ -48,10 +45,8 @@ bool grouped_launchable(int64_t rows, int64_t experts, int64_t outer, bool turne
 }
 
 template <int R, int C>
-void launch_few(const grouped_product::Args& p, Scales scales, dim3 grid, hipStream_t stream) {
-    auto kernel = scales == kPair ? grouped_product::few_kernel<R, C, kPair>
-                  : scales == kOne ? grouped_product::few_kernel<R, C, kOne> : grouped_product::few_kernel<R, C, kOdd>;
-    hipLaunchKernelGGL(kernel, grid, dim3(kFewThreads), 0, stream, p);
+void launch_few(const grouped_product::Args& p, dim3 grid, hipStream_t stream) {
+    hipLaunchKernelGGL((grouped_product::few_kernel<R, C>), grid, dim3(kFewThreads), 0, stream, p);
 }
 
 template <class T>
@@ -65,11 +60,10 @@ int run_grouped(grouped_product::Args p, bool turned, int block, hipStream_t str
     p.shift = block == 16 ? 4 : block == 32 ? 5 : block == 64 ? 6 : 7;
     p.tiles_n = ceil_div(p.outer, plan.width);
     const dim3 grid((unsigned)(most_tiles(p.rows, p.experts, plan.height) * p.tiles_n));
-    const Scales scales = p.shift > 4 ? kOne : p.k % 32 ? kOdd : kPair;
     if (plan.threads == Large::kThreads && plan.height == Large::M) launch_tiled<Large>(p, turned, grid, stream);
     else if (plan.height == Small::M) launch_tiled<Small>(p, turned, grid, stream);
-    else if (plan.height == 16) plan.width == 64 ? launch_few<4, 1>(p, scales, grid, stream) : plan.width == 32 ? launch_few<2, 1>(p, scales, grid, stream) : launch_few<1, 1>(p, scales, grid, stream);
-    else plan.width == 64 ? launch_few<4, 2>(p, scales, grid, stream) : plan.width == 32 ? launch_few<2, 2>(p, scales, grid, stream) : launch_few<1, 2>(p, scales, grid, stream);
+    else if (plan.height == 16) plan.width == 128 ? launch_few<2, 1>(p, grid, stream) : launch_few<1, 1>(p, grid, stream);
+    else plan.width == 128 ? launch_few<2, 2>(p, grid, stream) : launch_few<1, 2>(p, grid, stream);
     return launched();
 }
 

@@ -36,42 +36,48 @@ struct Place { int expert; int64_t first, left, begin, end, index; };
 
 __device__ __forceinline__ int at_lane(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
 
+// The sum, or the largest, of this lane's value and those of the lanes before it; values are not negative.
+template <int CTRL, int ROWS, bool SUM>
+__device__ __forceinline__ int scan_step(int v) {
+    const int o = __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, true);
+    return SUM ? v + o : v > o ? v : o;
+}
+template <bool SUM>
+__device__ __forceinline__ int scan(int v) {
+    v = scan_step<0x111, 0xF, SUM>(v);           // within rows of 16: 1, 2, 4, 8 lanes before
+    v = scan_step<0x112, 0xF, SUM>(v);
+    v = scan_step<0x114, 0xF, SUM>(v);
+    v = scan_step<0x118, 0xF, SUM>(v);
+    v = scan_step<0x142, 0xA, SUM>(v);           // rows 1 and 3: the last lane of the row before
+    return scan_step<0x143, 0xC, SUM>(v);        // rows 2 and 3: lane 31
+}
+
 // Offsets are taken within 0 .. rows and never descend: what does not fit makes a group shorter or empty.
 __device__ __forceinline__ Place place_of(const Args& p, int64_t index, int height, int lane) {
     const int rows = (int)p.rows;
     auto within = [&](int v) { return v < 0 ? 0 : v > rows ? rows : v; };
-    int before = within(p.offsets[0]);
+    auto end_of = [&](int e) { return e < p.experts ? p.offsets[e + 1] : 0; };
+    int next = end_of(lane), before = within(p.offsets[0]);
     const int begin = before;
+    int left = (int)index;                       // tiles are fewer than 2^31
     for (int base = 0; base < p.experts; base += kLanes) {
-        const int e = base + lane;
-        int end = e < p.experts ? within(p.offsets[e + 1]) : 0;
-#pragma unroll
-        for (int d = 1; d < kLanes; d *= 2) {
-            const int v = __shfl_up(end, d);
-            if (lane >= d && v > end) end = v;
-        }
+        int end = scan<false>(within(next));     // past the last expert: as the last one's
+        next = end_of(base + kLanes + lane);
         if (end < before) end = before;
         int start = __shfl_up(end, 1);
         if (lane == 0) start = before;
-        int64_t tiles = (end - start + (int64_t)height - 1) / height;
-        int64_t upto = tiles;
-#pragma unroll
-        for (int d = 1; d < kLanes; d *= 2) {
-            const int64_t v = __shfl_up(upto, d);
-            if (lane >= d) upto += v;
-        }
-        const uint64_t mine = __ballot(index < upto);
+        const int tiles = (end - start + height - 1) / height, upto = scan<true>(tiles);
+        const uint64_t mine = __ballot(left < upto);
         if (mine) {
             const int l = __builtin_ctzll(mine);
-            const int64_t skipped = at_lane((int)(upto - tiles), l);
             const int s = at_lane(start, l), t = at_lane(end, l);
-            const int64_t first = s + (index - skipped) * height;
+            const int64_t first = s + (int64_t)(left - at_lane(upto - tiles, l)) * height;
             return {base + l, first, t - first, 0, 0, 0};
         }
-        index -= at_lane((int)upto, kLanes - 1);
+        left -= at_lane(upto, kLanes - 1);
         before = at_lane(end, kLanes - 1);
     }
-    return {-1, 0, 0, begin, before, index};
+    return {-1, 0, 0, begin, before, left};
 }
 
 // Rows of no group: the workgroups that have no tile share them out.
@@ -100,99 +106,177 @@ __device__ __forceinline__ Work work_of(int64_t id, int64_t count, int64_t tiles
     return {first + in % height, in / height};
 }
 
+// ---- weights and scales by groups of 256 values of a row ------------------------------------------
+
+// A window of at most 2 GiB over the `left` bytes from `base` on: loads past it return zero without an access.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t window_of(const void* base, int64_t left) {
+    // by halves, in scalar registers
+    const uint32_t high = (uint32_t)((uint64_t)left >> 32), low = (uint32_t)left, most = low < kOutside ? low : kOutside;
+    const uint32_t size = high == 0 ? most : (int)high < 0 ? 0u : kOutside;
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, (int)size, 0x00020000);
+}
+
+// Stores to LDS that wait for nothing: as ordinary ones they would wait for all LDS loads on their way, which go to other
+// places (the compiler cannot know).  arrive() waits for them.  at: an address in LDS.
+template <int OFFSET>
+__device__ __forceinline__ void put8(uint32_t at, i32x2 v) { asm volatile("ds_write_b64 %0, %1 offset:%2" ::"v"(at), "v"(v), "n"(OFFSET)); }
+
+// The scales of a group of N rows, 16 bytes a row at most, by two threads a row: as words where rows of them are whole words,
+// else one by one.
+template <int N>
+struct GroupScales {
+    const uint8_t* from;
+    int64_t left;
+    uint32_t at;
+    int each, half;                              // of a row and group; of it, this thread's first
+    bool words;
+    __device__ __forceinline__ void init(const Args& p, int64_t w_row, int64_t n0, int tid) {
+        const int64_t ld = p.k >> p.shift;
+        from = p.scales + w_row * ld, left = (p.n - n0) * ld;
+        each = 256 >> p.shift, half = tid % 2 * 8;
+        at = tid < 2 * N && n0 + tid / 2 < p.n ? (uint32_t)(tid / 2) * (uint32_t)ld + half : kOutside;
+        words = ((each | (int)ld | (int)(uintptr_t)p.scales) & 3) == 0;
+    }
+    __device__ __forceinline__ i32x2 load(int group) const {
+        const int64_t done = (int64_t)group * each;
+        const __amdgpu_buffer_rsrc_t w = window_of(from + done, left - done);
+        if (words) return load8(w, at);
+        uint32_t c[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) c[i] = load1(w, half + i < each ? at + i : kOutside);
+        return i32x2{(int)(c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24), (int)(c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24)};
+    }
+};
+
 // ---- few rows a group ---------------------------------------------------------------------------
-// Reading the weights is all there is to do.  A workgroup owns 16 R weight rows and up to 16 C rows of one group; its waves
-// take turns along the contraction, 256 values (whole lines of the weights) each, loaded straight into the registers of
-// the matrix instructions, and one exchange through LDS adds their sums in a fixed order.
-constexpr int kFewWaves = 8, kFewGroup = 256;
+// Reading the weights is all there is to do.  A workgroup owns 64 R weight rows, 16 R a wave, and up to 16 C rows of one
+// group; weights, scales and rows go through LDS by whole lines, 256 values of the contraction at a time, the next ones while
+// these are multiplied.  512 rows, 128 groups, [1536, 4096]: 113 us, 4.0 TB/s (95 with no scales read: 16 bytes of each row at
+// a time).  Three workgroups a compute unit hide each other's first waits; deeper rings leave room for two or one (128 us).
+// Loaded straight into the registers of the matrix instructions, whose neighbouring lanes hold different rows, each lane's 16
+// bytes are an access of their own to the L1, which is then nine tenths of the time busy (135 us).
+constexpr int kFewThreads = 256;
 
-// How a lane gets the scales of its 32 values: two, one, or two of which the second may lie past the row (and so may half
-// of the values).
-enum Scales { kPair, kOne, kOdd };
-
-template <int R, int C, Scales SCALES>
-__global__ __launch_bounds__(kFewWaves * kLanes) void few_kernel(Args p) {
-    __shared__ f32x4 sums[kFewWaves][R * C][kLanes];
-    const int tid = threadIdx.x, lane = tid % kLanes, g = lane / 16, i16 = lane % 16;
+template <int R, int C>
+__global__ __launch_bounds__(kFewThreads, 2) void few_kernel(Args p) {
+    constexpr int N = 64 * R, kRows = 16 * C, kW = N * kStepBytes, kX = kRows * 512, kS = N * 16, kStage = kW + kX + kS;
+    using B = Side<N, kFewThreads, false>;
+    constexpr int kXLoads = kX / (kFewThreads * kChunk);
+    __shared__ __attribute__((aligned(1024))) char lds[2 * kStage];
+    const int tid = threadIdx.x, lane = tid % kLanes, g = lane / 16, l16 = lane % 16;
     const int wave = __builtin_amdgcn_readfirstlane(tid / kLanes);
     const Work work = work_of(blockIdx.x, gridDim.x, p.tiles_n);
-    const int64_t n0 = work.n * (16 * R);
-    const Place t = place_of(p, work.index, 16 * C, lane);
-    if (t.expert < 0) return clear_rows(p, t, n0, 16 * R, gridDim.x / p.tiles_n - (work.index - t.index), tid, kFewWaves * kLanes);
+    const int64_t n0 = work.n * N;
+    const Place t = place_of(p, work.index, kRows, lane);
+    if (t.expert < 0) return clear_rows(p, t, n0, N, gridDim.x / p.tiles_n - (work.index - t.index), tid, kFewThreads);
 
-    const uint32_t k = (uint32_t)p.k, q_ld = k / 2, s_ld = k >> p.shift;
-    const int64_t row0 = t.expert * p.n + n0;
-    const __amdgpu_buffer_rsrc_t rq = window(p.q + row0 * q_ld), rs = window(p.scales + row0 * s_ld), rx = window(p.x + t.first * p.ld);
-    bool row_in[R], x_in[C];
+    const float S = p.S[t.expert];
+    const int64_t q_ld = p.k / 2, w_row = t.expert * p.n + n0, q_left = (p.n - n0) * q_ld, x_bytes = p.k * 2;
+    const char *q0 = p.q + w_row * q_ld, *x0 = p.x + t.first * p.ld;
+    B sb;
+    sb.init(p.n - n0, q_ld, tid);
+    GroupScales<N> scales_of;
+    scales_of.init(p, w_row, n0, tid);
+    // 32 chunks of a row of x, their places exchanged by the row: reads take one chunk of 16 rows
+    uint32_t x_at[kXLoads];
+    const int x_chunk = tid % 32;
 #pragma unroll
-    for (int r = 0; r < R; ++r) row_in[r] = n0 + r * 16 + i16 < p.n;
+    for (int i = 0; i < kXLoads; ++i) {
+        const int row = (i * kFewThreads + tid) / 32;
+        x_at[i] = row < t.left ? (uint32_t)row * (uint32_t)p.ld + (x_chunk ^ row % 16) * kChunk : kOutside;
+    }
+    i32x2 scales[2];
+    auto fetch = [&](int s, auto dc) {
+        constexpr int d = decltype(dc)::value;
+        char* to = lds + d * kStage;
+        // A row's last chunk may hold the next row's first values: they meet zeros.
+        const int64_t done = (int64_t)s * kStepBytes, x_done = (int64_t)s * 512, q_ahead = q_ld - done, x_ahead = x_bytes - x_done;
+        const int q_in = q_ahead > kStepBytes ? kStepBytes : q_ahead > 0 ? (int)q_ahead : 0, x_in = x_ahead > 512 ? 512 : x_ahead > 0 ? (int)x_ahead : 0;
+        const __amdgpu_buffer_rsrc_t rq = window_of(q0 + done, q_left - done), rx = window(x0 + x_done);
 #pragma unroll
-    for (int c = 0; c < C; ++c) x_in[c] = c * 16 + i16 < t.left;
+        for (int i = 0; i < B::kLoads; ++i) {
+            const int at = ((tid % 8) ^ B::exchange((i * kFewThreads + tid) / 8)) * kChunk;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rq, (lds_void*)(to + (i * kFewThreads + wave * kLanes) * kChunk), kChunk,
+                                                     (int)(at < q_in ? sb.offset[i] : kOutside), 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < kXLoads; ++i) {
+            const int at = (x_chunk ^ (i * kFewThreads + tid) / 32 % 16) * kChunk;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (lds_void*)(to + kW + (i * kFewThreads + wave * kLanes) * kChunk), kChunk,
+                                                     (int)(at < x_in ? x_at[i] : kOutside), 0, 0, 0);
+        }
+        scales[d] = scales_of.load(s);
+    };
+
     f32x4 acc[R][C];
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int c = 0; c < C; ++c) acc[r][c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-
-    for (uint32_t at = (uint32_t)wave * kFewGroup; at < k; at += kFewWaves * kFewGroup) {
-        i32x4 w[2][R];
-        uint32_t s[2][R];
+    // A lane takes 64 neighbouring values of its row, chunks 2 g and 2 g + 1 of a stage's weights, under four scales at most.
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void*)lds;
+    const int w_row0 = wave * (16 * R) + l16;
+    auto compute = [&](auto dc) {
+        constexpr int d = decltype(dc)::value;
+        const char *w = lds + d * kStage, *x = w + kW, *c = x + kX;
+        uint32_t s[R];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const uint32_t v = at + h * 128 + g * 32;
-            const bool in0 = v < k, in1 = SCALES == kOdd ? v + 16 < k : in0;
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                const uint32_t row = r * 16 + i16, q_at = row * q_ld + v / 2, s_at = row * s_ld + (v >> p.shift);
-                if constexpr (SCALES == kOdd) {
-                    const i32x2 lo = load8(rq, row_in[r] && in0 ? q_at : kOutside), hi = load8(rq, row_in[r] && in1 ? q_at + 8 : kOutside);
-                    w[h][r] = i32x4{lo[0], lo[1], hi[0], hi[1]};
-                    s[h][r] = load1(rs, row_in[r] && in0 ? s_at : kOutside) | load1(rs, row_in[r] && in1 ? s_at + 1 : kOutside) << 8;
-                } else {
-                    w[h][r] = load16(rq, row_in[r] && in0 ? q_at : kOutside);
-                    if constexpr (SCALES == kPair)
-                        s[h][r] = (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rs, (int)(row_in[r] && in0 ? s_at : kOutside), 0, 0);
-                    else s[h][r] = load1(rs, row_in[r] && in0 ? s_at : kOutside);
-                }
-            }
+        for (int r = 0; r < R; ++r) {
+            const int row = w_row0 + r * 16;
+            s[r] = *reinterpret_cast<const uint32_t*>(c + row * 16 + ((4 * g) >> (p.shift - 4) & ~3));
+            if (p.shift > 4) s[r] >>= ((4 * g) >> (p.shift - 4)) % 4 * 8;
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const uint32_t v = at + h * 128 + g * 32;
-            const bool in0 = v < k, in1 = SCALES == kOdd ? v + 16 < k : in0;
-            i32x4 x[C][4];
+            i32x4 wv[R], xv[C][4];
 #pragma unroll
-            for (int c = 0; c < C; ++c)
+            for (int r = 0; r < R; ++r) {
+                const int row = w_row0 + r * 16;
+                wv[r] = *reinterpret_cast<const i32x4*>(w + row * kStepBytes + ((2 * g + h) ^ B::exchange(l16)) * kChunk);
+            }
+#pragma unroll
+            for (int i = 0; i < C; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    x[c][j] = load16(rx, x_in[c] && (j < 2 ? in0 : in1) ? (uint32_t)(c * 16 + i16) * (uint32_t)p.ld + v * 2 + j * 16 : kOutside);
+                    xv[i][j] = *reinterpret_cast<const i32x4*>(x + (i * 16 + l16) * 512 + ((8 * g + 4 * h + j) ^ l16) * kChunk);
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                const float f0 = e4m3_f32(s[h][r]), f1 = SCALES == kOne ? f0 : e4m3_f32(s[h][r] >> 8);
+                // blocks of 16: a scale for two of the four; of 32: for all four; of more: the same for both halves
+                const uint32_t c0 = p.shift == 4 ? s[r] >> 16 * h : p.shift == 5 ? s[r] >> 8 * h : s[r], c1 = p.shift == 4 ? c0 >> 8 : c0;
+                const float f0 = e4m3_f32(c0), f1 = e4m3_f32(c1);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const bf16x8 wv = expand8((uint32_t)w[h][r][j], j < 2 ? f0 : f1);
+                    const bf16x8 v = expand8((uint32_t)wv[r][j], j < 2 ? f0 : f1);
 #pragma unroll
-                    for (int c = 0; c < C; ++c)
-                        acc[r][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, __builtin_bit_cast(bf16x8, x[c][j]), acc[r][c], 0, 0, 0);
+                    for (int i = 0; i < C; ++i)
+                        acc[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8, xv[i][j]), acc[r][i], 0, 0, 0);
                 }
             }
         }
+    };
+    const int stages = (int)((p.k + 255) / 256);
+    auto stage = [&](int s, auto dc) {
+        constexpr int d = decltype(dc)::value;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        if (tid < 2 * N) put8<0>(lds0 + d * kStage + kW + kX + tid * 8, scales[d]);
+        arrive<0>();
+        fetch(s + 1, Const<1 - d>{});            // where the last stage was
+        compute(dc);
+    };
+    fetch(0, Const<0>{});
+    for (int s = 0; s < stages; s += 2) {
+        stage(s, Const<0>{});
+        if (s + 1 < stages) stage(s + 1, Const<1>{});
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // no load into LDS outlives the workgroup
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
-        for (int c = 0; c < C; ++c) sums[wave][r * C + c][lane] = acc[r][c];
-    __syncthreads();
-    const float S = p.S[t.expert];
-    for (int f = wave; f < R * C; f += kFewWaves) {
-        f32x4 v = sums[0][f][lane];
-#pragma unroll
-        for (int w = 1; w < kFewWaves; ++w) v += sums[w][f][lane];
-        // a lane holds outputs n .. n + 3 of row i16
-        const int64_t n = n0 + f / C * 16 + g * 4, row = f % C * 16 + i16;
-        if (row < t.left) store4(p.out, p.out_f32, (t.first + row) * p.outer + n, p.outer - n, p.outer % 4 == 0, v * S);
-    }
+        for (int i = 0; i < C; ++i) {
+            // a lane holds outputs n .. n + 3 of a row
+            const int64_t n = n0 + wave * (16 * R) + r * 16 + g * 4, row = i * 16 + l16;
+            if (row < t.left) store4(p.out, p.out_f32, (t.first + row) * p.outer + n, p.outer - n, p.outer % 4 == 0, acc[r][i] * S);
+        }
 }
 
 // ---- tiles --------------------------------------------------------------------------------------
@@ -214,19 +298,6 @@ struct Tile {
     static constexpr int kLds = kSteps * (kStage + N * 16);
     static constexpr int kMost = M_ / 32;                            // a wave's fragments of rows
 };
-
-// A window of at most 2 GiB over the `left` bytes from `base` on: loads past it return zero without an access.
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t window_of(const void* base, int64_t left) {
-    // by halves, in scalar registers
-    const uint32_t high = (uint32_t)((uint64_t)left >> 32), low = (uint32_t)left, most = low < kOutside ? low : kOutside;
-    const uint32_t size = high == 0 ? most : (int)high < 0 ? 0u : kOutside;
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, (int)size, 0x00020000);
-}
-
-// Stores to LDS that wait for nothing: as ordinary ones they would wait for all LDS loads on their way, which go to other
-// places (the compiler cannot know).  arrive() waits for them.  at: an address in LDS.
-template <int OFFSET>
-__device__ __forceinline__ void put8(uint32_t at, i32x2 v) { asm volatile("ds_write_b64 %0, %1 offset:%2" ::"v"(at), "v"(v), "n"(OFFSET)); }
 
 // A thread's turned weights of a step, 8 columns of four rows, and where they lie from the step's first row on.  Past the
 // group's weights they are zero.
@@ -340,11 +411,10 @@ __device__ __forceinline__ void product_raw(const Args& p, const Place& t, int64
     A sa;
     B sb;
     sa.init(t.left, p.ld, tid);
-    const int64_t q_ld = p.k / 2, s_ld = p.k >> p.shift, w_row = t.expert * p.n + n0;
+    const int64_t q_ld = p.k / 2, w_row = t.expert * p.n + n0;
     sb.init(p.n - n0, q_ld, tid);
     const char *a0 = p.x + t.first * p.ld, *q0 = p.q + w_row * q_ld;
-    const uint8_t* s0 = p.scales + w_row * s_ld;
-    const int64_t q_left = (p.n - n0) * q_ld, s_left = (p.n - n0) * s_ld, row_bytes = p.k * 2;
+    const int64_t q_left = (p.n - n0) * q_ld, row_bytes = p.k * 2;
     auto fetch_a = [&](int s, int slot) {
         sa.load(a0 + (int64_t)s * kStepBytes, nullptr, lds + slot * kA, row_bytes - (int64_t)s * kStepBytes, tid, wave);
     };
@@ -361,19 +431,8 @@ __device__ __forceinline__ void product_raw(const Args& p, const Place& t, int64
                                                      (int)(at < left ? sb.offset[i] : kOutside), 0, 0, 0);
         }
     };
-    // A group's scales of a row, 16 at most, by two threads: as words where rows of them are whole words, else one by one.
-    const uint32_t s_at = n0 + tid / 2 < p.n ? (uint32_t)(tid / 2) * (uint32_t)s_ld + tid % 2 * 8 : kOutside;
-    const int group_scales = 256 >> p.shift;
-    const bool words = ((group_scales | (int)s_ld | (int)(uintptr_t)p.scales) & 3) == 0;
-    auto fetch_s = [&](int group) {
-        const int64_t done = (int64_t)group * group_scales;
-        const __amdgpu_buffer_rsrc_t w = window_of(s0 + done, s_left - done);
-        if (words) return load8(w, s_at);
-        uint32_t c[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) c[i] = load1(w, tid % 2 * 8 + i < group_scales ? s_at + i : kOutside);
-        return i32x2{(int)(c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24), (int)(c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24)};
-    };
+    GroupScales<T::N> scales_of;
+    scales_of.init(p, w_row, n0, tid);
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void*)lds;
     auto put_s = [&](i32x2 v, int slot) { put8<0>(lds0 + kS0 + slot * kS + tid * 8, v); };
 
@@ -443,7 +502,7 @@ __device__ __forceinline__ void product_raw(const Args& p, const Place& t, int64
         if constexpr (U < 2 && g == kFetch) {
             in_order();
             fetch_q(s / 4 + 1, 1 - slot, Const<U>{});
-            if constexpr (U == 0) scales = fetch_s(s / 4 + 1);
+            if constexpr (U == 0) scales = scales_of.load(s / 4 + 1);
             in_order();
         }
         if constexpr (U == 2 && g == kFetch) put_s(scales, 1 - slot);
@@ -482,7 +541,7 @@ __device__ __forceinline__ void product_raw(const Args& p, const Place& t, int64
         at.remake();
     };
     if (steps > 0) {
-        scales = fetch_s(0);
+        scales = scales_of.load(0);
         fetch_q(0, 0, Const<0>{});
         fetch_q(0, 0, Const<1>{});
         fetch_a(0, 0);

@@ -45,13 +45,39 @@ struct Eight {
 
 // The whole number nearest to v / s, ties to the even one, |v| <= about 127 s, both far from binary32's ends.  The
 // quotient's estimate is off by one at most; the remainder v - r s is exact, and so is what it says about r.
-__device__ __forceinline__ int nearest(float v, float s, float inverse) {
-    float r = rintf(v * inverse);
+__device__ __forceinline__ float nearest(float v, float s, float r) {
     const float twice = 2.0f * fmaf(-r, s, v);
     const bool odd = ((int)r & 1) != 0;
     if (twice > s || (twice == s && odd)) r += 1.0f;
     else if (twice < -s || (twice == -s && odd)) r -= 1.0f;
-    return (int)fminf(fmaxf(r, -127.0f), 127.0f);
+    return fminf(fmaxf(r, -127.0f), 127.0f);
+}
+
+// Eight of them, in bytes.  Nearly all quotients lie far from a tie, and their estimates round as they do: only where a
+// remainder comes near half a step is each looked at.
+template <class E>
+__device__ __forceinline__ uint2 nearest8(const E& e, float by, float s, float inverse, float sure) {
+    float r[8], most = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float v = __uint_as_float(e.bits(i)) * by;
+        r[i] = rintf(v * inverse);
+        most = fmaxf(most, fabsf(fmaf(-r[i], s, v)));
+    }
+    if (most > sure) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r[i] = nearest(__uint_as_float(e.bits(i)) * by, s, r[i]);
+    }
+    // 1.5 2^23 more, a number's lowest byte is the whole number's
+    uint32_t w[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        uint32_t c[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c[i] = __float_as_uint(r[4 * h + i] + 12582912.0f);
+        w[h] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(c[3], c[2], 0x0C0C0400u), __builtin_amdgcn_perm(c[1], c[0], 0x0C0C0400u), 0x05040100u);
+    }
+    return make_uint2(w[0], w[1]);
 }
 
 template <bool F32, bool WAVE>
@@ -103,13 +129,10 @@ __global__ __launch_bounds__(kQuantThreads) void quant_kernel(const char* __rest
     // small scales and their rows times 2^64, exactly, so that neither the reciprocal nor a remainder leaves the range
     const float by = s < 0x1p-100f ? 0x1p64f : 1.0f, sb = s * by;
     const float inverse = finite && s > 0.0f ? 1.0f / sb : 0.0f;
+    // rows of subnormal scales, whose quotients may pass 127, are looked at one by one
+    const float sure = s < 0x1p-120f ? -1.0f : 0.4999f * sb;
     auto store = [&](const Eight<F32>& e, int64_t at) {
-        uint32_t w[2] = {0, 0};
-        if (inverse > 0.0f) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) w[i / 4] |= (uint32_t)(nearest(__uint_as_float(e.bits(i)) * by, sb, inverse) & 255) << i % 4 * 8;
-        }
-        *reinterpret_cast<uint2*>(q + row * q_ld + at) = make_uint2(w[0], w[1]);
+        *reinterpret_cast<uint2*>(q + row * q_ld + at) = inverse > 0.0f ? nearest8(e, by, sb, inverse, sure) : make_uint2(0, 0);
     };
 #pragma unroll
     for (int u = 0; u < kKept; ++u) {
@@ -217,35 +240,38 @@ void launch_dot(const DotArgs& p, hipStream_t stream) {
 
 // ---- tiles ------------------------------------------------------------------------------------
 
-// Sums of parts of the contraction, in 32-bit integers as a whole sum is.
-__global__ __launch_bounds__(kJoinThreads) void int8_join_kernel(const int* __restrict__ part, int parts, int64_t m, int64_t n,
+// Sums of parts of the contraction, in 32-bit integers as a whole sum is: a workgroup for kJoinColumns outputs of a row.
+constexpr int kJoinColumns = kJoinThreads * 4;
+
+__global__ __launch_bounds__(kJoinThreads) void int8_join_kernel(const int* __restrict__ part, int parts, int64_t m, int64_t n, uint32_t pieces,
                                                                  const float* __restrict__ scale_m, const float* __restrict__ scale_n,
                                                                  void* __restrict__ out, int f32) {
-    const int64_t count = m * n, at = ((int64_t)blockIdx.x * kJoinThreads + threadIdx.x) * 4;
-    if (at >= count) return;
-    i32x4 v = {0, 0, 0, 0};
-    const int64_t left = count - at;
-    const bool vec = count % 4 == 0;
+    const int64_t row = blockIdx.x / pieces, first = (int64_t)(blockIdx.x % pieces) * kJoinColumns + threadIdx.x;
+    const float s = scale_m[row];
+    int v[4] = {0, 0, 0, 0};
     for (int p = 0; p < parts; ++p) {
-        const int* from = part + p * count + at;
-        if (vec) v += *reinterpret_cast<const i32x4*>(from);
-        else {
+        const int* from = part + (p * m + row) * n + first;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) if (i < left) v[i] += from[i];
-        }
+        for (int i = 0; i < 4; ++i) if (first + i * kJoinThreads < n) v[i] += from[i * kJoinThreads];
     }
-    f32x4 y = to_f32(v);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) if (i < left) y[i] *= scale_n[(at + i) % n] * scale_m[(at + i) / n];
-    store4(out, f32, at, left, true, y);
+    for (int i = 0; i < 4; ++i) {
+        const int64_t c = first + i * kJoinThreads;
+        if (c >= n) break;
+        const float y = (float)v[i] * (scale_n[c] * s);
+        if (f32) static_cast<float*>(out)[row * n + c] = y;
+        else static_cast<uint16_t*>(out)[row * n + c] = (uint16_t)pack_bf16(y, y);
+    }
 }
+
+int64_t join_groups(int64_t m, int64_t n) { return m * ceil_div(n, kJoinColumns); }
 
 int64_t int8_workspace(int64_t m, int64_t n, int64_t k) {
     return m <= kDotRows ? 0 : parts_bytes<kInt8>(m, n, up(k, kRowUnit));
 }
 
 bool int8_launchable(int64_t m, int64_t n, int64_t k) {
-    return m <= kDotRows || product_launchable<kInt8>(m, n, up(k, kRowUnit));
+    return m <= kDotRows || (product_launchable<kInt8>(m, n, up(k, kRowUnit)) && launchable(join_groups(m, n), kJoinThreads));
 }
 
 int run_int8(const int8_t* a, const float* a_scales, const int8_t* b, const float* b_scales, int64_t m, int64_t n, int64_t k,
@@ -271,8 +297,8 @@ int run_int8(const int8_t* a, const float* a_scales, const int8_t* b, const floa
     if (plan.parts == 1) return launch_product<kInt8, kSums>(p, plan.tile, stream);
     p.out = ws;
     if (const int rc = launch_product<kInt8, kPartial>(p, plan.tile, stream)) return rc;
-    hipLaunchKernelGGL(int8_join_kernel, dim3((unsigned)ceil_div(m * n, kJoinThreads * 4)), dim3(kJoinThreads), 0, stream,
-                       static_cast<const int*>(ws), plan.parts, m, n, a_scales, b_scales, out, f32);
+    hipLaunchKernelGGL(int8_join_kernel, dim3((unsigned)join_groups(m, n)), dim3(kJoinThreads), 0, stream,
+                       static_cast<const int*>(ws), plan.parts, m, n, (uint32_t)ceil_div(n, kJoinColumns), a_scales, b_scales, out, f32);
     return launched();
 }
 
