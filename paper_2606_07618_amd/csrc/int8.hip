@@ -241,16 +241,18 @@ void launch_dot(const DotArgs& p, hipStream_t stream) {
 // ---- tiles ------------------------------------------------------------------------------------
 
 // Sums of parts of the contraction, in 32-bit integers as a whole sum is: a workgroup for kJoinColumns outputs of a row.
+// Rows of parts hold whole fours, which a tile stores at once.
 constexpr int kJoinColumns = kJoinThreads * 4;
 
-__global__ __launch_bounds__(kJoinThreads) void int8_join_kernel(const int* __restrict__ part, int parts, int64_t m, int64_t n, uint32_t pieces,
+__global__ __launch_bounds__(kJoinThreads) void int8_join_kernel(const int* __restrict__ part, int parts, int64_t m, int64_t n, int64_t ld, uint32_t pieces,
                                                                  const float* __restrict__ scale_m, const float* __restrict__ scale_n,
                                                                  void* __restrict__ out, int f32) {
     const int64_t row = blockIdx.x / pieces, first = (int64_t)(blockIdx.x % pieces) * kJoinColumns + threadIdx.x;
     const float s = scale_m[row];
     int v[4] = {0, 0, 0, 0};
+#pragma unroll 4
     for (int p = 0; p < parts; ++p) {
-        const int* from = part + (p * m + row) * n + first;
+        const int* from = part + (p * m + row) * ld + first;
 #pragma unroll
         for (int i = 0; i < 4; ++i) if (first + i * kJoinThreads < n) v[i] += from[i * kJoinThreads];
     }
@@ -267,7 +269,9 @@ __global__ __launch_bounds__(kJoinThreads) void int8_join_kernel(const int* __re
 int64_t join_groups(int64_t m, int64_t n) { return m * ceil_div(n, kJoinColumns); }
 
 int64_t int8_workspace(int64_t m, int64_t n, int64_t k) {
-    return m <= kDotRows ? 0 : parts_bytes<kInt8>(m, n, up(k, kRowUnit));
+    if (m <= kDotRows) return 0;
+    const int parts = plan_product<kInt8, kSums>(m, n, up(k, kRowUnit)).parts;
+    return parts > 1 ? up(parts * m * up(n, 4) * 4, 256) : 0;
 }
 
 bool int8_launchable(int64_t m, int64_t n, int64_t k) {
@@ -295,10 +299,10 @@ int run_int8(const int8_t* a, const float* a_scales, const int8_t* b, const floa
     const Plan plan = plan_product<kInt8, kSums>(m, n, k);
     p.parts = plan.parts;
     if (plan.parts == 1) return launch_product<kInt8, kSums>(p, plan.tile, stream);
-    p.out = ws;
+    p.out = ws, p.out_ld = up(n, 4);
     if (const int rc = launch_product<kInt8, kPartial>(p, plan.tile, stream)) return rc;
     hipLaunchKernelGGL(int8_join_kernel, dim3((unsigned)join_groups(m, n)), dim3(kJoinThreads), 0, stream,
-                       static_cast<const int*>(ws), plan.parts, m, n, (uint32_t)ceil_div(n, kJoinColumns), a_scales, b_scales, out, f32);
+                       static_cast<const int*>(ws), plan.parts, m, n, up(n, 4), (uint32_t)ceil_div(n, kJoinColumns), a_scales, b_scales, out, f32);
     return launched();
 }
 
