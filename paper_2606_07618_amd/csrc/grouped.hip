@@ -27,9 +27,12 @@ GroupedPlan plan_grouped(int64_t rows, int64_t experts, int64_t outer, bool turn
     return {Small::M, Small::N, Small::kThreads};
 }
 
-// Row tiles that there may be, and one more, which finds rows of no group to clear.
-int64_t most_tiles(int64_t rows, int64_t experts, int height) {
-    return rows / height + (rows < experts ? rows : experts) + 1;
+// Workgroups: for the row tiles that there may be, each XCD as many, and one at least that finds rows of no group to clear;
+// and for the parts that its last tiles are cut into.
+int64_t most_groups_of(int64_t rows, int64_t experts, int64_t outer, const GroupedPlan& plan) {
+    const int64_t tiles = rows / plan.height + (rows < experts ? rows : experts);
+    const int64_t more = plan.height == Large::M ? grouped_product::kUnits : 1;
+    return (ceil_div(tiles * ceil_div(outer, plan.width), kXcds) + more) * kXcds;
 }
 
 int check_grouped(int64_t rows, int64_t experts, int64_t n, int64_t k, int block) {
@@ -41,7 +44,7 @@ int check_grouped(int64_t rows, int64_t experts, int64_t n, int64_t k, int block
 
 bool grouped_launchable(int64_t rows, int64_t experts, int64_t outer, bool turned) {
     const GroupedPlan plan = plan_grouped(rows, experts, outer, turned);
-    return launchable(most_tiles(rows, experts, plan.height) * ceil_div(outer, plan.width), plan.threads);
+    return launchable(most_groups_of(rows, experts, outer, plan), plan.threads);
 }
 
 template <int R, int C>
@@ -59,7 +62,7 @@ int run_grouped(grouped_product::Args p, bool turned, int block, hipStream_t str
     const GroupedPlan plan = plan_grouped(p.rows, p.experts, p.outer, turned);
     p.shift = block == 16 ? 4 : block == 32 ? 5 : block == 64 ? 6 : 7;
     p.tiles_n = ceil_div(p.outer, plan.width);
-    const dim3 grid((unsigned)(most_tiles(p.rows, p.experts, plan.height) * p.tiles_n));
+    const dim3 grid((unsigned)most_groups_of(p.rows, p.experts, p.outer, plan));
     if (plan.threads == Large::kThreads && plan.height == Large::M) launch_tiled<Large>(p, turned, grid, stream);
     else if (plan.height == Small::M) launch_tiled<Small>(p, turned, grid, stream);
     else if (plan.height == 16) plan.width == 128 ? launch_few<2, 1>(p, grid, stream) : launch_few<1, 1>(p, grid, stream);

@@ -30,9 +30,10 @@ struct Args {
     int out_f32, clear;                          // clear: rows of no group become zero
 };
 
-// Where a tile lies: its expert, its rows first .. first + left - 1 (left: to the group's end).  expert < 0: none; then
-// the groups' rows are begin .. end - 1, and `index` counts on from the last tile.
-struct Place { int expert; int64_t first, left, begin, end, index; };
+// Where a row tile lies: its expert, its rows first .. first + left - 1 (left: to the group's end).
+struct Place { int expert; int64_t first, left; };
+// All groups: their row tiles, and their rows begin .. end - 1.
+struct Groups { int tiles, begin, end; };
 
 __device__ __forceinline__ int at_lane(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
 
@@ -52,58 +53,79 @@ __device__ __forceinline__ int scan(int v) {
     return scan_step<0x143, 0xC, SUM>(v);        // rows 2 and 3: lane 31
 }
 
-// Offsets are taken within 0 .. rows and never descend: what does not fit makes a group shorter or empty.
-__device__ __forceinline__ Place place_of(const Args& p, int64_t index, int height, int lane) {
+// Goes through the groups, a wave's lanes 64 at a time: each(first group, a lane's tiles, tiles up to it and with it, its
+// first row, its end) until that says true.  Offsets are taken within 0 .. rows and never descend: what does not fit makes
+// a group shorter or empty.
+template <class Each>
+__device__ __forceinline__ Groups through(const Args& p, int height, int lane, Each each) {
     const int rows = (int)p.rows;
     auto within = [&](int v) { return v < 0 ? 0 : v > rows ? rows : v; };
     auto end_of = [&](int e) { return e < p.experts ? p.offsets[e + 1] : 0; };
-    int next = end_of(lane), before = within(p.offsets[0]);
+    int next = end_of(lane), before = within(p.offsets[0]), total = 0;
     const int begin = before;
-    int left = (int)index;                       // tiles are fewer than 2^31
     for (int base = 0; base < p.experts; base += kLanes) {
         int end = scan<false>(within(next));     // past the last expert: as the last one's
         next = end_of(base + kLanes + lane);
         if (end < before) end = before;
         int start = __shfl_up(end, 1);
         if (lane == 0) start = before;
-        const int tiles = (end - start + height - 1) / height, upto = scan<true>(tiles);
-        const uint64_t mine = __ballot(left < upto);
-        if (mine) {
-            const int l = __builtin_ctzll(mine);
-            const int s = at_lane(start, l), t = at_lane(end, l);
-            const int64_t first = s + (int64_t)(left - at_lane(upto - tiles, l)) * height;
-            return {base + l, first, t - first, 0, 0, 0};
-        }
-        left -= at_lane(upto, kLanes - 1);
+        const int tiles = (int)((end - start + (int64_t)height - 1) / height), upto = scan<true>(tiles);
+        if (each(base, total, tiles, upto, start, end)) break;
+        total += at_lane(upto, kLanes - 1);      // tiles are fewer than 2^31
         before = at_lane(end, kLanes - 1);
     }
-    return {-1, 0, 0, begin, before, left};
+    return {total, begin, before};
+}
+
+__device__ __forceinline__ Groups groups_of(const Args& p, int height, int lane) {
+    return through(p, height, lane, [](int, int, int, int, int, int) { return false; });
+}
+
+// Row tile `index` of those that there are.
+__device__ __forceinline__ Place place_of(const Args& p, int index, int height, int lane) {
+    Place t = {0, 0, 0};
+    through(p, height, lane, [&](int base, int total, int tiles, int upto, int start, int end) {
+        const uint64_t mine = __ballot(index - total < upto);
+        if (!mine) return false;
+        const int l = __builtin_ctzll(mine), s = at_lane(start, l);
+        const int64_t first = s + (int64_t)(index - total - at_lane(upto - tiles, l)) * height;
+        t = {base + l, first, at_lane(end, l) - first};
+        return true;
+    });
+    return t;
+}
+
+// What a workgroup does.  An XCD gets a run of the sequence of tiles, which walks kDeep row tiles at a time, so that what
+// it works on at one time shares rows and weights in its L2.  Where an XCD's last tiles would keep few of its compute
+// units busy (SPLIT, one workgroup each), they are cut into two or four parts of their rows ([8192, 14336] x eight times
+// [14336, 4096], 72 tiles for 32 units: XX us, XX without).  The workgroups that are over: `spare` of `sharers`.
+constexpr int kDeep = 8, kUnits = 32;
+struct Work { bool tile; int index; int64_t n; int part, parts; int64_t spare, sharers; };
+template <bool SPLIT>
+__device__ __forceinline__ Work work_of(int64_t id, int64_t launched, int tiles_m, int64_t tiles_n) {
+    const int64_t count = tiles_m * tiles_n, xcd = id % kXcds, local = id / kXcds;
+    const int64_t each = count / kXcds, rest = count % kXcds, mine = each + (xcd < rest), last = SPLIT ? mine % kUnits : 0, whole = mine - last;
+    const int parts = last <= kUnits / 4 ? 4 : last <= kUnits / 2 ? 2 : 1;
+    const int64_t used = whole + last * parts;
+    if (local >= used) return {false, 0, 0, 0, 0, (local - used) * kXcds + xcd, (launched / kXcds - used) * kXcds};
+    const bool cut = local >= whole;
+    const int64_t in_run = cut ? whole + (local - whole) / parts : local;
+    const int64_t seq = xcd * each + (xcd < rest ? xcd : rest) + in_run;
+    const int64_t first = seq / (kDeep * tiles_n) * kDeep, height = tiles_m - first < kDeep ? tiles_m - first : kDeep;
+    const int64_t in = seq % (kDeep * tiles_n);
+    return {true, (int)(first + in % height), in / height, cut ? (int)((local - whole) % parts) : 0, cut ? parts : 1, 0, 0};
 }
 
 // Rows of no group: the workgroups that have no tile share them out.
-__device__ __forceinline__ void clear_rows(const Args& p, const Place& t, int64_t n0, int64_t width, int64_t sharers, int tid,
-                                           int threads) {
+__device__ __forceinline__ void clear_rows(const Args& p, const Groups& all, const Work& w, int tid, int threads) {
     if (!p.clear) return;
-    const int64_t end = n0 + width < p.outer ? n0 + width : p.outer;
-    for (int64_t i = t.index; i < t.begin + (p.rows - t.end); i += sharers) {
-        const int64_t m = i < t.begin ? i : t.end + (i - t.begin);
-        for (int64_t n = n0 + tid; n < end; n += threads) {
+    for (int64_t i = w.spare; i < all.begin + (p.rows - all.end); i += w.sharers) {
+        const int64_t m = i < all.begin ? i : all.end + (i - all.begin);
+        for (int64_t n = tid; n < p.outer; n += threads) {
             if (p.out_f32) static_cast<float*>(p.out)[m * p.outer + n] = 0.0f;
             else static_cast<uint16_t*>(p.out)[m * p.outer + n] = 0;
         }
     }
-}
-
-// Row tile and columns from a workgroup's number: an XCD gets a run of the sequence, which walks kDeep row tiles at a
-// time, so that what it works on at one time shares rows and weights in its L2.
-constexpr int kDeep = 8;
-struct Work { int64_t index, n; };
-__device__ __forceinline__ Work work_of(int64_t id, int64_t count, int64_t tiles_n) {
-    const int64_t xcd = id % kXcds, each = count / kXcds, rest = count % kXcds, tiles_m = count / tiles_n;
-    const int64_t seq = xcd * each + (xcd < rest ? xcd : rest) + id / kXcds;
-    const int64_t first = seq / (kDeep * tiles_n) * kDeep, height = tiles_m - first < kDeep ? tiles_m - first : kDeep;
-    const int64_t in = seq % (kDeep * tiles_n);
-    return {first + in % height, in / height};
 }
 
 // ---- weights and scales by groups of 256 values of a row ------------------------------------------
@@ -165,10 +187,11 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_kernel(Args p) {
     __shared__ __attribute__((aligned(1024))) char lds[2 * kStage];
     const int tid = threadIdx.x, lane = tid % kLanes, g = lane / 16, l16 = lane % 16;
     const int wave = __builtin_amdgcn_readfirstlane(tid / kLanes);
-    const Work work = work_of(blockIdx.x, gridDim.x, p.tiles_n);
+    const Groups all = groups_of(p, kRows, lane);
+    const Work work = work_of<false>(blockIdx.x, gridDim.x, all.tiles, p.tiles_n);
+    if (!work.tile) return clear_rows(p, all, work, tid, kFewThreads);
     const int64_t n0 = work.n * N;
     const Place t = place_of(p, work.index, kRows, lane);
-    if (t.expert < 0) return clear_rows(p, t, n0, N, gridDim.x / p.tiles_n - (work.index - t.index), tid, kFewThreads);
 
     const float S = p.S[t.expert];
     const int64_t q_ld = p.k / 2, w_row = t.expert * p.n + n0, q_left = (p.n - n0) * q_ld, x_bytes = p.k * 2;
@@ -290,12 +313,14 @@ constexpr int kSteps = 2;                        // in LDS
 // Turned weights: a row's chunks of 16 bytes exchanged by the row, as reads take one chunk of 16 neighbouring rows and
 // writes one of rows 8 apart.
 __device__ __forceinline__ int exchange(int row) { return ((row >> 1) ^ (row >> 4)) & 7; }
+__device__ __forceinline__ int swapped(int row) { return row ^ (row >> 3 & 1); }
 
 template <int M_, int WN_>
 struct Tile {
     static constexpr int M = M_, WM = 2, WN = WN_, N = WN_ * 64, kThreads = WM * WN_ * kLanes;
     static constexpr int kStage = (M + N) * kStepBytes;              // of LDS, a step of rows and turned weights; a power of two
     static constexpr int kLds = kSteps * (kStage + N * 16);
+    static constexpr bool kSplit = M_ == 256;                        // one workgroup a compute unit
     static constexpr int kMost = M_ / 32;                            // a wave's fragments of rows
 };
 
@@ -304,11 +329,14 @@ struct Tile {
 template <class T>
 struct Turned {
     static constexpr int kLoads = 8, kParts = 4;
+    // half a wave: 16 times 8 neighbouring columns of 8 neighbouring rows, which it writes to all banks at once
+    __device__ static __forceinline__ int column_of(int tid) { return (tid % 16 + tid / 32 * 16 % (T::N / 8)) * 8; }
+    __device__ static __forceinline__ int row_of(int tid) { return (tid / 16 % 2 + tid / (T::N / 4) * 2) * 4; }
     struct From {
         uint32_t q, s, q_ld, s_ld;
         __device__ __forceinline__ void init(const Args& p, int64_t n0, int tid) {
             q_ld = (uint32_t)(p.k / 2), s_ld = (uint32_t)(p.k >> p.shift);
-            const int column = tid % (T::N / 8) * 8, row = tid / (T::N / 8) * 4;
+            const int column = column_of(tid), row = row_of(tid);
             const bool in = n0 + column < p.k;
             q = in ? (uint32_t)row * q_ld + (uint32_t)column / 2 : kOutside;
             s = in ? (uint32_t)row * s_ld + (((uint32_t)n0 + column) >> p.shift) : kOutside;
@@ -326,10 +354,11 @@ struct Turned {
         }
     }
 
-    // Where a thread's weights go in LDS: with its chunks' places exchanged, part Q lies at base ^ 16 Q, 256 Q on.
+    // Where a thread's weights go in LDS: with its chunks' places and every second eight's pairs of columns exchanged, column
+    // 2 Q + J lies at base ^ (16 Q + 128 J), 256 Q on.
     __device__ static __forceinline__ uint32_t base(int tid) {
-        const int column = tid % (T::N / 8) * 8, row = tid / (T::N / 8) * 4;
-        return column * kStepBytes + ((row / 8) ^ exchange(column)) * kChunk + row % 8 * 2;
+        const int column = column_of(tid), row = row_of(tid);
+        return swapped(column) * kStepBytes + ((row / 8) ^ exchange(column)) * kChunk + row % 8 * 2;
     }
     // Part Q, two columns of the four rows, to LDS at base address `to`.
     template <int Q>
@@ -341,7 +370,7 @@ struct Turned {
         // the upper halves of the products hold all of them
         const auto pair = [](float lo, float hi) { return (int)__builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u); };
         put8<2 * Q * kStepBytes>(to ^ (Q * kChunk), i32x2{pair(a[0], b[0]), pair(c[0], d[0])});
-        put8<(2 * Q + 1) * kStepBytes>(to ^ (Q * kChunk), i32x2{pair(a[1], b[1]), pair(c[1], d[1])});
+        put8<2 * Q * kStepBytes>(to ^ (Q * kChunk + kStepBytes), i32x2{pair(a[1], b[1]), pair(c[1], d[1])});
     }
 };
 
@@ -610,7 +639,7 @@ __device__ __forceinline__ void product_turned(const Args& p, const Place& t, in
     // their row, so other chunks and the next step's LDS are some bits away.  Made in each step, not kept for all.
     const int l16 = lane % 16, chunk = lane / 16;
     uint32_t a_at = (a_row(0) + l16) * kStepBytes + (chunk ^ A::exchange(l16)) * kChunk;
-    uint32_t b_at = (T::M + b_row(0) + l16) * kStepBytes + (chunk ^ exchange(b_row(0) + l16)) * kChunk;
+    uint32_t b_at = (T::M + swapped(b_row(0) + l16)) * kStepBytes + (chunk ^ exchange(b_row(0) + l16)) * kChunk;
     uint32_t w_at = (uint32_t)(uintptr_t)(lds_void*)lds + T::M * kStepBytes + B::base(tid);   // the kernel's LDS begins with it
     static_assert((T::kStage & (T::kStage - 1)) == 0 && T::M * kStepBytes >= 1024, "bits apart");
     B b[2];
@@ -664,6 +693,7 @@ __device__ __forceinline__ void product_turned(const Args& p, const Place& t, in
             if constexpr (stores) __builtin_amdgcn_sched_group_barrier(0x002, 5 * kPer, 0);                  // vector instructions
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                                               // matrix instructions
         }
+        if constexpr (g % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // not over all of a step: registers
     };
     static_assert(MF == 2 || MF == 4 || MF == 8, "groups of a step");
     auto step = [&](int s, auto dc) {
@@ -706,10 +736,17 @@ template <class T, bool TURNED>
 __global__ __launch_bounds__(T::kThreads, 2) void grouped_kernel(Args p) {
     __shared__ __attribute__((aligned(1024))) char lds[TURNED ? kSteps * T::kStage : T::kLds];
     const int tid = threadIdx.x;
-    const Work work = work_of(blockIdx.x, gridDim.x, p.tiles_n);
+    const Groups all = groups_of(p, T::M, tid % kLanes);
+    const Work work = work_of<T::kSplit>(blockIdx.x, gridDim.x, all.tiles, p.tiles_n);
+    if (!work.tile) return clear_rows(p, all, work, tid, T::kThreads);
     const int64_t n0 = work.n * T::N;
-    const Place t = place_of(p, work.index, T::M, tid % kLanes);
-    if (t.expert < 0) return clear_rows(p, t, n0, T::N, gridDim.x / p.tiles_n - (work.index - t.index), tid, T::kThreads);
+    Place t = place_of(p, work.index, T::M, tid % kLanes);
+    if constexpr (T::kSplit) {
+        const int64_t height = T::M / work.parts;
+        t.first += work.part * height, t.left -= work.part * height;
+        if (t.left <= 0) return;
+        if (work.parts > 1 && t.left > height) t.left = height;
+    }
     auto product = [&](auto mc) {
         constexpr int MF = decltype(mc)::value;
         if constexpr (TURNED) product_turned<T, MF>(p, t, n0, lds, tid);
