@@ -313,7 +313,6 @@ constexpr int kSteps = 2;                        // in LDS
 // Turned weights: a row's chunks of 16 bytes exchanged by the row, as reads take one chunk of 16 neighbouring rows and
 // writes one of rows 8 apart.
 __device__ __forceinline__ int exchange(int row) { return ((row >> 1) ^ (row >> 4)) & 7; }
-__device__ __forceinline__ int swapped(int row) { return row ^ (row >> 3 & 1); }
 
 template <int M_, int WN_>
 struct Tile {
@@ -329,9 +328,8 @@ struct Tile {
 template <class T>
 struct Turned {
     static constexpr int kLoads = 8, kParts = 4;
-    // half a wave: 16 times 8 neighbouring columns of 8 neighbouring rows, which it writes to all banks at once
-    __device__ static __forceinline__ int column_of(int tid) { return (tid % 16 + tid / 32 * 16 % (T::N / 8)) * 8; }
-    __device__ static __forceinline__ int row_of(int tid) { return (tid / 16 % 2 + tid / (T::N / 4) * 2) * 4; }
+    __device__ static __forceinline__ int column_of(int tid) { return tid % (T::N / 8) * 8; }
+    __device__ static __forceinline__ int row_of(int tid) { return tid / (T::N / 8) * 4; }
     struct From {
         uint32_t q, s, q_ld, s_ld;
         __device__ __forceinline__ void init(const Args& p, int64_t n0, int tid) {
@@ -354,11 +352,10 @@ struct Turned {
         }
     }
 
-    // Where a thread's weights go in LDS: with its chunks' places and every second eight's pairs of columns exchanged, column
-    // 2 Q + J lies at base ^ (16 Q + 128 J), 256 Q on.
+    // Where a thread's weights go in LDS: with its chunks' places exchanged, column 2 Q + J lies at base ^ 16 Q, 256 Q + 128 J on.
     __device__ static __forceinline__ uint32_t base(int tid) {
         const int column = column_of(tid), row = row_of(tid);
-        return swapped(column) * kStepBytes + ((row / 8) ^ exchange(column)) * kChunk + row % 8 * 2;
+        return column * kStepBytes + ((row / 8) ^ exchange(column)) * kChunk + row % 8 * 2;
     }
     // Part Q, two columns of the four rows, to LDS at base address `to`.
     template <int Q>
@@ -370,7 +367,7 @@ struct Turned {
         // the upper halves of the products hold all of them
         const auto pair = [](float lo, float hi) { return (int)__builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u); };
         put8<2 * Q * kStepBytes>(to ^ (Q * kChunk), i32x2{pair(a[0], b[0]), pair(c[0], d[0])});
-        put8<2 * Q * kStepBytes>(to ^ (Q * kChunk + kStepBytes), i32x2{pair(a[1], b[1]), pair(c[1], d[1])});
+        put8<(2 * Q + 1) * kStepBytes>(to ^ (Q * kChunk), i32x2{pair(a[1], b[1]), pair(c[1], d[1])});
     }
 };
 
@@ -423,6 +420,37 @@ __device__ __forceinline__ void finish(const Args& p, const Place& t, int64_t n0
     }
 }
 
+// Rows of 128 bytes in LDS, loaded as Side's but for their exchange: a lane of a fragment reads chunk 2 (lane / 16) or the
+// one behind it, and of the 16 lanes that LDS serves at once some are of the next sixteen, two chunks on: their rows' places
+// (a pair of rows' each) must differ from the first ones' by more than that.  (With Side's, half of LDS' time was conflicts.)
+template <int R, int THREADS>
+struct Rows {
+    static constexpr int kLoads = R * kStepBytes / (THREADS * kChunk);
+    static_assert(THREADS / 8 % 16 == 0 && kLoads * THREADS * kChunk == R * kStepBytes, "a thread's rows have one exchange");
+    __device__ static __forceinline__ int exchange(int row) {
+        const int i = row >> 1 & 7;
+        return ((i >> 2 ^ i >> 1) & 1) << 2 | (i >> 2) << 1 | (i & 1);
+    }
+    uint32_t offset[kLoads];
+    int at;                                      // of this thread's chunk in a row
+    __device__ __forceinline__ void init(int64_t left, int64_t ld, int tid) {
+        at = (tid % 8 ^ exchange(tid / 8)) * kChunk;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int row = (i * THREADS + tid) / 8;
+            offset[i] = row < left ? (uint32_t)row * (uint32_t)ld + at : kOutside;
+        }
+    }
+    __device__ __forceinline__ void load(const char* base, char* lds, int64_t ahead, int wave) const {
+        const __amdgpu_buffer_rsrc_t w = window(base);
+        const int left = ahead > kStepBytes ? kStepBytes : ahead > 0 ? (int)ahead : 0;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(w, (lds_void*)(lds + (i * THREADS + wave * kLanes) * kChunk), kChunk,
+                                                     (int)(at < left ? offset[i] : kOutside), 0, 0, 0);
+    }
+};
+
 // The product of one tile with weights as they lie, MF fragments of 16 rows a wave.
 //
 // Weights go into LDS as they are, 256 values of each row (whole lines) at a time, and from there into the registers of
@@ -433,7 +461,7 @@ template <class T, int MF>
 __device__ __forceinline__ void product_raw(const Args& p, const Place& t, int64_t n0, char* lds, int tid) {
     constexpr int NF = 4, kRows = MF * 32, kA = T::M * kStepBytes, kB = T::N * kStepBytes, kS = T::N * 16;
     constexpr int kB0 = 2 * kA, kS0 = kB0 + 2 * kB;        // of LDS: rows, weights, scales, two of each
-    using A = Side<kRows, T::kThreads, false>;
+    using A = Rows<kRows, T::kThreads>;
     using B = Side<T::N, T::kThreads, false>;              // 256 values in 128 bytes
     static_assert(B::kLoads == 4 && T::kThreads == 2 * T::N, "the loads' order");
     const int lane = tid % kLanes, wave = __builtin_amdgcn_readfirstlane(tid / kLanes), wm = wave / T::WN, wn = wave % T::WN;
@@ -445,7 +473,7 @@ __device__ __forceinline__ void product_raw(const Args& p, const Place& t, int64
     const char *a0 = p.x + t.first * p.ld, *q0 = p.q + w_row * q_ld;
     const int64_t q_left = (p.n - n0) * q_ld, row_bytes = p.k * 2;
     auto fetch_a = [&](int s, int slot) {
-        sa.load(a0 + (int64_t)s * kStepBytes, nullptr, lds + slot * kA, row_bytes - (int64_t)s * kStepBytes, tid, wave);
+        sa.load(a0 + (int64_t)s * kStepBytes, lds + slot * kA, row_bytes - (int64_t)s * kStepBytes, wave);
     };
     // Half of a group's weights.  A row's last chunk may hold the next row's first values: they meet zeros.
     auto fetch_q = [&](int group, int slot, auto hc) {
@@ -639,7 +667,7 @@ __device__ __forceinline__ void product_turned(const Args& p, const Place& t, in
     // their row, so other chunks and the next step's LDS are some bits away.  Made in each step, not kept for all.
     const int l16 = lane % 16, chunk = lane / 16;
     uint32_t a_at = (a_row(0) + l16) * kStepBytes + (chunk ^ A::exchange(l16)) * kChunk;
-    uint32_t b_at = (T::M + swapped(b_row(0) + l16)) * kStepBytes + (chunk ^ exchange(b_row(0) + l16)) * kChunk;
+    uint32_t b_at = (T::M + b_row(0) + l16) * kStepBytes + (chunk ^ exchange(b_row(0) + l16)) * kChunk;
     uint32_t w_at = (uint32_t)(uintptr_t)(lds_void*)lds + T::M * kStepBytes + B::base(tid);   // the kernel's LDS begins with it
     static_assert((T::kStage & (T::kStage - 1)) == 0 && T::M * kStepBytes >= 1024, "bits apart");
     B b[2];
