@@ -347,3 +347,62 @@ def test_long_offsets(nv):
         want, bound = plain64.product(plain64.f64(dy), v.t())
         s = float(last[2][0])
         plain64.check(dx[:, :128], want * s, bound * s + 2.0 ** -24 * (want.abs() + bound) * s, "dx")
+
+
+def xcd_runs(sizes, outer, height=256, width=256):
+    """Tiles of each of the eight XCDs' runs, as the kernel deals them out."""
+    count = sum(-(-s // height) for s in sizes) * -(-outer // width)
+    return [count // 8 + (x < count % 8) for x in range(8)]
+
+
+# one, two, four and three quarters of 32 compute units' worth of tiles over: cut into four, four, two parts, and whole
+@pytest.mark.parametrize("turned", [False, True])
+@pytest.mark.parametrize("extra,over", [(1, 8), (0, 0), (2, 16), (3, 24)])
+def test_last_tiles_in_parts(nv, extra, over, turned):
+    g = gen(18, extra, turned)
+    outer, inner = 16384, 64                               # 64 tiles across
+    sizes = [700, 0, 256 + 1, 260, 200, 300, 256, 40][:6] + [256] * (extra + 2)
+    tiles = sum(-(-s // 256) for s in sizes)
+    while tiles % 4 != extra:
+        sizes.append(130)
+        tiles += 1
+    assert set(r % 32 for r in xcd_runs(sizes, outer)) == {over}
+    n, k = (inner, outer) if turned else (outer, inner)
+    w = weights(len(sizes), n, k, 16, g)
+    offsets = offsets_of(sizes, 3)
+    x = rand((sum(sizes) + 10, inner), g)
+    f = nv.grouped_matmul_grad_input if turned else nv.grouped_matmul
+    want, lim = expected(x, spans(offsets), w, 16, turned)
+    plain64.check(f(x, offsets, *w), want, lim, "y")
+
+
+@pytest.mark.parametrize("first", [1, 2, 3])
+@pytest.mark.parametrize("each", [5, 40, 200])
+def test_scales_that_start_at_any_byte(nv, each, first):
+    """One expert's share of a buffer, from any byte on; what lies before and behind does not matter."""
+    g = gen(19, each, first)
+    n, k = 72, 512
+    q, sc, S = weights(2, n, k, 16, g)
+    offsets = offsets_of([each, each + 1])
+    x, dy = rand((2 * each + 1, k), g), rand((2 * each + 1, n), g)
+    buffer = torch.full((sc.numel() + 8,), 0x7F, dtype=torch.uint8, device=DEV)
+    moved = buffer[first:first + sc.numel()].view(sc.shape)
+    moved.copy_(sc)
+    assert torch.equal(nv.grouped_matmul(x, offsets, q, moved, S), nv.grouped_matmul(x, offsets, q, sc, S))
+    assert torch.equal(nv.grouped_matmul_grad_input(dy, offsets, q, moved, S), nv.grouped_matmul_grad_input(dy, offsets, q, sc, S))
+
+
+@pytest.mark.parametrize("each", [5, 200])
+def test_last_weights_at_the_end_of_their_storage(nv, each):
+    """Rows of an odd number of eights of bytes, the last of which end with a storage that goes on with other bytes."""
+    g = gen(20, each)
+    n, k = 33, 272
+    q, sc, S = weights(2, n, k, 16, g)
+    offsets = offsets_of([each, each])
+    x = rand((2 * each, k), g)
+    want, lim = expected(x, spans(offsets), (q, sc, S), 16, False)
+    for fill in (0x00, 0xFF):
+        big = torch.full((q.numel() + 64,), fill, dtype=torch.uint8, device=DEV)
+        view = big[:q.numel()].view(q.shape)
+        view.copy_(q)
+        plain64.check(nv.grouped_matmul(x, offsets, view, sc, S), want, lim, "y")
