@@ -430,7 +430,7 @@ int nvfp4_grouped_product_grad_input(const void* dy, int64_t ld, const int* offs
  * Activations have a scale for each token so, weights [n, k] one for each output channel.
  */
 
-/* s = max|x| / 127 of the row, rounded to binary32; q the whole number nearest to the quotient x / s, ties to the even
+/* s = RN32(max|x| RN32(1 / 127)) of the row; q the whole number nearest to the quotient x / s, ties to the even
  * one, at most 127 in magnitude; s = 0: q = 0.  A row that holds an infinity or a NaN gets s = NaN (and q = 0): its
  * products are NaN.  x: [rows, cols], rows ldx elements apart, binary32 or bfloat16, aligned to its elements;
  * cols < 2^17.  One kernel, no workspace. */

@@ -1,4 +1,5 @@
-// Linear layers in 8-bit integers: rows x = s q with s = max|x| / 127, and the products of two operands quantized so,
+// Linear layers in 8-bit integers: rows x = s q with s = max|x| / 127 (the product with binary32's 1/127, as elementary
+// operations on tensors divide by a number: at most 1.5 units of its last place off), and the products of two operands so,
 //   y[m][n] = s_a[m] s_b[n] sum_k a[m][k] b[n][k],   dx[m][k] = sum_n dy[m][n] s_b[n] b[n][k].
 // Integer sums are exact; an output is rounded where the sum becomes a binary32 number, in the product of the scales, in
 // their product, and to its type.
@@ -124,7 +125,7 @@ __global__ __launch_bounds__(kQuantThreads) void quant_kernel(const char* __rest
         for (int w = 0; w < kQuantWaves; ++w) top = tops[w] > top ? tops[w] : top;
     }
     const bool finite = top < 0x7F800000u;
-    const float s = __uint_as_float(top) / 127.0f;        // correctly rounded
+    const float s = __uint_as_float(top) * 0x1.020408p-7f;
     if ((WAVE ? lane : tid) == 0) scales[row] = finite ? s : __uint_as_float(0x7FC00000u);
     // small scales and their rows times 2^64, exactly, so that neither the reciprocal nor a remainder leaves the range
     const float by = s < 0x1p-100f ? 0x1p64f : 1.0f, sb = s * by;

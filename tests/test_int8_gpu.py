@@ -30,7 +30,7 @@ def quantized(x):
     x = plain64.f64(x).numpy()
     top = np.abs(x).max(-1) if x.shape[1] else np.zeros(x.shape[0])
     bad = ~np.isfinite(top)
-    s = np.where(bad, 0.0, top / 127.0).astype(np.float32).astype(np.float64)[:, None]
+    s = (np.where(bad, 0.0, top).astype(np.float32) * (np.float32(1) / np.float32(127))).astype(np.float64)[:, None]
     with np.errstate(invalid="ignore", divide="ignore"):
         r = np.floor(np.where(bad[:, None] | (s == 0), 0.0, x) / np.where(s == 0, 1.0, s))
         mid = (r + 0.5) * s
