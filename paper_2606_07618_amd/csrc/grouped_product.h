@@ -98,7 +98,7 @@ __device__ __forceinline__ Place place_of(const Args& p, int index, int height, 
 // What a workgroup does.  An XCD gets a run of the sequence of tiles, which walks kDeep row tiles at a time, so that what
 // it works on at one time shares rows and weights in its L2.  Where an XCD's last tiles would keep few of its compute
 // units busy (SPLIT, one workgroup each), they are cut into two or four parts of their rows ([8192, 14336] x eight times
-// [14336, 4096], 72 tiles for 32 units: XX us, XX without).  The workgroups that are over: `spare` of `sharers`.
+// [14336, 4096], 72 tiles for 32 units: 979 us, 1058 without).  The workgroups that are over: `spare` of `sharers`.
 constexpr int kDeep = 8, kUnits = 32;
 struct Work { bool tile; int index; int64_t n; int part, parts; int64_t spare, sharers; };
 template <bool SPLIT>
@@ -170,19 +170,52 @@ struct GroupScales {
     }
 };
 
+// Rows of 128 bytes in LDS, loaded as Side's but for their exchange: a lane of a fragment reads chunk 2 (lane / 16) or the
+// one behind it, and of the lanes that LDS serves at once rows 0 to 3 and 12 to 15 are from one sixteen, rows 4 to 11 from the
+// next, two chunks on.  The places of these two sets of rows are apart from each other, moved by two or not.  (With Side's
+// exchange half of LDS' time was conflicts: 16384 rows, eight groups, [14336, 4096] 1.59 ms, 1.51 so.)
+template <int R, int THREADS>
+struct Rows {
+    static constexpr int kLoads = R * kStepBytes / (THREADS * kChunk);
+    static_assert(THREADS / 8 % 16 == 0 && kLoads * THREADS * kChunk == R * kStepBytes, "a thread's rows have one exchange");
+    __device__ static __forceinline__ int exchange(int row) {
+        const int i = row >> 1 & 7;
+        return ((i >> 2 ^ i >> 1) & 1) << 2 | (i >> 2) << 1 | (i & 1);
+    }
+    uint32_t offset[kLoads];
+    int at;                                      // of this thread's chunk in a row
+    __device__ __forceinline__ void init(int64_t left, int64_t ld, int tid) {
+        at = (tid % 8 ^ exchange(tid / 8)) * kChunk;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int row = (i * THREADS + tid) / 8;
+            offset[i] = row < left ? (uint32_t)row * (uint32_t)ld + at : kOutside;
+        }
+    }
+    __device__ __forceinline__ void load(const char* base, char* lds, int64_t ahead, int wave) const {
+        const __amdgpu_buffer_rsrc_t w = window(base);
+        const int left = ahead > kStepBytes ? kStepBytes : ahead > 0 ? (int)ahead : 0;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(w, (lds_void*)(lds + (i * THREADS + wave * kLanes) * kChunk), kChunk,
+                                                     (int)(at < left ? offset[i] : kOutside), 0, 0, 0);
+    }
+};
+
 // ---- few rows a group ---------------------------------------------------------------------------
 // Reading the weights is all there is to do.  A workgroup owns 64 R weight rows, 16 R a wave, and up to 16 C rows of one
 // group; weights, scales and rows go through LDS by whole lines, 256 values of the contraction at a time, the next ones while
-// these are multiplied.  512 rows, 128 groups, [1536, 4096]: 113 us, 4.0 TB/s (95 with no scales read: 16 bytes of each row at
-// a time).  Three workgroups a compute unit hide each other's first waits; deeper rings leave room for two or one (128 us).
-// Loaded straight into the registers of the matrix instructions, whose neighbouring lanes hold different rows, each lane's 16
-// bytes are an access of their own to the L1, which is then nine tenths of the time busy (135 us).
+// these are multiplied.  512 rows, 128 groups, [1536, 4096]: 106 us, 4.3 TB/s of the 5.05 that a large copy reaches; a tenth of
+// the bytes are the scales, 16 bytes of a row at a time.  Three workgroups a compute unit hide each other's first waits;
+// rings of three or four stages leave room for two (128 us where two stages took 113).  Loaded straight into the registers of
+// the matrix instructions, whose neighbouring lanes hold different rows, each lane's 16 bytes are an access of their own to the
+// L1, which was then nine tenths of the time busy (135 us).
 constexpr int kFewThreads = 256;
 
 template <int R, int C>
 __global__ __launch_bounds__(kFewThreads, 2) void few_kernel(Args p) {
     constexpr int N = 64 * R, kRows = 16 * C, kW = N * kStepBytes, kX = kRows * 512, kS = N * 16, kStage = kW + kX + kS;
-    using B = Side<N, kFewThreads, false>;
+    using B = Rows<N, kFewThreads>;
     constexpr int kXLoads = kX / (kFewThreads * kChunk);
     __shared__ __attribute__((aligned(1024))) char lds[2 * kStage];
     const int tid = threadIdx.x, lane = tid % kLanes, g = lane / 16, l16 = lane % 16;
@@ -200,31 +233,30 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_kernel(Args p) {
     sb.init(p.n - n0, q_ld, tid);
     GroupScales<N> scales_of;
     scales_of.init(p, w_row, n0, tid);
-    // 32 chunks of a row of x, their places exchanged by the row: reads take one chunk of 16 rows
+    // 32 chunks of a row of x, their places exchanged by the row, as Rows' are for chunks eight apart
+    auto place = [](int row) { return (row & 8) | ((row >> 3 ^ row >> 2) & 1) << 2 | (row & 3); };
     uint32_t x_at[kXLoads];
     const int x_chunk = tid % 32;
 #pragma unroll
     for (int i = 0; i < kXLoads; ++i) {
         const int row = (i * kFewThreads + tid) / 32;
-        x_at[i] = row < t.left ? (uint32_t)row * (uint32_t)p.ld + (x_chunk ^ row % 16) * kChunk : kOutside;
+        x_at[i] = row < t.left ? (uint32_t)row * (uint32_t)p.ld + (x_chunk ^ place(row)) * kChunk : kOutside;
     }
     i32x2 scales[2];
     auto fetch = [&](int s, auto dc) {
         constexpr int d = decltype(dc)::value;
         char* to = lds + d * kStage;
-        // A row's last chunk may hold the next row's first values: they meet zeros.
+        // A row's last chunk may hold the next row's first values, finite numbers: they meet zeros.
         const int64_t done = (int64_t)s * kStepBytes, x_done = (int64_t)s * 512, q_ahead = q_ld - done, x_ahead = x_bytes - x_done;
         const int q_in = q_ahead > kStepBytes ? kStepBytes : q_ahead > 0 ? (int)q_ahead : 0, x_in = x_ahead > 512 ? 512 : x_ahead > 0 ? (int)x_ahead : 0;
         const __amdgpu_buffer_rsrc_t rq = window_of(q0 + done, q_left - done), rx = window(x0 + x_done);
 #pragma unroll
-        for (int i = 0; i < B::kLoads; ++i) {
-            const int at = ((tid % 8) ^ B::exchange((i * kFewThreads + tid) / 8)) * kChunk;
+        for (int i = 0; i < B::kLoads; ++i)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rq, (lds_void*)(to + (i * kFewThreads + wave * kLanes) * kChunk), kChunk,
-                                                     (int)(at < q_in ? sb.offset[i] : kOutside), 0, 0, 0);
-        }
+                                                     (int)(sb.at < q_in ? sb.offset[i] : kOutside), 0, 0, 0);
 #pragma unroll
         for (int i = 0; i < kXLoads; ++i) {
-            const int at = (x_chunk ^ (i * kFewThreads + tid) / 32 % 16) * kChunk;
+            const int at = (x_chunk ^ place((i * kFewThreads + tid) / 32)) * kChunk;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (lds_void*)(to + kW + (i * kFewThreads + wave * kLanes) * kChunk), kChunk,
                                                      (int)(at < x_in ? x_at[i] : kOutside), 0, 0, 0);
         }
@@ -261,7 +293,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_kernel(Args p) {
             for (int i = 0; i < C; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    xv[i][j] = *reinterpret_cast<const i32x4*>(x + (i * 16 + l16) * 512 + ((8 * g + 4 * h + j) ^ l16) * kChunk);
+                    xv[i][j] = *reinterpret_cast<const i32x4*>(x + (i * 16 + l16) * 512 + ((8 * g + 4 * h + j) ^ place(l16)) * kChunk);
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 // blocks of 16: a scale for two of the four; of 32: for all four; of more: the same for both halves
@@ -303,11 +335,13 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_kernel(Args p) {
 }
 
 // ---- tiles --------------------------------------------------------------------------------------
-// Weights are expanded by the threads that load them, once for a tile's rows, on their way into LDS, where they lie as
-// bfloat16 rows along the contraction, turned or not: turning costs nothing, as the pairs that share a register are put
-// together from single values anyway.  The rows of the other operand go from memory straight into LDS.  A step of the
-// contraction is 64 values; registers hold the weights of the next two steps, LDS the rows and weights of two.
-// A group's last tile computes as many rows as it needs, in halves.
+// 256 rows by 256 outputs, or 128 by 128, of one group; a group's last tile computes as many rows as it needs, in halves.  A
+// step of the contraction is 64 values.  The rows go from memory straight into LDS, one step ahead.  Weights as they lie go
+// there too, as nibbles, and each wave expands what it multiplies.  Turned ones are expanded by the threads that load them,
+// once for a tile's rows, on their way into LDS, where they lie as bfloat16 rows along the contraction: turning costs nothing
+// there, as the pairs that share a register are put together from single values anyway.
+//   16384 rows, eight groups, [14336, 4096]: 1.55 ms (1.24 PFLOP/s; the clock is held at 1.5 to 1.6 GHz by the power limit,
+//   and the matrix instructions are busy two thirds of a compute unit's time); turned, 8192 rows: 0.95 ms (1.01 PFLOP/s).
 constexpr int kSteps = 2;                        // in LDS
 
 // Turned weights: a row's chunks of 16 bytes exchanged by the row, as reads take one chunk of 16 neighbouring rows and
@@ -420,43 +454,12 @@ __device__ __forceinline__ void finish(const Args& p, const Place& t, int64_t n0
     }
 }
 
-// Rows of 128 bytes in LDS, loaded as Side's but for their exchange: a lane of a fragment reads chunk 2 (lane / 16) or the
-// one behind it, and of the 16 lanes that LDS serves at once some are of the next sixteen, two chunks on: their rows' places
-// (a pair of rows' each) must differ from the first ones' by more than that.  (With Side's, half of LDS' time was conflicts.)
-template <int R, int THREADS>
-struct Rows {
-    static constexpr int kLoads = R * kStepBytes / (THREADS * kChunk);
-    static_assert(THREADS / 8 % 16 == 0 && kLoads * THREADS * kChunk == R * kStepBytes, "a thread's rows have one exchange");
-    __device__ static __forceinline__ int exchange(int row) {
-        const int i = row >> 1 & 7;
-        return ((i >> 2 ^ i >> 1) & 1) << 2 | (i >> 2) << 1 | (i & 1);
-    }
-    uint32_t offset[kLoads];
-    int at;                                      // of this thread's chunk in a row
-    __device__ __forceinline__ void init(int64_t left, int64_t ld, int tid) {
-        at = (tid % 8 ^ exchange(tid / 8)) * kChunk;
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int row = (i * THREADS + tid) / 8;
-            offset[i] = row < left ? (uint32_t)row * (uint32_t)ld + at : kOutside;
-        }
-    }
-    __device__ __forceinline__ void load(const char* base, char* lds, int64_t ahead, int wave) const {
-        const __amdgpu_buffer_rsrc_t w = window(base);
-        const int left = ahead > kStepBytes ? kStepBytes : ahead > 0 ? (int)ahead : 0;
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(w, (lds_void*)(lds + (i * THREADS + wave * kLanes) * kChunk), kChunk,
-                                                     (int)(at < left ? offset[i] : kOutside), 0, 0, 0);
-    }
-};
-
 // The product of one tile with weights as they lie, MF fragments of 16 rows a wave.
 //
 // Weights go into LDS as they are, 256 values of each row (whole lines) at a time, and from there into the registers of
 // each wave, which expands the fragments that it multiplies, once for its 16 MF rows.  (Expanded once for the whole tile,
-// as turned ones are, each weight would be written to LDS, four times as wide: those stores took 0.45 of a step's 1.5 us,
-// more than expanding twice, which fits between the matrix instructions.)
+// as turned ones are, each weight is written to LDS, four times as wide: those stores took 0.45 of a step's 1.6 us, and
+// expanding, twice as often so, fits between the matrix instructions.)
 template <class T, int MF>
 __device__ __forceinline__ void product_raw(const Args& p, const Place& t, int64_t n0, char* lds, int tid) {
     constexpr int NF = 4, kRows = MF * 32, kA = T::M * kStepBytes, kB = T::N * kStepBytes, kS = T::N * 16;
@@ -475,7 +478,7 @@ __device__ __forceinline__ void product_raw(const Args& p, const Place& t, int64
     auto fetch_a = [&](int s, int slot) {
         sa.load(a0 + (int64_t)s * kStepBytes, lds + slot * kA, row_bytes - (int64_t)s * kStepBytes, wave);
     };
-    // Half of a group's weights.  A row's last chunk may hold the next row's first values: they meet zeros.
+    // Half of a group's weights.  A row's last chunk may hold the next row's first values, finite numbers: they meet zeros.
     auto fetch_q = [&](int group, int slot, auto hc) {
         constexpr int H = decltype(hc)::value;
         const int64_t done = (int64_t)group * kStepBytes, ahead = q_ld - done;

@@ -27,6 +27,11 @@ inline int check_dims(int64_t m, int64_t n, int64_t k) {
     return NVFP4_OK;
 }
 
+inline int check_workspace(const void* ws, size_t bytes, int64_t need) {
+    if (need > 0 && (!ws || (int64_t)bytes < need)) return NVFP4_ERR_WORKSPACE;
+    return aligned(ws, 256) || need == 0 ? NVFP4_OK : NVFP4_ERR_ALIGN;
+}
+
 inline int launched() { return hipGetLastError() == hipSuccess ? NVFP4_OK : NVFP4_ERR_HIP; }
 
 // Rows of `width` values as the tiles read them: 16-byte chunks, zeros past the width.

@@ -72,8 +72,8 @@ float product_us(int t, int parts, int64_t m, int64_t n, int64_t inner) {
     const float many = load > 1.0f ? kLaunchUs + (float)(int64_t)(load + 0.999f) * (cost.fixed + own * cost.among) : 0.0f;
     float us = few > many ? few : many;
     if (kMicroscaled<KIND> && t == 0) us += kLayUs;
-    // kInt8: parts whose steps are half as many take memory's time more of the way ([777, 14336] x [1001, 14336], the whole
-    // product: 49 us in eight parts of the second tile, which half of these bytes' cost would choose, 45 in two of the third)
+    // kInt8: with steps of twice the values the parts' sums weigh more ([777, 14336] x [1001, 14336], quantized in the same
+    // call: 49 us in eight parts of the second tile, which bfloat16's cost of them chooses, 45 in two of the third)
     constexpr int kBytes = KIND == kInt8 ? 16 : 8;
     if (parts > 1) us += kJoinUs + (float)m * (float)n * (float)(kBytes * kHalf<OUT> * parts) / kJoinBytesUs;
     return us;
