@@ -17,7 +17,8 @@ constexpr int64_t kMostInner = ((int64_t)1 << 17) - kRowUnit;
 // ---- quantization -----------------------------------------------------------------------------
 // One pass: a row stays in registers between its maximum and its quotients, as long as it has at most 8 kKept values a
 // thread; what is longer is read again.  A wave a row, or a workgroup where a wave would hold more than half of that.
-// [8192, 4096] bfloat16: 27 us, of which 20 to move; [777, 14330] binary32: 12 us (rows that all wait, then all compute).
+// From memory, [8192, 4096] bfloat16: 32 us, of which 20 to move; [777, 14330] binary32: 15 us, 11 to move (rows that all wait
+// first and compute then).
 constexpr int kQuantThreads = 256, kQuantWaves = kQuantThreads / kLanes, kUnit = 8, kKept = 8;   // units of 8 values
 
 // 8 values from `from`, of which `left` are there: bits of binary32 numbers.
@@ -154,7 +155,7 @@ int64_t quant_groups(int64_t rows, int64_t cols) { return cols <= kWaveCols ? ce
 
 // ---- one to four rows -------------------------------------------------------------------------
 // As the NVFP4 products of so few rows: lanes along the contraction, 16 values each, eight weight rows on their way at
-// once, four products an instruction.  One row, [14336, 4096]: 10.4 us, 5.6 TB/s.
+// once, four products an instruction.  One row, [14336, 4096], from memory: 12 us, 4.9 TB/s.
 constexpr int kDotSpan = kLanes * 16, kDotN = 8, kDotWaves = dot_product::kWaves;
 
 struct DotArgs {
@@ -241,8 +242,8 @@ void launch_dot(const DotArgs& p, hipStream_t stream) {
 }
 
 // ---- tiles ------------------------------------------------------------------------------------
-// The tiled product of the other operands: a step's 128 bytes of a row are 128 values.  [8192, 4096] x [14336, 4096]: 374 us,
-// 2.6 POP/s (a library's [8192, 8192] x [8192, 8192] of integers: 2.1).
+// The tiled product of the other operands: a step's 128 bytes of a row are 128 values.  [8192, 4096] x [14336, 4096]: 374 to
+// 409 us, 2.6 to 2.4 POP/s (a library's [8192, 8192] x [8192, 8192] of integers: 2.1).
 
 // Sums of parts of the contraction, in 32-bit integers as a whole sum is: a workgroup for kJoinColumns outputs of a row.
 // Rows of parts hold whole fours, which a tile stores at once.
