@@ -50,9 +50,9 @@ bool grouped_launchable(int64_t rows, int64_t experts, int64_t outer, bool turne
     return launchable(most_groups_of(rows, experts, outer, plan), plan.threads);
 }
 
-template <int R, int C>
+template <int R, int C, int H>
 void launch_few(const grouped_product::Args& p, dim3 grid, hipStream_t stream) {
-    hipLaunchKernelGGL((grouped_product::few_kernel<R, C>), grid, dim3(kFewThreads), 0, stream, p);
+    hipLaunchKernelGGL((grouped_product::few_kernel<R, C, H>), grid, dim3(kFewThreads * H), 0, stream, p);
 }
 
 template <class T>
@@ -68,8 +68,8 @@ int run_grouped(grouped_product::Args p, bool turned, int block, hipStream_t str
     const dim3 grid((unsigned)most_groups_of(p.rows, p.experts, p.outer, plan));
     if (plan.threads == Large::kThreads && plan.height == Large::M) launch_tiled<Large>(p, turned, grid, stream);
     else if (plan.height == Small::M) launch_tiled<Small>(p, turned, grid, stream);
-    else if (plan.height == 16) plan.width == 128 ? launch_few<2, 1>(p, grid, stream) : launch_few<1, 1>(p, grid, stream);
-    else plan.width == 128 ? launch_few<2, 2>(p, grid, stream) : launch_few<1, 2>(p, grid, stream);
+    else if (plan.height == 16) plan.width == 128 ? launch_few<2, 1, 1>(p, grid, stream) : launch_few<1, 1, 2>(p, grid, stream);
+    else plan.width == 128 ? launch_few<2, 2, 1>(p, grid, stream) : launch_few<1, 2, 1>(p, grid, stream);
     return launched();
 }
 

@@ -53,15 +53,21 @@ __device__ __forceinline__ int scan(int v) {
     return scan_step<0x143, 0xC, SUM>(v);        // rows 2 and 3: lane 31
 }
 
+// What every look at the groups begins with: offsets[0], and offsets[lane + 1].
+struct Offsets { int zero, next; };
+__device__ __forceinline__ Offsets offsets_of(const Args& p, int lane) {
+    return {p.offsets[0], lane < p.experts ? p.offsets[lane + 1] : 0};
+}
+
 // Goes through the groups, a wave's lanes 64 at a time: each(first group, a lane's tiles, tiles up to it and with it, its
 // first row, its end) until that says true.  Offsets are taken within 0 .. rows and never descend: what does not fit makes
 // a group shorter or empty.
 template <class Each>
-__device__ __forceinline__ Groups through(const Args& p, int height, int lane, Each each) {
+__device__ __forceinline__ Groups through(const Args& p, Offsets o, int height, int lane, Each each) {
     const int rows = (int)p.rows;
     auto within = [&](int v) { return v < 0 ? 0 : v > rows ? rows : v; };
     auto end_of = [&](int e) { return e < p.experts ? p.offsets[e + 1] : 0; };
-    int next = end_of(lane), before = within(p.offsets[0]), total = 0;
+    int next = o.next, before = within(o.zero), total = 0;
     const int begin = before;
     for (int base = 0; base < p.experts; base += kLanes) {
         int end = scan<false>(within(next));     // past the last expert: as the last one's
@@ -77,14 +83,14 @@ __device__ __forceinline__ Groups through(const Args& p, int height, int lane, E
     return {total, begin, before};
 }
 
-__device__ __forceinline__ Groups groups_of(const Args& p, int height, int lane) {
-    return through(p, height, lane, [](int, int, int, int, int, int) { return false; });
+__device__ __forceinline__ Groups groups_of(const Args& p, Offsets o, int height, int lane) {
+    return through(p, o, height, lane, [](int, int, int, int, int, int) { return false; });
 }
 
 // Row tile `index` of those that there are.
-__device__ __forceinline__ Place place_of(const Args& p, int index, int height, int lane) {
+__device__ __forceinline__ Place place_of(const Args& p, Offsets o, int index, int height, int lane) {
     Place t = {0, 0, 0};
-    through(p, height, lane, [&](int base, int total, int tiles, int upto, int start, int end) {
+    through(p, o, height, lane, [&](int base, int total, int tiles, int upto, int start, int end) {
         const uint64_t mine = __ballot(index - total < upto);
         if (!mine) return false;
         const int l = __builtin_ctzll(mine), s = at_lane(start, l);
@@ -203,28 +209,35 @@ struct Rows {
 };
 
 // ---- few rows a group ---------------------------------------------------------------------------
-// Reading the weights is all there is to do.  A workgroup owns 64 R weight rows, 16 R a wave, and up to 16 C rows of one
-// group; weights, scales and rows go through LDS by whole lines, 256 values of the contraction at a time, the next ones while
-// these are multiplied.  512 rows, 128 groups, [1536, 4096]: 106 us, 4.3 TB/s of the 5.05 that a large copy reaches; a tenth of
-// the bytes are the scales, 16 bytes of a row at a time.  Three workgroups a compute unit hide each other's first waits;
+// Reading the weights is all there is to do.  A workgroup owns 64 R weight rows, 16 R for each of four waves, and up to 16 C
+// rows of one group; weights, scales and rows go through LDS by whole lines, 256 values of the contraction at a time, the next
+// ones while these are multiplied.  512 rows, 128 groups, [1536, 4096]: 102 us, 4.5 TB/s of the 5.05 that a large copy reaches; a
+// tenth of the bytes are the scales, 16 bytes of a row at a time.  Three workgroups a compute unit hide each other's first waits;
 // rings of three or four stages leave room for two (128 us where two stages took 113).  Loaded straight into the registers of
 // the matrix instructions, whose neighbouring lanes hold different rows, each lane's 16 bytes are an access of their own to the
 // L1, which was then nine tenths of the time busy (135 us).
+// H: fours of waves that take turns along the contraction, whose sums meet in LDS at the end: where workgroups are few, a
+// stage's way from LDS through the matrix instructions is what there is to wait for (two rows of eight groups, [14336, 4096]:
+// 18.4 us with two fours, 20.4 with one, 23.2 with four).
 constexpr int kFewThreads = 256;
 
-template <int R, int C>
-__global__ __launch_bounds__(kFewThreads, 2) void few_kernel(Args p) {
+template <int R, int C, int H>
+__global__ __launch_bounds__(kFewThreads * H, 2) void few_kernel(Args p) {
     constexpr int N = 64 * R, kRows = 16 * C, kW = N * kStepBytes, kX = kRows * 512, kS = N * 16, kStage = kW + kX + kS;
     using B = Rows<N, kFewThreads>;
     constexpr int kXLoads = kX / (kFewThreads * kChunk);
-    __shared__ __attribute__((aligned(1024))) char lds[2 * kStage];
-    const int tid = threadIdx.x, lane = tid % kLanes, g = lane / 16, l16 = lane % 16;
+    __shared__ __attribute__((aligned(1024))) char lds_of[H][2 * kStage];
+    static_assert((H - 1) * kFewThreads * R * C * sizeof(f32x4) <= sizeof(lds_of), "the other part's sums");
+    const int part = H > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / kFewThreads) : 0;   // of the contraction's stages, every H-th
+    const int tid = threadIdx.x % kFewThreads, lane = tid % kLanes, g = lane / 16, l16 = lane % 16;
     const int wave = __builtin_amdgcn_readfirstlane(tid / kLanes);
-    const Groups all = groups_of(p, kRows, lane);
+    char* lds = lds_of[part];
+    const Offsets offsets = offsets_of(p, lane);
+    const Groups all = groups_of(p, offsets, kRows, lane);
     const Work work = work_of<false>(blockIdx.x, gridDim.x, all.tiles, p.tiles_n);
-    if (!work.tile) return clear_rows(p, all, work, tid, kFewThreads);
+    if (!work.tile) return clear_rows(p, all, work, threadIdx.x, kFewThreads * H);
     const int64_t n0 = work.n * N;
-    const Place t = place_of(p, work.index, kRows, lane);
+    const Place t = place_of(p, offsets, work.index, kRows, lane);
 
     const float S = p.S[t.expert];
     const int64_t q_ld = p.k / 2, w_row = t.expert * p.n + n0, q_left = (p.n - n0) * q_ld, x_bytes = p.k * 2;
@@ -243,8 +256,9 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_kernel(Args p) {
         x_at[i] = row < t.left ? (uint32_t)row * (uint32_t)p.ld + (x_chunk ^ place(row)) * kChunk : kOutside;
     }
     i32x2 scales[2];
-    auto fetch = [&](int s, auto dc) {
+    auto fetch = [&](int turn, auto dc) {
         constexpr int d = decltype(dc)::value;
+        const int s = turn * H + part;
         char* to = lds + d * kStage;
         // A row's last chunk may hold the next row's first values, finite numbers: they meet zeros.
         const int64_t done = (int64_t)s * kStepBytes, x_done = (int64_t)s * 512, q_ahead = q_ld - done, x_ahead = x_bytes - x_done;
@@ -309,7 +323,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_kernel(Args p) {
             }
         }
     };
-    const int stages = (int)((p.k + 255) / 256);
+    const int turns = (int)((p.k + 256 * H - 1) / (256 * H));   // past the last stage: zeros
     auto stage = [&](int s, auto dc) {
         constexpr int d = decltype(dc)::value;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -319,11 +333,25 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_kernel(Args p) {
         compute(dc);
     };
     fetch(0, Const<0>{});
-    for (int s = 0; s < stages; s += 2) {
+    for (int s = 0; s < turns; s += 2) {
         stage(s, Const<0>{});
-        if (s + 1 < stages) stage(s + 1, Const<1>{});
+        if (s + 1 < turns) stage(s + 1, Const<1>{});
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // no load into LDS outlives the workgroup
+    if constexpr (H > 1) {
+        __syncthreads();
+        f32x4* sums = reinterpret_cast<f32x4*>(lds_of[0]);
+        if (part > 0) {
+#pragma unroll
+            for (int f = 0; f < R * C; ++f) sums[((part - 1) * R * C + f) * kFewThreads + tid] = acc[f / C][f % C];
+        }
+        __syncthreads();
+        if (part > 0) return;
+#pragma unroll
+        for (int o = 0; o < H - 1; ++o)
+#pragma unroll
+            for (int f = 0; f < R * C; ++f) acc[f / C][f % C] += sums[(o * R * C + f) * kFewThreads + tid];
+    }
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
@@ -767,11 +795,12 @@ template <class T, bool TURNED>
 __global__ __launch_bounds__(T::kThreads, 2) void grouped_kernel(Args p) {
     __shared__ __attribute__((aligned(1024))) char lds[TURNED ? kSteps * T::kStage : T::kLds];
     const int tid = threadIdx.x;
-    const Groups all = groups_of(p, T::M, tid % kLanes);
+    const Offsets offsets = offsets_of(p, tid % kLanes);
+    const Groups all = groups_of(p, offsets, T::M, tid % kLanes);
     const Work work = work_of<T::kSplit>(blockIdx.x, gridDim.x, all.tiles, p.tiles_n);
     if (!work.tile) return clear_rows(p, all, work, tid, T::kThreads);
     const int64_t n0 = work.n * T::N;
-    Place t = place_of(p, work.index, T::M, tid % kLanes);
+    Place t = place_of(p, offsets, work.index, T::M, tid % kLanes);
     if constexpr (T::kSplit) {
         const int64_t height = T::M / work.parts;
         t.first += work.part * height, t.left -= work.part * height;
