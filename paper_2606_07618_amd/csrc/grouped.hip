@@ -10,21 +10,25 @@ using grouped_product::kFewThreads;
 constexpr int64_t kMostGroupedRows = 0x7FFFFFFF, kMostExperts = (int64_t)1 << 20;
 
 // Which kernel, by the rows that a group has on average (how many each has is known on the device alone; every kernel takes
-// any number).  Few rows: 16 or 32 of a group at a time, and 128 weight rows a workgroup, or 64 where those would be few.
-// Measured: 777 rows over 16 groups, 49 each, [1001, 2080]: 25 us in 32s, 37 in tiles.  The largest tile where groups fill it
-// more than half and three quarters of the compute units have one.
+// any number).  Few rows: 16 or 32 of a group at a time, and 128 weight rows a workgroup, or 64 where those would be few; up to
+// 64 where tiles would keep less than half of the chip busy.  Measured, 50 rows a group: eight of [4096, 14336] 123 us in 32s,
+// 144 in tiles; 16 of [1001, 2080] 25 and 37; 128 of [1536, 4096] 213 and 185.  The largest tile where groups fill it more than
+// half and three quarters of the compute units have one (128 of 200 rows: 345 us, 454 in the smaller one).
 struct GroupedPlan { int height, width, threads; };
+
+// Fours of waves along the contraction, of 16 rows where workgroups are few.
+constexpr int kFewFours = 2;
 
 using Large = grouped_product::Tile<256, 4>;
 using Small = grouped_product::Tile<128, 2>;
 
 GroupedPlan plan_grouped(int64_t rows, int64_t experts, int64_t outer, bool turned) {
     const int64_t active = rows < experts ? rows : experts, each = active ? ceil_div(rows, active) : 0;
-    if (!turned && each <= 64) {
+    if (!turned && (each <= 32 || (each <= 64 && active * ceil_div(outer, Small::N) < 512))) {
         const int height = each <= 16 ? 16 : 32;
         const int64_t tiles = active * ceil_div(each, height);
         const int width = tiles * ceil_div(outer, 128) >= 512 ? 128 : 64;
-        return {height, width, kFewThreads};
+        return {height, width, kFewThreads * (height == 16 && width == 64 ? kFewFours : 1)};
     }
     if (each > 128 && active * ceil_div(each, 256) * ceil_div(outer, 256) >= 192) return {Large::M, Large::N, Large::kThreads};
     return {Small::M, Small::N, Small::kThreads};
@@ -68,7 +72,7 @@ int run_grouped(grouped_product::Args p, bool turned, int block, hipStream_t str
     const dim3 grid((unsigned)most_groups_of(p.rows, p.experts, p.outer, plan));
     if (plan.threads == Large::kThreads && plan.height == Large::M) launch_tiled<Large>(p, turned, grid, stream);
     else if (plan.height == Small::M) launch_tiled<Small>(p, turned, grid, stream);
-    else if (plan.height == 16) plan.width == 128 ? launch_few<2, 1, 1>(p, grid, stream) : launch_few<1, 1, 2>(p, grid, stream);
+    else if (plan.height == 16) plan.width == 128 ? launch_few<2, 1, 1>(p, grid, stream) : launch_few<1, 1, kFewFours>(p, grid, stream);
     else plan.width == 128 ? launch_few<2, 2, 1>(p, grid, stream) : launch_few<1, 2, 1>(p, grid, stream);
     return launched();
 }

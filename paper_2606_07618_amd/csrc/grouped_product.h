@@ -490,8 +490,9 @@ __device__ __forceinline__ void finish(const Args& p, const Place& t, int64_t n0
 // expanding, twice as often so, fits between the matrix instructions.)
 template <class T, int MF>
 __device__ __forceinline__ void product_raw(const Args& p, const Place& t, int64_t n0, char* lds, int tid) {
-    constexpr int NF = 4, kRows = MF * 32, kA = T::M * kStepBytes, kB = T::N * kStepBytes, kS = T::N * 16;
-    constexpr int kB0 = 2 * kA, kS0 = kB0 + 2 * kB;        // of LDS: rows, weights, scales, two of each
+    constexpr int NF = 4, kRows = MF * 32, kA = kRows * kStepBytes, kB = T::N * kStepBytes, kS = T::N * 16;
+    constexpr int kB0 = 2 * T::M * kStepBytes, kS0 = kB0 + 2 * kB;     // of LDS: rows, weights, scales, two of each
+    constexpr int kSlots = MF < T::kMost ? 4 : 2;          // of rows: fewer of them, whose steps are short, further ahead
     using A = Rows<kRows, T::kThreads>;
     using B = Side<T::N, T::kThreads, false>;              // 256 values in 128 bytes
     static_assert(B::kLoads == 4 && T::kThreads == 2 * T::N, "the loads' order");
@@ -577,20 +578,27 @@ __device__ __forceinline__ void product_raw(const Args& p, const Place& t, int64
     };
     auto in_order = [] { asm volatile("" ::: "memory"); };   // the waits count on it
     auto group = [&](int s, int slot, auto uc, auto gc) {
-        constexpr int U = decltype(uc)::value, g = decltype(gc)::value, H = g / MF, i = g % MF, ahead = g + kLead, d = U % 2;
+        constexpr int U = decltype(uc)::value, g = decltype(gc)::value, H = g / MF, i = g % MF, ahead = g + kLead, d = U % 2, a = U % kSlots, next_a = (U + 1) % kSlots;
         constexpr bool first = ahead == kGroups;       // the first group whose reads ahead are the next step's
         constexpr int kFetch = MF == 8 ? 2 : 0, kRead = MF == 8 ? 4 : MF == 4 ? 2 : 1;
         constexpr int kPer = MF == 8 ? 1 : MF == 4 ? 2 : 4;    // halves of fragments, a group
         if constexpr (first) {
-            // what may still be on its way: loads of weights and scales begun behind the next step's rows
-            arrive<U == 0 ? 3 : U == 1 ? 2 : 0>();
-            fetch_a(s + 2, d);
+            // what may still be on its way: loads begun behind the next step's rows, and in a group's third step none of the
+            // next group's weights, which the fourth one reads (of scales, one load at least)
+            constexpr int kLater = (kSlots - 2) * A::kLoads, kWeights = U == 3 ? 3 : U == 0 ? (kSlots > 2 ? 5 : 2) : U == 1 && kSlots > 2 ? 5 : 0;
+            arrive<kLater + kWeights>();
+            fetch_a(s + kSlots, a);
         }
-        read_a(Const<ahead % kGroups>{}, ahead < kGroups ? at.a ^ (d * kA) : at.a ^ ((1 - d) * kA));
-        if constexpr (U < 2 && g == kFetch) {
+        read_a(Const<ahead % kGroups>{}, ahead < kGroups ? at.a ^ (a * kA) : at.a ^ (next_a * kA));
+        if constexpr ((U == 3 || U == 0) && g == kFetch) {
+            // half of the weights two groups on, where this group's are read; the other half a step later
             in_order();
-            fetch_q(s / 4 + 1, 1 - slot, Const<U>{});
-            if constexpr (U == 0) scales = scales_of.load(s / 4 + 1);
+            if constexpr (U == 3) {
+                fetch_q(s / 4 + 2, slot, Const<0>{});
+                scales = scales_of.load(s / 4 + 2);
+            } else {
+                fetch_q(s / 4 + 1, 1 - slot, Const<1>{});
+            }
             in_order();
         }
         if constexpr (U == 2 && g == kFetch) put_s(scales, 1 - slot);
@@ -609,7 +617,7 @@ __device__ __forceinline__ void product_raw(const Args& p, const Place& t, int64
             acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fb[H][j]), __builtin_bit_cast(bf16x8, fa[g % kRing]),
                                                                 acc[i][j], 0, 0, 0);
         // the order of a group: what else it does among its matrix instructions
-        constexpr int kReads = 1 + (g == kRead ? 2 * NF : 0), kStarts = first ? A::kLoads : U < 2 && g == kFetch ? 3 : 0;
+        constexpr int kReads = 1 + (g == kRead ? 2 * NF : 0), kStarts = first ? A::kLoads : (U == 3 || U == 0) && g == kFetch ? 3 : 0;
 #pragma unroll
         for (int r = 0; r < NF; ++r) {
             __builtin_amdgcn_sched_group_barrier(0x100, (kReads + NF - 1) / NF, 0);                          // LDS reads
@@ -632,10 +640,13 @@ __device__ __forceinline__ void product_raw(const Args& p, const Place& t, int64
         scales = scales_of.load(0);
         fetch_q(0, 0, Const<0>{});
         fetch_q(0, 0, Const<1>{});
-        fetch_a(0, 0);
-        fetch_a(1, 1);
+#pragma unroll
+        for (int i = 0; i < kSlots; ++i) fetch_a(i, i);
         put_s(scales, 0);
         arrive<0>();
+        fetch_q(1, 1, Const<0>{});
+        scales = scales_of.load(1);
+        in_order();
         read_b(Const<0>{}, Const<0>{}, 0);
         scale_of(Const<0>{});
         auto whole = [&](auto jc) { expand(Const<0>{}, Const<0>{}, jc, Const<0>{}), expand(Const<0>{}, Const<0>{}, jc, Const<1>{}); };
