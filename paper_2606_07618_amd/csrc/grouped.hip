@@ -12,8 +12,8 @@ constexpr int64_t kMostGroupedRows = 0x7FFFFFFF, kMostExperts = (int64_t)1 << 20
 // Which kernel, by the rows that a group has on average (how many each has is known on the device alone; every kernel takes
 // any number).  Few rows: 16 or 32 of a group at a time, and 128 weight rows a workgroup, or 64 where those would be few; up to
 // 64 where tiles would keep less than half of the chip busy.  Measured, 50 rows a group: eight of [4096, 14336] 123 us in 32s,
-// 144 in tiles; 16 of [1001, 2080] 25 and 37; 128 of [1536, 4096] 213 and 185.  The largest tile where groups fill it more than
-// half and three quarters of the compute units have one (128 of 200 rows: 345 us, 454 in the smaller one).
+// 144 in tiles; 16 of [1001, 2080] 25 and 37; 128 of [1536, 4096] 213 and 161.  The largest tile where groups fill it more than
+// half and three quarters of the compute units have one (128 of 200 rows: 340 us, 454 in the smaller one).
 struct GroupedPlan { int height, width, threads; };
 
 // Fours of waves along the contraction, of 16 rows where workgroups are few.

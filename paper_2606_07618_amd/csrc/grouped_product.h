@@ -368,6 +368,8 @@ __global__ __launch_bounds__(kFewThreads * H, 2) void few_kernel(Args p) {
 // there too, as nibbles, and each wave expands what it multiplies.  Turned ones are expanded by the threads that load them,
 // once for a tile's rows, on their way into LDS, where they lie as bfloat16 rows along the contraction: turning costs nothing
 // there, as the pairs that share a register are put together from single values anyway.
+// 64 rows: each wave takes all of them against half as many weight rows, and so expands half as many, and the rows are four
+// steps ahead (6400 rows, 128 groups, [1536, 4096]: 161 us, 185 without either).
 //   16384 rows, eight groups, [14336, 4096]: 1.55 ms (1.24 PFLOP/s; the clock is held at 1.5 to 1.6 GHz by the power limit,
 //   and the matrix instructions are busy two thirds of a compute unit's time); turned, 8192 rows: 0.95 ms (1.01 PFLOP/s).
 constexpr int kSteps = 2;                        // in LDS
@@ -434,12 +436,12 @@ struct Turned {
 };
 
 // The sums of a tile, times the global scale, to the rows that there are.  All waves are done with LDS' contents.
-template <class T, int MF>
-__device__ __forceinline__ void finish(const Args& p, const Place& t, int64_t n0, char* lds, int tid, const f32x4 (&acc)[MF][4]) {
-    constexpr int NF = 4, kRows = MF * 32;
-    const int lane = tid % kLanes, wave = __builtin_amdgcn_readfirstlane(tid / kLanes), wm = wave / T::WN, wn = wave % T::WN;
+template <class T, int MF, int NF>
+__device__ __forceinline__ void finish(const Args& p, const Place& t, int64_t n0, char* lds, int tid, const f32x4 (&acc)[MF][NF]) {
+    constexpr int WN = T::N / (NF * 16), kRows = MF * 16 * (T::kThreads / kLanes / WN);
+    const int lane = tid % kLanes, wave = __builtin_amdgcn_readfirstlane(tid / kLanes), wm = wave / WN, wn = wave % WN;
     auto a_row = [&](int i) { return wm * (MF * 16) + i * 16; };
-    auto b_row = [&](int j) { return wn * 64 + j * 16; };
+    auto b_row = [&](int j) { return (wn * NF + j) * 16; };
     const float S = p.S[t.expert];
     if (!p.out_f32 && p.outer % 8 == 0) {
         // through LDS, as whole rows of the tile
@@ -482,21 +484,21 @@ __device__ __forceinline__ void finish(const Args& p, const Place& t, int64_t n0
     }
 }
 
-// The product of one tile with weights as they lie, MF fragments of 16 rows a wave.
+// The product of one tile with weights as they lie, MF fragments of 16 rows by NF of 16 weight rows a wave.
 //
 // Weights go into LDS as they are, 256 values of each row (whole lines) at a time, and from there into the registers of
 // each wave, which expands the fragments that it multiplies, once for its 16 MF rows.  (Expanded once for the whole tile,
 // as turned ones are, each weight is written to LDS, four times as wide: those stores took 0.45 of a step's 1.6 us, and
 // expanding, twice as often so, fits between the matrix instructions.)
-template <class T, int MF>
+template <class T, int MF, int NF>
 __device__ __forceinline__ void product_raw(const Args& p, const Place& t, int64_t n0, char* lds, int tid) {
-    constexpr int NF = 4, kRows = MF * 32, kA = kRows * kStepBytes, kB = T::N * kStepBytes, kS = T::N * 16;
+    constexpr int WN = T::N / (NF * 16), kRows = MF * 16 * (T::kThreads / kLanes / WN), kA = kRows * kStepBytes, kB = T::N * kStepBytes, kS = T::N * 16;
     constexpr int kB0 = 2 * T::M * kStepBytes, kS0 = kB0 + 2 * kB;     // of LDS: rows, weights, scales, two of each
-    constexpr int kSlots = MF < T::kMost ? 4 : 2;          // of rows: fewer of them, whose steps are short, further ahead
+    constexpr int kSlots = kRows < T::M ? 4 : 2;            // of rows: fewer of them, whose steps are short, further ahead
     using A = Rows<kRows, T::kThreads>;
     using B = Side<T::N, T::kThreads, false>;              // 256 values in 128 bytes
     static_assert(B::kLoads == 4 && T::kThreads == 2 * T::N, "the loads' order");
-    const int lane = tid % kLanes, wave = __builtin_amdgcn_readfirstlane(tid / kLanes), wm = wave / T::WN, wn = wave % T::WN;
+    const int lane = tid % kLanes, wave = __builtin_amdgcn_readfirstlane(tid / kLanes), wm = wave / WN, wn = wave % WN;
     A sa;
     B sb;
     sa.init(t.left, p.ld, tid);
@@ -539,13 +541,14 @@ __device__ __forceinline__ void product_raw(const Args& p, const Place& t, int64
         uint32_t a, b, c;
         __device__ __forceinline__ void remake() { asm volatile("" : "+v"(a), "+v"(b), "+v"(c)); }
     } at = {(uint32_t)((wm * (MF * 16) + l16) * kStepBytes + ((2 * g4) ^ A::exchange(l16)) * kChunk),
-            (uint32_t)(kB0 + (wn * 64 + l16) * kStepBytes + ((g4 / 2) ^ B::exchange(l16)) * kChunk + g4 % 2 * 8),
-            (uint32_t)(kS0 + (wn * 64 + l16) * 16)};
+            (uint32_t)(kB0 + (wn * (NF * 16) + l16) * kStepBytes + ((g4 / 2) ^ B::exchange(l16)) * kChunk + g4 % 2 * 8),
+            (uint32_t)(kS0 + (wn * (NF * 16) + l16) * 16)};
     const int down = p.shift - 4;
 
     // A step is 2 MF groups of NF matrix instructions.  While one half's are multiplied the other half's weights are
     // expanded: this step's second half, then the next step's first.
-    constexpr int kLead = MF >= 8 ? 3 : MF >= 4 ? 2 : 1, kRing = 4, kGroups = 2 * MF;
+    constexpr int kParts = 2 * NF / MF;                    // halves of fragments that a group expands
+    constexpr int kLead = MF >= 8 ? 3 : 2, kRing = 4, kGroups = 2 * MF;
     const int steps = (int)((p.k + 63) / 64);
     i32x4 fa[kRing], fb[2][NF];
     i32x2 raw[2][NF], scales = {0, 0};
@@ -580,8 +583,8 @@ __device__ __forceinline__ void product_raw(const Args& p, const Place& t, int64
     auto group = [&](int s, int slot, auto uc, auto gc) {
         constexpr int U = decltype(uc)::value, g = decltype(gc)::value, H = g / MF, i = g % MF, ahead = g + kLead, d = U % 2, a = U % kSlots, next_a = (U + 1) % kSlots;
         constexpr bool first = ahead == kGroups;       // the first group whose reads ahead are the next step's
-        constexpr int kFetch = MF == 8 ? 2 : 0, kRead = MF == 8 ? 4 : MF == 4 ? 2 : 1;
-        constexpr int kPer = MF == 8 ? 1 : MF == 4 ? 2 : 4;    // halves of fragments, a group
+        constexpr int kFetch = MF == 8 ? 2 : 0, kRead = MF == 8 ? 4 : 2;
+        constexpr int kPer = kParts;
         if constexpr (first) {
             // what may still be on its way: loads begun behind the next step's rows, and in a group's third step none of the
             // next group's weights, which the fourth one reads (of scales, one load at least)
@@ -605,13 +608,12 @@ __device__ __forceinline__ void product_raw(const Args& p, const Place& t, int64
         if constexpr (g == kRead) read_b(Const<1 - d>{}, Const<(U + 1) % 4>{}, U == 3 ? 1 - slot : slot);
         if constexpr (g == MF) scale_of(Const<1 - d>{});
         auto part = [&](auto ec) {
-            constexpr int e = g % MF * kPer + decltype(ec)::value;     // of the half's eight
+            constexpr int e = g % MF * kPer + decltype(ec)::value;     // of the half's 2 NF
             if constexpr (H == 0) expand(Const<d>{}, Const<1>{}, Const<e / 2>{}, Const<e % 2>{});
             else expand(Const<1 - d>{}, Const<0>{}, Const<e / 2>{}, Const<e % 2>{});
         };
         part(Const<0>{});
         if constexpr (kPer >= 2) part(Const<1>{});
-        if constexpr (kPer >= 4) part(Const<2>{}), part(Const<3>{});
 #pragma unroll
         for (int j = 0; j < NF; ++j)
             acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fb[H][j]), __builtin_bit_cast(bf16x8, fa[g % kRing]),
@@ -626,10 +628,10 @@ __device__ __forceinline__ void product_raw(const Args& p, const Place& t, int64
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                                               // matrix instructions
         }
     };
-    static_assert(MF == 2 || MF == 4 || MF == 8, "groups of a step");
+    static_assert((MF == 4 || MF == 8) && (kParts == 1 || kParts == 2), "groups of a step");
     auto step = [&](int s, int slot, auto uc) {
         group(s, slot, uc, Const<0>{}), group(s, slot, uc, Const<1>{}), group(s, slot, uc, Const<2>{}), group(s, slot, uc, Const<3>{});
-        if constexpr (MF >= 4) group(s, slot, uc, Const<4>{}), group(s, slot, uc, Const<5>{}), group(s, slot, uc, Const<6>{}), group(s, slot, uc, Const<7>{});
+        group(s, slot, uc, Const<4>{}), group(s, slot, uc, Const<5>{}), group(s, slot, uc, Const<6>{}), group(s, slot, uc, Const<7>{});
         if constexpr (MF >= 8) {
             group(s, slot, uc, Const<8>{}), group(s, slot, uc, Const<9>{}), group(s, slot, uc, Const<10>{}), group(s, slot, uc, Const<11>{});
             group(s, slot, uc, Const<12>{}), group(s, slot, uc, Const<13>{}), group(s, slot, uc, Const<14>{}), group(s, slot, uc, Const<15>{});
@@ -650,9 +652,9 @@ __device__ __forceinline__ void product_raw(const Args& p, const Place& t, int64
         read_b(Const<0>{}, Const<0>{}, 0);
         scale_of(Const<0>{});
         auto whole = [&](auto jc) { expand(Const<0>{}, Const<0>{}, jc, Const<0>{}), expand(Const<0>{}, Const<0>{}, jc, Const<1>{}); };
-        whole(Const<0>{}), whole(Const<1>{}), whole(Const<2>{}), whole(Const<3>{});
-        read_a(Const<0>{}, at.a);
-        if constexpr (kLead > 1) read_a(Const<1>{}, at.a);
+        whole(Const<0>{}), whole(Const<1>{});
+        if constexpr (NF > 2) whole(Const<2>{}), whole(Const<3>{});
+        read_a(Const<0>{}, at.a), read_a(Const<1>{}, at.a);
         if constexpr (kLead > 2) read_a(Const<2>{}, at.a);
         int slot = 0;
         for (int s = 0; s < steps; s += 4, slot = 1 - slot) {
@@ -663,7 +665,7 @@ __device__ __forceinline__ void product_raw(const Args& p, const Place& t, int64
         }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // no load into LDS outlives the workgroup
-    finish<T, MF>(p, t, n0, lds, tid, acc);
+    finish<T, MF, NF>(p, t, n0, lds, tid, acc);
 }
 
 // The product of one tile with turned weights.
@@ -799,7 +801,7 @@ __device__ __forceinline__ void product_turned(const Args& p, const Place& t, in
         }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // no load into LDS outlives the workgroup
-    finish<T, MF>(p, t, n0, lds, tid, acc);
+    finish<T, MF, NF>(p, t, n0, lds, tid, acc);
 }
 
 template <class T, bool TURNED>
@@ -819,9 +821,11 @@ __global__ __launch_bounds__(T::kThreads, 2) void grouped_kernel(Args p) {
         if (work.parts > 1 && t.left > height) t.left = height;
     }
     auto product = [&](auto mc) {
-        constexpr int MF = decltype(mc)::value;
+        constexpr int MF = decltype(mc)::value;            // 32 MF rows
         if constexpr (TURNED) product_turned<T, MF>(p, t, n0, lds, tid);
-        else product_raw<T, MF>(p, t, n0, lds, tid);
+        // 64 rows: all of them and half as many weights a wave, which then expands half as many
+        else if constexpr (MF == 2) product_raw<T, 4, 2>(p, t, n0, lds, tid);
+        else product_raw<T, MF, 4>(p, t, n0, lds, tid);
     };
     if (t.left <= 64) return product(Const<2>{});
     if constexpr (T::kMost > 4) if (t.left <= 128) return product(Const<4>{});
