@@ -509,7 +509,8 @@ __device__ __forceinline__ void product_raw(const Args& p, const Place& t, int64
     auto fetch_a = [&](int s, int slot) {
         sa.load(a0 + (int64_t)s * kStepBytes, lds + slot * kA, row_bytes - (int64_t)s * kStepBytes, wave);
     };
-    // Half of a group's weights.  A row's last chunk may hold the next row's first values, finite numbers: they meet zeros.
+    // Half of a group's weights.  A row's last chunk may hold the next row's first values, finite numbers, which meet zeros;
+    // behind the last row the window ends, and each word past it is zero.
     auto fetch_q = [&](int group, int slot, auto hc) {
         constexpr int H = decltype(hc)::value;
         const int64_t done = (int64_t)group * kStepBytes, ahead = q_ld - done;

@@ -406,3 +406,40 @@ def test_last_weights_at_the_end_of_their_storage(nv, each):
         view = big[:q.numel()].view(q.shape)
         view.copy_(q)
         plain64.check(nv.grouped_matmul(x, offsets, view, sc, S), want, lim, "y")
+
+
+@pytest.mark.parametrize("k", [16, 64, 80, 128, 144, 192, 256, 272, 320, 384, 448, 512, 528, 576, 784, 848])
+@pytest.mark.parametrize("sizes", [[70, 64, 128, 200], [100, 1, 400, 65]])
+def test_every_turn_of_the_pipeline(nv, sizes, k):
+    """Contractions that end in every step of a group of four and of two, tiles of 64 and of 128 rows."""
+    both(nv, sizes, 136, k, 16, torch.bfloat16, 21)
+
+
+@pytest.mark.parametrize("inner", [16, 64, 144, 192, 272, 320, 448, 512])
+def test_every_turn_of_the_largest_tiles(nv, inner):
+    """The same for 64, 128 and 256 rows of the largest tile, by its first and last columns."""
+    g = gen(22, inner)
+    sizes, outer = [300, 600, 513, 130, 380, 256], 8192
+    offsets = offsets_of(sizes)
+    x = rand((sum(sizes), inner), g)
+    for turned, f in ((False, nv.grouped_matmul), (True, nv.grouped_matmul_grad_input)):
+        n, k = (inner, outer) if turned else (outer, inner)
+        w = weights(len(sizes), n, k, 16, g)
+        got = f(x, offsets, *w)
+        for cut in (slice(0, 512), slice(outer - 512, outer)):
+            part = (w[0][:, :, cut.start // 2:cut.stop // 2], w[1][:, :, cut.start // 16:cut.stop // 16], w[2]) if turned else \
+                (w[0][:, cut], w[1][:, cut], w[2])
+            want, lim = expected(x, spans(offsets), tuple(t.contiguous() for t in part), 16, turned)
+            plain64.check(got[:, cut].contiguous(), want, lim, "y")
+
+
+@pytest.mark.parametrize("k", [16, 256, 272, 512, 528, 768, 1024, 1040, 1280])
+def test_every_turn_of_few_rows(nv, k):
+    """Contractions of an odd and an even number of stages, shared by two fours of waves or not."""
+    for n, sizes in ((48, [3, 0, 16]), (2056, [9, 12] * 16), (40, [30, 25])):
+        g = gen(23, n, k)
+        w = weights(len(sizes), n, k, 16, g)
+        offsets = offsets_of(sizes)
+        x = rand((sum(sizes), k), g)
+        want, lim = expected(x, spans(offsets), w, 16, False)
+        plain64.check(nv.grouped_matmul(x, offsets, *w, out_dtype=torch.float32), want, lim, "y")
