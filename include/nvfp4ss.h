@@ -443,7 +443,8 @@ int int8_matmul(const int8_t* a_q, const float* a_scales, const int8_t* b_q, con
                 int64_t k, int out_dtype, void* out, void* workspace, size_t workspace_bytes, void* stream);
 
 /* dx = dy B of bfloat16 dy [m, n] (any ld >= n) and B [n, k]: the gradient of the product above with respect to A,
- * straight through A's quantization.  The weights s q are rounded to bfloat16 as operands. */
+ * straight through A's quantization.  For a bfloat16 dx the weights RN32(s q) are rounded to bfloat16 as operands; for a
+ * binary32 one they enter as they are (from 2^-109 on), in three products. */
 int64_t int8_matmul_grad_input_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t ld);
 int int8_matmul_grad_input(const void* dy, int64_t ld, const int8_t* q, const float* scales, int64_t m, int64_t n, int64_t k,
                            int out_dtype, void* dx, void* workspace, size_t workspace_bytes, void* stream);

@@ -312,11 +312,26 @@ int run_int8(const int8_t* a, const float* a_scales, const int8_t* b, const floa
 }
 
 // ---- the gradient with respect to the rows ------------------------------------------------------
-// The scales run along the contraction here, so the weights are expanded to bfloat16, rows turned: s q has up to 31
-// significant bits and is rounded to 8, which takes a gradient's relative error from 0.0017, its own rounding to bfloat16,
-// to 0.0024 (two products on two bfloat16 numbers a weight would take twice the time).
+// The scales run along the contraction here, so the weights are expanded to bfloat16, rows turned.  s q has up to 31
+// significant bits.  For a bfloat16 gradient it is rounded to 8, which takes the gradient's relative error from 0.0017, its
+// own rounding, to 0.0024 (whole weights would take three times the time).  A binary32 gradient is for those who need more:
+// binary32's s q is three bfloat16 numbers, each the upper half of what those before it leave (exact from 2^-109 on), and
+// three products, one on top of the other, through one buffer of weights.
+enum Term { kRounded, kFirst, kSecond, kThird };
+
+template <Term TERM>
+__device__ __forceinline__ float term_of(float w) {
+    const auto upper = [](float v) { return __uint_as_float(__float_as_uint(v) & 0xFFFF0000u); };
+    if constexpr (TERM == kRounded) return w;                 // by the conversion
+    const float first = upper(w);
+    if constexpr (TERM == kFirst) return first;
+    const float rest = fabsf(w) < __builtin_inff() ? w - first : 0.0f, second = upper(rest);
+    return TERM == kSecond ? second : rest - second;
+}
+
 constexpr int kTurnThreads = 256, kTurnN = 64, kTurnK = 128;
 
+template <Term TERM>
 __global__ __launch_bounds__(kTurnThreads) void int8_turned_kernel(const int8_t* __restrict__ q, const float* __restrict__ scales,
                                                                    int64_t n, uint32_t k, uint32_t tiles_k, int64_t ld,
                                                                    uint16_t* __restrict__ out) {
@@ -339,7 +354,7 @@ __global__ __launch_bounds__(kTurnThreads) void int8_turned_kernel(const int8_t*
 #pragma unroll
         for (int j = 0; j < 16; j += 2) {
             const int a = (int)(int8_t)(w[p][j / 4] >> j % 4 * 8), b = (int)(int8_t)(w[p][j / 4] >> (j % 4 + 1) * 8);
-            const uint32_t v = pack_bf16((float)a * s, (float)b * s);
+            const uint32_t v = pack_bf16(term_of<TERM>((float)a * s), term_of<TERM>((float)b * s));
             reinterpret_cast<uint16_t*>(tile[p * 64 + part * 16 + j])[row] = (uint16_t)v;
             reinterpret_cast<uint16_t*>(tile[p * 64 + part * 16 + j + 1])[row] = (uint16_t)(v >> 16);
         }
@@ -362,16 +377,22 @@ int64_t int8_grad_workspace(int64_t m, int64_t n, int64_t k, int64_t ld) {
     return c.at + parts_bytes<kBf16>(m, k, n);
 }
 
-int run_int8_grad(const void* dy, int64_t ld, const int8_t* q, const float* scales, int64_t m, int64_t n, int64_t k, int out_dtype,
-                  void* out, void* ws, hipStream_t stream) {
-    Carver c{static_cast<char*>(ws)};
+// One product on a term of the weights, which `w` holds until it is done.
+template <Term TERM, Out OUT>
+int grad_product(const int8_t* q, const float* scales, int64_t n, int64_t k, void* w, const Args& p, float* partial, hipStream_t stream) {
     const int64_t row = up(k, kRowUnit);
-    void* w = c.take(row * packed_ld(n) * 2);
     if (n > 0) {
-        hipLaunchKernelGGL(int8_turned_kernel, dim3((unsigned)turned_groups(n, k)), dim3(kTurnThreads), 0, stream, q, scales, n,
+        hipLaunchKernelGGL((int8_turned_kernel<TERM>), dim3((unsigned)turned_groups(n, k)), dim3(kTurnThreads), 0, stream, q, scales, n,
                            (uint32_t)row, (uint32_t)ceil_div(row, kTurnK), packed_ld(n), static_cast<uint16_t*>(w));
         if (const int rc = launched()) return rc;
     }
+    return run_sums<kBf16, OUT>(p, partial, stream);
+}
+
+int run_int8_grad(const void* dy, int64_t ld, const int8_t* q, const float* scales, int64_t m, int64_t n, int64_t k, int out_dtype,
+                  void* out, void* ws, hipStream_t stream) {
+    Carver c{static_cast<char*>(ws)};
+    void* w = c.take(up(k, kRowUnit) * packed_ld(n) * 2);
     if (needs_pack(n, ld)) {
         void* packed = c.take(m * packed_ld(n) * 2);
         if (const int rc = pack_bf16_rows(dy, m, n, ld, packed, stream)) return rc;
@@ -381,7 +402,11 @@ int run_int8_grad(const void* dy, int64_t ld, const int8_t* q, const float* scal
     p.a.p = static_cast<const char*>(dy), p.a.ld = ld * 2;
     p.b.p = static_cast<const char*>(w), p.b.ld = packed_ld(n) * 2;
     p.m = m, p.n = k, p.inner = n, p.out = out, p.out_ld = k, p.out_f32 = out_dtype == NVFP4_IN_F32;
-    return run_sums<kBf16>(p, static_cast<float*>(c.take(0)), stream);
+    float* partial = static_cast<float*>(c.take(0));
+    if (!p.out_f32) return grad_product<kRounded, kSums>(q, scales, n, k, w, p, partial, stream);
+    if (const int rc = grad_product<kFirst, kSums>(q, scales, n, k, w, p, partial, stream)) return rc;
+    if (const int rc = grad_product<kSecond, kAdded>(q, scales, n, k, w, p, partial, stream)) return rc;
+    return grad_product<kThird, kAdded>(q, scales, n, k, w, p, partial, stream);
 }
 
 int check_int8(int64_t m, int64_t n, int64_t k) {

@@ -24,7 +24,7 @@ __global__ __launch_bounds__(kPackThreads) void pack_kernel(const uint16_t* __re
 template <bool VEC>
 __global__ __launch_bounds__(kJoinThreads) void join_kernel(const float* __restrict__ part, int parts, int64_t count,
                                                             const float* __restrict__ scale, void* __restrict__ out,
-                                                            int f32, int64_t first, void* __restrict__ out2) {
+                                                            int f32, int64_t first, void* __restrict__ out2, int add) {
     constexpr int kPer = VEC ? 4 : 1;
     const int64_t at = ((int64_t)blockIdx.x * kJoinThreads + threadIdx.x) * kPer;
     if (at >= count) return;
@@ -41,6 +41,10 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(const float* __restr
     const float s = scale ? *scale : 1.0f;
     void* to = at < first ? out : out2;
     const int64_t place = at < first ? at : at - first;
+    if (add) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) v[i] += static_cast<const float*>(to)[place + i];
+    }
     if constexpr (VEC) store4(to, f32, place, 4, true, f32x4{v[0], v[1], v[2], v[3]} * s);
     else store4(to, f32, place, 1, false, f32x4{v[0] * s, 0.0f, 0.0f, 0.0f});
 }
@@ -56,12 +60,12 @@ int pack_bf16_rows(const void* src, int64_t rows, int64_t width, int64_t ld, voi
 }
 
 int join_parts(const float* part, int parts, int64_t count, const float* scale, void* out, int f32, int64_t first, void* out2,
-               hipStream_t stream) {
+               hipStream_t stream, bool add) {
     const bool vec = count % 4 == 0 && first % 4 == 0;
     const int64_t groups = ceil_div(vec ? count / 4 : count, kJoinThreads);
     if (!launchable(groups, kJoinThreads)) return NVFP4_ERR_SHAPE;
     hipLaunchKernelGGL((vec ? join_kernel<true> : join_kernel<false>), dim3((unsigned)groups), dim3(kJoinThreads), 0, stream,
-                       part, parts, count, scale, out, f32, first, out2);
+                       part, parts, count, scale, out, f32, first, out2, (int)add);
     return launched();
 }
 

@@ -87,11 +87,12 @@ int launch_product(const Args& p, int tile, hipStream_t stream) {
     }
 }
 
-// out = scale * (the parts' sums [parts, count], added in order); values from `first` on go to out2.
+// out = scale * (the parts' sums [parts, count], added in order); values from `first` on go to out2.  add: on top of
+// what a binary32 out holds.
 int join_parts(const float* part, int parts, int64_t count, const float* scale, void* out, int f32, int64_t first, void* out2,
-               hipStream_t stream);
+               hipStream_t stream, bool add = false);
 
-// A product whose sums are stored (kSums, kTwoRows): split where the plan says so, the parts' sums in `partial`.
+// A product whose sums are stored (kSums, kTwoRows, kAdded): split where the plan says so, the parts' sums in `partial`.
 template <Kind KIND, Out OUT = kSums>
 int run_sums(Args p, float* partial, hipStream_t stream) {
     const Plan plan = plan_product<KIND, OUT>(p.m, p.n, p.inner);
@@ -101,7 +102,7 @@ int run_sums(Args p, float* partial, hipStream_t stream) {
     p.out = partial;
     if (const int rc = launch_product<KIND, kPartial>(p, plan.tile, stream)) return rc;
     return join_parts(partial, plan.parts, p.m * p.n, p.scale, out, p.out_f32, OUT == kTwoRows ? p.half_rows * p.n : p.m * p.n,
-                      p.out2, stream);
+                      p.out2, stream, OUT == kAdded);
 }
 
 }  // namespace product_host

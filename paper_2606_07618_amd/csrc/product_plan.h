@@ -23,7 +23,8 @@ enum Out {
     kGate,        // B is two matrices: silu(sum of the first) * sum of the second, and both sums where asked for;
                   // a tile's outer indexes of B are taken half from each, so that an output's two sums meet in one lane
     kGatePartial, // both sums of this part of the contraction, [part][2][m][n] in binary32
-    kTwoRows      // rows below `half_rows` to the first output, those from there on to the second
+    kTwoRows,     // rows below `half_rows` to the first output, those from there on to the second
+    kAdded        // the sum on top of what the binary32 output holds
 };
 
 // ---- the tile and the split of a product --------------------------------------------------------

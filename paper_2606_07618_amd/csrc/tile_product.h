@@ -22,7 +22,7 @@ namespace tile_product {
 
 using product_plan::Kind, product_plan::kBf16, product_plan::kMx, product_plan::kMxLaid, product_plan::kInt8;
 using product_plan::Out, product_plan::kSums, product_plan::kPartial, product_plan::kGate, product_plan::kGatePartial,
-    product_plan::kTwoRows;
+    product_plan::kTwoRows, product_plan::kAdded;
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -461,7 +461,7 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
         else return __builtin_bit_cast(f32x4, acc[i][j]);
     };
     auto column = [&](int j) { return HALF ? wn * (kOutN / T::WN) + j * 16 : b_row(j); };
-    if (OUT != kPartial && OUT != kGatePartial && !p.out_f32 && p.out_ld % 8 == 0) {
+    if (OUT != kPartial && OUT != kGatePartial && OUT != kAdded && !p.out_f32 && p.out_ld % 8 == 0) {
         constexpr int kOutChunks = kOutN / 8, kMask = kOutChunks < 16 ? kOutChunks - 1 : 15;
         static_assert(T::M * kOutN * 2 <= kSlots * kStage, "the tile in LDS");
         char* tile = lds[0];
@@ -525,6 +525,11 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
             else v = acc[i][j];
             if constexpr (OUT == kSums) {
                 store4(p.out, p.out_f32, m * p.out_ld + n, left, vec, KIND == kInt8 ? v : v * scale);
+            } else if constexpr (OUT == kAdded) {
+                const float* held = static_cast<const float*>(p.out) + m * p.out_ld + n;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) if (e < left) v[e] += held[e];
+                store4(p.out, 1, m * p.out_ld + n, left, vec, v);
             } else if constexpr (OUT == kPartial) {
                 store4(p.out, 1, (part * p.m + m) * p.out_ld + n, left, vec, v);
             } else if constexpr (OUT == kGatePartial) {

@@ -385,8 +385,8 @@ def int8_matmul_grad_input(dy: torch.Tensor, q: torch.Tensor, scales: torch.Tens
                            out_dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None,
                            ws: torch.Tensor | None = None) -> torch.Tensor:
     """dx = dy B [m, cols] of a bfloat16 dy [m, n] and B [n, cols] in 8-bit integers: the gradient of int8_matmul's A
-    (straight through its quantization).  B's values are rounded to bfloat16 as operands.  cols: whole rows of q by
-    default."""
+    (straight through its quantization).  For a bfloat16 dx B's values are rounded to bfloat16 as operands; a float32 one
+    takes them whole, in three times the time.  cols: whole rows of q by default."""
     dt = _dtype_id(out_dtype, "out_dtype")
     ld = _rows(dy, "dy")
     m = dy.shape[0]
