@@ -437,7 +437,8 @@ int nvfp4_grouped_product_grad_input(const void* dy, int64_t ld, const int* offs
 int int8_quant(const void* x, int dtype, int64_t rows, int64_t cols, int64_t ldx, int8_t* q, float* scales, void* stream);
 
 /* y = A B^T of A [m, k] and B [n, k] quantized so: y[i][j] = s_a[i] s_b[j] sum q_a q_b, the sum exact (k < 2^17,
- * else NVFP4_ERR_SHAPE), then rounded to binary32, times the product of the scales, and to the output.  q may hold -128. */
+ * else NVFP4_ERR_SHAPE), then rounded to binary32, times the product of the scales, and to the output, as if binary32 had no
+ * smallest and no largest number before the last of these.  q may hold -128. */
 int64_t int8_matmul_workspace_bytes(int64_t m, int64_t n, int64_t k);
 int int8_matmul(const int8_t* a_q, const float* a_scales, const int8_t* b_q, const float* b_scales, int64_t m, int64_t n,
                 int64_t k, int out_dtype, void* out, void* workspace, size_t workspace_bytes, void* stream);

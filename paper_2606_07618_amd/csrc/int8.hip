@@ -230,7 +230,7 @@ __global__ __launch_bounds__(kDotWaves * kLanes) void int8_dot_kernel(DotArgs p)
     for (int a = 0; a < along; ++a) v += sums[of * along + a][m][r];
     const int64_t n = (int64_t)blockIdx.x * rows + of * kDotN + r;
     if (n >= p.n) return;
-    const float y = (float)v * (p.scale_n[n] * p.scale_m[m]);
+    const float y = scaled(v, p.scale_n[n], p.scale_m[m]);
     if (p.out_f32) static_cast<float*>(p.out)[m * p.n + n] = y;
     else static_cast<uint16_t*>(p.out)[m * p.n + n] = (uint16_t)pack_bf16(y, y);
 }
@@ -265,7 +265,7 @@ __global__ __launch_bounds__(kJoinThreads) void int8_join_kernel(const int* __re
     for (int i = 0; i < 4; ++i) {
         const int64_t c = first + i * kJoinThreads;
         if (c >= n) break;
-        const float y = (float)v[i] * (scale_n[c] * s);
+        const float y = scaled(v[i], scale_n[c], s);
         if (f32) static_cast<float*>(out)[row * n + c] = y;
         else static_cast<uint16_t*>(out)[row * n + c] = (uint16_t)pack_bf16(y, y);
     }
