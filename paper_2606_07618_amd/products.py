@@ -343,7 +343,11 @@ def int8_quantize(x: torch.Tensor, out=None):
     """8-bit integers of the rows of a bfloat16 or float32 device matrix [rows, cols] (rows may be strided):
     (q [rows, 16 ceil(cols / 16)] int8, zeros past the width, scales [rows] float32), x about q * scale with
     scale = max|x| / 127 of the row: a scale for each token of an activation, for each output channel of weights
-    [n, k].  See int8_quant."""
+    [n, k].  See int8_quant.  Integers carry no gradient, so an x that requires one is refused where autograd records:
+    pass x.detach(), or quantize in an autograd.Function whose backward is int8_matmul_grad_input (straight through)."""
+    if x.requires_grad and torch.is_grad_enabled():
+        raise ValueError("x requires a gradient, which its integers would not carry: pass x.detach(), or quantize in an "
+                         "autograd.Function whose backward is int8_matmul_grad_input")
     ldx = _rows(x, "x", (torch.bfloat16, torch.float32))
     rows, cols = x.shape
     q, sc = (None, None) if out is None else out
