@@ -48,7 +48,9 @@ inline const TileCost* tile_costs() {
                                             {64, 128, 5.1f, 0.64f, 1.4f, 0.48f}, {64, 64, 4.4f, 0.40f, 1.3f, 0.31f}};
     static constexpr TileCost bf16[kTiles] = {{256, 256, 9.8f, 1.05f, 8.5f, 1.54f}, {128, 128, 5.1f, 0.77f, 2.5f, 0.51f},
                                               {64, 128, 4.7f, 0.38f, 1.7f, 0.34f}, {64, 64, 3.7f, 0.31f, 1.3f, 0.23f}};
-    return kMicroscaled<KIND> ? mx : bf16;                   // kInt8: a step's bytes and instructions take what bfloat16's do
+    // kInt8: a step has as many bytes and takes as long in the matrix instructions as bfloat16's.  (No estimate counts how fast
+    // operands come from memory: [48, 8192] x [28672, 8192] in integers is estimated at 29 us and takes 56.)
+    return kMicroscaled<KIND> ? mx : bf16;
 }
 
 // Fragments of a wave's rows of A and of B.
@@ -73,8 +75,10 @@ float product_us(int t, int parts, int64_t m, int64_t n, int64_t inner) {
     const float many = load > 1.0f ? kLaunchUs + (float)(int64_t)(load + 0.999f) * (cost.fixed + own * cost.among) : 0.0f;
     float us = few > many ? few : many;
     if (kMicroscaled<KIND> && t == 0) us += kLayUs;
-    // kInt8: with steps of twice the values the parts' sums weigh more ([777, 14336] x [1001, 14336], quantized in the same
-    // call: 49 us in eight parts of the second tile, which bfloat16's cost of them chooses, 45 in two of the third)
+    // kInt8: a step's values are twice as many, so that parts are short and cost more than their sums' bytes; these are counted
+    // twice.  That changes one plan in forty (of 5 to 8192 rows, 64 to 28672 outputs, 64 to 14336 values); 54 such products
+    // timed both ways take 4 % less on average: 14 % where it takes fewer parts of a split ([777, 14336] x [1001, 14336]: 33 us in
+    // two parts of the third tile, 36 in eight of the second), but 4 % more where it takes a whole product in place of a split.
     constexpr int kBytes = KIND == kInt8 ? 16 : 8;
     if (parts > 1) us += kJoinUs + (float)m * (float)n * (float)(kBytes * kHalf<OUT> * parts) / kJoinBytesUs;
     return us;
