@@ -1,46 +1,21 @@
 // Products of grouped rows with NVFP4 weights of each group's own: the experts of a mixture, y = x W_e^T and dx = dy W_e.
+#include "grouped_plan.h"
 #include "grouped_product.h"
 #include "product_host.h"
 
 namespace {
 
 using namespace product_host;
-using grouped_product::kFewThreads;
+using grouped_plan::GroupedPlan, grouped_plan::plan_grouped, grouped_plan::most_groups_of;
+using grouped_plan::kLargeTile, grouped_plan::kLargeThreads, grouped_plan::kSmallTile, grouped_plan::kSmallThreads;
+using grouped_plan::kFewThreads, grouped_plan::kFewFours;
 
 constexpr int64_t kMostGroupedRows = 0x7FFFFFFF, kMostExperts = (int64_t)1 << 20;
 
-// Which kernel, by the rows that a group has on average (how many each has is known on the device alone; every kernel takes
-// any number).  Few rows: 16 or 32 of a group at a time, and 128 weight rows a workgroup, or 64 where those would be few; up to
-// 64 where tiles would keep less than half of the chip busy.  Measured, 50 rows a group: eight of [4096, 14336] 123 us in 32s,
-// 144 in tiles; 16 of [1001, 2080] 25 and 37; 128 of [1536, 4096] 213 and 161.  The largest tile where groups fill it more than
-// half and three quarters of the compute units have one (128 of 200 rows: 340 us, 454 in the smaller one).
-struct GroupedPlan { int height, width, threads; };
-
-// Fours of waves along the contraction, of 16 rows where workgroups are few.
-constexpr int kFewFours = 2;
-
 using Large = grouped_product::Tile<256, 4>;
 using Small = grouped_product::Tile<128, 2>;
-
-GroupedPlan plan_grouped(int64_t rows, int64_t experts, int64_t outer, bool turned) {
-    const int64_t active = rows < experts ? rows : experts, each = active ? ceil_div(rows, active) : 0;
-    if (!turned && (each <= 32 || (each <= 64 && active * ceil_div(outer, Small::N) < 512))) {
-        const int height = each <= 16 ? 16 : 32;
-        const int64_t tiles = active * ceil_div(each, height);
-        const int width = tiles * ceil_div(outer, 128) >= 512 ? 128 : 64;
-        return {height, width, kFewThreads * (height == 16 && width == 64 ? kFewFours : 1)};
-    }
-    if (each > 128 && active * ceil_div(each, 256) * ceil_div(outer, 256) >= 192) return {Large::M, Large::N, Large::kThreads};
-    return {Small::M, Small::N, Small::kThreads};
-}
-
-// Workgroups: for the row tiles that there may be, each XCD as many, and one at least that finds rows of no group to clear;
-// and for the parts that its last tiles are cut into.
-int64_t most_groups_of(int64_t rows, int64_t experts, int64_t outer, const GroupedPlan& plan) {
-    const int64_t tiles = rows / plan.height + (rows < experts ? rows : experts);
-    const int64_t more = plan.height == Large::M ? grouped_product::kUnits : 1;
-    return (ceil_div(tiles * ceil_div(outer, plan.width), kXcds) + more) * kXcds;
-}
+static_assert(Large::M == kLargeTile && Large::N == kLargeTile && Large::kThreads == kLargeThreads &&
+              Small::M == kSmallTile && Small::N == kSmallTile && Small::kThreads == kSmallThreads, "the plan's tiles");
 
 int check_grouped(int64_t rows, int64_t experts, int64_t n, int64_t k, int block) {
     if (block != 16 && block != 32 && block != 64 && block != 128) return NVFP4_ERR_BLOCK;
@@ -70,7 +45,7 @@ int run_grouped(grouped_product::Args p, bool turned, int block, hipStream_t str
     p.shift = block == 16 ? 4 : block == 32 ? 5 : block == 64 ? 6 : 7;
     p.tiles_n = ceil_div(p.outer, plan.width);
     const dim3 grid((unsigned)most_groups_of(p.rows, p.experts, p.outer, plan));
-    if (plan.threads == Large::kThreads && plan.height == Large::M) launch_tiled<Large>(p, turned, grid, stream);
+    if (plan.height == Large::M) launch_tiled<Large>(p, turned, grid, stream);
     else if (plan.height == Small::M) launch_tiled<Small>(p, turned, grid, stream);
     else if (plan.height == 16) plan.width == 128 ? launch_few<2, 1, 1>(p, grid, stream) : launch_few<1, 1, kFewFours>(p, grid, stream);
     else plan.width == 128 ? launch_few<2, 2, 1>(p, grid, stream) : launch_few<1, 2, 1>(p, grid, stream);

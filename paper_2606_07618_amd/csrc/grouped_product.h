@@ -8,6 +8,7 @@
 // A weight q s has six significant bits and is exact in bfloat16, the type of the rows; sums are binary32.
 #pragma once
 
+#include "grouped_plan.h"
 #include "stream_product.h"
 
 namespace grouped_product {
@@ -105,7 +106,8 @@ __device__ __forceinline__ Place place_of(const Args& p, Offsets o, int index, i
 // it works on at one time shares rows and weights in its L2.  Where an XCD's last tiles would keep few of its compute
 // units busy (SPLIT, one workgroup each), they are cut into two or four parts of their rows ([8192, 14336] x eight times
 // [14336, 4096], 72 tiles for 32 units: 979 us, 1058 without).  The workgroups that are over: `spare` of `sharers`.
-constexpr int kDeep = 8, kUnits = 32;
+using grouped_plan::kUnits, grouped_plan::kFewThreads;
+constexpr int kDeep = 8;
 struct Work { bool tile; int index; int64_t n; int part, parts; int64_t spare, sharers; };
 template <bool SPLIT>
 __device__ __forceinline__ Work work_of(int64_t id, int64_t launched, int tiles_m, int64_t tiles_n) {
@@ -219,8 +221,6 @@ struct Rows {
 // H: fours of waves that take turns along the contraction, whose sums meet in LDS at the end: where workgroups are few, a
 // stage's way from LDS through the matrix instructions is what there is to wait for (two rows of eight groups, [14336, 4096]:
 // 18.4 us with two fours, 20.4 with one, 23.2 with four).
-constexpr int kFewThreads = 256;
-
 template <int R, int C, int H>
 __global__ __launch_bounds__(kFewThreads * H, 2) void few_kernel(Args p) {
     constexpr int N = 64 * R, kRows = 16 * C, kW = N * kStepBytes, kX = kRows * 512, kS = N * 16, kStage = kW + kX + kS;
