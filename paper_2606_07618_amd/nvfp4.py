@@ -140,6 +140,13 @@ except ImportError:                                  # not part of torch's publi
         return torch.cuda.current_stream(index).cuda_stream
 
 
+try:
+    from torch._C import _cuda_getDevice as _current_device
+except ImportError:
+    def _current_device():
+        return torch.cuda.current_device()
+
+
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
@@ -149,7 +156,12 @@ def _stream(t):
     index = t.get_device()
     if index < 0:                                    # it would stand for the current device
         raise ValueError(f"Expected a cuda device, but got: {t.device}")
-    return _raw_stream(index)
+    stream = _raw_stream(index)
+    # Every device's default stream has the handle 0, which HIP takes for the current device's.
+    if not stream and index != _current_device():
+        raise ValueError(f"the tensors are on cuda:{index}, whose default stream is reached with that device current only: "
+                         f"call under torch.cuda.device({index}), or on a stream of its own")
+    return stream
 
 
 def workspace(device) -> torch.Tensor:

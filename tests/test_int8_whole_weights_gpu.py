@@ -100,3 +100,12 @@ def test_own_buffers_captured_and_replayed(nv, m, n, k):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, nv.int8_matmul_grad_input(dy, q, s, cols=k, out_dtype=torch.float32))
+
+
+@pytest.mark.parametrize("m,k", [(3, 48), (70, 100)])
+def test_no_outputs_of_the_layer(nv, m, k):
+    """Nothing to sum: zeros, also on top of what the output held."""
+    q, s = weights(0, k, gen(6))
+    out = torch.full((m, k), float("nan"), device=DEV)
+    dy = torch.empty((m, 0), dtype=torch.bfloat16, device=DEV)
+    assert not nv.int8_matmul_grad_input(dy, q, s, cols=k, out_dtype=torch.float32, out=out).any()
