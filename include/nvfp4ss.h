@@ -430,8 +430,8 @@ int nvfp4_grouped_product_grad_input(const void* dy, int64_t ld, const int* offs
  * Activations have a scale for each token so, weights [n, k] one for each output channel.
  */
 
-/* s = RN32(max|x| RN32(1 / 127)) of the row; q the whole number nearest to the quotient x / s, ties to the even
- * one, at most 127 in magnitude; s = 0: q = 0.  A row that holds an infinity or a NaN gets s = NaN (and q = 0): its
+/* s = RN32(max|x| RN32(1 / 127)) of the row, at most 0.56 units of its last place from max|x| / 127; q the whole number
+ * nearest to the quotient x / s, ties to the even one, at most 127 in magnitude; s = 0: q = 0.  A row that holds an infinity or a NaN gets s = NaN (and q = 0): its
  * products are NaN.  x: [rows, cols], rows ldx elements apart, binary32 or bfloat16, aligned to its elements;
  * cols < 2^17.  One kernel, no workspace. */
 int int8_quant(const void* x, int dtype, int64_t rows, int64_t cols, int64_t ldx, int8_t* q, float* scales, void* stream);

@@ -17,10 +17,13 @@ constexpr int kUnits = 32, kXcds = 8;                    // compute units of an 
 struct GroupedPlan { int height, width, threads; };
 
 // By the rows that a group has on average (how many each has is known on the device alone; every kernel takes
-// any number).  Few rows: 16 or 32 of a group at a time, and 128 weight rows a workgroup, or 64 where those would be few; up to
-// 64 where tiles would keep less than half of the chip busy.  Measured, 50 rows a group: eight of [4096, 14336] 123 us in 32s,
-// 144 in tiles; 16 of [1001, 2080] 25 and 37; 128 of [1536, 4096] 213 and 161.  The largest tile where groups fill it more than
-// half and three quarters of the compute units have one (128 of 200 rows: 340 us, 454 in the smaller one).
+// any number).  Few rows: 16 or 32 of a group at a time, and 128 weight rows a workgroup, or 64 where those would be few.  Measured
+// with 12 to 32 rows a group, 8 to 128 groups, contractions of 1024 to 14336: 0.34 to 0.99 of the tiles' time.  33 to 64 rows a
+// group go that way below 512 tiles.  With 256 to 480 tiles and groups as uneven as a router's (shares of 1 / (i + 1)^0.6 and 1.2) that
+// took 0.53 to 0.99 of the tiles' time in 38 of 40 cases (60 groups of 36 rows, [1024, 4096]: 56 to 66 us, 70 to 93 in tiles); groups that
+// are all alike are faster in tiles from 320 on (60 of 48 rows: 66 and 49), which their average does not tell.  From 512 on: 128
+// groups of 50 rows, [1536, 4096], 215 us, 171 in tiles.  The largest tile where groups fill it more than half and three quarters
+// of the compute units have one (128 of 200 rows, [1536, 4096]: 350 us, 457 in the smaller one).
 inline GroupedPlan plan_grouped(int64_t rows, int64_t experts, int64_t outer, bool turned) {
     const int64_t active = rows < experts ? rows : experts, each = active ? ceil_div(rows, active) : 0;
     if (!turned && (each <= 32 || (each <= 64 && active * ceil_div(outer, kSmallTile) < 512))) {

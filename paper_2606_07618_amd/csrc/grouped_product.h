@@ -105,7 +105,7 @@ __device__ __forceinline__ Place place_of(const Args& p, Offsets o, int index, i
 // What a workgroup does.  An XCD gets a run of the sequence of tiles, which walks kDeep row tiles at a time, so that what
 // it works on at one time shares rows and weights in its L2.  Where an XCD's last tiles would keep few of its compute
 // units busy (SPLIT, one workgroup each), they are cut into two or four parts of their rows ([8192, 14336] x eight times
-// [14336, 4096], 72 tiles for 32 units: 979 us, 1058 without).  The workgroups that are over: `spare` of `sharers`.
+// [14336, 4096], 72 tiles for 32 units: 957 us, 1082 without).  The workgroups that are over: `spare` of `sharers`.
 using grouped_plan::kUnits, grouped_plan::kFewThreads;
 constexpr int kDeep = 8;
 struct Work { bool tile; int index; int64_t n; int part, parts; int64_t spare, sharers; };
@@ -181,7 +181,8 @@ struct GroupScales {
 // Rows of 128 bytes in LDS, loaded as Side's but for their exchange: a lane of a fragment reads chunk 2 (lane / 16) or the
 // one behind it, and of the lanes that LDS serves at once rows 0 to 3 and 12 to 15 are from one sixteen, rows 4 to 11 from the
 // next, two chunks on.  The places of these two sets of rows are apart from each other, moved by two or not.  (With Side's
-// exchange half of LDS' time was conflicts: 16384 rows, eight groups, [14336, 4096] 1.59 ms, 1.51 so.)
+// exchange conflicts are half of LDS' time, 0.22 of it so; 16384 rows, eight groups, [14336, 4096] take 1.58 ms either way, held by
+// the power limit.)
 template <int R, int THREADS>
 struct Rows {
     static constexpr int kLoads = R * kStepBytes / (THREADS * kChunk);
@@ -213,14 +214,14 @@ struct Rows {
 // ---- few rows a group ---------------------------------------------------------------------------
 // Reading the weights is all there is to do.  A workgroup owns 64 R weight rows, 16 R for each of four waves, and up to 16 C
 // rows of one group; weights, scales and rows go through LDS by whole lines, 256 values of the contraction at a time, the next
-// ones while these are multiplied.  512 rows, 128 groups, [1536, 4096]: 102 us, 4.5 TB/s of the 5.05 that a large copy reaches; a
-// tenth of the bytes are the scales, 16 bytes of a row at a time.  Three workgroups a compute unit hide each other's first waits;
-// rings of three or four stages leave room for two (128 us where two stages took 113).  Loaded straight into the registers of
+// ones while these are multiplied.  512 rows, 128 groups, [1536, 4096]: 103 us, 4.5 TB/s, where a large copy reaches 5.1 and a large
+// read 6.2; a tenth of the bytes are the scales, 16 bytes of a row at a time.  Three workgroups a compute unit hide each other's first waits;
+// rings of three or four stages leave room for two (an eighth longer).  Loaded straight into the registers of
 // the matrix instructions, whose neighbouring lanes hold different rows, each lane's 16 bytes are an access of their own to the
-// L1, which was then nine tenths of the time busy (135 us).
+// L1, which was then nine tenths of the time busy (a fifth longer).
 // H: fours of waves that take turns along the contraction, whose sums meet in LDS at the end: where workgroups are few, a
 // stage's way from LDS through the matrix instructions is what there is to wait for (two rows of eight groups, [14336, 4096]:
-// 18.4 us with two fours, 20.4 with one, 23.2 with four).
+// 19.4 us with two fours, 21.1 with one, 24.0 with four).
 template <int R, int C, int H>
 __global__ __launch_bounds__(kFewThreads * H, 2) void few_kernel(Args p) {
     constexpr int N = 64 * R, kRows = 16 * C, kW = N * kStepBytes, kX = kRows * 512, kS = N * 16, kStage = kW + kX + kS;
@@ -369,9 +370,9 @@ __global__ __launch_bounds__(kFewThreads * H, 2) void few_kernel(Args p) {
 // once for a tile's rows, on their way into LDS, where they lie as bfloat16 rows along the contraction: turning costs nothing
 // there, as the pairs that share a register are put together from single values anyway.
 // 64 rows: each wave takes all of them against half as many weight rows, and so expands half as many, and the rows are four
-// steps ahead (6400 rows, 128 groups, [1536, 4096]: 161 us, 185 without either).
-//   16384 rows, eight groups, [14336, 4096]: 1.55 ms (1.24 PFLOP/s; the clock is held at 1.5 to 1.6 GHz by the power limit,
-//   and the matrix instructions are busy two thirds of a compute unit's time); turned, 8192 rows: 0.95 ms (1.01 PFLOP/s).
+// steps ahead (6400 rows, 128 groups, [1536, 4096]: 171 us; a seventh longer without either).
+//   16384 rows, eight groups, [14336, 4096]: 1.58 ms (1.22 PFLOP/s; the clock is held below 1.8 GHz by the power limit,
+//   and the matrix instructions are busy two thirds of a compute unit's time); turned, 8192 rows: 0.96 ms (1.00 PFLOP/s).
 constexpr int kSteps = 2;                        // in LDS
 
 // Turned weights: a row's chunks of 16 bytes exchanged by the row, as reads take one chunk of 16 neighbouring rows and

@@ -1,5 +1,5 @@
 // Linear layers in 8-bit integers: rows x = s q with s = max|x| / 127 (the product with binary32's 1/127, as elementary
-// operations on tensors divide by a number: at most 1.5 units of its last place off), and the products of two operands so,
+// operations on tensors divide by a number: at most 0.56 units of its last place off), and the products of two operands so,
 //   y[m][n] = s_a[m] s_b[n] sum_k a[m][k] b[n][k],   dx[m][k] = sum_n dy[m][n] s_b[n] b[n][k].
 // Integer sums are exact; an output is rounded where the sum becomes a binary32 number, in the product of the scales, in
 // their product, and to its type.
@@ -17,8 +17,9 @@ constexpr int64_t kMostInner = ((int64_t)1 << 17) - kRowUnit;
 // ---- quantization -----------------------------------------------------------------------------
 // One pass: a row stays in registers between its maximum and its quotients, as long as it has at most 8 kKept values a
 // thread; what is longer is read again.  A wave a row, or a workgroup where a wave would hold more than half of that.
-// From memory, [8192, 4096] bfloat16: 32 us, of which 20 to move; [777, 14330] binary32: 15 us, 11 to move (rows that all wait
-// first and compute then).
+// From memory, [8192, 4096] bfloat16: 32 us, of which 20 to move: the vector instructions of a quotient and of packing are issued
+// 0.6 of the time, and a row waits before it computes.  [777, 14330] binary32: 15 us, 11 to move (three rows a compute unit,
+// which all wait first and compute then: 0.2).
 constexpr int kQuantThreads = 256, kQuantWaves = kQuantThreads / kLanes, kUnit = 8, kKept = 8;   // units of 8 values
 
 // 8 values from `from`, of which `left` are there: bits of binary32 numbers.
@@ -242,8 +243,8 @@ void launch_dot(const DotArgs& p, hipStream_t stream) {
 }
 
 // ---- tiles ------------------------------------------------------------------------------------
-// The tiled product of the other operands: a step's 128 bytes of a row are 128 values.  [8192, 4096] x [14336, 4096]: 374 to
-// 409 us, 2.6 to 2.4 POP/s (a library's [8192, 8192] x [8192, 8192] of integers: 2.1).
+// The tiled product of the other operands: a step's 128 bytes of a row are 128 values.  [8192, 4096] x [14336, 4096]: 380 us
+// on one card, 400 from memory on another, 2.5 and 2.4 POP/s (a library's [8192, 8192] x [8192, 8192] of integers: 2.1).
 
 // Sums of parts of the contraction, in 32-bit integers as a whole sum is: a workgroup for kJoinColumns outputs of a row.
 // Rows of parts hold whole fours, which a tile stores at once.
@@ -314,7 +315,7 @@ int run_int8(const int8_t* a, const float* a_scales, const int8_t* b, const floa
 // ---- the gradient with respect to the rows ------------------------------------------------------
 // The scales run along the contraction here, so the weights are expanded to bfloat16, rows turned.  s q has up to 31
 // significant bits.  For a bfloat16 gradient it is rounded to 8, which takes the gradient's relative error from 0.0017, its
-// own rounding, to 0.0024 (whole weights would take three times the time).  A binary32 gradient is for those who need more:
+// own rounding, to 0.0023 or 0.0024 ([4096, 14336] x [14336, 4096]: 375 us; 1210 with whole weights).  A binary32 gradient is for those who need more:
 // binary32's s q is three bfloat16 numbers, each the upper half of what those before it leave (exact from 2^-109 on), and
 // three products, one on top of the other, through one buffer of weights.
 enum Term { kRounded, kFirst, kSecond, kThird };

@@ -449,7 +449,7 @@ __global__ __launch_bounds__(T::kThreads, T::kWavesPerSimd) void product_kernel(
     // operands (the same product: 282 -> 252 us).
     const float scale = OUT == kSums && p.scale ? *p.scale : 1.0f;
     // integers: the scales of this lane's columns and of its rows.  A wave whose scales are all moderate multiplies them first
-    // ([8192, 4096] x [14336, 4096]: 396 us, 406 with powers of two for all).
+    // ([8192, 4096] x [14336, 4096] with its quantization: 396 us, 406 with powers of two for all).
     f32x4 scale_n[KIND == kInt8 && OUT == kSums ? NF : 1];
     float scale_m[KIND == kInt8 && OUT == kSums ? MF : 1];
     bool inside = true;

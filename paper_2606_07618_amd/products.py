@@ -342,7 +342,7 @@ class _GroupedMatmul(torch.autograd.Function):
 def int8_quantize(x: torch.Tensor, out=None):
     """8-bit integers of the rows of a bfloat16 or float32 device matrix [rows, cols] (rows may be strided):
     (q [rows, 16 ceil(cols / 16)] int8, zeros past the width, scales [rows] float32), x about q * scale with
-    scale = max|x| / 127 of the row: a scale for each token of an activation, for each output channel of weights
+    scale = max|x| / 127 of the row, as the product with float32's 1/127: a scale for each token of an activation, for each output channel of weights
     [n, k].  See int8_quant.  Integers carry no gradient, so an x that requires one is refused where autograd records:
     pass x.detach(), or quantize in an autograd.Function whose backward is int8_matmul_grad_input (straight through)."""
     if x.requires_grad and torch.is_grad_enabled():
