@@ -315,19 +315,22 @@ int run_int8(const int8_t* a, const float* a_scales, const int8_t* b, const floa
 // ---- the gradient with respect to the rows ------------------------------------------------------
 // The scales run along the contraction here, so the weights are expanded to bfloat16, rows turned.  s q has up to 31
 // significant bits.  For a bfloat16 gradient it is rounded to 8, which takes the gradient's relative error from 0.0017, its
-// own rounding, to 0.0023 or 0.0024 ([4096, 14336] x [14336, 4096]: 375 us; 1210 with whole weights).  A binary32 gradient is for those who need more:
-// binary32's s q is three bfloat16 numbers, each the upper half of what those before it leave (exact from 2^-109 on), and
-// three products, one on top of the other, through one buffer of weights.
+// own rounding, to 0.0023 or 0.0024 ([4096, 14336] x [14336, 4096]: 375 us; 1210 with whole weights).  A binary32 gradient is for
+// those who need more: binary32's s q is three bfloat16 numbers, each the largest below what those before it leave (exact from
+// 2^-109 on), and three products, one on top of the other, through one buffer of weights.  Below, not up to: none of the three is
+// zero then, and an infinite dy gives an infinity as it does with the weight itself.
 enum Term { kRounded, kFirst, kSecond, kThird };
 
 template <Term TERM>
 __device__ __forceinline__ float term_of(float w) {
-    const auto upper = [](float v) { return __uint_as_float(__float_as_uint(v) & 0xFFFF0000u); };
     if constexpr (TERM == kRounded) return w;                 // by the conversion
-    const float first = upper(w);
-    if constexpr (TERM == kFirst) return first;
-    const float rest = fabsf(w) < __builtin_inff() ? w - first : 0.0f, second = upper(rest);
-    return TERM == kSecond ? second : rest - second;
+    const auto below = [](float v) {                          // in magnitude
+        const uint32_t bits = __float_as_uint(v), size = bits & 0x7FFFFFFFu;
+        return __uint_as_float((bits & 0x80000000u) | (size == 0 ? 0 : (size - 1) & 0xFFFF0000u));
+    };
+    if (!(fabsf(w) < __builtin_inff())) return w;             // an infinity or a NaN three times
+    const float first = below(w), rest = w - first, second = below(rest);
+    return TERM == kFirst ? first : TERM == kSecond ? second : rest - second;
 }
 
 constexpr int kTurnThreads = 256, kTurnN = 64, kTurnK = 128;
@@ -405,9 +408,10 @@ int run_int8_grad(const void* dy, int64_t ld, const int8_t* q, const float* scal
     p.m = m, p.n = k, p.inner = n, p.out = out, p.out_ld = k, p.out_f32 = out_dtype == NVFP4_IN_F32;
     float* partial = static_cast<float*>(c.take(0));
     if (!p.out_f32) return grad_product<kRounded, kSums>(q, scales, n, k, w, p, partial, stream);
-    if (const int rc = grad_product<kFirst, kSums>(q, scales, n, k, w, p, partial, stream)) return rc;
+    // the smallest first: with the second it adds up to all that the first leaves, and that with the first to the weight
+    if (const int rc = grad_product<kThird, kSums>(q, scales, n, k, w, p, partial, stream)) return rc;
     if (const int rc = grad_product<kSecond, kAdded>(q, scales, n, k, w, p, partial, stream)) return rc;
-    return grad_product<kThird, kAdded>(q, scales, n, k, w, p, partial, stream);
+    return grad_product<kFirst, kAdded>(q, scales, n, k, w, p, partial, stream);
 }
 
 int check_int8(int64_t m, int64_t n, int64_t k) {

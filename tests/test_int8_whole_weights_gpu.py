@@ -109,3 +109,20 @@ def test_no_outputs_of_the_layer(nv, m, k):
     out = torch.full((m, k), float("nan"), device=DEV)
     dy = torch.empty((m, 0), dtype=torch.bfloat16, device=DEV)
     assert not nv.int8_matmul_grad_input(dy, q, s, cols=k, out_dtype=torch.float32, out=out).any()
+
+
+@pytest.mark.parametrize("m,n,k", [(3, 7, 33), (64, 256, 512), (137, 619, 11216)])
+def test_infinite_and_no_numbers_of_dy(nv, m, n, k):
+    """As with the weights themselves: a weight that is one bfloat16 number has no part that is zero, whose product would be none."""
+    g = gen(7, m, n, k)
+    q, s = weights(n, k, g)
+    s[0] = 0.25                                           # powers of two among its weights
+    q[0, :8] = torch.tensor([1, 2, 64, -128, 3, -1, 0, 127], dtype=torch.int8, device=DEV)
+    dy = torch.randn((m, n), generator=g, device=DEV).to(torch.bfloat16)
+    dy[0, 0], dy[1, 0], dy[m - 1, n - 1] = float("inf"), -float("inf"), float("nan")
+    got = nv.int8_matmul_grad_input(dy, q, s, cols=k, out_dtype=torch.float32)
+    sign = q[0, :k].float().sign()
+    want = torch.where(sign == 0, torch.full_like(sign, float("nan")), sign * float("inf"))
+    for row, w in ((0, want), (1, -want)):
+        assert bool((got[row].isnan() == w.isnan()).all()) and torch.equal(got[row][sign != 0], w[sign != 0])
+    assert bool(got[m - 1].isnan().all()) and bool(got[2:m - 1].isfinite().all())
